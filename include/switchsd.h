@@ -24,7 +24,11 @@
  * the decode loop's commit with the draft model's lazy-propagation counters
  * (switchsd_commit, or `commit` in switchsd_step; Sec. 3.3, KV Cache
  * Synchronization), and the copy-mode labels the probe is trained on
- * (switchsd_copy_labels; Sec. 3.2).
+ * (switchsd_copy_labels; Sec. 3.2).  Next to it, what an engine around the
+ * step needs per step: penalties, biases and grammar masks on the logits
+ * (switchsd_process_logits, switchsd_verify_processed) and the pages and slots
+ * of a paged KV cache (switchsd_page_plan, switchsd_span_slots,
+ * switchsd_compact_cache).
  *
  * Conventions for every entry point:
  *   - All array pointers are DEVICE pointers owned by the caller; arrays are
@@ -358,6 +362,152 @@ int switchsd_copy_labels(const int32_t *tokens, const int32_t *lengths, int32_t 
                          hipStream_t stream);
 /* 0 for a negative argument or Lmax > 2^28. */
 size_t switchsd_label_workspace_bytes(int32_t B, int32_t Lmax);
+
+/* ---- What an engine calls next to the step ------------------------------- */
+
+#define SWITCHSD_MAX_BIAS 511           /* most bias entries per sequence          */
+#define SWITCHSD_MAX_HISTORY 2097151    /* longest history (2^21 - 1)              */
+#define SWITCHSD_MAX_PLAN_B 65536       /* most sequences of a plan                */
+
+/* Types of logits. */
+typedef enum { SWITCHSD_BF16 = 0, SWITCHSD_F16 = 1, SWITCHSD_F32 = 2 } switchsd_type;
+
+/* Penalties for repeated tokens, biases and a grammar's mask on the logits of
+ * the drafted rows.  Row r of sequence b is the target's output after node r,
+ * so its history is the context and the drafted tokens on the path from the
+ * anchor to node r (the anchor is the context's last token and is counted
+ * there; the walk stops at a parent outside [0, node), as in
+ * switchsd_tree_mask).  With L = clamp(lengths[b], 0, Lmax), P =
+ * clamp(prompt_lens[b], 0, L), for token v:
+ *   c = occurrences of v in tokens[b, P..L-1] and among the path's tokens,
+ *   seen = c > 0 or v occurs in tokens[b, 0..P-1],
+ *   y = seen ? (l > 0 ? l / repetition[b] : l * repetition[b]) : l,
+ *   c > 0:  y = y - frequency[b] * c, then y = y - presence[b],
+ *   v listed in bias_ids[b, :]:  y = y + bias_vals of the last such entry,
+ *   allowed_on[b] != 0 and bit v of allowed[b, r, :] clear:  y = -inf,
+ * each operation rounded to float, the result rounded once to the output's
+ * type (a value that none of them touches is passed on as it is).  NaN and
+ * infinities follow the arithmetic.  A row whose mask allows nothing is all
+ * -inf, of which the greedy choice is token 0.
+ * Token ids outside [0, V) (pads, -1) count for nothing.
+ *   logits [B, R, V] of logits_type, aligned to its elements; dtok [B, R],
+ *   dpar [B, R] or NULL (chains), dn [B]; tokens [B, Lmax], lengths [B]
+ *   (needed with any of the three penalties, else not read; prompt_lens NULL:
+ *   no prompt, every token counts), Lmax <= SWITCHSD_MAX_HISTORY; repetition,
+ *   frequency, presence [B] float, each NULL for none; bias_ids [B, n_bias]
+ *   int32 and bias_vals [B, n_bias] float, n_bias <= SWITCHSD_MAX_BIAS;
+ *   allowed [B, R, (V + 31) / 32] uint32 (bit v % 32 of word v / 32; NULL:
+ *   everything is allowed), allowed_on [B] int32 (NULL: every sequence; the
+ *   masks of the others are not read). */
+typedef struct {
+    const void *logits;
+    int32_t logits_type; /* switchsd_type */
+    int32_t B, R, V, Lmax, n_bias;
+    const int32_t *dtok, *dpar, *dn;
+    const int32_t *tokens, *lengths, *prompt_lens;
+    const float *repetition, *frequency, *presence;
+    const int32_t *bias_ids;
+    const float *bias_vals;
+    const uint32_t *allowed;
+    const int32_t *allowed_on;
+} switchsd_logits_args;
+
+/* The processed logits of rows r < clamp(dn[b], 1, R), written to out
+ * [B, R, V]; the other rows are neither read nor written.  out_type is
+ * SWITCHSD_BF16 (what the verification takes) or logits_type.  out may be
+ * logits itself (same type): the values that change are then rewritten in
+ * place; any other overlap is refused.  One launch. */
+int switchsd_process_logits(const switchsd_logits_args *args, void *out, int32_t out_type,
+                            hipStream_t stream);
+
+/* The greedy verification of processed logits that are never written: the
+ * results of switchsd_process_logits into bf16 followed by
+ * switchsd_verify_accept, in one launch that reads the logits once.  Outputs
+ * and workspace as in switchsd_verify_accept. */
+int switchsd_verify_processed(const switchsd_logits_args *args, int32_t *accept_len,
+                              int32_t *accept_node, int32_t *bonus, int32_t *out_tokens,
+                              int32_t *amax, void *workspace, size_t workspace_bytes,
+                              hipStream_t stream);
+
+/* Pages of a paged KV cache for the drafted rows, and where each row's entry
+ * goes.  With L = clamp(lengths[b], 0, Lmax) and n = clamp(dn[b], 1, R), node r
+ * is stored at cache position L - 1 + r (the anchor, the context's last token,
+ * is not in the cache yet) and sits at sequence position L - 1 + its depth.  A
+ * sequence with L > 0 needs ceil((L - 1 + n) / page_size) pages, at most
+ * max_pages; it takes what it lacks over held[b] from the free ring and gives
+ * nothing back while it lives.  A sequence with L = 0 is finished: its pages
+ * return to the ring (for later calls; pages given back by a call are not
+ * handed out by it), its table entries become -1 and held[b] = 0.
+ * The ring holds ring_state = {head, count}: the free pages are
+ * ring[(head + i) mod ring_pages], i < count.  Pages are taken from the head,
+ * for the sequences in order, as long as the running total of what they lack
+ * fits count: the first sequence that does not fit and all later ones that
+ * lack pages get none, and missing[b] is what such a sequence lacks (0 for all
+ * others).  Returned pages are appended in sequence order (cut at ring_pages).
+ *   slots[b, r] = table[b, p / page_size] * page_size + p % page_size for
+ *   p = L - 1 + r, r < n, where the page is held, else -1;
+ *   positions[b, r] = L - 1 + depth(r) for r < n and L > 0, else -1 (the walk
+ *   to the anchor stops at a parent outside [0, node)).
+ *   lengths, dn [B], dpar [B, R] or NULL (chains); table [B, max_pages], held
+ *   [B], ring [ring_pages], ring_state [2] int32 in/out; slots [B, R] int64
+ *   and positions [B, R] int32 (each may be NULL), missing [B] int32 out.
+ *   B <= SWITCHSD_MAX_PLAN_B, B * max_pages < 2^31, 1 <= page_size <= 65536,
+ *   max_pages * page_size < 2^31.  held and ring_state are clamped to their
+ *   ranges; page numbers are not looked at. */
+typedef struct {
+    const int32_t *lengths;
+    const int32_t *dpar, *dn;
+    int32_t B, R, Lmax, page_size, max_pages, ring_pages;
+    int32_t *table, *held, *ring, *ring_state;
+    int64_t *slots;
+    int32_t *positions;
+    int32_t *missing;
+} switchsd_page_args;
+
+/* One launch; workspace as for the other calls, of at least
+ * switchsd_workspace_bytes(B, 0, 0, 0) bytes. */
+int switchsd_page_plan(const switchsd_page_args *args, void *workspace, size_t workspace_bytes,
+                       hipStream_t stream);
+
+/* Slots of ragged ranges, packed: sequence b contributes the positions
+ * i = begin[b] .. end[b] - 1 (clamped to 0 <= begin <= end <= Lmax) of its
+ * context, one after another -- a prompt, or with begin = draft_pos and end =
+ * lengths after a commit the tokens a lagging draft model has yet to read
+ * (Sec. 3.3, lazy propagation).  cu[b] = the number of positions before
+ * sequence b (cu[B] the total).  For entry j = cu[b] + i - begin[b] < capacity:
+ *   slots[j] = table[b, i / page_size] * page_size + i % page_size, or -1 where
+ *   i / page_size >= clamp(held[b], 0, max_pages);
+ *   positions[j] = i, packed[j] = tokens[b, i], seq[j] = b.
+ * Entries from cu[B] on are left as they are; cu tells a total beyond capacity.
+ *   begin, end, held [B], tokens [B, Lmax], table [B, max_pages] int32;
+ *   outputs cu [B + 1] int32, slots [capacity] int64, positions, packed, seq
+ *   [capacity] int32, each but cu NULL if not wanted (tokens may be NULL
+ *   without packed, table and held without slots).
+ *   B <= SWITCHSD_MAX_PLAN_B, B * Lmax and B * max_pages < 2^31, 1 <= page_size
+ *   <= 65536.  One launch.  B = 0 writes nothing. */
+int switchsd_span_slots(const int32_t *begin, const int32_t *end, const int32_t *tokens,
+                        const int32_t *table, const int32_t *held, int32_t B, int32_t Lmax,
+                        int32_t max_pages, int32_t page_size, int32_t *cu, int64_t *slots,
+                        int32_t *positions, int32_t *packed, int32_t *seq, int32_t capacity,
+                        hipStream_t stream);
+
+/* The accepted nodes' cache entries moved to their final places: after the
+ * verification, the node at depth j of the accepted path moves from its slot
+ * to that of node j (cache position L - 1 + j), for j = 1 .. depth of
+ * accept_node[b]; a path already in place (a chain, the most recent copy
+ * candidate) moves nothing.  The cache is `planes` planes (layers times keys
+ * and values) of n_slots rows of row_bytes, plane_stride bytes apart; slots
+ * [B, R] int64 as from switchsd_page_plan.  Nothing is moved for a sequence
+ * whose accept_node lies outside [0, clamp(dn[b], 1, R)) or whose path does
+ * not lead to the anchor, nor for a node with a slot outside [0, n_slots).
+ * The slots of a call's drafted nodes must be distinct.
+ *   dpar [B, R] or NULL (chains: nothing to move), dn, accept_node [B];
+ *   cache 4-byte aligned, row_bytes and plane_stride multiples of 4,
+ *   plane_stride >= n_slots * row_bytes (one plane: not looked at).  One launch. */
+int switchsd_compact_cache(void *cache, int32_t planes, int64_t plane_stride, int64_t n_slots,
+                           int32_t row_bytes, const int64_t *slots, const int32_t *dpar,
+                           const int32_t *dn, const int32_t *accept_node, int32_t B, int32_t R,
+                           hipStream_t stream);
 
 /* Workspace bytes needed by calls with B sequences of R rows, contexts of up
  * to Lmax tokens and n_cand copy candidates (pass 0 for what a call does not

@@ -17,7 +17,10 @@ LIB_PATH = os.path.join(HERE, "libswitchsd.so")
 
 MAX_NGRAM = 8
 MAX_CAND = 16
+MAX_BIAS = 511
+MAX_HISTORY = 2 ** 21 - 1
 MODE_AUTO, MODE_FUSED, MODE_SPLIT = 0, 1, 2
+BF16, F16, F32 = 0, 1, 2
 
 STATUS = {0: "OK", -1: "EINVAL", -2: "ESHAPE", -3: "EHIP", -4: "EWORKSPACE", -5: "EDEVICE",
           -6: "ESCRATCH"}
@@ -27,6 +30,8 @@ EXPORTS = ("switchsd_ngram_match", "switchsd_probe_score", "switchsd_select_draf
            "switchsd_commit", "switchsd_step", "switchsd_copy_labels",
            "switchsd_workspace_bytes", "switchsd_sample_workspace_bytes",
            "switchsd_label_workspace_bytes", "switchsd_workspace_status", "switchsd_step_noalloc",
+           "switchsd_process_logits", "switchsd_verify_processed", "switchsd_page_plan",
+           "switchsd_span_slots", "switchsd_compact_cache",
            "switchsd_test_withhold_probe_flag", "switchsd_test_withhold_segment",
            "switchsd_status_string")
 
@@ -77,6 +82,22 @@ class StepArgs(ctypes.Structure):
                 ("draft_logits", _P), ("accept_uniforms", _P)]
 
 
+class LogitsArgs(ctypes.Structure):
+    _fields_ = [("logits", _P), ("logits_type", _I),
+                ("B", _I), ("R", _I), ("V", _I), ("Lmax", _I), ("n_bias", _I),
+                ("dtok", _P), ("dpar", _P), ("dn", _P),
+                ("tokens", _P), ("lengths", _P), ("prompt_lens", _P),
+                ("repetition", _P), ("frequency", _P), ("presence", _P),
+                ("bias_ids", _P), ("bias_vals", _P), ("allowed", _P), ("allowed_on", _P)]
+
+
+class PageArgs(ctypes.Structure):
+    _fields_ = [("lengths", _P), ("dpar", _P), ("dn", _P),
+                ("B", _I), ("R", _I), ("Lmax", _I), ("page_size", _I), ("max_pages", _I),
+                ("ring_pages", _I), ("table", _P), ("held", _P), ("ring", _P),
+                ("ring_state", _P), ("slots", _P), ("positions", _P), ("missing", _P)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run `python -m paper_2609_20186_amd.build`")
@@ -103,6 +124,14 @@ def _load():
     lib.switchsd_workspace_bytes.argtypes = [_I, _I, _I, _I]
     lib.switchsd_workspace_bytes.restype = S
     lib.switchsd_workspace_status.argtypes = [_P, S, _I, _P, _P]
+    lib.switchsd_process_logits.argtypes = [ctypes.POINTER(LogitsArgs), _P, _I, _P]
+    lib.switchsd_verify_processed.argtypes = [ctypes.POINTER(LogitsArgs), _P, _P, _P, _P, _P, _P,
+                                              S, _P]
+    lib.switchsd_page_plan.argtypes = [ctypes.POINTER(PageArgs), _P, S, _P]
+    lib.switchsd_span_slots.argtypes = [_P, _P, _P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P, _P,
+                                        _I, _P]
+    lib.switchsd_compact_cache.argtypes = [_P, _I, ctypes.c_int64, ctypes.c_int64, _I, _P, _P,
+                                           _P, _P, _I, _I, _P]
     for knob in ("switchsd_test_withhold_probe_flag", "switchsd_test_withhold_segment"):
         getattr(lib, knob).argtypes = [_I]
         getattr(lib, knob).restype = None
@@ -370,3 +399,183 @@ def switchsd_step_noalloc(args, stream=None):
     argument; args.sample_workspace is ignored)."""
     _check("switchsd_step_noalloc", lib.switchsd_step_noalloc(ctypes.byref(args),
                                                               _stream(stream)))
+
+
+# ------------------------------------------------------------------ calls around the step
+
+_TYPES = {torch.bfloat16: BF16, torch.int16: BF16, torch.uint16: BF16, torch.float16: F16,
+          torch.float32: F32}
+_DT["i64"] = (torch.int64,)
+_DT["logits"] = tuple(_TYPES)
+
+
+def _arr(t, kind, name, shape, optional=False):
+    """Device pointer of a tensor of exactly this shape on the current device."""
+    ptr = _ptr(t, kind, name, optional)
+    if ptr is not None:
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+        _here(t, name)
+    return ptr
+
+
+def _here(t, name):
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is on device {t.get_device()}, the current device is "
+                         f"{torch.cuda.current_device()}")
+
+
+def build_logits_args(logits, dtok, dpar, dn, tokens=None, lengths=None, prompt_lens=None,
+                      repetition=None, frequency=None, presence=None, bias_ids=None,
+                      bias_vals=None, allowed=None, allowed_on=None):
+    """LogitsArgs for switchsd_process_logits and switchsd_verify_processed:
+    logits [B, R, V] (bf16 or its bits, fp16 or fp32) of the drafted rows and the
+    draft's dtok, dpar (None: chains) [B, R] and dn [B].  repetition, frequency,
+    presence: float [B] each, with the context tokens [B, Lmax], lengths [B] and
+    prompt_lens [B] (None: no prompt); bias_ids int32 and bias_vals float
+    [B, n]; allowed: bits, uint32 (or int32) [B, R, (V + 31) // 32], for the
+    sequences with allowed_on[b] != 0 (None: all).  The tensors are kept alive by
+    the result."""
+    if not isinstance(logits, _Tensor) or logits.dim() != 3:
+        raise ValueError("logits must be a device tensor [B, R, V]")
+    B, R, V = logits.shape
+    a = LogitsArgs()
+    a.logits = _arr(logits, "logits", "logits", (B, R, V))
+    a.logits_type = _TYPES[logits.dtype]
+    a.B, a.R, a.V = B, R, V
+    a.dtok = _arr(dtok, "i32", "dtok", (B, R))
+    a.dpar = _arr(dpar, "i32", "dpar", (B, R), True)
+    a.dn = _arr(dn, "i32", "dn", (B,))
+    penal = any(t is not None for t in (repetition, frequency, presence))
+    if tokens is not None:
+        if not isinstance(tokens, _Tensor) or tokens.dim() != 2:
+            raise ValueError("tokens must be a device tensor [B, Lmax]")
+        a.Lmax = tokens.shape[1]
+        a.tokens = _arr(tokens, "i32", "tokens", (B, a.Lmax))
+    elif penal:
+        raise ValueError("tokens is required")
+    a.lengths = _arr(lengths, "i32", "lengths", (B,), not penal)
+    a.prompt_lens = _arr(prompt_lens, "i32", "prompt_lens", (B,), True)
+    for name, t in (("repetition", repetition), ("frequency", frequency),
+                    ("presence", presence)):
+        setattr(a, name, _arr(t, "f32", name, (B,), True))
+    if (bias_ids is None) != (bias_vals is None):
+        raise ValueError("bias_ids and bias_vals come together")
+    if bias_ids is not None:
+        if not isinstance(bias_ids, _Tensor) or bias_ids.dim() != 2:
+            raise ValueError("bias_ids must be a device tensor [B, n]")
+        a.n_bias = bias_ids.shape[1]
+        a.bias_ids = _arr(bias_ids, "i32", "bias_ids", (B, a.n_bias))
+        a.bias_vals = _arr(bias_vals, "f32", "bias_vals", (B, a.n_bias))
+    a.allowed = _arr(allowed, "u32", "allowed", (B, R, (V + 31) // 32), True)
+    a.allowed_on = _arr(allowed_on, "i32", "allowed_on", (B,), True)
+    a.shape, a.device = (B, R, V), logits.get_device()
+    a.keep = (logits, dtok, dpar, dn, tokens, lengths, prompt_lens, repetition, frequency,
+              presence, bias_ids, bias_vals, allowed, allowed_on)
+    return a
+
+
+def _args_here(args):
+    if args.device != torch.cuda.current_device():
+        raise ValueError(f"the arguments are on device {args.device}, the current device is "
+                         f"{torch.cuda.current_device()}")
+
+
+def switchsd_process_logits(args, out, stream=None):
+    """out [B, R, V]: bf16 or the logits' type (the logits themselves: in place)."""
+    _args_here(args)
+    _check("switchsd_process_logits", lib.switchsd_process_logits(
+        ctypes.byref(args), _arr(out, "logits", "out", args.shape), _TYPES[out.dtype],
+        _stream(stream)))
+
+
+def switchsd_verify_processed(args, accept_len, accept_node, bonus, out_tokens, amax, workspace,
+                              stream=None):
+    _args_here(args)
+    B, R, _ = args.shape
+    _here(workspace, "workspace")
+    _check("switchsd_verify_processed", lib.switchsd_verify_processed(
+        ctypes.byref(args), _arr(accept_len, "i32", "accept_len", (B,)),
+        _arr(accept_node, "i32", "accept_node", (B,)), _arr(bonus, "i32", "bonus", (B,)),
+        _arr(out_tokens, "i32", "out_tokens", (B, R)), _arr(amax, "i32", "amax", (B, R), True),
+        _ptr(workspace, "u8", "workspace"), workspace.numel(), _stream(stream)))
+
+
+def build_page_args(lengths, dpar, dn, Lmax, page_size, table, held, ring, ring_state, slots,
+                    positions, missing, R=None):
+    """PageArgs for switchsd_page_plan: lengths, dn, held, missing [B], dpar
+    [B, R] (None: chains), table [B, max_pages], ring [ring_pages], ring_state [2]
+    int32; slots int64 and positions int32 [B, R] (None: not wanted; R then comes
+    from dpar or R).  The tensors are kept alive by the result."""
+    if not isinstance(table, _Tensor) or table.dim() != 2:
+        raise ValueError("table must be a device tensor [B, max_pages]")
+    for t in (slots, positions, dpar):
+        if R is None and isinstance(t, _Tensor) and t.dim() == 2:
+            R = t.shape[1]
+    if R is None:
+        raise ValueError("R is required")
+    B, most = table.shape
+    a = PageArgs()
+    a.B, a.R, a.Lmax, a.page_size, a.max_pages = B, R, int(Lmax), int(page_size), most
+    a.table = _arr(table, "i32", "table", (B, most))
+    for name, t in (("lengths", lengths), ("dn", dn), ("held", held), ("missing", missing)):
+        setattr(a, name, _arr(t, "i32", name, (B,)))
+    a.dpar = _arr(dpar, "i32", "dpar", (B, R), True)
+    if not isinstance(ring, _Tensor) or ring.dim() != 1:
+        raise ValueError("ring must be a device tensor [ring_pages]")
+    a.ring_pages = ring.shape[0]
+    a.ring = _arr(ring, "i32", "ring", (a.ring_pages,))
+    a.ring_state = _arr(ring_state, "i32", "ring_state", (2,))
+    a.slots = _arr(slots, "i64", "slots", (B, R), True)
+    a.positions = _arr(positions, "i32", "positions", (B, R), True)
+    a.device = table.get_device()
+    a.keep = (lengths, dpar, dn, table, held, ring, ring_state, slots, positions, missing)
+    return a
+
+
+def switchsd_page_plan(args, workspace, stream=None):
+    _args_here(args)
+    _here(workspace, "workspace")
+    _check("switchsd_page_plan", lib.switchsd_page_plan(
+        ctypes.byref(args), _ptr(workspace, "u8", "workspace"), workspace.numel(),
+        _stream(stream)))
+
+
+def switchsd_span_slots(begin, end, tokens, table, held, page_size, cu, slots, positions, packed,
+                        seq, stream=None):
+    """begin, end, held [B], tokens [B, Lmax], table [B, max_pages] int32; cu
+    [B + 1] int32, slots int64 and positions, packed, seq int32 of one length
+    (each None if not wanted)."""
+    B, Lmax = tokens.shape
+    if slots is not None and (table is None or held is None):
+        raise ValueError("slots need table and held")
+    most = table.shape[1] if slots is not None else 0
+    n = [t.shape[0] for t in (slots, positions, packed, seq) if t is not None]
+    cap = (n[0] if n else 0,)
+    _check("switchsd_span_slots", lib.switchsd_span_slots(
+        _arr(begin, "i32", "begin", (B,)), _arr(end, "i32", "end", (B,)),
+        _arr(tokens, "i32", "tokens", (B, Lmax)),
+        _arr(table, "i32", "table", (B, most), True) if most else None,
+        _arr(held, "i32", "held", (B,), True) if most else None, B, Lmax, most, int(page_size),
+        _arr(cu, "i32", "cu", (B + 1,)), _arr(slots, "i64", "slots", cap, True),
+        _arr(positions, "i32", "positions", cap, True),
+        _arr(packed, "i32", "packed", cap, True), _arr(seq, "i32", "seq", cap, True), cap[0],
+        _stream(stream)))
+
+
+def switchsd_compact_cache(cache, slots, dpar, dn, accept_node, stream=None):
+    """cache [planes, n_slots, ...] of any type, each plane contiguous; slots
+    [B, R] int64, dpar [B, R] (None: chains), dn, accept_node [B] int32."""
+    if not isinstance(cache, _Tensor) or not cache.is_cuda or cache.dim() < 2:
+        raise ValueError("cache must be a device tensor [planes, n_slots, ...]")
+    planes, n_slots = cache.shape[:2]
+    if not cache.is_contiguous() and not cache[0].is_contiguous():
+        raise ValueError("cache planes must be contiguous")
+    _here(cache, "cache")
+    B, R = slots.shape
+    row = cache.element_size() * (cache.numel() // (planes * n_slots) if cache.numel() else 0)
+    _check("switchsd_compact_cache", lib.switchsd_compact_cache(
+        cache.data_ptr(), planes, cache.stride(0) * cache.element_size(), n_slots, row,
+        _arr(slots, "i64", "slots", (B, R)), _arr(dpar, "i32", "dpar", (B, R), True),
+        _arr(dn, "i32", "dn", (B,)), _arr(accept_node, "i32", "accept_node", (B,)), B, R,
+        _stream(stream)))

@@ -955,3 +955,248 @@ int switchsd_tree_mask(const int32_t *dpar, const int32_t *dn, int32_t B, int32_
 }
 
 }  // extern "C"
+
+// ---- calls around the step
+
+namespace {
+
+size_t type_size(int32_t type) { return type == SWITCHSD_F32 ? 4 : 2; }
+
+// Work-groups of a launch: 256 lanes each, fewer than 2^32 lanes together.
+bool launch_ok(int64_t g) { return g >= 1 && g < (1 << 24); }
+
+bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+int check_logits(const switchsd_logits_args *a) {
+    if (!a)
+        return SWITCHSD_EINVAL;
+    if (a->logits_type < SWITCHSD_BF16 || a->logits_type > SWITCHSD_F32)
+        return SWITCHSD_EINVAL;
+    if (!shape_ok_B(a->B) || a->R < 1 || a->R > SWITCHSD_MAX_R || a->V < 1 || a->V > (1 << 28) ||
+        a->Lmax < 0 || a->Lmax > SWITCHSD_MAX_HISTORY || a->n_bias < 0 ||
+        a->n_bias > SWITCHSD_MAX_BIAS)
+        return SWITCHSD_ESHAPE;
+    if (a->B == 0)
+        return SWITCHSD_OK;
+    if (!a->logits || !aligned(a->logits, type_size(a->logits_type)) || !a->dtok || !a->dn)
+        return SWITCHSD_EINVAL;
+    const bool penal = a->repetition || a->frequency || a->presence;
+    if (penal && (!a->tokens || !a->lengths))
+        return SWITCHSD_EINVAL;
+    if (penal && a->Lmax < 1)
+        return SWITCHSD_ESHAPE;
+    if (a->n_bias > 0 && (!a->bias_ids || !a->bias_vals))
+        return SWITCHSD_EINVAL;
+    return SWITCHSD_OK;
+}
+
+// The grid of the logits kernels: a work-group per vocabulary chunk and group
+// of rows of one sequence, each of which counts the history's tokens in its
+// chunk anew.  Large chunks and many rows per work-group count least often;
+// both shrink while there are fewer than two work-groups per compute unit.
+int set_logits_grid(LogitsParams &p) {
+    int cus = 0;
+    const int rc = cu_count(&cus);
+    if (rc)
+        return rc;
+    const switchsd_logits_args &a = p.a;
+    const int64_t want = 2 * (int64_t)cus;
+    const int64_t per = a.logits_type == SWITCHSD_F32 ? 4 : 8;  // elements of a vector
+    p.penal = a.repetition || a.frequency || a.presence;
+    int64_t rows = a.R < kRowGroup ? a.R : kRowGroup;
+    int64_t groups = (a.R + rows - 1) / rows;
+    p.unroll = a.logits_type == SWITCHSD_F32 ? 8 : 4;
+    for (;; p.unroll >>= 1) {
+        const int64_t elems = (int64_t)kThreads * per * p.unroll;
+        p.chunks = (int32_t)((a.V + elems - 1) / elems);
+        if (p.unroll == 1 || (int64_t)a.B * groups * p.chunks >= want)
+            break;
+    }
+    if ((int64_t)a.B * groups * p.chunks < want) {
+        rows = (int64_t)a.B * a.R * p.chunks / want;
+        rows = rows < 1 ? 1 : rows > kRowGroup ? kRowGroup : rows;
+        groups = (a.R + rows - 1) / rows;
+    }
+    p.rows = (int32_t)rows;
+    p.groups = (int32_t)groups;
+    return launch_ok((int64_t)a.B * groups * p.chunks) ? SWITCHSD_OK : SWITCHSD_ESHAPE;
+}
+
+}  // namespace
+
+extern "C" {
+
+int switchsd_process_logits(const switchsd_logits_args *a, void *out, int32_t out_type,
+                            hipStream_t stream) {
+    int rc = check_logits(a);
+    if (rc)
+        return rc;
+    if (out_type != SWITCHSD_BF16 && out_type != a->logits_type)
+        return SWITCHSD_EINVAL;
+    if (a->B == 0)
+        return SWITCHSD_OK;
+    if (!out || !aligned(out, type_size(out_type)))
+        return SWITCHSD_EINVAL;
+    // out is logits itself, or apart from it
+    const uint64_t n = (uint64_t)a->B * a->R * a->V;
+    const uintptr_t i0 = (uintptr_t)a->logits, i1 = i0 + n * type_size(a->logits_type);
+    const uintptr_t o0 = (uintptr_t)out, o1 = o0 + n * type_size(out_type);
+    const bool same = i0 == o0 && out_type == a->logits_type;
+    if (!same && o0 < i1 && i0 < o1)
+        return SWITCHSD_EINVAL;
+    LogitsParams p;
+    memset(&p, 0, sizeof p);
+    p.a = *a;
+    p.out = out;
+    p.in_place = same ? 1 : 0;
+    if ((rc = set_logits_grid(p)))
+        return rc;
+    return launch_logits_kernel(p, out_type, stream);
+}
+
+int switchsd_verify_processed(const switchsd_logits_args *a, int32_t *accept_len,
+                              int32_t *accept_node, int32_t *bonus, int32_t *out_tokens,
+                              int32_t *amax, void *workspace, size_t workspace_bytes,
+                              hipStream_t stream) {
+    int rc = check_logits(a);
+    if (rc || a->B == 0)
+        return rc;
+    if (!accept_len || !accept_node || !bonus || !out_tokens)
+        return SWITCHSD_EINVAL;
+    if ((rc = check_workspace(workspace, workspace_bytes, a->B, a->R, 0, 0)))
+        return rc;
+    LogitsParams p;
+    memset(&p, 0, sizeof p);
+    p.a = *a;
+    p.accept_len = accept_len;
+    p.accept_node = accept_node;
+    p.bonus = bonus;
+    p.out_tokens = out_tokens;
+    p.amax = amax;
+    const Workspace w = carve(workspace, a->B, a->R, 0, 0);
+    p.keys = w.keys;
+    p.key_stride = w.key_stride;
+    p.tickets = w.tk_all;
+    if ((rc = set_logits_grid(p)))
+        return rc;
+    return launch_logits_kernel(p, SWITCHSD_BF16, stream);
+}
+
+int switchsd_page_plan(const switchsd_page_args *a, void *workspace, size_t workspace_bytes,
+                       hipStream_t stream) {
+    if (!a)
+        return SWITCHSD_EINVAL;
+    if (a->B < 0 || a->B > SWITCHSD_MAX_PLAN_B || a->R < 1 || a->R > SWITCHSD_MAX_R ||
+        a->Lmax < 1 || a->Lmax > (1 << 30) || a->page_size < 1 || a->page_size > 65536 ||
+        a->max_pages < 1 || a->ring_pages < 1 ||
+        (int64_t)a->max_pages * a->page_size > 0x7FFFFFFFll ||
+        (int64_t)a->B * a->max_pages > 0x7FFFFFFFll)
+        return SWITCHSD_ESHAPE;
+    if (a->B == 0)
+        return SWITCHSD_OK;
+    if (!a->lengths || !a->dn || !a->table || !a->held || !a->ring || !a->ring_state ||
+        !a->missing || !aligned(a->slots, 8))
+        return SWITCHSD_EINVAL;
+    int rc = check_workspace(workspace, workspace_bytes, a->B, 0, 0, 0);
+    if (rc)
+        return rc;
+    PageParams p;
+    memset(&p, 0, sizeof p);
+    p.lengths = a->lengths;
+    p.dpar = a->dpar;
+    p.dn = a->dn;
+    p.B = a->B;
+    p.R = a->R;
+    p.Lmax = a->Lmax;
+    p.page_size = a->page_size;
+    p.max_pages = a->max_pages;
+    p.ring_pages = a->ring_pages;
+    p.table = a->table;
+    p.held = a->held;
+    p.ring = a->ring;
+    p.ring_state = a->ring_state;
+    p.slots = a->slots;
+    p.positions = a->positions;
+    p.missing = a->missing;
+    p.seqs = kPlanNodes / a->R < kThreads ? kPlanNodes / a->R : kThreads;
+    p.ticket = carve(workspace, a->B, 0, 0, 0).tk_all;
+    return launch_page_plan_kernel(p, stream);
+}
+
+int switchsd_span_slots(const int32_t *begin, const int32_t *end, const int32_t *tokens,
+                        const int32_t *table, const int32_t *held, int32_t B, int32_t Lmax,
+                        int32_t max_pages, int32_t page_size, int32_t *cu, int64_t *slots,
+                        int32_t *positions, int32_t *packed, int32_t *seq, int32_t capacity,
+                        hipStream_t stream) {
+    if (B < 0 || B > SWITCHSD_MAX_PLAN_B || Lmax < 1 || Lmax > (1 << 30) ||
+        (int64_t)B * Lmax > 0x7FFFFFFFll || page_size < 1 || page_size > 65536 || capacity < 0 ||
+        (slots && (max_pages < 1 || (int64_t)B * max_pages > 0x7FFFFFFFll)))
+        return SWITCHSD_ESHAPE;
+    if (B == 0)
+        return SWITCHSD_OK;
+    if (!begin || !end || !cu || (packed && !tokens) || (slots && (!table || !held)) ||
+        !aligned(slots, 8))
+        return SWITCHSD_EINVAL;
+    SpanParams p;
+    memset(&p, 0, sizeof p);
+    p.begin = begin;
+    p.end = end;
+    p.tokens = tokens;
+    p.table = table;
+    p.held = held;
+    p.B = B;
+    p.Lmax = Lmax;
+    p.max_pages = max_pages;
+    p.page_size = page_size;
+    p.cu = cu;
+    p.slots = slots;
+    p.positions = positions;
+    p.packed = packed;
+    p.seq = seq;
+    p.capacity = capacity;
+    // every work-group sums the sizes of all earlier sequences
+    p.seqs = (B + 2047) / 2048;
+    p.parts = (Lmax + kSpanPart - 1) / kSpanPart;
+    return launch_span_kernel(p, stream);
+}
+
+int switchsd_compact_cache(void *cache, int32_t planes, int64_t plane_stride, int64_t n_slots,
+                           int32_t row_bytes, const int64_t *slots, const int32_t *dpar,
+                           const int32_t *dn, const int32_t *accept_node, int32_t B, int32_t R,
+                           hipStream_t stream) {
+    if (!shape_ok_B(B) || R < 1 || R > SWITCHSD_MAX_R || planes < 0 || n_slots < 0 ||
+        row_bytes < 0 || (row_bytes > 0 && n_slots > INT64_MAX / row_bytes))
+        return SWITCHSD_ESHAPE;
+    if (row_bytes % 4 != 0 || (planes > 1 && plane_stride % 4 != 0))
+        return SWITCHSD_EINVAL;
+    if (planes > 1 && plane_stride < n_slots * row_bytes)
+        return SWITCHSD_ESHAPE;
+    if (B == 0 || planes == 0 || n_slots == 0 || row_bytes == 0)
+        return SWITCHSD_OK;
+    if (!cache || !aligned(cache, 4) || !slots || !aligned(slots, 8) || !dn || !accept_node)
+        return SWITCHSD_EINVAL;
+    if (!dpar)
+        return SWITCHSD_OK;  // chains are in place
+    CompactParams p;
+    memset(&p, 0, sizeof p);
+    const bool wide = aligned(cache, 16) && row_bytes % 16 == 0 &&
+                      (planes == 1 || plane_stride % 16 == 0);
+    p.cache = cache;
+    p.plane_stride = plane_stride;
+    p.n_slots = n_slots;
+    p.row_vecs = row_bytes / (wide ? 16 : 4);
+    p.pieces = (int64_t)planes * p.row_vecs;
+    p.slots = slots;
+    p.dpar = dpar;
+    p.dn = dn;
+    p.accept_node = accept_node;
+    p.B = B;
+    p.R = R;
+    const int64_t blocks = (p.pieces + kThreads - 1) / kThreads;
+    if (!launch_ok(blocks) || !launch_ok((int64_t)B * blocks))
+        return SWITCHSD_ESHAPE;
+    p.blocks = (int32_t)blocks;
+    return launch_compact_kernel(p, wide, stream);
+}
+
+}  // extern "C"

@@ -195,4 +195,69 @@ int launch_status_kernel(int32_t *mslot, int32_t B, int32_t *out, hipStream_t st
 int launch_tree_mask_kernel(const int32_t *dpar, const int32_t *dn, int32_t B, int32_t R,
                             uint32_t *mask, hipStream_t stream);
 
+// ---- calls around the step (switchsd_logits.hip, switchsd_pages.hip)
+
+// Rows a work-group of the logits kernels takes, at most (one wave handles a
+// row's result per lane).
+constexpr int kRowGroup = 64;
+
+// Drafted rows a work-group of the page plan takes, at most (one sequence at
+// least), and positions of a range that one of the packed slots takes.
+constexpr int kPlanNodes = 1024;
+constexpr int kSpanPart = 1024;
+static_assert(kPlanNodes >= SWITCHSD_MAX_R, "a plan work-group holds a sequence's rows");
+
+struct LogitsParams {
+    switchsd_logits_args a;
+    void *out;          // process: the processed logits; verify: null
+    int32_t in_place;   // out is logits: only what changes is written
+    int32_t penal;      // any of the three penalties
+    // grid: [sequence][row group][vocabulary chunk]
+    int32_t unroll;     // 16-byte vectors per lane and row
+    int32_t chunks;     // vocabulary chunks
+    int32_t rows;       // rows per group (at most kRowGroup)
+    int32_t groups;
+    // verify
+    int32_t *accept_len, *accept_node, *bonus, *out_tokens, *amax;
+    unsigned long long *keys;  // [B] x key_stride row maxima
+    int32_t key_stride;
+    uint32_t *tickets;         // [B] x kLineU32
+};
+
+struct PageParams {
+    const int32_t *lengths, *dpar, *dn;
+    int32_t B, R, Lmax, page_size, max_pages, ring_pages;
+    int32_t *table, *held, *ring, *ring_state;
+    int64_t *slots;
+    int32_t *positions, *missing;
+    int32_t seqs;      // sequences per work-group
+    uint32_t *ticket;
+};
+
+struct SpanParams {
+    const int32_t *begin, *end, *tokens, *table, *held;
+    int32_t B, Lmax, max_pages, page_size;
+    int32_t *cu;
+    int64_t *slots;
+    int32_t *positions, *packed, *seq;
+    int32_t capacity;
+    int32_t seqs, parts;  // sequences per work-group, parts of a range
+};
+
+struct CompactParams {
+    void *cache;
+    int64_t plane_stride, n_slots;
+    int32_t row_vecs;    // pieces per row (16 or 4 bytes each)
+    int64_t pieces;      // planes * row_vecs
+    const int64_t *slots;
+    const int32_t *dpar, *dn, *accept_node;
+    int32_t B, R;
+    int32_t blocks;      // work-groups per sequence
+};
+
+int launch_logits_kernel(const LogitsParams &p, int32_t out_type, hipStream_t stream);
+int launch_page_plan_kernel(const PageParams &p, hipStream_t stream);
+int launch_span_kernel(const SpanParams &p, hipStream_t stream);
+int launch_compact_kernel(const CompactParams &p, bool wide, hipStream_t stream);
+
 }  // namespace switchsd

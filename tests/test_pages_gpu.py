@@ -1,0 +1,248 @@
+"""Pages, slots and cache rows around the step (switchsd_page_plan,
+switchsd_span_slots, switchsd_compact_cache) against plain loops, exactly."""
+import numpy as np
+import pytest
+import torch
+
+import engine_ref as ref
+from gpu_helpers import say
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2609_20186_amd import binding  # noqa: F401
+
+
+def draft(rng, B, R, kind, k=5):
+    i = np.arange(R)
+    if kind == "chain":
+        return None
+    if kind == "candidates":
+        par = np.tile(np.where((i - 1) % k == 0, 0, i - 1), (B, 1)).astype(np.int32)
+    elif kind == "long":                                # a chain given by its parents
+        par = np.tile(i - 1, (B, 1)).astype(np.int32)
+    else:
+        par = (rng.random((B, R)) * i).astype(np.int32)
+        bad = rng.random((B, R)) < 0.1
+        par[bad] = rng.integers(-3, R + 3, int(bad.sum()))
+    par[:, 0] = -1
+    return par
+
+
+def plan_state(B, R, Lmax, page, kind, seed, spare):
+    rng = np.random.default_rng(seed)
+    most = (Lmax + R + page - 1) // page
+    most = max(1, most - (seed % 2))                    # sometimes a page short
+    P = max(1, B * most // 2 + spare)
+    s = {"B": B, "R": R, "Lmax": Lmax, "page": page, "dpar": draft(rng, B, R, kind),
+         "lengths": np.zeros(B, np.int32), "dn": np.zeros(B, np.int32),
+         "table": np.full((B, most), -1, np.int32), "held": np.zeros(B, np.int32),
+         "ring": rng.permutation(P).astype(np.int32),
+         "ring_state": np.array([rng.integers(0, P), P], np.int32)}
+    return s, rng
+
+
+def device_plan(s):
+    from paper_2609_20186_amd import binding as sd
+    t = {k: None if v is None else torch.from_numpy(v.copy()).cuda()
+         for k, v in s.items() if not isinstance(v, int)}
+    B, R = s["B"], s["R"]
+    t["slots"] = torch.full((B, R), -7, dtype=torch.int64, device="cuda")
+    t["positions"] = torch.full((B, R), -7, dtype=torch.int32, device="cuda")
+    t["missing"] = torch.full((B,), -7, dtype=torch.int32, device="cuda")
+    args = sd.build_page_args(t["lengths"], t["dpar"], t["dn"], s["Lmax"], s["page"], t["table"],
+                              t["held"], t["ring"], t["ring_state"], t["slots"], t["positions"],
+                              t["missing"])
+    return t, args, sd.alloc_workspace(B, 0)
+
+
+def compare_plan(s, t, res, what):
+    for name, want in list(zip(("slots", "positions", "missing"), res)) + [
+            (n, s[n]) for n in ("table", "held", "ring_state", "ring")]:
+        np.testing.assert_array_equal(t[name].cpu().numpy(), want, err_msg=f"{what}: {name}")
+
+
+@pytest.mark.parametrize("B,R,Lmax,page,kind,spare", [
+    (1, 1, 1, 1, "chain", 3), (1, 1, 40, 16, "chain", 0), (5, 8, 100, 16, "chain", 0),
+    (5, 8, 100, 16, "tree", 40), (3, 201, 500, 7, "candidates", 100), (40, 60, 300, 1, "tree", 0),
+    (300, 3, 64, 16, "tree", 9), (700, 1, 33, 3, "chain", 50), (2, 1024, 90, 64, "long", 20),
+    (33, 100, 2000, 256, "tree", 4),
+])
+def test_plan_over_steps(B, R, Lmax, page, kind, spare):
+    """A few dozen calls on living state: sequences arrive, grow, finish and
+    come back, the ring wraps around and sometimes runs out."""
+    from paper_2609_20186_amd import binding as sd
+    say(f"[plan] {B} {R} {Lmax} {page} {kind}")
+    s, rng = plan_state(B, R, Lmax, page, kind, B + R, spare)
+    t, args, ws = device_plan(s)
+    short = 0
+    for step in range(30):
+        L = s["lengths"]
+        L[:] = np.minimum(L + rng.integers(1, max(2, Lmax // 8), B), Lmax + 5)
+        L[rng.random(B) < 0.15] = 0
+        L[rng.random(B) < 0.05] = -3
+        s["dn"][:] = rng.integers(0, R + 2, B)
+        t["lengths"].copy_(torch.from_numpy(L))
+        t["dn"].copy_(torch.from_numpy(s["dn"]))
+        res = ref.page_plan(s)
+        sd.switchsd_page_plan(args, ws)
+        compare_plan(s, t, res, f"step {step}")
+        short += int((res[2] > 0).sum())
+        assert int(ws.count_nonzero()) == 0
+    say(f"[plan] sequences short of pages: {short}")
+    live = sorted(s["table"][b, j] for b in range(B) for j in range(s["held"][b]))
+    free = [s["ring"][(s["ring_state"][0] + i) % len(s["ring"])]
+            for i in range(s["ring_state"][1])]
+    assert sorted(live + free) == sorted(range(len(s["ring"])))   # no page lost or doubled
+
+
+def test_plan_clamps_its_state():
+    """held and the ring's state out of range stay inside the buffers."""
+    from paper_2609_20186_amd import binding as sd
+    say("[plan] clamps")
+    s, rng = plan_state(6, 4, 50, 8, "tree", 2, 0)
+    s["held"][:] = [-4, 99, 3, 0, 1, 2]
+    s["table"][:] = rng.integers(0, 1000, s["table"].shape)
+    s["lengths"][:] = [9, 20, 0, 50, 77, 1]
+    s["dn"][:] = 3
+    for state in ([-5, 4], [2, 1 << 30], [1 << 30, -1], [0, len(s["ring"])]):
+        s["ring_state"][:] = state
+        t, args, ws = device_plan(s)
+        res = ref.page_plan(s)
+        sd.switchsd_page_plan(args, ws)
+        compare_plan(s, t, res, str(state))
+
+
+def test_plan_captured():
+    from paper_2609_20186_amd import binding as sd
+    say("[plan] graph")
+    s, rng = plan_state(9, 6, 200, 16, "tree", 4, 30)
+    t, args, ws = device_plan(s)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        sd.switchsd_page_plan(args, ws, side)
+    for step in range(6):
+        s["lengths"][:] = np.minimum(s["lengths"] + rng.integers(1, 30, 9), 200)
+        s["lengths"][rng.random(9) < 0.2] = 0
+        s["dn"][:] = rng.integers(1, 7, 9)
+        t["lengths"].copy_(torch.from_numpy(s["lengths"]))
+        t["dn"].copy_(torch.from_numpy(s["dn"]))
+        res = ref.page_plan(s)
+        graph.replay()
+        torch.cuda.synchronize()
+        compare_plan(s, t, res, f"replay {step}")
+
+
+def test_plan_outputs_left_out():
+    from paper_2609_20186_amd import binding as sd
+    say("[plan] without slots and positions")
+    s, rng = plan_state(5, 8, 100, 16, "tree", 8, 10)
+    s["lengths"][:] = rng.integers(0, 100, 5)
+    s["dn"][:] = 8
+    t, _, ws = device_plan(s)
+    args = sd.build_page_args(t["lengths"], t["dpar"], t["dn"], 100, 16, t["table"], t["held"],
+                              t["ring"], t["ring_state"], None, None, t["missing"])
+    slots, positions, missing = ref.page_plan(s)
+    sd.switchsd_page_plan(args, ws)
+    minus = np.full((5, 8), -7)
+    compare_plan(s, t, (minus, minus, missing), "left out")
+
+
+@pytest.mark.parametrize("B,Lmax,page,most_short", [(1, 1, 1, 0), (4, 50, 16, 0), (3, 5000, 7, 2),
+                                                    (300, 40, 16, 1), (2500, 9, 4, 0)])
+def test_spans(B, Lmax, page, most_short):
+    from paper_2609_20186_amd import binding as sd
+    say(f"[spans] {B} {Lmax} {page}")
+    rng = np.random.default_rng(B + Lmax)
+    most = max(1, (Lmax + page - 1) // page - most_short)
+    tokens = rng.integers(-1, 1000, (B, Lmax)).astype(np.int32)
+    table = rng.integers(0, 2 ** 31 - 1, (B, most)).astype(np.int32)
+    held = rng.integers(-1, most + 3, B).astype(np.int32)
+    end = rng.integers(-2, Lmax + 4, B).astype(np.int32)
+    begin = (end - rng.integers(-1, Lmax + 2, B)).astype(np.int32)
+    cu, rec = ref.spans(begin, end, tokens, table, held, page, 1 << 40)
+    dev = [torch.from_numpy(x).cuda() for x in (begin, end, tokens, table, held)]
+    for cap in (len(rec) + 9, len(rec), max(1, len(rec) // 2)):
+        c = torch.full((B + 1,), -7, dtype=torch.int32, device="cuda")
+        o = [torch.full((cap,), -7, dtype=dt, device="cuda")
+             for dt in (torch.int64, torch.int32, torch.int32, torch.int32)]
+        sd.switchsd_span_slots(*dev, page, c, *o)
+        np.testing.assert_array_equal(c.cpu().numpy(), cu)
+        want = np.array(rec[:cap], np.int64).reshape(-1, 4)
+        for j, t in enumerate(o):
+            got = t.cpu().numpy()
+            np.testing.assert_array_equal(got[:len(want)], want[:, j], err_msg=f"{cap} {j}")
+            assert (got[len(want):] == -7).all()        # behind the last: as they were
+    c.fill_(-7)                                          # only some of the outputs
+    sd.switchsd_span_slots(*dev, page, c, None, o[1], None, None)
+    np.testing.assert_array_equal(c.cpu().numpy(), cu)
+
+
+@pytest.mark.parametrize("B,R,kind,planes,row,dtype", [
+    (1, 1, "tree", 1, 8, torch.bfloat16), (3, 9, "tree", 4, 64, torch.bfloat16),
+    (5, 60, "tree", 3, 130, torch.float16), (4, 201, "candidates", 2, 512, torch.bfloat16),
+    (2, 1024, "tree", 1, 16, torch.float32), (6, 30, "long", 5, 33, torch.float32),
+    (3, 40, "tree", 7, 1004, torch.uint8),
+])
+def test_compact(B, R, kind, planes, row, dtype):
+    from paper_2609_20186_amd import binding as sd
+    say(f"[compact] {B} {R} {kind} {planes} {row}")
+    rng = np.random.default_rng(B * R + row)
+    par = draft(rng, B, R, kind)
+    n_slots = B * R + 7
+    for trial in range(4):
+        slots = rng.permutation(n_slots)[:B * R].reshape(B, R).astype(np.int64)
+        drop = rng.random((B, R)) < 0.03
+        slots[drop] = rng.choice([-1, n_slots, 1 << 40], int(drop.sum()))
+        dn = rng.integers(0, R + 2, B).astype(np.int32)
+        node = rng.integers(-1, R + 1, B).astype(np.int32)
+        raw = rng.integers(0, 120, (planes, n_slots, row)).astype(np.float32)
+        want = raw.copy()
+        ref.compact(want, slots, par, dn, node)
+        # planes apart from each other: a slice of a wider tensor
+        wide = torch.zeros((planes, n_slots + 4, row), dtype=dtype, device="cuda")
+        cache = wide[:, :n_slots]
+        cache.copy_(torch.from_numpy(raw))
+        sd.switchsd_compact_cache(cache, *(torch.from_numpy(x).cuda()
+                                           for x in (slots, par, dn, node)))
+        np.testing.assert_array_equal(cache.float().cpu().numpy(), want)
+        assert float(wide[:, n_slots:].float().abs().sum()) == 0.0
+
+
+def test_compact_beyond_4_gib():
+    """Slots whose rows lie beyond 2^32 bytes of a plane."""
+    from paper_2609_20186_amd import binding as sd
+    say("[compact] large offsets")
+    n_slots, row = (1 << 22) + 100, 1040                 # 4.4e9 bytes a plane
+    cache = torch.zeros((2, n_slots, row), dtype=torch.uint8, device="cuda")
+    par = np.array([[-1, 0, 0, 2, 3]], np.int32)         # accepted: 2, 3, 4
+    slots = torch.tensor([[5, n_slots - 1, n_slots - 2, 7, n_slots - 4]], dtype=torch.int64)
+    for p in range(2):
+        for j in range(5):
+            cache[p, slots[0, j]] = 10 * p + j + 1
+    sd.switchsd_compact_cache(cache, slots.cuda(), torch.from_numpy(par).cuda(),
+                              torch.tensor([5], dtype=torch.int32, device="cuda"),
+                              torch.tensor([4], dtype=torch.int32, device="cuda"))
+    for p in range(2):
+        got = [int(cache[p, slots[0, j], c]) for j in range(5) for c in (0, row - 1)]
+        assert got == [10 * p + v + 1 for v in (0, 0, 2, 2, 3, 3, 4, 4, 4, 4)]
+
+
+def test_compact_chains_move_nothing():
+    from paper_2609_20186_amd import binding as sd
+    say("[compact] chains")
+    cache = torch.randn((2, 40, 8), device="cuda")
+    before = cache.clone()
+    slots = torch.arange(40, device="cuda").view(4, 10)
+    dn = torch.full((4,), 10, dtype=torch.int32, device="cuda")
+    node = torch.tensor([0, 3, 9, 5], dtype=torch.int32, device="cuda")
+    sd.switchsd_compact_cache(cache, slots, None, dn, node)
+    par = torch.arange(-1, 9, dtype=torch.int32, device="cuda").repeat(4, 1)
+    sd.switchsd_compact_cache(cache, slots, par, dn, node)
+    assert torch.equal(cache, before)

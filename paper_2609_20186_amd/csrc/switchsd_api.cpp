@@ -993,22 +993,25 @@ int check_logits(const switchsd_logits_args *a) {
 // The grid of the logits kernels: a work-group per vocabulary chunk and group
 // of rows of one sequence, each of which counts the history's tokens in its
 // chunk anew.  Large chunks and many rows per work-group count least often;
-// both shrink while there are fewer than two work-groups per compute unit.
+// both shrink while there are too few work-groups.
 int set_logits_grid(LogitsParams &p) {
     int cus = 0;
     const int rc = cu_count(&cus);
     if (rc)
         return rc;
     const switchsd_logits_args &a = p.a;
-    const int64_t want = 2 * (int64_t)cus;
-    const int64_t per = a.logits_type == SWITCHSD_F32 ? 4 : 8;  // elements of a vector
+    const int64_t want = 4 * (int64_t)cus;
+    const int64_t blk = a.logits_type == SWITCHSD_F32 ? 256 : 512;  // tokens of 64 vectors
+    const int64_t blocks = (a.V + blk - 1) / blk;
     p.penal = a.repetition || a.frequency || a.presence;
     int64_t rows = a.R < kRowGroup ? a.R : kRowGroup;
     int64_t groups = (a.R + rows - 1) / rows;
-    p.unroll = a.logits_type == SWITCHSD_F32 ? 8 : 4;
-    for (;; p.unroll >>= 1) {
-        const int64_t elems = (int64_t)kThreads * per * p.unroll;
-        p.chunks = (int32_t)((a.V + elems - 1) / elems);
+    for (p.unroll = kLogitsUnroll;; p.unroll >>= 1) {
+        const int64_t per = (int64_t)(kThreads / 64) * p.unroll;  // blocks of a chunk, at most
+        p.chunk_log = 0;
+        while (((int64_t)1 << p.chunk_log) * per < blocks)
+            ++p.chunk_log;
+        p.chunks = 1 << p.chunk_log;
         if (p.unroll == 1 || (int64_t)a.B * groups * p.chunks >= want)
             break;
     }

@@ -200,6 +200,8 @@ int launch_tree_mask_kernel(const int32_t *dpar, const int32_t *dn, int32_t B, i
 // Rows a work-group of the logits kernels takes, at most (one wave handles a
 // row's result per lane).
 constexpr int kRowGroup = 64;
+// 16-byte vectors per lane and row of the logits kernels, at most.
+constexpr int kLogitsUnroll = 2;
 
 // Drafted rows a work-group of the page plan takes, at most (one sequence at
 // least), and positions of a range that one of the packed slots takes.
@@ -214,7 +216,8 @@ struct LogitsParams {
     int32_t penal;      // any of the three penalties
     // grid: [sequence][row group][vocabulary chunk]
     int32_t unroll;     // 16-byte vectors per lane and row
-    int32_t chunks;     // vocabulary chunks
+    int32_t chunks;     // vocabulary chunks: a power of two, 2^chunk_log
+    int32_t chunk_log;
     int32_t rows;       // rows per group (at most kRowGroup)
     int32_t groups;
     // verify

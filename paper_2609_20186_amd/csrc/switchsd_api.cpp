@@ -1001,13 +1001,13 @@ int set_logits_grid(LogitsParams &p) {
         return rc;
     const switchsd_logits_args &a = p.a;
     const int64_t want = 4 * (int64_t)cus;
-    const int64_t blk = a.logits_type == SWITCHSD_F32 ? 256 : 512;  // tokens of 64 vectors
+    const int64_t blk = a.logits_type == SWITCHSD_F32 ? 64 : 128;  // tokens of 16 vectors
     const int64_t blocks = (a.V + blk - 1) / blk;
     p.penal = a.repetition || a.frequency || a.presence;
     int64_t rows = a.R < kRowGroup ? a.R : kRowGroup;
     int64_t groups = (a.R + rows - 1) / rows;
     for (p.unroll = kLogitsUnroll;; p.unroll >>= 1) {
-        const int64_t per = (int64_t)(kThreads / 64) * p.unroll;  // blocks of a chunk, at most
+        const int64_t per = (int64_t)(kThreads / 16) * p.unroll;  // blocks of a chunk, at most
         p.chunk_log = 0;
         while (((int64_t)1 << p.chunk_log) * per < blocks)
             ++p.chunk_log;

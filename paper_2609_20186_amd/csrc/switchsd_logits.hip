@@ -5,13 +5,17 @@
 // A work-group takes one chunk of the vocabulary and a group of rows of one
 // sequence.  It first makes a word per token of the chunk in LDS (how often the
 // history holds it, whether the prompt does, its first draft node, the bias
-// entry that names it) and lists the tokens that have one.  Then it streams the
-// chunk of each of its rows, two rows ahead: 16-byte vectors that hold a listed
-// token pass through LDS, where the list's tokens are computed one per lane.
-// All others pass as they are, so the work per row is the row's bytes plus the
-// listed tokens, however they lie.
+// entry that names it) and lists the tokens that have one (list_tokens).  Then it
+// streams the chunk of each of its rows, two rows ahead.
+//   k_process: vectors that hold a listed token pass through LDS, where the
+//     listed tokens are computed one per lane; all others pass as they are.
+//   k_verify: the rows' maxima are taken over the vectors without their listed
+//     tokens, which are read and computed one per lane beside them; nothing is
+//     exchanged between the waves until the rows are done.
+// So the work per row is the row's bytes plus the listed tokens, however they
+// lie.
 //
-// A chunk is every chunks-th block of 64 vectors: low token ids, which are the
+// A chunk is every 2^k-th block of 16 vectors: low token ids, which are the
 // frequent ones, spread over all work-groups of a row.
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
@@ -125,9 +129,10 @@ struct Elem<SWITCHSD_F32> {
 // LDS of a work-group, carved from one array.
 struct Lds {
     uint32_t *word;   // [tokens]
-    void *stage;      // [tokens] of the input's type: vectors with listed tokens
+    void *stage;      // process: [tokens] of the input's type, vectors with listed tokens;
+                      // verify: [rows][kWaves] the vector with the wave's maximum
     uint16_t *list;   // [tokens] the tokens that have a word
-    uint32_t *key;    // [rows][kWaves] row maxima (verify)
+    uint32_t *key;    // [rows][kWaves] maxima over the vectors, then over the listed tokens
     float *bias;      // [n_bias]
     uint32_t *entry;  // [R] drafted tokens of the chunk: token << kNodeBits | node
     uint32_t *count;  // [R] count and prompt bit of a drafted token, at its first entry
@@ -138,22 +143,27 @@ struct Lds {
 
 constexpr size_t kEpiBytesPerNode = 20;
 
+__host__ __device__ inline size_t stage_bytes(int tokens, int size, int rows, bool verify) {
+    return verify ? (size_t)rows * kWaves * 16 : (size_t)tokens * size;
+}
+
 __host__ __device__ inline size_t lds_bytes(int tokens, int size, int R, int rows, int n_bias,
                                             bool verify) {
-    const size_t n = (size_t)tokens * (4 + size + 2) + (size_t)rows * kWaves * 4 +
-                     (size_t)n_bias * 4 + (size_t)R * 12 + (size_t)rows * ((R + 31) / 32) * 4;
+    const size_t n = (size_t)tokens * 6 + stage_bytes(tokens, size, rows, verify) +
+                     (verify ? (size_t)rows * kWaves * 8 : 0) + (size_t)n_bias * 4 +
+                     (size_t)R * 12 + (size_t)rows * ((R + 31) / 32) * 4;
     const size_t epi = verify ? R * kEpiBytesPerNode : 0;
     return n > epi ? n : epi;
 }
 
 __device__ __forceinline__ Lds lds_carve(unsigned char *m, int tokens, int size, int R, int rows,
-                                         int n_bias) {
+                                         int n_bias, bool verify) {
     Lds l;
     l.word = (uint32_t *)m;
     l.stage = l.word + tokens;
-    l.list = (uint16_t *)((unsigned char *)l.stage + tokens * size);
+    l.list = (uint16_t *)((unsigned char *)l.stage + stage_bytes(tokens, size, rows, verify));
     l.key = (uint32_t *)(l.list + tokens);
-    l.bias = (float *)(l.key + rows * kWaves);
+    l.bias = (float *)(l.key + (verify ? 2 * rows * kWaves : 0));
     l.entry = (uint32_t *)(l.bias + n_bias);
     l.count = l.entry + R;
     l.anc = l.count + R;
@@ -272,269 +282,396 @@ __device__ __forceinline__ uint32_t keep16(uint32_t x, uint32_t ok, int q, uint3
     return (x & m) | (fill & ~m);
 }
 
-// One lane's part of a row: kU vectors and the allowed bits of their tokens.
+// What a work-group and its lanes have to do.
+template <int kIn, int kU>
+struct Tile {
+    typedef Elem<kIn> In;
+    static constexpr int kPer = In::per;
+    static constexpr int kBits = 128 / kPer;                  // of an element
+    static constexpr int kBlkLog = kPer == 8 ? 7 : 6;         // tokens of a block: 16 vectors
+    static constexpr int kTokens = kThreads * kU * kPer;      // of a chunk
+    static constexpr uint32_t kAll = (1u << kPer) - 1u;
+
+    uint32_t chunk;
+    int chunk_log, b, n, r0, r1, aw;
+    bool masked;
+    // this lane's vectors: first token, which of its tokens exist, and where it
+    // is read (the row's last whole vector where fewer exist)
+    int v0[kU], at[kU];
+    uint32_t own[kU];
+
+    __device__ __forceinline__ void init(const LogitsParams &p) {
+        chunk_log = p.chunk_log;
+        chunk = blockIdx.x & ((uint32_t)p.chunks - 1u);
+        const int gb = blockIdx.x >> chunk_log;
+        const int group = gb % p.groups;
+        b = gb / p.groups;
+        r0 = group * p.rows;
+        aw = (p.a.R + 31) / 32;
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            v0[u] = (int)token((uint32_t)(u * kThreads + threadIdx.x) * kPer);
+            const int left = p.a.V - v0[u];
+            own[u] = left >= kPer ? kAll : left > 0 ? (1u << left) - 1u : 0u;
+            at[u] = v0[u] < p.a.V - kPer ? v0[u] : p.a.V - kPer;
+        }
+    }
+    // the rows, once the draft's length is needed; false: none to do
+    __device__ __forceinline__ bool rows(const LogitsParams &p) {
+        n = clampi(p.a.dn[b], 1, p.a.R);
+        r1 = r0 + p.rows < n ? r0 + p.rows : n;
+        masked = p.a.allowed && (!p.a.allowed_on || p.a.allowed_on[b] != 0);
+        return r0 < n;
+    }
+    // the token at place `off` of the chunk (tokens ascend with the places)
+    __device__ __forceinline__ uint32_t token(uint32_t off) const {
+        const uint32_t blk = ((off >> kBlkLog) << chunk_log) | chunk;
+        return (blk << kBlkLog) | (off & ((1u << kBlkLog) - 1u));
+    }
+    // a token's place in the chunk, if it has one
+    __device__ __forceinline__ bool place(int32_t t, int V, uint32_t &off) const {
+        const uint32_t blk = (uint32_t)t >> kBlkLog;
+        off = ((blk >> chunk_log) << kBlkLog) | ((uint32_t)t & ((1u << kBlkLog) - 1u));
+        return (uint32_t)t < (uint32_t)V && ((blk ^ chunk) & ((1u << chunk_log) - 1u)) == 0u;
+    }
+};
+
+// One lane's part of a row: kU vectors, and the bytes with the allowed bits of
+// their tokens.
 template <int kU>
 struct RowRegs {
     u32x4 x[kU];
-    uint32_t ok[kU];
+    uint32_t bits[kU];
 };
 
+// Requests row r.  The requests are unconditional, so that a wait for one row's
+// leaves the later rows' in flight: behind the last row every lane reads that
+// row's first vector, and without a mask the first byte of the logits.
 // kTiny: V below one vector's tokens (read one by one).
-template <int kIn, int kOut, int kU, bool kVerify, bool kTiny>
-__global__ __launch_bounds__(kThreads) void k_logits(LogitsParams p) {
-    typedef Elem<kIn> In;
-    typedef Elem<kOut> Out;
-    constexpr int kPer = In::per;
-    constexpr int kBits = 128 / kPer;                  // of an element
-    constexpr int kBlk = 64 * kPer;                    // tokens of a block
-    constexpr int kBlkLog = kPer == 8 ? 9 : 8;
-    constexpr int kTokens = kWaves * kU * kBlk;        // of a chunk
-    constexpr uint32_t kAll = (1u << kPer) - 1u;
-    extern __shared__ __align__(16) unsigned char mem[];
-    __shared__ int s_entries, s_last, s_sum[kWaves];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const uint32_t cmask = (uint32_t)p.chunks - 1u;
-    const uint32_t chunk = blockIdx.x & cmask;
-    const int gb = blockIdx.x >> p.chunk_log;
-    const int group = gb % p.groups, b = gb / p.groups;
-    const int R = p.a.R, V = p.a.V;
-    const int n = clampi(p.a.dn[b], 1, R);
-    const int r0 = group * p.rows;
-    if (r0 >= n)
-        return;
-    const int r1 = r0 + p.rows < n ? r0 + p.rows : n;
-    const int aw = (R + 31) / 32;
-    const Lds s = lds_carve(mem, kTokens, sizeof(typename In::type), R, p.rows, p.a.n_bias);
-    const bool masked = p.a.allowed && (!p.a.allowed_on || p.a.allowed_on[b] != 0);
-    const int64_t mstride = (int64_t)((V + 31) / 32) * 4;
-
-    // ---- this lane's vectors: first token, how many of its tokens exist, and
-    // where it is read (the row's last whole vector where fewer exist)
-    int v0[kU], at[kU];
-    uint32_t own[kU];
+template <int kIn, int kU, bool kMask, bool kTiny>
+__device__ __forceinline__ void load_row(const LogitsParams &p, const Tile<kIn, kU> &t, int r,
+                                         RowRegs<kU> &g) {
+    typedef Tile<kIn, kU> T;
+    typedef typename T::In::type E;
+    const int V = p.a.V;
+    const bool live = r < t.r1;
+    const int64_t row = (int64_t)t.b * p.a.R + (live ? r : t.r1 - 1);
+    const E *src = (const E *)p.a.logits + row * V;
+    const bool use = live && t.masked;
+    const uint8_t *bits = use ? (const uint8_t *)p.a.allowed + row * ((int64_t)((V + 31) / 32) * 4)
+                              : (const uint8_t *)p.a.logits;
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-        const uint32_t blk = ((uint32_t)(u * kWaves + wave) << p.chunk_log) | chunk;
-        v0[u] = (int)(blk * kBlk) + lane * kPer;
-        const int left = V - v0[u];
-        own[u] = left >= kPer ? kAll : left > 0 ? (1u << left) - 1u : 0u;
-        at[u] = v0[u] < V - kPer ? v0[u] : V - kPer;
-    }
-    const int tail = V % kPer;  // tokens of the row's last, partial vector
-
-    auto load_row = [&](RowRegs<kU> &g, int r) {
-        const int64_t row = (int64_t)b * R + r;
-        const typename In::type *src = (const typename In::type *)p.a.logits + row * V;
-        const uint8_t *bits = (const uint8_t *)p.a.allowed + row * mstride;
+        if constexpr (kTiny) {
+            union {
+                E e[T::kPer];
+                u32x4 v;
+            } x;
 #pragma unroll
-        for (int u = 0; u < kU; ++u) {
-            if constexpr (kTiny) {
-                union {
-                    typename In::type e[kPer];
-                    u32x4 v;
-                } t;
-#pragma unroll
-                for (int j = 0; j < kPer; ++j)
-                    t.e[j] = src[v0[u] + j < V ? v0[u] + j : 0];
-                g.x[u] = t.v;
-            } else {
-                g.x[u] = __builtin_nontemporal_load((const u32x4_a *)(src + at[u]));
-            }
-            g.ok[u] = kAll;
-            if (masked)
-                g.ok[u] = (uint32_t)bits[(v0[u] < V ? v0[u] : 0) >> 3] >> (v0[u] & 7);
+            for (int j = 0; j < T::kPer; ++j)
+                x.e[j] = src[t.v0[u] + j < V ? t.v0[u] + j : 0];
+            g.x[u] = x.v;
+        } else {
+            const uint32_t o = live ? (uint32_t)t.at[u] * (uint32_t)sizeof(E) : 0u;
+            g.x[u] = __builtin_nontemporal_load((const u32x4_a *)((const char *)src + o));
         }
-    };
-    // in place without a mask, only the listed tokens are read and written
-    const bool sparse = !kVerify && p.in_place && !masked;
-    RowRegs<kU> ra, rb;
-    if (!sparse) {
-        load_row(ra, r0);
-        if (r0 + 1 < r1)
-            load_row(rb, r0 + 1);
+        if constexpr (kMask)
+            g.bits[u] = bits[use && t.v0[u] < V ? (uint32_t)t.v0[u] >> 3 : 0u];
     }
+}
 
-    // ---- the words
-    const bool touched = p.penal || p.a.n_bias > 0;
-    Penalty pe = {1.0f, 0.0f, 0.0f};
-    uint32_t hit = 0u;  // bit u * kPer + j: token j of vector u is listed
-    int T = 0;          // listed tokens
-    if (kVerify)
-        for (int i = tid; i < p.rows * kWaves; i += kThreads)
-            s.key[i] = 0u;
-    if (touched) {
-        // a token's place in the chunk, or none
-        auto place = [&](int32_t t, uint32_t &off) {
-            const uint32_t blk = (uint32_t)t >> kBlkLog;
-            off = ((blk >> p.chunk_log) << kBlkLog) | ((uint32_t)t & (kBlk - 1u));
-            return (uint32_t)t < (uint32_t)V && (blk & cmask) == chunk;
-        };
-        for (int i = tid; i < kTokens / 4; i += kThreads)
-            ((u32x4 *)s.word)[i] = u32x4{0u, 0u, 0u, 0u};
-        if (tid == 0)
-            s_entries = 0;
-        __syncthreads();
-        if (p.a.n_bias > 0) {
-            // the last entry of a token holds; entries before counts, so that
-            // the maximum is over entries alone
-            for (int e = tid; e < p.a.n_bias; e += kThreads) {
-                const int64_t i = (int64_t)b * p.a.n_bias + e;
-                uint32_t off;
-                s.bias[e] = p.a.bias_vals[i];
-                if (place(p.a.bias_ids[i], off))
+// The allowed bits of vector u.
+template <int kIn, int kU, bool kMask>
+__device__ __forceinline__ uint32_t allowed_of(const Tile<kIn, kU> &t, int u,
+                                               const RowRegs<kU> &g) {
+    typedef Tile<kIn, kU> T;
+    if (!kMask || !t.masked)
+        return T::kAll;
+    return (g.bits[u] >> (t.v0[u] & 7)) & T::kAll;
+}
+
+// The row's last, partial vector was read as a whole one: its own tokens first.
+template <int kIn, int kU, bool kTiny>
+__device__ __forceinline__ u32x4 own_first(const LogitsParams &p, const Tile<kIn, kU> &t, int u,
+                                           u32x4 x) {
+    typedef Tile<kIn, kU> T;
+    typedef unsigned __int128 u128;
+    if (!kTiny && t.own[u] != T::kAll && t.own[u] != 0u)
+        x = __builtin_bit_cast(u32x4, __builtin_bit_cast(u128, x) >>
+                                          ((T::kPer - p.a.V % T::kPer) * T::kBits));
+    return x;
+}
+
+constexpr float kOne = 1.0f, kZero = 0.0f;
+__constant__ float c_none[2] = {kOne, kZero};
+
+// What the list is made from, requested before anything is waited for: the
+// biases, the first 4096 tokens of the context, the first 256 nodes.
+constexpr int kAhead = 4;  // vectors of 4 context tokens per lane requested first
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef i32x4 i32x4_a __attribute__((aligned(4)));
+
+struct Ahead {
+    int32_t bi[2];
+    float bv[2];
+    i32x4 c[kAhead];
+    int32_t tok, par;
+};
+
+// Vector v of the context: its 4 tokens, from the last whole one where fewer
+// exist (Lmax >= 4).
+__device__ __forceinline__ int ctx_start(int v, int Lmax) {
+    return 4 * v < Lmax - 4 ? 4 * v : Lmax - 4;
+}
+
+__device__ __forceinline__ void request(const LogitsParams &p, int b, Ahead &h) {
+    const int tid = threadIdx.x, nb = p.a.n_bias, R = p.a.R, Lmax = p.a.Lmax;
+    if (nb > 0)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int e = tid + q * kThreads;
+            const int64_t i = (int64_t)b * nb + (e < nb ? e : nb - 1);
+            h.bi[q] = p.a.bias_ids[i];
+            h.bv[q] = p.a.bias_vals[i];
+        }
+    if (p.penal) {
+        const int32_t *x = p.a.tokens + (int64_t)b * Lmax;
+        if (Lmax >= 4)
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q)
+                h.c[q] = *(const i32x4_a *)(x + ctx_start(tid + q * kThreads, Lmax));
+        const int64_t i = (int64_t)b * R + (tid < R ? tid : R - 1);
+        h.tok = p.a.dtok[i];
+        h.par = p.a.dpar ? p.a.dpar[i] : tid - 1;
+    }
+}
+
+// The words and the list.  `hit`: bit u * kPer + j of a lane is set where token
+// j of its vector u is listed; returns the number of listed tokens.
+template <int kIn, int kU>
+__device__ __forceinline__ int list_tokens(const LogitsParams &p, const Tile<kIn, kU> &t,
+                                           const Lds &s, const Ahead &h, Penalty &pe,
+                                           uint32_t &hit) {
+    typedef Tile<kIn, kU> T;
+    constexpr int kPer = T::kPer;
+    __shared__ int s_entries, s_sum[kWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int b = t.b, R = p.a.R, V = p.a.V, nb = p.a.n_bias, Lmax = p.a.Lmax;
+    const int32_t *x = p.a.tokens + (int64_t)b * Lmax;
+    const int32_t *dt = p.a.dtok + (int64_t)b * R;
+    const int32_t *dp = p.a.dpar ? p.a.dpar + (int64_t)b * R : nullptr;
+    hit = 0u;
+    pe = {1.0f, 0.0f, 0.0f};
+    if (!p.penal && nb == 0)
+        return 0;
+    int L = 0, P = 0;
+    if (p.penal) {
+        // one entry for every sequence where an array is not given
+        const float *rho = p.a.repetition ? p.a.repetition + b : &c_none[0];
+        const float *freq = p.a.frequency ? p.a.frequency + b : &c_none[1];
+        const float *pres = p.a.presence ? p.a.presence + b : &c_none[1];
+        pe = {*rho, *freq, *pres};
+        L = clampi(p.a.lengths[b], 0, Lmax);
+        if (p.a.prompt_lens)
+            P = clampi(p.a.prompt_lens[b], 0, L);
+    }
+    for (int i = tid; i < T::kTokens / 4; i += kThreads)
+        ((u32x4 *)s.word)[i] = u32x4{0u, 0u, 0u, 0u};
+    if (tid == 0)
+        s_entries = 0;
+    __syncthreads();
+    if (nb > 0) {
+        // the last entry of a token holds; entries before counts, so that the
+        // maximum is over entries alone
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int e = tid + q * kThreads;
+            uint32_t off;
+            if (e < nb) {
+                s.bias[e] = h.bv[q];
+                if (t.place(h.bi[q], V, off))
                     atomicMax(&s.word[off], (uint32_t)(e + 1) << kBiasShift);
             }
-            __syncthreads();
         }
-        if (p.penal) {
-            const int L = clampi(p.a.lengths[b], 0, p.a.Lmax);
-            const int P = p.a.prompt_lens ? clampi(p.a.prompt_lens[b], 0, L) : 0;
-            const int32_t *x = p.a.tokens + (int64_t)b * p.a.Lmax;
-            for (int i0 = tid; i0 < L; i0 += 8 * kThreads) {
-                int32_t t[8];
-#pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const int i = i0 + q * kThreads;
-                    t[q] = x[i < L ? i : L - 1];
-                }
-#pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const int i = i0 + q * kThreads;
-                    uint32_t off;
-                    if (i < L && place(t[q], off)) {
-                        if (i < P)
-                            atomicOr(&s.word[off], kPrompt);
-                        else
-                            atomicAdd(&s.word[off], 1u);
-                    }
-                }
-            }
-            for (int i = tid; i < n; i += kThreads) {
-                const int64_t d = (int64_t)b * R + i;
-                uint32_t off;
-                s.par[i] = (int16_t)clampi(p.a.dpar ? p.a.dpar[d] : i - 1, -1, R);
-                if (i >= 1 && place(p.a.dtok[d], off)) {
-                    atomicOr(&s.word[off], kDrafted);
-                    s.entry[atomicAdd(&s_entries, 1)] = (off << kNodeBits) | (uint32_t)i;
-                }
-            }
-            if (p.a.repetition)
-                pe.rho = p.a.repetition[b];
-            if (p.a.frequency)
-                pe.freq = p.a.frequency[b];
-            if (p.a.presence)
-                pe.pres = p.a.presence[b];
-            __syncthreads();
-        }
-        // the list, in token order
-#pragma unroll
-        for (int u = 0; u < kU; ++u)
-#pragma unroll
-            for (int q = 0; q < kPer / 4; ++q) {
-                const u32x4 w = ((const u32x4 *)s.word)[(u * kThreads + tid) * (kPer / 4) + q];
-                hit |= ((w.x ? 1u : 0u) | (w.y ? 2u : 0u) | (w.z ? 4u : 0u) | (w.w ? 8u : 0u))
-                       << (u * kPer + q * 4);
-            }
-        const int mine = __popc(hit);
-        int upto = mine;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int q = __shfl_up(upto, o);
-            upto += lane >= o ? q : 0;
-        }
-        if (lane == 63)
-            s_sum[wave] = upto;
         __syncthreads();
-        int k = upto - mine;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            k += w < wave ? s_sum[w] : 0;
-            T += s_sum[w];
-        }
-        for (uint32_t h = hit; h; h &= h - 1u) {
-            const int j = __ffs(h) - 1;
-            s.list[k++] = (uint16_t)(((j / kPer) * kThreads + tid) * kPer + j % kPer);
-        }
-        const int entries = s_entries;
-        if (entries > 0) {
-            // the entries of one token chained, its count moved to the first
-            for (int e = tid; e < entries; e += kThreads) {
-                const uint32_t off = s.entry[e] >> kNodeBits;
-                uint32_t nx = kNone;
-                bool first = true;
-                for (int f = 0; f < entries; ++f)
-                    if ((s.entry[f] >> kNodeBits) == off) {
-                        if (f > e && nx == kNone)
-                            nx = (uint32_t)f;
-                        first = first && f >= e;
-                    }
-                s.next[e] = (uint16_t)nx;
-                if (first) {
-                    const uint32_t w = s.word[off];
-                    s.count[e] = w & (kCount | kPrompt);
-                    s.word[off] = (w & ~(kCount | kPrompt)) | (uint32_t)e;
-                }
+    }
+    if (p.penal) {
+        auto add = [&](int32_t tok, int i) {
+            uint32_t off;
+            if (t.place(tok, V, off)) {
+                if (i < P)
+                    atomicOr(&s.word[off], kPrompt);
+                else
+                    atomicAdd(&s.word[off], 1u);
             }
-            if (tid < r1 - r0) {
-                uint32_t *a = s.anc + tid * aw;
-                for (int w = 0; w < aw; ++w)
-                    a[w] = 0u;
-                for (int node = r0 + tid; node > 0;) {
-                    a[node >> 5] |= 1u << (node & 31);
-                    const int q = s.par[node];
-                    if (q < 0 || q >= node)
-                        break;
-                    node = q;
+        };
+        auto add4 = [&](const i32x4 &c, int v) {
+            const int i0 = ctx_start(v, Lmax);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (i0 + j >= 4 * v && i0 + j < L)
+                    add(c[j], i0 + j);
+        };
+        if (Lmax >= 4) {
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q)
+                add4(h.c[q], tid + q * kThreads);
+            for (int v = tid + kAhead * kThreads; 4 * v < L; v += 8 * kThreads) {
+                i32x4 c[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    c[q] = *(const i32x4_a *)(x + ctx_start(v + q * kThreads, Lmax));
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    add4(c[q], v + q * kThreads);
+            }
+        } else if (tid < L) {
+            add(x[tid], tid);
+        }
+        int32_t d_tok = h.tok, d_par = h.par;
+        for (int i = tid; i < t.n; i += kThreads) {
+            if (i != tid) {
+                d_tok = dt[i];
+                d_par = dp ? dp[i] : i - 1;
+            }
+            uint32_t off;
+            s.par[i] = (int16_t)clampi(d_par, -1, R);
+            if (i >= 1 && t.place(d_tok, V, off)) {
+                atomicOr(&s.word[off], kDrafted);
+                s.entry[atomicAdd(&s_entries, 1)] = (off << kNodeBits) | (uint32_t)i;
+            }
+        }
+        __syncthreads();
+    }
+    // the list, each lane's tokens together
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+#pragma unroll
+        for (int q = 0; q < kPer / 4; ++q) {
+            const u32x4 w = ((const u32x4 *)s.word)[(u * kThreads + tid) * (kPer / 4) + q];
+            hit |= ((w.x ? 1u : 0u) | (w.y ? 2u : 0u) | (w.z ? 4u : 0u) | (w.w ? 8u : 0u))
+                   << (u * kPer + q * 4);
+        }
+    const int mine = __popc(hit);
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int q = __shfl_up(upto, o);
+        upto += lane >= o ? q : 0;
+    }
+    if (lane == 63)
+        s_sum[wave] = upto;
+    __syncthreads();
+    int k = upto - mine, total = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        k += w < wave ? s_sum[w] : 0;
+        total += s_sum[w];
+    }
+    for (uint32_t h = hit; h; h &= h - 1u) {
+        const int j = __ffs(h) - 1;
+        s.list[k++] = (uint16_t)(((j / kPer) * kThreads + tid) * kPer + j % kPer);
+    }
+    const int entries = s_entries;
+    if (entries > 0) {
+        // the entries of one token chained, its count moved to the first
+        for (int e = tid; e < entries; e += kThreads) {
+            const uint32_t off = s.entry[e] >> kNodeBits;
+            uint32_t nx = kNone;
+            bool first = true;
+            for (int f = 0; f < entries; ++f)
+                if ((s.entry[f] >> kNodeBits) == off) {
+                    if (f > e && nx == kNone)
+                        nx = (uint32_t)f;
+                    first = first && f >= e;
                 }
+            s.next[e] = (uint16_t)nx;
+            if (first) {
+                const uint32_t w = s.word[off];
+                s.count[e] = w & (kCount | kPrompt);
+                s.word[off] = (w & ~(kCount | kPrompt)) | (uint32_t)e;
+            }
+        }
+        if (tid < t.r1 - t.r0) {
+            uint32_t *a = s.anc + tid * t.aw;
+            for (int w = 0; w < t.aw; ++w)
+                a[w] = 0u;
+            for (int node = t.r0 + tid; node > 0;) {
+                a[node >> 5] |= 1u << (node & 31);
+                const int q = s.par[node];
+                if (q < 0 || q >= node)
+                    break;
+                node = q;
             }
         }
     }
     __syncthreads();
+    return total;
+}
 
+// A store that a lane can leave out without a branch: an offset behind the row's
+// bytes is dropped.
+constexpr uint32_t kNowhere = 0x80000000u;
+
+template <int kIn, int kOut, int kU, bool kMask, bool kTiny>
+__global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
+    typedef Tile<kIn, kU> T;
+    typedef Elem<kIn> In;
+    typedef Elem<kOut> Out;
+    typedef typename Out::type O;
+    constexpr int kPer = T::kPer;
+    constexpr uint32_t kAll = T::kAll;
+    extern __shared__ __align__(16) unsigned char mem[];
+    const int tid = threadIdx.x, R = p.a.R, V = p.a.V;
+    T t;
+    t.init(p);
+    Ahead h;
+    request(p, t.b, h);
+    if (!t.rows(p))
+        return;
+    const Lds s = lds_carve(mem, T::kTokens, sizeof(typename In::type), R, p.rows, p.a.n_bias,
+                            false);
+    // in place without a mask, only the listed tokens are read and written
+    const bool sparse = p.in_place && !(kMask && t.masked);
+    RowRegs<kU> ra, rb, rc;
+    if (!sparse) {
+        load_row<kIn, kU, kMask, kTiny>(p, t, t.r0, ra);
+        load_row<kIn, kU, kMask, kTiny>(p, t, t.r0 + 1, rb);
+    }
+    Penalty pe;
+    uint32_t hit;
+    const int listed = list_tokens(p, t, s, h, pe, hit);
     if (sparse) {
-        if constexpr (!kVerify && kIn == kOut) {
-            for (int r = r0; r < r1; ++r) {
-                typename Out::type *dst =
-                    (typename Out::type *)p.out + ((int64_t)b * R + r) * V;
-                for (int k = tid; k < T; k += kThreads) {
+        if constexpr (kIn == kOut)
+            for (int r = t.r0; r < t.r1; ++r) {
+                O *dst = (O *)p.out + ((int64_t)t.b * R + r) * V;
+                for (int k = tid; k < listed; k += kThreads) {
                     const uint32_t off = s.list[k];
-                    const uint32_t blk = ((off >> kBlkLog) << p.chunk_log) | chunk;
-                    typename Out::type *d = dst + (blk * kBlk + (off & (kBlk - 1u)));
+                    O *d = dst + t.token(off);
                     *d = Out::put(processed(In::get(*d), s.word[off], pe, s,
-                                            s.anc + (r - r0) * aw));
+                                            s.anc + (r - t.r0) * t.aw));
                 }
             }
-        }
         return;
     }
-
-    // ---- the rows
     typename In::type *stage = (typename In::type *)s.stage;
-    for (int r = r0; r < r1; ++r) {
-        RowRegs<kU> rc;
-        if (r + 2 < r1)
-            load_row(rc, r + 2);
-        typename Out::type *dst = (typename Out::type *)p.out + ((int64_t)b * R + r) * V;
-        const uint32_t *anc = s.anc + (r - r0) * aw;
-        if constexpr (!kTiny) {
-            // the row's last, partial vector was read whole: its own tokens first
+    auto step = [&](RowRegs<kU> &g, int r) {
+        O *dst = (O *)p.out + ((int64_t)t.b * R + r) * V;
+        const __amdgpu_buffer_rsrc_t rs =
+            __builtin_amdgcn_make_buffer_rsrc(dst, 0, V * (int)sizeof(O), 0x00027000);
 #pragma unroll
-            for (int u = 0; u < kU; ++u)
-                if (own[u] != kAll && own[u] != 0u) {
-                    const int sh = (kPer - tail) * kBits;
-                    typedef unsigned __int128 u128;
-                    ra.x[u] = __builtin_bit_cast(u32x4, __builtin_bit_cast(u128, ra.x[u]) >> sh);
-                }
-        }
-        if (T > 0) {
+        for (int u = 0; u < kU; ++u)
+            g.x[u] = own_first<kIn, kU, kTiny>(p, t, u, g.x[u]);
+        if (listed > 0) {
 #pragma unroll
             for (int u = 0; u < kU; ++u)
                 if ((hit >> (u * kPer)) & kAll)
-                    ((u32x4 *)stage)[u * kThreads + tid] = ra.x[u];
+                    ((u32x4 *)stage)[u * kThreads + tid] = g.x[u];
             __syncthreads();
-            for (int k = tid; k < T; k += kThreads) {
+            for (int k = tid; k < listed; k += kThreads) {
                 const uint32_t off = s.list[k];
-                const float y = processed(In::get(stage[off]), s.word[off], pe, s, anc);
+                const float y = processed(In::get(stage[off]), s.word[off], pe, s,
+                                          s.anc + (r - t.r0) * t.aw);
                 if constexpr (sizeof(typename In::type) == 4)
                     stage[off] = y;
                 else
@@ -542,173 +679,322 @@ __global__ __launch_bounds__(kThreads) void k_logits(LogitsParams p) {
             }
             __syncthreads();
         }
-        uint32_t best = 0u;         // order key of this lane's maximum, 0: none
-        uint32_t pk[kU][kPer / 2];  // 16-bit results, in pairs
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
             const uint32_t hu = (hit >> (u * kPer)) & kAll;
-            u32x4 x = ra.x[u];
+            const uint32_t ok = allowed_of<kIn, kU, kMask>(t, u, g);
+            const u32x4 x = g.x[u];
             u32x4 y = x;
             if (hu)
                 y = ((const u32x4 *)stage)[u * kThreads + tid];
-            uint32_t ok = ra.ok[u] & kAll;
+            uint32_t pk[kPer / 2];  // 16-bit results, in pairs
             if constexpr (kOut == SWITCHSD_F32) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    y[j] = (ok >> j) & 1u ? y[j] : 0xFF800000u;
+                    y[j] = !kMask || ((ok >> j) & 1u) ? y[j] : 0xFF800000u;
             } else {
                 constexpr uint32_t kInf = kOut == SWITCHSD_BF16 ? 0xFF80FF80u : 0xFC00FC00u;
 #pragma unroll
                 for (int q = 0; q < kPer / 2; ++q) {
-                    uint32_t v;
                     if constexpr (kIn == kOut) {
-                        v = y[q];
+                        pk[q] = y[q];
                     } else if constexpr (kIn == SWITCHSD_F32) {
-                        v = (uint32_t)Out::put(__uint_as_float(y[2 * q])) |
-                            (uint32_t)Out::put(__uint_as_float(y[2 * q + 1])) << 16;
+                        pk[q] = (uint32_t)Out::put(__uint_as_float(y[2 * q])) |
+                                (uint32_t)Out::put(__uint_as_float(y[2 * q + 1])) << 16;
                     } else {
-                        v = (uint32_t)Out::put(In::get((uint16_t)x[q])) |
-                            (uint32_t)Out::put(In::get((uint16_t)(x[q] >> 16))) << 16;
+                        pk[q] = (uint32_t)Out::put(In::get((uint16_t)x[q])) |
+                                (uint32_t)Out::put(In::get((uint16_t)(x[q] >> 16))) << 16;
                         if (hu)  // listed tokens already have the output's type
-                            v = keep16(v, ~hu, q, 0u) | keep16(y[q], hu, q, 0u);
+                            pk[q] = keep16(pk[q], ~hu, q, 0u) | keep16(y[q], hu, q, 0u);
                     }
-                    if (ok != kAll)
-                        v = keep16(v, ok, q, kInf);
-                    pk[u][q] = v;
+                    if (kMask && ok != kAll)
+                        pk[q] = keep16(pk[q], ok, q, kInf);
                 }
             }
-            if constexpr (!kVerify) {
-                const bool write = !p.in_place || hu || ok != kAll;
-                if (own[u] == kAll && write) {
-                    if constexpr (kOut == SWITCHSD_F32)
-                        *(u32x4_a *)(dst + v0[u]) = y;
-                    else if constexpr (kPer == 8)
-                        *(u32x4_a *)(dst + v0[u]) =
-                            u32x4{pk[u][0], pk[u][1], pk[u][2], pk[u][3]};
-                    else
-                        *(u32x2_a *)(dst + v0[u]) = u32x2{pk[u][0], pk[u][1]};
-                } else if (own[u] != 0u && write) {
+            const bool write = !p.in_place || hu || ok != kAll;
+            const uint32_t o = t.own[u] == kAll && write
+                                   ? (uint32_t)t.v0[u] * (uint32_t)sizeof(O)
+                                   : kNowhere;
+            if constexpr (kOut == SWITCHSD_F32)
+                __builtin_amdgcn_raw_buffer_store_b128(y, rs, o, 0, 0);
+            else if constexpr (kPer == 8)
+                __builtin_amdgcn_raw_buffer_store_b128(u32x4{pk[0], pk[1], pk[2], pk[3]}, rs, o, 0,
+                                                       0);
+            else
+                __builtin_amdgcn_raw_buffer_store_b64(u32x2{pk[0], pk[1]}, rs, o, 0, 0);
+            if (t.own[u] != kAll && t.own[u] != 0u && write) {
 #pragma unroll
-                    for (int j = 0; j < kPer; ++j)
-                        if ((own[u] >> j) & 1u) {
-                            if constexpr (kOut == SWITCHSD_F32)
-                                dst[v0[u] + j] = __uint_as_float(y[j]);
-                            else
-                                dst[v0[u] + j] = (uint16_t)(pk[u][j / 2] >> (16 * (j & 1)));
-                        }
-                }
-            } else {
-#pragma unroll
-                for (int q = 0; q < kPer / 2; ++q)  // tokens that do not exist: NaN, negative
-                    if (own[u] != kAll)
-                        pk[u][q] = keep16(pk[u][q], own[u], q, 0xFFFFFFFFu);
-            }
-        }
-        if constexpr (kVerify) {
-            // Maximum of the lane's bf16 patterns: as signed integers where it
-            // is not negative, as unsigned ones (the smallest) where all are
-            // negative; a positive NaN takes the slow way.
-            uint32_t m = pk[0][0], lo = pk[0][0];
-#pragma unroll
-            for (int u = 0; u < kU; ++u)
-#pragma unroll
-                for (int q = 0; q < kPer / 2; ++q) {
-                    m = pk_max_i16(m, pk[u][q]);
-                    lo = pk_min_u16(lo, pk[u][q]);
-                }
-            const int32_t m0 = (int16_t)m, m1 = (int16_t)(m >> 16);
-            const int32_t mx = m0 > m1 ? m0 : m1;
-            if (mx > 0x7F80) {
-#pragma unroll
-                for (int u = 0; u < kU; ++u)
-#pragma unroll
-                    for (int q = 0; q < kPer / 2; ++q) {
-                        const uint32_t k0 = order16(pk[u][q] & 0xFFFFu),
-                                       k1 = order16(pk[u][q] >> 16);
-                        const uint32_t k = k0 > k1 ? k0 : k1;
-                        best = k > best ? k : best;
+                for (int j = 0; j < kPer; ++j)
+                    if ((t.own[u] >> j) & 1u) {
+                        if constexpr (kOut == SWITCHSD_F32)
+                            dst[t.v0[u] + j] = __uint_as_float(y[j]);
+                        else
+                            dst[t.v0[u] + j] = (uint16_t)(pk[j / 2] >> (16 * (j & 1)));
                     }
-            } else if (mx >= 0) {
-                best = (uint32_t)mx | 0x8000u;
-            } else {
-                const uint32_t l0 = lo & 0xFFFFu, l1 = lo >> 16;
-                best = order16(l0 < l1 ? l0 : l1);
-            }
-            const uint32_t top = wave_max(best);
-            if (top != 0u) {
-                // the lowest token that holds it
-                uint32_t first = kNone;
-                if (best == top) {
-#pragma unroll
-                    for (int u = kU - 1; u >= 0; --u)
-#pragma unroll
-                        for (int q = kPer / 2 - 1; q >= 0; --q) {
-                            const uint32_t o = (uint32_t)((u * kThreads + tid) * kPer + 2 * q);
-                            if (order16(pk[u][q] >> 16) == top)
-                                first = o + 1u;
-                            if (order16(pk[u][q] & 0xFFFFu) == top)
-                                first = o;
-                        }
-                }
-                const uint32_t low = kNone - wave_max(kNone - first);
-                if (lane == 0)
-                    s.key[(r - r0) * kWaves + wave] = (top << 16) | (kNone - low);
             }
         }
-        ra = rb;
-        rb = rc;
-    }
-    if constexpr (kVerify) {
-        __syncthreads();
-        if (tid < 64) {
-            // one row per lane (at most kRowGroup = 64 rows)
-            uint32_t k = 0u;
-            if (tid < r1 - r0)
-#pragma unroll
-                for (int w = 0; w < kWaves; ++w) {
-                    const uint32_t o = s.key[tid * kWaves + w];
-                    k = o > k ? o : k;
-                }
-            if (k) {
-                const uint32_t off = kNone - (k & 0xFFFFu);
-                const uint32_t blk = ((off >> kBlkLog) << p.chunk_log) | chunk;
-                const uint32_t t = blk * kBlk + (off & (kBlk - 1u));
-                __hip_atomic_fetch_max(
-                    &p.keys[(int64_t)b * p.key_stride + r0 + tid],
-                    ((unsigned long long)order32(k >> 16) << 32) | (0xFFFFFFFFu - t),
-                    __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
-            const bool last = arrive(&p.tickets[(int64_t)b * kLineU32],
-                                     (uint32_t)(p.chunks * ((n + p.rows - 1) / p.rows)));
-            if (tid == 0)
-                s_last = last;
-        }
-        __syncthreads();
-        if (s_last)
-            accept(p, b, mem);
+    };
+    for (int r = t.r0; r < t.r1; r += 3) {
+        load_row<kIn, kU, kMask, kTiny>(p, t, r + 2, rc);
+        step(ra, r);
+        load_row<kIn, kU, kMask, kTiny>(p, t, r + 3, ra);
+        if (r + 1 < t.r1)
+            step(rb, r + 1);
+        load_row<kIn, kU, kMask, kTiny>(p, t, r + 4, rb);
+        if (r + 2 < t.r1)
+            step(rc, r + 2);
     }
 }
 
-template <int kIn, int kOut, int kU, bool kVerify, bool kTiny>
+// The order key (of its value in bf16) of element j of a vector.
+template <int kIn>
+__device__ __forceinline__ uint32_t elem_key(const u32x4 &x, int j) {
+    typedef Elem<kIn> In;
+    if constexpr (kIn == SWITCHSD_F32) {
+        return order16(Elem<SWITCHSD_BF16>::put(__uint_as_float(x[j])));
+    } else {
+        const uint32_t e = (x[j / 2] >> (16 * (j & 1))) & 0xFFFFu;
+        if constexpr (kIn == SWITCHSD_BF16)
+            return order16(e);
+        else
+            return order16(Elem<SWITCHSD_BF16>::put(In::get((uint16_t)e)));
+    }
+}
+
+// The order key of a vector's maximum (0: nothing but NaN).  Rounding to bf16
+// keeps the order, so the maximum is taken on the input's patterns: as signed
+// integers where one is not negative, as unsigned ones (the smallest) where all
+// are; a positive NaN takes the slow way.
+template <int kIn>
+__device__ __forceinline__ uint32_t vector_key(const u32x4 &x) {
+    if constexpr (kIn == SWITCHSD_F32) {
+        const int32_t a = (int32_t)x.x > (int32_t)x.y ? (int32_t)x.x : (int32_t)x.y;
+        const int32_t c = (int32_t)x.z > (int32_t)x.w ? (int32_t)x.z : (int32_t)x.w;
+        const int32_t mx = a > c ? a : c;
+        if (mx > 0x7F800000) {
+            uint32_t k = 0u;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                k = elem_key<kIn>(x, j) > k ? elem_key<kIn>(x, j) : k;
+            return k;
+        }
+        uint32_t m = (uint32_t)mx;
+        if (mx < 0) {
+            const uint32_t d = x.x < x.y ? x.x : x.y, e = x.z < x.w ? x.z : x.w;
+            m = d < e ? d : e;
+        }
+        return order16(Elem<SWITCHSD_BF16>::put(__uint_as_float(m)));
+    } else {
+        constexpr int32_t kTop = kIn == SWITCHSD_BF16 ? 0x7F80 : 0x7C00;
+        const uint32_t m2 = pk_max_i16(pk_max_i16(x.x, x.y), pk_max_i16(x.z, x.w));
+        const int32_t m0 = (int16_t)m2, m1 = (int32_t)m2 >> 16;
+        const int32_t mx = m0 > m1 ? m0 : m1;
+        if (mx > kTop) {
+            uint32_t k = 0u;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                k = elem_key<kIn>(x, j) > k ? elem_key<kIn>(x, j) : k;
+            return k;
+        }
+        uint32_t m = (uint32_t)mx;
+        if (mx < 0) {
+            const uint32_t l2 = pk_min_u16(pk_min_u16(x.x, x.y), pk_min_u16(x.z, x.w));
+            m = (l2 & 0xFFFFu) < (l2 >> 16) ? l2 & 0xFFFFu : l2 >> 16;
+        }
+        if constexpr (kIn == SWITCHSD_BF16)
+            return order16(m);
+        else
+            return order16(Elem<SWITCHSD_BF16>::put(Elem<kIn>::get((uint16_t)m)));
+    }
+}
+
+template <int kIn, int kU, bool kMask, bool kTiny>
+__global__ __launch_bounds__(kThreads) void k_verify(LogitsParams p) {
+    typedef Tile<kIn, kU> T;
+    typedef Elem<kIn> In;
+    typedef typename In::type E;
+    constexpr int kPer = T::kPer;
+    constexpr uint32_t kAll = T::kAll;
+    extern __shared__ __align__(16) unsigned char mem[];
+    __shared__ int s_last;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int R = p.a.R, V = p.a.V;
+    T t;
+    t.init(p);
+    Ahead h;
+    request(p, t.b, h);
+    if (!t.rows(p))
+        return;
+    const Lds s = lds_carve(mem, T::kTokens, sizeof(E), R, p.rows, p.a.n_bias, true);
+    RowRegs<kU> ra, rb, rc;
+    load_row<kIn, kU, kMask, kTiny>(p, t, t.r0, ra);
+    load_row<kIn, kU, kMask, kTiny>(p, t, t.r0 + 1, rb);
+    for (int i = tid; i < 2 * p.rows * kWaves; i += kThreads)
+        s.key[i] = 0u;
+    __syncthreads();
+    Penalty pe;
+    uint32_t hit;
+    const int listed = list_tokens(p, t, s, h, pe, hit);
+    const int64_t words = (V + 31) / 32;
+    // A listed token of this lane: its logit and the word with its allowed bit
+    // are requested two rows ahead like the vectors (lanes without one: the
+    // row's first token).
+    struct Item {
+        E x;
+        uint32_t bits;
+    };
+    auto item = [&](uint32_t tok, int r, Item &i) {
+        const int64_t row = (int64_t)t.b * R + (r < t.r1 ? r : t.r1 - 1);
+        i.x = ((const E *)p.a.logits)[row * V + tok];
+        if constexpr (kMask)
+            i.bits = t.masked ? p.a.allowed[row * words + (tok >> 5)] : 0u;
+    };
+    // its key: order key, then the lowest place
+    auto item_key = [&](const Item &i, uint32_t tok, uint32_t off, uint32_t w, int r) {
+        const float y = processed(In::get(i.x), w, pe, s, s.anc + (r - t.r0) * t.aw);
+        const bool ok = !kMask || !t.masked || ((i.bits >> (tok & 31u)) & 1u);
+        const uint32_t k = order16(ok ? Elem<SWITCHSD_BF16>::put(y) : 0xFF80u);
+        return k ? (k << 16) | (kNone - off) : 0u;
+    };
+    uint32_t off = 0u, word = 0u, tok = 0u;
+    if (tid < listed) {
+        off = s.list[tid];
+        word = s.word[off];
+        tok = t.token(off);
+    }
+    Item ia, ib, ic;
+    item(tok, t.r0, ia);
+    item(tok, t.r0 + 1, ib);
+    auto step = [&](RowRegs<kU> &g, const Item &it, int r) {
+        uint32_t best = 0u;  // order key, then the lowest vector
+        u32x4 top = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            const uint32_t out = ((hit >> (u * kPer)) & kAll) | (kAll & ~t.own[u]);
+            const uint32_t ok = allowed_of<kIn, kU, kMask>(t, u, g);
+            u32x4 x = own_first<kIn, kU, kTiny>(p, t, u, g.x[u]);
+            if (ok != kAll || out) {
+                // what is not allowed is -inf, what is listed or does not exist NaN
+                if constexpr (kIn == SWITCHSD_F32) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        x[j] = (ok >> j) & 1u ? x[j] : 0xFF800000u;
+                        x[j] = (out >> j) & 1u ? 0xFFFFFFFFu : x[j];
+                    }
+                } else {
+                    constexpr uint32_t kInf = kIn == SWITCHSD_BF16 ? 0xFF80FF80u : 0xFC00FC00u;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        x[q] = keep16(keep16(x[q], ok, q, kInf), ~out, q, 0xFFFFFFFFu);
+                }
+            }
+            const uint32_t k = vector_key<kIn>(x);
+            const uint32_t k2 = k ? (k << 16) | (kNone - (uint32_t)(u * kThreads + tid)) : 0u;
+            if (k2 > best) {
+                best = k2;
+                top = x;
+            }
+        }
+        const uint32_t wb = wave_max(best);
+        if (best == wb && wb != 0u) {  // one lane: keys of different vectors differ
+            s.key[(r - t.r0) * kWaves + wave] = wb;
+            ((u32x4 *)s.stage)[(r - t.r0) * kWaves + wave] = top;
+        }
+        if (wave * 64 < listed) {
+            uint32_t k = tid < listed ? item_key(it, tok, off, word, r) : 0u;
+            for (int q = tid + kThreads; q < listed; q += kThreads) {
+                const uint32_t o = s.list[q];
+                Item i;
+                item(t.token(o), r, i);
+                const uint32_t k2 = item_key(i, t.token(o), o, s.word[o], r);
+                k = k2 > k ? k2 : k;
+            }
+            k = wave_max(k);
+            if (lane == 0)
+                s.key[(p.rows + r - t.r0) * kWaves + wave] = k;
+        }
+    };
+    for (int r = t.r0; r < t.r1; r += 3) {
+        load_row<kIn, kU, kMask, kTiny>(p, t, r + 2, rc);
+        item(tok, r + 2, ic);
+        step(ra, ia, r);
+        load_row<kIn, kU, kMask, kTiny>(p, t, r + 3, ra);
+        item(tok, r + 3, ia);
+        if (r + 1 < t.r1)
+            step(rb, ib, r + 1);
+        load_row<kIn, kU, kMask, kTiny>(p, t, r + 4, rb);
+        item(tok, r + 4, ib);
+        if (r + 2 < t.r1)
+            step(rc, ic, r + 2);
+    }
+    __syncthreads();
+    if (tid < 64) {
+        // one row per lane (at most kRowGroup = 64 rows)
+        if (tid < t.r1 - t.r0) {
+            uint32_t kb = 0u, ki = 0u;
+            int w = 0;
+#pragma unroll
+            for (int q = 0; q < kWaves; ++q) {
+                const uint32_t a = s.key[tid * kWaves + q];
+                const uint32_t c = s.key[(p.rows + tid) * kWaves + q];
+                w = a > kb ? q : w;
+                kb = a > kb ? a : kb;
+                ki = c > ki ? c : ki;
+            }
+            // the lowest token of the vector that holds the maximum
+            if (kb && (kb >> 16) >= (ki >> 16)) {
+                const u32x4 x = ((const u32x4 *)s.stage)[tid * kWaves + w];
+                uint32_t first = 0u;
+#pragma unroll
+                for (int j = kPer - 1; j >= 0; --j)
+                    first = elem_key<kIn>(x, j) == (kb >> 16) ? (uint32_t)j : first;
+                kb = (kb & 0xFFFF0000u) | (kNone - ((kNone - (kb & 0xFFFFu)) * kPer + first));
+                ki = kb > ki ? kb : ki;
+            }
+            if (ki)
+                __hip_atomic_fetch_max(
+                    &p.keys[(int64_t)t.b * p.key_stride + t.r0 + tid],
+                    ((unsigned long long)order32(ki >> 16) << 32) |
+                        (0xFFFFFFFFu - t.token(kNone - (ki & 0xFFFFu))),
+                    __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        const bool last = arrive(&p.tickets[(int64_t)t.b * kLineU32],
+                                 (uint32_t)(p.chunks * ((t.n + p.rows - 1) / p.rows)));
+        if (tid == 0)
+            s_last = last;
+    }
+    __syncthreads();
+    if (s_last)
+        accept(p, t.b, mem);
+}
+
+template <int kIn, int kOut, int kU, bool kVerify, bool kTiny, bool kMask>
 int launch(const LogitsParams &p, hipStream_t stream) {
-    const int tokens = kThreads * kU * Elem<kIn>::per;
-    const unsigned grid = (unsigned)((int64_t)p.a.B * p.groups * p.chunks);
-    const size_t lds = lds_bytes(tokens, sizeof(typename Elem<kIn>::type), p.a.R, p.rows,
-                                 p.a.n_bias, kVerify);
-    hipLaunchKernelGGL((k_logits<kIn, kOut, kU, kVerify, kTiny>), dim3(grid), dim3(kThreads), lds,
-                       stream, p);
+    const dim3 grid((unsigned)((int64_t)p.a.B * p.groups * p.chunks));
+    const size_t lds = lds_bytes(Tile<kIn, kU>::kTokens, sizeof(typename Elem<kIn>::type), p.a.R,
+                                 p.rows, p.a.n_bias, kVerify);
+    if constexpr (kVerify)
+        hipLaunchKernelGGL((k_verify<kIn, kU, kMask, kTiny>), grid, dim3(kThreads), lds, stream,
+                           p);
+    else
+        hipLaunchKernelGGL((k_process<kIn, kOut, kU, kMask, kTiny>), grid, dim3(kThreads), lds,
+                           stream, p);
     return hipGetLastError() == hipSuccess ? SWITCHSD_OK : SWITCHSD_EHIP;
 }
 
-template <int kIn, int kOut, bool kVerify>
+template <int kIn, int kOut, bool kVerify, bool kMask>
 int launch_unroll(const LogitsParams &p, hipStream_t stream) {
     if (p.a.V < Elem<kIn>::per)
-        return launch<kIn, kOut, 1, kVerify, true>(p, stream);
-    if (p.unroll == 4)
-        return launch<kIn, kOut, 4, kVerify, false>(p, stream);
+        return launch<kIn, kOut, 1, kVerify, true, kMask>(p, stream);
     if (p.unroll == 2)
-        return launch<kIn, kOut, 2, kVerify, false>(p, stream);
-    return launch<kIn, kOut, 1, kVerify, false>(p, stream);
+        return launch<kIn, kOut, 2, kVerify, false, kMask>(p, stream);
+    return launch<kIn, kOut, 1, kVerify, false, kMask>(p, stream);
+}
+
+template <int kIn, int kOut, bool kVerify>
+int launch_mask(const LogitsParams &p, hipStream_t stream) {
+    return p.a.allowed ? launch_unroll<kIn, kOut, kVerify, true>(p, stream)
+                       : launch_unroll<kIn, kOut, kVerify, false>(p, stream);
 }
 
 }  // namespace
@@ -717,16 +1003,16 @@ int launch_logits_kernel(const LogitsParams &p, int32_t out_type, hipStream_t st
     constexpr int BF = SWITCHSD_BF16, HF = SWITCHSD_F16, FF = SWITCHSD_F32;
     const int in = p.a.logits_type;
     if (!p.out)  // verify
-        return in == BF   ? launch_unroll<BF, BF, true>(p, stream)
-               : in == HF ? launch_unroll<HF, BF, true>(p, stream)
-                          : launch_unroll<FF, BF, true>(p, stream);
+        return in == BF   ? launch_mask<BF, BF, true>(p, stream)
+               : in == HF ? launch_mask<HF, BF, true>(p, stream)
+                          : launch_mask<FF, BF, true>(p, stream);
     if (in == BF)
-        return launch_unroll<BF, BF, false>(p, stream);
+        return launch_mask<BF, BF, false>(p, stream);
     if (in == HF)
-        return out_type == BF ? launch_unroll<HF, BF, false>(p, stream)
-                              : launch_unroll<HF, HF, false>(p, stream);
-    return out_type == BF ? launch_unroll<FF, BF, false>(p, stream)
-                          : launch_unroll<FF, FF, false>(p, stream);
+        return out_type == BF ? launch_mask<HF, BF, false>(p, stream)
+                              : launch_mask<HF, HF, false>(p, stream);
+    return out_type == BF ? launch_mask<FF, BF, false>(p, stream)
+                          : launch_mask<FF, FF, false>(p, stream);
 }
 
 }  // namespace switchsd

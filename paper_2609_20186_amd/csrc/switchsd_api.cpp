@@ -1000,11 +1000,19 @@ int set_logits_grid(LogitsParams &p) {
     if (rc)
         return rc;
     const switchsd_logits_args &a = p.a;
-    const int64_t want = 4 * (int64_t)cus;
+    p.penal = a.repetition || a.frequency || a.presence;
+    // Four work-groups per compute unit, down to one where each would count a
+    // long history.
+    int64_t want = 4 * (int64_t)cus;
+    if (p.penal && a.Lmax > 4096)
+        want = want * 4096 / a.Lmax;
+    want = want < cus ? cus : want;
     const int64_t blk = a.logits_type == SWITCHSD_F32 ? 64 : 128;  // tokens of 16 vectors
     const int64_t blocks = (a.V + blk - 1) / blk;
-    p.penal = a.repetition || a.frequency || a.presence;
+    // rows of a work-group, at most: their path counts take 16 KB of LDS
+    const int64_t most = kPathBytes / (a.R * (a.R > 256 ? 2 : 1));
     int64_t rows = a.R < kRowGroup ? a.R : kRowGroup;
+    rows = rows < most ? rows : most;
     int64_t groups = (a.R + rows - 1) / rows;
     for (p.unroll = kLogitsUnroll;; p.unroll >>= 1) {
         const int64_t per = (int64_t)(kThreads / 16) * p.unroll;  // blocks of a chunk, at most
@@ -1015,9 +1023,9 @@ int set_logits_grid(LogitsParams &p) {
         if (p.unroll == 1 || (int64_t)a.B * groups * p.chunks >= want)
             break;
     }
-    if ((int64_t)a.B * groups * p.chunks < want) {
-        rows = (int64_t)a.B * a.R * p.chunks / want;
-        rows = rows < 1 ? 1 : rows > kRowGroup ? kRowGroup : rows;
+    const int64_t more = want / ((int64_t)a.B * p.chunks);  // groups that want would take
+    if (more > groups) {
+        rows = (a.R + more - 1) / more;
         groups = (a.R + rows - 1) / rows;
     }
     p.rows = (int32_t)rows;

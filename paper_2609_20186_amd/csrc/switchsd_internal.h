@@ -202,6 +202,8 @@ int launch_tree_mask_kernel(const int32_t *dpar, const int32_t *dn, int32_t B, i
 constexpr int kRowGroup = 64;
 // 16-byte vectors per lane and row of the logits kernels, at most.
 constexpr int kLogitsUnroll = 2;
+// LDS bytes of the path counts of a work-group's rows.
+constexpr int kPathBytes = 16384;
 
 // Drafted rows a work-group of the page plan takes, at most (one sequence at
 // least), and positions of a range that one of the packed slots takes.

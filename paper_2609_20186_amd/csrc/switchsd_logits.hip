@@ -32,16 +32,15 @@ namespace {
 constexpr int kWaves = kThreads / 64;
 
 // Word of a token: occurrences in the generated part of the context (at most
-// SWITCHSD_MAX_HISTORY), in the prompt, drafted (then the low bits are its first
-// entry in the draft's table and the count is there), bias entry + 1.
+// SWITCHSD_MAX_HISTORY), in the prompt, drafted (then the low bits are the draft
+// node that stands for it and the count is kept there), bias entry + 1.
 constexpr uint32_t kCount = 0x1FFFFFu;
 constexpr uint32_t kPrompt = 1u << 21;
 constexpr uint32_t kDrafted = 1u << 22;
 constexpr int kBiasShift = 23;
 static_assert(SWITCHSD_MAX_HISTORY == kCount, "the count field");
 static_assert(SWITCHSD_MAX_BIAS == (1 << (32 - kBiasShift)) - 1, "the bias field");
-constexpr int kNodeBits = 10;
-static_assert(SWITCHSD_MAX_R == 1 << kNodeBits, "the node field");
+static_assert(SWITCHSD_MAX_R <= kCount, "a node in the count field");
 constexpr uint32_t kNone = 0xFFFFu;
 
 // Loads and stores of vectors at any element's address.
@@ -134,11 +133,11 @@ struct Lds {
     uint16_t *list;   // [tokens] the tokens that have a word
     uint32_t *key;    // [rows][kWaves] maxima over the vectors, then over the listed tokens
     float *bias;      // [n_bias]
-    uint32_t *entry;  // [R] drafted tokens of the chunk: token << kNodeBits | node
-    uint32_t *count;  // [R] count and prompt bit of a drafted token, at its first entry
-    uint32_t *anc;    // [rows][aw] the nodes on each row's path
-    uint16_t *next;   // [R] the next entry of the same token
-    int16_t *par;     // [R]
+    uint32_t *count;  // [R] count and prompt bit of a drafted token, at its node
+    uint32_t *node;   // [R] parent, and << 16 the node that stands for the token (kNone:
+                      // not of this chunk)
+    uint8_t *path;    // [rows][R] occurrences of a drafted token on a row's path, one
+                      // byte each, two for R > 256
 };
 
 constexpr size_t kEpiBytesPerNode = 20;
@@ -147,11 +146,15 @@ __host__ __device__ inline size_t stage_bytes(int tokens, int size, int rows, bo
     return verify ? (size_t)rows * kWaves * 16 : (size_t)tokens * size;
 }
 
+__host__ __device__ inline size_t path_bytes(int rows, int R) {
+    return ((size_t)rows * R * (R > 256 ? 2 : 1) + 3) / 4 * 4;
+}
+
 __host__ __device__ inline size_t lds_bytes(int tokens, int size, int R, int rows, int n_bias,
                                             bool verify) {
     const size_t n = (size_t)tokens * 6 + stage_bytes(tokens, size, rows, verify) +
                      (verify ? (size_t)rows * kWaves * 8 : 0) + (size_t)n_bias * 4 +
-                     (size_t)R * 12 + (size_t)rows * ((R + 31) / 32) * 4;
+                     (size_t)R * 8 + path_bytes(rows, R);
     const size_t epi = verify ? R * kEpiBytesPerNode : 0;
     return n > epi ? n : epi;
 }
@@ -164,11 +167,9 @@ __device__ __forceinline__ Lds lds_carve(unsigned char *m, int tokens, int size,
     l.list = (uint16_t *)((unsigned char *)l.stage + stage_bytes(tokens, size, rows, verify));
     l.key = (uint32_t *)(l.list + tokens);
     l.bias = (float *)(l.key + (verify ? 2 * rows * kWaves : 0));
-    l.entry = (uint32_t *)(l.bias + n_bias);
-    l.count = l.entry + R;
-    l.anc = l.count + R;
-    l.next = (uint16_t *)(l.anc + rows * ((R + 31) / 32));
-    l.par = (int16_t *)(l.next + R);
+    l.count = (uint32_t *)(l.bias + n_bias);
+    l.node = l.count + R;
+    l.path = (uint8_t *)(l.node + R);
     return l;
 }
 
@@ -176,18 +177,14 @@ struct Penalty {
     float rho, freq, pres;
 };
 
-// A listed token's logit l with word w in the row whose path is `anc`.
+// A listed token's logit l with word w in the row whose path counts start at
+// entry `row` of s.path.
 __device__ __forceinline__ float processed(float l, uint32_t w, const Penalty &pe, const Lds &s,
-                                           const uint32_t *anc) {
+                                           int row, bool wide) {
     uint32_t c = w;
     if (w & kDrafted) {
-        uint32_t e = w & ((1u << kNodeBits) - 1u);
-        c = s.count[e];
-        do {
-            const uint32_t node = s.entry[e] & ((1u << kNodeBits) - 1u);
-            c += (anc[node >> 5] >> (node & 31u)) & 1u;
-            e = s.next[e];
-        } while (e != kNone);
+        const uint32_t e = w & kCount;
+        c = s.count[e] + (wide ? ((const uint16_t *)s.path)[row + e] : s.path[row + e]);
     }
     const bool prompt = c & kPrompt;
     c &= kCount;
@@ -293,7 +290,7 @@ struct Tile {
     static constexpr uint32_t kAll = (1u << kPer) - 1u;
 
     uint32_t chunk;
-    int chunk_log, b, n, r0, r1, aw;
+    int chunk_log, b, n, r0, r1;
     bool masked;
     // this lane's vectors: first token, which of its tokens exist, and where it
     // is read (the row's last whole vector where fewer exist)
@@ -307,7 +304,6 @@ struct Tile {
         const int group = gb % p.groups;
         b = gb / p.groups;
         r0 = group * p.rows;
-        aw = (p.a.R + 31) / 32;
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
             v0[u] = (int)token((uint32_t)(u * kThreads + threadIdx.x) * kPer);
@@ -454,7 +450,7 @@ __device__ __forceinline__ int list_tokens(const LogitsParams &p, const Tile<kIn
                                            uint32_t &hit) {
     typedef Tile<kIn, kU> T;
     constexpr int kPer = T::kPer;
-    __shared__ int s_entries, s_sum[kWaves];
+    __shared__ int s_low, s_sum[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int b = t.b, R = p.a.R, V = p.a.V, nb = p.a.n_bias, Lmax = p.a.Lmax;
     const int32_t *x = p.a.tokens + (int64_t)b * Lmax;
@@ -478,7 +474,7 @@ __device__ __forceinline__ int list_tokens(const LogitsParams &p, const Tile<kIn
     for (int i = tid; i < T::kTokens / 4; i += kThreads)
         ((u32x4 *)s.word)[i] = u32x4{0u, 0u, 0u, 0u};
     if (tid == 0)
-        s_entries = 0;
+        s_low = R;
     __syncthreads();
     if (nb > 0) {
         // the last entry of a token holds; entries before counts, so that the
@@ -496,38 +492,49 @@ __device__ __forceinline__ int list_tokens(const LogitsParams &p, const Tile<kIn
         __syncthreads();
     }
     if (p.penal) {
-        auto add = [&](int32_t tok, int i) {
-            uint32_t off;
-            if (t.place(tok, V, off)) {
-                if (i < P)
-                    atomicOr(&s.word[off], kPrompt);
-                else
-                    atomicAdd(&s.word[off], 1u);
+        // the prompt sets a bit, what follows it counts
+        auto part = [&](int lo, int hi, auto mark) {
+            auto one = [&](int32_t tok, int i) {
+                uint32_t off;
+                if ((uint32_t)(i - lo) < (uint32_t)(hi - lo) && t.place(tok, V, off))
+                    mark(&s.word[off]);
+            };
+            const int v0 = lo / 4;
+            if (Lmax < 4) {
+                if (tid < Lmax)
+                    one(x[tid], tid);
+                return;
             }
-        };
-        auto add4 = [&](const i32x4 &c, int v) {
-            const int i0 = ctx_start(v, Lmax);
+            auto four = [&](const i32x4 &c, int v) {
+                // of a vector that starts early, the tokens of the one before
+                // it do not count again
+                const int i = ctx_start(v, Lmax);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (i0 + j >= 4 * v && i0 + j < L)
-                    add(c[j], i0 + j);
-        };
-        if (Lmax >= 4) {
+                for (int j = 0; j < 4; ++j)
+                    one(c[j], i + j >= 4 * v ? i + j : hi);
+            };
+            if (v0 < kAhead * kThreads)
 #pragma unroll
-            for (int q = 0; q < kAhead; ++q)
-                add4(h.c[q], tid + q * kThreads);
-            for (int v = tid + kAhead * kThreads; 4 * v < L; v += 8 * kThreads) {
+                for (int q = 0; q < kAhead; ++q)
+                    four(h.c[q], tid + q * kThreads);
+            int v = v0 / kThreads * kThreads;
+            v = (v > kAhead * kThreads ? v : kAhead * kThreads) + tid;
+            for (; 4 * (v - tid) < hi; v += 8 * kThreads) {
                 i32x4 c[8];
 #pragma unroll
                 for (int q = 0; q < 8; ++q)
                     c[q] = *(const i32x4_a *)(x + ctx_start(v + q * kThreads, Lmax));
 #pragma unroll
                 for (int q = 0; q < 8; ++q)
-                    add4(c[q], v + q * kThreads);
+                    if (4 * (v - tid + q * kThreads) < hi)
+                        four(c[q], v + q * kThreads);
             }
-        } else if (tid < L) {
-            add(x[tid], tid);
-        }
+        };
+        if (P > 0)
+            part(0, P, [](uint32_t *w) { atomicOr(w, kPrompt); });
+        if (P < L)
+            part(P, L, [](uint32_t *w) { atomicAdd(w, 1u); });
+        // the draft's nodes, with their tokens' places
         int32_t d_tok = h.tok, d_par = h.par;
         for (int i = tid; i < t.n; i += kThreads) {
             if (i != tid) {
@@ -535,13 +542,35 @@ __device__ __forceinline__ int list_tokens(const LogitsParams &p, const Tile<kIn
                 d_par = dp ? dp[i] : i - 1;
             }
             uint32_t off;
-            s.par[i] = (int16_t)clampi(d_par, -1, R);
-            if (i >= 1 && t.place(d_tok, V, off)) {
-                atomicOr(&s.word[off], kDrafted);
-                s.entry[atomicAdd(&s_entries, 1)] = (off << kNodeBits) | (uint32_t)i;
+            const bool here = t.place(d_tok, V, off) && i >= 1;
+            const uint32_t par = d_par >= 0 && d_par < i ? (uint32_t)d_par : kNone;
+            s.node[i] = par | (here ? off : kNone) << 16;
+            if (here)
+                atomicMin(&s_low, i);
+        }
+        for (int i = tid; i < (int)path_bytes(t.r1 - t.r0, R) / 4; i += kThreads)
+            ((uint32_t *)s.path)[i] = 0u;
+        __syncthreads();
+        // one of a token's nodes, the first to arrive, stands for it and keeps
+        // its count
+        if (s_low < R) {
+            for (int i = tid; i < t.n; i += kThreads) {
+                const uint32_t off = s.node[i] >> 16;
+                if (off == kNone)
+                    continue;
+                const uint32_t w = atomicOr(&s.word[off], kDrafted);
+                if (!(w & kDrafted)) {
+                    s.count[i] = w & (kCount | kPrompt);
+                    s.word[off] = (w & ~(kCount | kPrompt)) | kDrafted | (uint32_t)i;
+                }
+            }
+            __syncthreads();
+            for (int i = tid; i < t.n; i += kThreads) {
+                const uint32_t nd = s.node[i], off = nd >> 16;
+                if (off != kNone)
+                    s.node[i] = (nd & 0xFFFFu) | (s.word[off] & kCount) << 16;
             }
         }
-        __syncthreads();
     }
     // the list, each lane's tokens together
 #pragma unroll
@@ -572,37 +601,18 @@ __device__ __forceinline__ int list_tokens(const LogitsParams &p, const Tile<kIn
         const int j = __ffs(h) - 1;
         s.list[k++] = (uint16_t)(((j / kPer) * kThreads + tid) * kPer + j % kPer);
     }
-    const int entries = s_entries;
-    if (entries > 0) {
-        // the entries of one token chained, its count moved to the first
-        for (int e = tid; e < entries; e += kThreads) {
-            const uint32_t off = s.entry[e] >> kNodeBits;
-            uint32_t nx = kNone;
-            bool first = true;
-            for (int f = 0; f < entries; ++f)
-                if ((s.entry[f] >> kNodeBits) == off) {
-                    if (f > e && nx == kNone)
-                        nx = (uint32_t)f;
-                    first = first && f >= e;
-                }
-            s.next[e] = (uint16_t)nx;
-            if (first) {
-                const uint32_t w = s.word[off];
-                s.count[e] = w & (kCount | kPrompt);
-                s.word[off] = (w & ~(kCount | kPrompt)) | (uint32_t)e;
+    if (p.penal && s_low < R && tid < t.r1 - t.r0) {
+        // each row's path, down to the lowest node with a token of the chunk
+        const int low = s_low, row = tid * R;
+        for (uint32_t i = (uint32_t)(t.r0 + tid); i != kNone && (int)i >= low;) {
+            const uint32_t nd = s.node[i], e = nd >> 16;
+            if (e != kNone) {
+                if (R > 256)
+                    ((uint16_t *)s.path)[row + e] += 1;
+                else
+                    s.path[row + e] += 1;
             }
-        }
-        if (tid < t.r1 - t.r0) {
-            uint32_t *a = s.anc + tid * t.aw;
-            for (int w = 0; w < t.aw; ++w)
-                a[w] = 0u;
-            for (int node = t.r0 + tid; node > 0;) {
-                a[node >> 5] |= 1u << (node & 31);
-                const int q = s.par[node];
-                if (q < 0 || q >= node)
-                    break;
-                node = q;
-            }
+            i = nd & 0xFFFFu;
         }
     }
     __syncthreads();
@@ -649,7 +659,7 @@ __global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
                     const uint32_t off = s.list[k];
                     O *d = dst + t.token(off);
                     *d = Out::put(processed(In::get(*d), s.word[off], pe, s,
-                                            s.anc + (r - t.r0) * t.aw));
+                                            (r - t.r0) * R, R > 256));
                 }
             }
         return;
@@ -671,7 +681,7 @@ __global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
             for (int k = tid; k < listed; k += kThreads) {
                 const uint32_t off = s.list[k];
                 const float y = processed(In::get(stage[off]), s.word[off], pe, s,
-                                          s.anc + (r - t.r0) * t.aw);
+                                          (r - t.r0) * R, R > 256);
                 if constexpr (sizeof(typename In::type) == 4)
                     stage[off] = y;
                 else
@@ -851,7 +861,7 @@ __global__ __launch_bounds__(kThreads) void k_verify(LogitsParams p) {
     };
     // its key: order key, then the lowest place
     auto item_key = [&](const Item &i, uint32_t tok, uint32_t off, uint32_t w, int r) {
-        const float y = processed(In::get(i.x), w, pe, s, s.anc + (r - t.r0) * t.aw);
+        const float y = processed(In::get(i.x), w, pe, s, (r - t.r0) * R, R > 256);
         const bool ok = !kMask || !t.masked || ((i.bits >> (tok & 31u)) & 1u);
         const uint32_t k = order16(ok ? Elem<SWITCHSD_BF16>::put(y) : 0xFF80u);
         return k ? (k << 16) | (kNone - off) : 0u;

@@ -1001,13 +1001,14 @@ int set_logits_grid(LogitsParams &p) {
         return rc;
     const switchsd_logits_args &a = p.a;
     p.penal = a.repetition || a.frequency || a.presence;
-    // Four work-groups per compute unit, down to one where each would count a
+    // Four work-groups per compute unit, down to two where each would count a
     // long history.
     int64_t want = 4 * (int64_t)cus;
     if (p.penal && a.Lmax > 4096)
         want = want * 4096 / a.Lmax;
-    want = want < cus ? cus : want;
-    const int64_t blk = a.logits_type == SWITCHSD_F32 ? 64 : 128;  // tokens of 16 vectors
+    want = want < 2 * cus ? 2 * cus : want;
+    const int64_t vecs = p.out ? kProcessBlk : kVerifyBlk;  // of a block
+    const int64_t blk = vecs * (a.logits_type == SWITCHSD_F32 ? 4 : 8);
     const int64_t blocks = (a.V + blk - 1) / blk;
     // rows of a work-group, at most: their path counts take 16 KB of LDS
     const int64_t most = kPathBytes / (a.R * (a.R > 256 ? 2 : 1));
@@ -1015,7 +1016,7 @@ int set_logits_grid(LogitsParams &p) {
     rows = rows < most ? rows : most;
     int64_t groups = (a.R + rows - 1) / rows;
     for (p.unroll = kLogitsUnroll;; p.unroll >>= 1) {
-        const int64_t per = (int64_t)(kThreads / 16) * p.unroll;  // blocks of a chunk, at most
+        const int64_t per = kThreads / vecs * p.unroll;  // blocks of a chunk, at most
         p.chunk_log = 0;
         while (((int64_t)1 << p.chunk_log) * per < blocks)
             ++p.chunk_log;

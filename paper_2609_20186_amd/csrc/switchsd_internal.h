@@ -202,6 +202,9 @@ int launch_tree_mask_kernel(const int32_t *dpar, const int32_t *dn, int32_t B, i
 constexpr int kRowGroup = 64;
 // 16-byte vectors per lane and row of the logits kernels, at most.
 constexpr int kLogitsUnroll = 2;
+// 16-byte vectors of the blocks that make a chunk: every 2^k-th of a row.
+constexpr int kVerifyBlk = 16;
+constexpr int kProcessBlk = 32;
 // LDS bytes of the path counts of a work-group's rows.
 constexpr int kPathBytes = 16384;
 

@@ -15,8 +15,8 @@
 // So the work per row is the row's bytes plus the listed tokens, however they
 // lie.
 //
-// A chunk is every 2^k-th block of 16 vectors: low token ids, which are the
-// frequent ones, spread over all work-groups of a row.
+// A chunk is every 2^k-th block of 16 vectors (k_process: 32): low token ids,
+// which are the frequent ones, spread over all work-groups of a row.
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 
@@ -270,22 +270,23 @@ __device__ void accept(const LogitsParams &p, int b, unsigned char *mem) {
     }
 }
 
-// A 16-byte vector of 16-bit pairs with the halves of clear bits of `ok` (two
-// bits per word) replaced by `fill` (the same 16 bits twice).
-__device__ __forceinline__ uint32_t keep16(uint32_t x, uint32_t ok, int q, uint32_t fill) {
-    const uint32_t lo = (uint32_t)((int32_t)(ok << (31 - 2 * q)) >> 31);
-    const uint32_t hi = (uint32_t)((int32_t)(ok << (30 - 2 * q)) >> 31);
-    const uint32_t m = (lo & 0xFFFFu) | (hi << 16);
-    return (x & m) | (fill & ~m);
+// Bits 2q and 2q + 1 of `bits`, each spread over one half of a word.
+__device__ __forceinline__ uint32_t halves(uint32_t bits, int q) {
+    const uint32_t lo = (uint32_t)((int32_t)(bits << (31 - 2 * q)) >> 31);
+    const uint32_t hi = (uint32_t)((int32_t)(bits << (30 - 2 * q)) >> 31);
+    return (lo & 0xFFFFu) | (hi & 0xFFFF0000u);
+}
+__device__ __forceinline__ uint32_t select16(uint32_t m, uint32_t x, uint32_t y) {
+    return (x & m) | (y & ~m);
 }
 
-// What a work-group and its lanes have to do.
-template <int kIn, int kU>
+// What a work-group and its lanes have to do.  kBlkVecs: vectors of a block.
+template <int kIn, int kU, int kBlkVecs>
 struct Tile {
     typedef Elem<kIn> In;
     static constexpr int kPer = In::per;
     static constexpr int kBits = 128 / kPer;                  // of an element
-    static constexpr int kBlkLog = kPer == 8 ? 7 : 6;         // tokens of a block: 16 vectors
+    static constexpr int kBlkLog = __builtin_ctz(kBlkVecs * kPer);  // tokens of a block
     static constexpr int kTokens = kThreads * kU * kPer;      // of a chunk
     static constexpr uint32_t kAll = (1u << kPer) - 1u;
 
@@ -344,10 +345,9 @@ struct RowRegs {
 // leaves the later rows' in flight: behind the last row every lane reads that
 // row's first vector, and without a mask the first byte of the logits.
 // kTiny: V below one vector's tokens (read one by one).
-template <int kIn, int kU, bool kMask, bool kTiny>
-__device__ __forceinline__ void load_row(const LogitsParams &p, const Tile<kIn, kU> &t, int r,
+template <bool kMask, bool kTiny, typename T, int kU>
+__device__ __forceinline__ void load_row(const LogitsParams &p, const T &t, int r,
                                          RowRegs<kU> &g) {
-    typedef Tile<kIn, kU> T;
     typedef typename T::In::type E;
     const int V = p.a.V;
     const bool live = r < t.r1;
@@ -377,20 +377,16 @@ __device__ __forceinline__ void load_row(const LogitsParams &p, const Tile<kIn, 
 }
 
 // The allowed bits of vector u.
-template <int kIn, int kU, bool kMask>
-__device__ __forceinline__ uint32_t allowed_of(const Tile<kIn, kU> &t, int u,
-                                               const RowRegs<kU> &g) {
-    typedef Tile<kIn, kU> T;
+template <bool kMask, typename T, int kU>
+__device__ __forceinline__ uint32_t allowed_of(const T &t, int u, const RowRegs<kU> &g) {
     if (!kMask || !t.masked)
         return T::kAll;
     return (g.bits[u] >> (t.v0[u] & 7)) & T::kAll;
 }
 
 // The row's last, partial vector was read as a whole one: its own tokens first.
-template <int kIn, int kU, bool kTiny>
-__device__ __forceinline__ u32x4 own_first(const LogitsParams &p, const Tile<kIn, kU> &t, int u,
-                                           u32x4 x) {
-    typedef Tile<kIn, kU> T;
+template <bool kTiny, typename T>
+__device__ __forceinline__ u32x4 own_first(const LogitsParams &p, const T &t, int u, u32x4 x) {
     typedef unsigned __int128 u128;
     if (!kTiny && t.own[u] != T::kAll && t.own[u] != 0u)
         x = __builtin_bit_cast(u32x4, __builtin_bit_cast(u128, x) >>
@@ -444,11 +440,9 @@ __device__ __forceinline__ void request(const LogitsParams &p, int b, Ahead &h) 
 
 // The words and the list.  `hit`: bit u * kPer + j of a lane is set where token
 // j of its vector u is listed; returns the number of listed tokens.
-template <int kIn, int kU>
-__device__ __forceinline__ int list_tokens(const LogitsParams &p, const Tile<kIn, kU> &t,
-                                           const Lds &s, const Ahead &h, Penalty &pe,
-                                           uint32_t &hit) {
-    typedef Tile<kIn, kU> T;
+template <int kU, typename T>
+__device__ __forceinline__ int list_tokens(const LogitsParams &p, const T &t, const Lds &s,
+                                           const Ahead &h, Penalty &pe, uint32_t &hit) {
     constexpr int kPer = T::kPer;
     __shared__ int s_low, s_sum[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -622,10 +616,11 @@ __device__ __forceinline__ int list_tokens(const LogitsParams &p, const Tile<kIn
 // A store that a lane can leave out without a branch: an offset behind the row's
 // bytes is dropped.
 constexpr uint32_t kNowhere = 0x80000000u;
+constexpr int kNt = 2;  // nontemporal
 
 template <int kIn, int kOut, int kU, bool kMask, bool kTiny>
 __global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
-    typedef Tile<kIn, kU> T;
+    typedef Tile<kIn, kU, kProcessBlk> T;
     typedef Elem<kIn> In;
     typedef Elem<kOut> Out;
     typedef typename Out::type O;
@@ -645,12 +640,12 @@ __global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
     const bool sparse = p.in_place && !(kMask && t.masked);
     RowRegs<kU> ra, rb, rc;
     if (!sparse) {
-        load_row<kIn, kU, kMask, kTiny>(p, t, t.r0, ra);
-        load_row<kIn, kU, kMask, kTiny>(p, t, t.r0 + 1, rb);
+        load_row<kMask, kTiny>(p, t, t.r0, ra);
+        load_row<kMask, kTiny>(p, t, t.r0 + 1, rb);
     }
     Penalty pe;
     uint32_t hit;
-    const int listed = list_tokens(p, t, s, h, pe, hit);
+    const int listed = list_tokens<kU>(p, t, s, h, pe, hit);
     if (sparse) {
         if constexpr (kIn == kOut)
             for (int r = t.r0; r < t.r1; ++r) {
@@ -671,7 +666,7 @@ __global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
             __builtin_amdgcn_make_buffer_rsrc(dst, 0, V * (int)sizeof(O), 0x00027000);
 #pragma unroll
         for (int u = 0; u < kU; ++u)
-            g.x[u] = own_first<kIn, kU, kTiny>(p, t, u, g.x[u]);
+            g.x[u] = own_first<kTiny>(p, t, u, g.x[u]);
         if (listed > 0) {
 #pragma unroll
             for (int u = 0; u < kU; ++u)
@@ -692,7 +687,7 @@ __global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
             const uint32_t hu = (hit >> (u * kPer)) & kAll;
-            const uint32_t ok = allowed_of<kIn, kU, kMask>(t, u, g);
+            const uint32_t ok = allowed_of<kMask>(t, u, g);
             const u32x4 x = g.x[u];
             u32x4 y = x;
             if (hu)
@@ -715,10 +710,10 @@ __global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
                         pk[q] = (uint32_t)Out::put(In::get((uint16_t)x[q])) |
                                 (uint32_t)Out::put(In::get((uint16_t)(x[q] >> 16))) << 16;
                         if (hu)  // listed tokens already have the output's type
-                            pk[q] = keep16(pk[q], ~hu, q, 0u) | keep16(y[q], hu, q, 0u);
+                            pk[q] = select16(halves(hu, q), y[q], pk[q]);
                     }
                     if (kMask && ok != kAll)
-                        pk[q] = keep16(pk[q], ok, q, kInf);
+                        pk[q] = select16(halves(ok, q), pk[q], kInf);
                 }
             }
             const bool write = !p.in_place || hu || ok != kAll;
@@ -726,12 +721,12 @@ __global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
                                    ? (uint32_t)t.v0[u] * (uint32_t)sizeof(O)
                                    : kNowhere;
             if constexpr (kOut == SWITCHSD_F32)
-                __builtin_amdgcn_raw_buffer_store_b128(y, rs, o, 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b128(y, rs, o, 0, kNt);
             else if constexpr (kPer == 8)
                 __builtin_amdgcn_raw_buffer_store_b128(u32x4{pk[0], pk[1], pk[2], pk[3]}, rs, o, 0,
-                                                       0);
+                                                       kNt);
             else
-                __builtin_amdgcn_raw_buffer_store_b64(u32x2{pk[0], pk[1]}, rs, o, 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b64(u32x2{pk[0], pk[1]}, rs, o, 0, kNt);
             if (t.own[u] != kAll && t.own[u] != 0u && write) {
 #pragma unroll
                 for (int j = 0; j < kPer; ++j)
@@ -745,12 +740,12 @@ __global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
         }
     };
     for (int r = t.r0; r < t.r1; r += 3) {
-        load_row<kIn, kU, kMask, kTiny>(p, t, r + 2, rc);
+        load_row<kMask, kTiny>(p, t, r + 2, rc);
         step(ra, r);
-        load_row<kIn, kU, kMask, kTiny>(p, t, r + 3, ra);
+        load_row<kMask, kTiny>(p, t, r + 3, ra);
         if (r + 1 < t.r1)
             step(rb, r + 1);
-        load_row<kIn, kU, kMask, kTiny>(p, t, r + 4, rb);
+        load_row<kMask, kTiny>(p, t, r + 4, rb);
         if (r + 2 < t.r1)
             step(rc, r + 2);
     }
@@ -771,56 +766,76 @@ __device__ __forceinline__ uint32_t elem_key(const u32x4 &x, int j) {
     }
 }
 
-// The order key of a vector's maximum (0: nothing but NaN).  Rounding to bf16
-// keeps the order, so the maximum is taken on the input's patterns: as signed
-// integers where one is not negative, as unsigned ones (the smallest) where all
-// are; a positive NaN takes the slow way.
-template <int kIn>
-__device__ __forceinline__ uint32_t vector_key(const u32x4 &x) {
-    if constexpr (kIn == SWITCHSD_F32) {
-        const int32_t a = (int32_t)x.x > (int32_t)x.y ? (int32_t)x.x : (int32_t)x.y;
-        const int32_t c = (int32_t)x.z > (int32_t)x.w ? (int32_t)x.z : (int32_t)x.w;
-        const int32_t mx = a > c ? a : c;
-        if (mx > 0x7F800000) {
-            uint32_t k = 0u;
+// The order key of the maximum of kU vectors (0: nothing but NaN).  Rounding to
+// bf16 keeps the order, so the maximum is taken on the input's patterns: as
+// signed integers where one is not negative, as unsigned ones (the smallest)
+// where all are; a positive NaN takes the slow way.
+template <int kIn, int kU>
+__device__ __forceinline__ uint32_t lane_key(const u32x4 (&x)[kU]) {
+    typedef Elem<SWITCHSD_BF16> B;
+    constexpr bool k32 = kIn == SWITCHSD_F32;
+    constexpr int32_t kTop = k32 ? 0x7F800000 : kIn == SWITCHSD_BF16 ? 0x7F80 : 0x7C00;
+    auto smax = [](uint32_t a, uint32_t c) {
+        return k32 ? (uint32_t)((int32_t)a > (int32_t)c ? (int32_t)a : (int32_t)c)
+                   : pk_max_i16(a, c);
+    };
+    auto umin = [](uint32_t a, uint32_t c) { return k32 ? (a < c ? a : c) : pk_min_u16(a, c); };
+    uint32_t m = x[0].x;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                k = elem_key<kIn>(x, j) > k ? elem_key<kIn>(x, j) : k;
-            return k;
-        }
-        uint32_t m = (uint32_t)mx;
-        if (mx < 0) {
-            const uint32_t d = x.x < x.y ? x.x : x.y, e = x.z < x.w ? x.z : x.w;
-            m = d < e ? d : e;
-        }
-        return order16(Elem<SWITCHSD_BF16>::put(__uint_as_float(m)));
-    } else {
-        constexpr int32_t kTop = kIn == SWITCHSD_BF16 ? 0x7F80 : 0x7C00;
-        const uint32_t m2 = pk_max_i16(pk_max_i16(x.x, x.y), pk_max_i16(x.z, x.w));
-        const int32_t m0 = (int16_t)m2, m1 = (int32_t)m2 >> 16;
-        const int32_t mx = m0 > m1 ? m0 : m1;
-        if (mx > kTop) {
-            uint32_t k = 0u;
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                k = elem_key<kIn>(x, j) > k ? elem_key<kIn>(x, j) : k;
-            return k;
-        }
-        uint32_t m = (uint32_t)mx;
-        if (mx < 0) {
-            const uint32_t l2 = pk_min_u16(pk_min_u16(x.x, x.y), pk_min_u16(x.z, x.w));
-            m = (l2 & 0xFFFFu) < (l2 >> 16) ? l2 & 0xFFFFu : l2 >> 16;
-        }
-        if constexpr (kIn == SWITCHSD_BF16)
-            return order16(m);
-        else
-            return order16(Elem<SWITCHSD_BF16>::put(Elem<kIn>::get((uint16_t)m)));
+    for (int u = 0; u < kU; ++u)
+        m = smax(smax(smax(m, x[u].x), x[u].y), smax(x[u].z, x[u].w));
+    int32_t mx = (int32_t)m;
+    if constexpr (!k32) {
+        const int32_t m0 = (int16_t)m, m1 = (int32_t)m >> 16;
+        mx = m0 > m1 ? m0 : m1;
     }
+    if (mx > kTop) {
+        uint32_t k = 0u;
+        for (int u = 0; u < kU; ++u)
+#pragma unroll
+            for (int j = 0; j < Elem<kIn>::per; ++j) {
+                const uint32_t e = elem_key<kIn>(x[u], j);
+                k = e > k ? e : k;
+            }
+        return k;
+    }
+    uint32_t v = (uint32_t)mx;
+    if (mx < 0) {
+        uint32_t l = x[0].x;
+#pragma unroll
+        for (int u = 0; u < kU; ++u)
+            l = umin(umin(umin(l, x[u].x), x[u].y), umin(x[u].z, x[u].w));
+        v = k32 ? l : (l & 0xFFFFu) < (l >> 16) ? l & 0xFFFFu : l >> 16;
+    }
+    if constexpr (k32)
+        return order16(B::put(__uint_as_float(v)));
+    else if constexpr (kIn == SWITCHSD_BF16)
+        return order16(v);
+    else
+        return order16(B::put(Elem<kIn>::get((uint16_t)v)));
 }
+
+// The lowest token's place with key `top` among a lane's vectors (the first is
+// number `v` of the chunk).
+template <int kIn, int kU>
+__device__ __forceinline__ uint32_t lane_place(const u32x4 (&x)[kU], uint32_t top, uint32_t v) {
+    constexpr int kPer = Elem<kIn>::per;
+    uint32_t at = kNone;
+#pragma unroll
+    for (int u = kU - 1; u >= 0; --u)
+#pragma unroll
+        for (int j = kPer - 1; j >= 0; --j)
+            at = elem_key<kIn>(x[u], j) == top ? (u * kThreads + v) * kPer + j : at;
+    return at;
+}
+
+// A wave's maximum of a row in LDS: order key << 15 | place, or | the vector
+// that holds it, which is then in LDS too.
+constexpr uint32_t kPlaced = 0x80000000u;
 
 template <int kIn, int kU, bool kMask, bool kTiny>
 __global__ __launch_bounds__(kThreads) void k_verify(LogitsParams p) {
-    typedef Tile<kIn, kU> T;
+    typedef Tile<kIn, kU, kVerifyBlk> T;
     typedef Elem<kIn> In;
     typedef typename In::type E;
     constexpr int kPer = T::kPer;
@@ -837,14 +852,14 @@ __global__ __launch_bounds__(kThreads) void k_verify(LogitsParams p) {
         return;
     const Lds s = lds_carve(mem, T::kTokens, sizeof(E), R, p.rows, p.a.n_bias, true);
     RowRegs<kU> ra, rb, rc;
-    load_row<kIn, kU, kMask, kTiny>(p, t, t.r0, ra);
-    load_row<kIn, kU, kMask, kTiny>(p, t, t.r0 + 1, rb);
+    load_row<kMask, kTiny>(p, t, t.r0, ra);
+    load_row<kMask, kTiny>(p, t, t.r0 + 1, rb);
     for (int i = tid; i < 2 * p.rows * kWaves; i += kThreads)
         s.key[i] = 0u;
     __syncthreads();
     Penalty pe;
     uint32_t hit;
-    const int listed = list_tokens(p, t, s, h, pe, hit);
+    const int listed = list_tokens<kU>(p, t, s, h, pe, hit);
     const int64_t words = (V + 31) / 32;
     // A listed token of this lane: its logit and the word with its allowed bit
     // are requested two rows ahead like the vectors (lanes without one: the
@@ -876,96 +891,114 @@ __global__ __launch_bounds__(kThreads) void k_verify(LogitsParams p) {
     item(tok, t.r0, ia);
     item(tok, t.r0 + 1, ib);
     auto step = [&](RowRegs<kU> &g, const Item &it, int r) {
-        uint32_t best = 0u;  // order key, then the lowest vector
-        u32x4 top = u32x4{0u, 0u, 0u, 0u};
+        // What is listed, not allowed or does not exist leaves the maximum (all
+        // bits set: a negative NaN); -inf, which an allowed or a forbidden token
+        // may be, matters only where nothing is above it.
+        constexpr uint32_t kLow = 0x007Fu;  // the key of -inf
+        u32x4 x[kU];
+        bool forbidden = false;
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
-            const uint32_t out = ((hit >> (u * kPer)) & kAll) | (kAll & ~t.own[u]);
-            const uint32_t ok = allowed_of<kIn, kU, kMask>(t, u, g);
-            u32x4 x = own_first<kIn, kU, kTiny>(p, t, u, g.x[u]);
-            if (ok != kAll || out) {
-                // what is not allowed is -inf, what is listed or does not exist NaN
-                if constexpr (kIn == SWITCHSD_F32) {
+            const uint32_t ok = allowed_of<kMask>(t, u, g);
+            const uint32_t out = (hit >> (u * kPer)) | ~t.own[u] | (kMask ? ~ok : 0u);
+            x[u] = own_first<kTiny>(p, t, u, g.x[u]);
+            if (out & kAll) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        x[j] = (ok >> j) & 1u ? x[j] : 0xFF800000u;
-                        x[j] = (out >> j) & 1u ? 0xFFFFFFFFu : x[j];
-                    }
-                } else {
-                    constexpr uint32_t kInf = kIn == SWITCHSD_BF16 ? 0xFF80FF80u : 0xFC00FC00u;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        x[q] = keep16(keep16(x[q], ok, q, kInf), ~out, q, 0xFFFFFFFFu);
-                }
+                for (int q = 0; q < 4; ++q)
+                    x[u][q] |= kIn == SWITCHSD_F32 ? (uint32_t)((int32_t)(out << (31 - q)) >> 31)
+                                                   : halves(out, q);
             }
-            const uint32_t k = vector_key<kIn>(x);
-            const uint32_t k2 = k ? (k << 16) | (kNone - (uint32_t)(u * kThreads + tid)) : 0u;
-            if (k2 > best) {
-                best = k2;
-                top = x;
-            }
+            if (kMask)
+                forbidden = forbidden || (~ok & t.own[u] & ~(hit >> (u * kPer)));
         }
-        const uint32_t wb = wave_max(best);
-        if (best == wb && wb != 0u) {  // one lane: keys of different vectors differ
-            s.key[(r - t.r0) * kWaves + wave] = wb;
-            ((u32x4 *)s.stage)[(r - t.r0) * kWaves + wave] = top;
+        uint32_t k = lane_key<kIn, kU>(x);
+        if (kMask && forbidden)
+            k = k > kLow ? k : kLow;
+        const uint32_t top = wave_max(k);
+        const unsigned long long who = __ballot(k == top);
+        uint32_t *key = s.key + (r - t.r0) * kWaves + wave;
+        if (top > kLow && (who & (who - 1ull)) == 0ull) {
+            // one lane holds it: its token is looked up when the rows are done
+            if (k == top) {
+                uint32_t u = 0u;
+                u32x4 v = x[0];
+                if constexpr (kU == 2) {
+                    u = lane_key<kIn, 1>({x[0]}) == top ? 0u : 1u;
+                    v = u ? x[kU - 1] : v;
+                }
+                *key = (top << 15) | (u * kThreads + (uint32_t)tid);
+                ((u32x4 *)s.stage)[(r - t.r0) * kWaves + wave] = v;
+            }
+        } else if (top != 0u) {
+            uint32_t at = kNone;
+            if (lane_key<kIn, kU>(x) == top)
+                at = lane_place<kIn, kU>(x, top, (uint32_t)tid);
+            if (kMask && top == kLow)  // a forbidden token is -inf too
+#pragma unroll
+                for (int u = kU - 1; u >= 0; --u) {
+                    const uint32_t no = ~allowed_of<kMask>(t, u, g) & t.own[u] &
+                                        ~(hit >> (u * kPer));
+                    const uint32_t o = (uint32_t)((u * kThreads + tid) * kPer + __ffs(no) - 1);
+                    at = no && o < at ? o : at;
+                }
+            const uint32_t low = kNone - wave_max(kNone - at);
+            if (lane == 0)
+                *key = kPlaced | (top << 15) | low;
         }
         if (wave * 64 < listed) {
-            uint32_t k = tid < listed ? item_key(it, tok, off, word, r) : 0u;
+            uint32_t ki = tid < listed ? item_key(it, tok, off, word, r) : 0u;
             for (int q = tid + kThreads; q < listed; q += kThreads) {
                 const uint32_t o = s.list[q];
                 Item i;
                 item(t.token(o), r, i);
                 const uint32_t k2 = item_key(i, t.token(o), o, s.word[o], r);
-                k = k2 > k ? k2 : k;
+                ki = k2 > ki ? k2 : ki;
             }
-            k = wave_max(k);
+            ki = wave_max(ki);
             if (lane == 0)
-                s.key[(p.rows + r - t.r0) * kWaves + wave] = k;
+                s.key[(p.rows + r - t.r0) * kWaves + wave] = ki;
         }
     };
     for (int r = t.r0; r < t.r1; r += 3) {
-        load_row<kIn, kU, kMask, kTiny>(p, t, r + 2, rc);
+        load_row<kMask, kTiny>(p, t, r + 2, rc);
         item(tok, r + 2, ic);
         step(ra, ia, r);
-        load_row<kIn, kU, kMask, kTiny>(p, t, r + 3, ra);
+        load_row<kMask, kTiny>(p, t, r + 3, ra);
         item(tok, r + 3, ia);
         if (r + 1 < t.r1)
             step(rb, ib, r + 1);
-        load_row<kIn, kU, kMask, kTiny>(p, t, r + 4, rb);
+        load_row<kMask, kTiny>(p, t, r + 4, rb);
         item(tok, r + 4, ib);
         if (r + 2 < t.r1)
             step(rc, ic, r + 2);
     }
     __syncthreads();
+    // the places of the maxima that one lane held, a row and wave per lane
+    if (tid < (t.r1 - t.r0) * kWaves) {
+        const uint32_t e = s.key[tid];
+        const uint32_t top = (e & ~kPlaced) >> 15;
+        uint32_t at = e & 0x7FFFu;
+        if (!(e & kPlaced))
+            at = lane_place<kIn, 1>({((const u32x4 *)s.stage)[tid]}, top, at);
+        s.key[tid] = e != 0u ? (top << 16) | (kNone - at) : 0u;
+    }
+    __syncthreads();
     if (tid < 64) {
         // one row per lane (at most kRowGroup = 64 rows)
         if (tid < t.r1 - t.r0) {
-            uint32_t kb = 0u, ki = 0u;
-            int w = 0;
+            uint32_t k = 0u;
 #pragma unroll
             for (int q = 0; q < kWaves; ++q) {
                 const uint32_t a = s.key[tid * kWaves + q];
                 const uint32_t c = s.key[(p.rows + tid) * kWaves + q];
-                w = a > kb ? q : w;
-                kb = a > kb ? a : kb;
-                ki = c > ki ? c : ki;
+                k = a > k ? a : k;
+                k = c > k ? c : k;
             }
-            // the lowest token of the vector that holds the maximum
-            if (kb && (kb >> 16) >= (ki >> 16)) {
-                const u32x4 x = ((const u32x4 *)s.stage)[tid * kWaves + w];
-                uint32_t first = 0u;
-#pragma unroll
-                for (int j = kPer - 1; j >= 0; --j)
-                    first = elem_key<kIn>(x, j) == (kb >> 16) ? (uint32_t)j : first;
-                kb = (kb & 0xFFFF0000u) | (kNone - ((kNone - (kb & 0xFFFFu)) * kPer + first));
-                ki = kb > ki ? kb : ki;
-            }
-            if (ki)
+            if (k)
                 __hip_atomic_fetch_max(
                     &p.keys[(int64_t)t.b * p.key_stride + t.r0 + tid],
-                    ((unsigned long long)order32(ki >> 16) << 32) |
-                        (0xFFFFFFFFu - t.token(kNone - (ki & 0xFFFFu))),
+                    ((unsigned long long)order32(k >> 16) << 32) |
+                        (0xFFFFFFFFu - t.token(kNone - (k & 0xFFFFu))),
                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
         const bool last = arrive(&p.tickets[(int64_t)t.b * kLineU32],
@@ -981,7 +1014,7 @@ __global__ __launch_bounds__(kThreads) void k_verify(LogitsParams p) {
 template <int kIn, int kOut, int kU, bool kVerify, bool kTiny, bool kMask>
 int launch(const LogitsParams &p, hipStream_t stream) {
     const dim3 grid((unsigned)((int64_t)p.a.B * p.groups * p.chunks));
-    const size_t lds = lds_bytes(Tile<kIn, kU>::kTokens, sizeof(typename Elem<kIn>::type), p.a.R,
+    const size_t lds = lds_bytes(Tile<kIn, kU, 16>::kTokens, sizeof(typename Elem<kIn>::type), p.a.R,
                                  p.rows, p.a.n_bias, kVerify);
     if constexpr (kVerify)
         hipLaunchKernelGGL((k_verify<kIn, kU, kMask, kTiny>), grid, dim3(kThreads), lds, stream,

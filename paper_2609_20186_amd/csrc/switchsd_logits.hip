@@ -333,52 +333,88 @@ struct Tile {
     }
 };
 
-// One lane's part of a row: kU vectors, and the bytes with the allowed bits of
-// their tokens.
-template <int kU>
+// One lane's part of a row: kU vectors, the bytes with the allowed bits of their
+// tokens, and (k_verify) its first listed token with the word of its bit.
+template <int kIn, int kU>
 struct RowRegs {
     u32x4 x[kU];
     uint32_t bits[kU];
+    typename Elem<kIn>::type ix;
+    uint32_t ibits;
 };
 
-// Requests row r.  The requests are unconditional, so that a wait for one row's
-// leaves the later rows' in flight: behind the last row every lane reads that
-// row's first vector, and without a mask the first byte of the logits.
-// kTiny: V below one vector's tokens (read one by one).
-template <bool kMask, bool kTiny, typename T, int kU>
-__device__ __forceinline__ void load_row(const LogitsParams &p, const T &t, int r,
-                                         RowRegs<kU> &g) {
-    typedef typename T::In::type E;
-    const int V = p.a.V;
-    const bool live = r < t.r1;
-    const int64_t row = (int64_t)t.b * p.a.R + (live ? r : t.r1 - 1);
-    const E *src = (const E *)p.a.logits + row * V;
-    const bool use = live && t.masked;
-    const uint8_t *bits = use ? (const uint8_t *)p.a.allowed + row * ((int64_t)((V + 31) / 32) * 4)
-                              : (const uint8_t *)p.a.logits;
+// The rows to read, in order.  The requests are unconditional, so that a wait
+// for one row's leaves the later rows' in flight: behind the last row every lane
+// reads that row's first vector, and without a mask the first bytes of the
+// logits.  kTiny: V below one vector's tokens (read one by one).
+template <int kIn, int kU, bool kMask, bool kTiny>
+struct RowStream {
+    typedef Elem<kIn> In;
+    typedef typename In::type E;
+    const char *src;
+    const uint8_t *bits;
+    int64_t step, bstep;
+    int left;  // rows
+    uint32_t o[kU], bo[kU], io, ibo;
+
+    template <typename T>
+    __device__ __forceinline__ void init(const LogitsParams &p, const T &t) {
+        const int V = p.a.V;
+        const int64_t row = (int64_t)t.b * p.a.R + t.r0;
+        step = (int64_t)V * (int)sizeof(E);
+        bstep = kMask && t.masked ? (int64_t)((V + 31) / 32) * 4 : 0;
+        src = (const char *)p.a.logits + row * step;
+        bits = kMask && t.masked ? (const uint8_t *)p.a.allowed + row * bstep
+                                 : (const uint8_t *)p.a.logits;
+        left = t.r1 - t.r0;
+        io = ibo = 0u;
 #pragma unroll
-    for (int u = 0; u < kU; ++u) {
-        if constexpr (kTiny) {
-            union {
-                E e[T::kPer];
-                u32x4 v;
-            } x;
-#pragma unroll
-            for (int j = 0; j < T::kPer; ++j)
-                x.e[j] = src[t.v0[u] + j < V ? t.v0[u] + j : 0];
-            g.x[u] = x.v;
-        } else {
-            const uint32_t o = live ? (uint32_t)t.at[u] * (uint32_t)sizeof(E) : 0u;
-            g.x[u] = __builtin_nontemporal_load((const u32x4_a *)((const char *)src + o));
+        for (int u = 0; u < kU; ++u) {
+            o[u] = (uint32_t)t.at[u] * (uint32_t)sizeof(E);
+            bo[u] = kMask && t.masked && t.v0[u] < V ? (uint32_t)t.v0[u] >> 3 : 0u;
         }
-        if constexpr (kMask)
-            g.bits[u] = bits[use && t.v0[u] < V ? (uint32_t)t.v0[u] >> 3 : 0u];
     }
-}
+    // the listed token that is read beside the vectors
+    template <typename T>
+    __device__ __forceinline__ void item(const T &t, uint32_t tok) {
+        io = tok * (uint32_t)sizeof(E);
+        ibo = kMask && t.masked ? (tok >> 5) * 4u : 0u;
+    }
+    template <bool kItem, typename T>
+    __device__ __forceinline__ void next(const LogitsParams &p, const T &t, RowRegs<kIn, kU> &g) {
+        const bool live = left > 0;
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            if constexpr (kTiny) {
+                union {
+                    E e[In::per];
+                    u32x4 v;
+                } x;
+#pragma unroll
+                for (int j = 0; j < In::per; ++j)
+                    x.e[j] = ((const E *)src)[t.v0[u] + j < p.a.V ? t.v0[u] + j : 0];
+                g.x[u] = x.v;
+            } else {
+                g.x[u] = __builtin_nontemporal_load((const u32x4_a *)(src + (live ? o[u] : 0u)));
+            }
+            if constexpr (kMask)
+                g.bits[u] = bits[bo[u]];
+        }
+        if constexpr (kItem) {
+            g.ix = *(const E *)(src + io);
+            if constexpr (kMask)
+                g.ibits = *(const uint32_t *)(bits + ibo);
+        }
+        left -= 1;
+        const bool more = left > 0;
+        src += more ? step : 0;
+        bits += more ? bstep : 0;
+    }
+};
 
 // The allowed bits of vector u.
-template <bool kMask, typename T, int kU>
-__device__ __forceinline__ uint32_t allowed_of(const T &t, int u, const RowRegs<kU> &g) {
+template <bool kMask, typename T, typename G>
+__device__ __forceinline__ uint32_t allowed_of(const T &t, int u, const G &g) {
     if (!kMask || !t.masked)
         return T::kAll;
     return (g.bits[u] >> (t.v0[u] & 7)) & T::kAll;
@@ -396,6 +432,15 @@ __device__ __forceinline__ u32x4 own_first(const LogitsParams &p, const T &t, in
 
 constexpr float kOne = 1.0f, kZero = 0.0f;
 __constant__ float c_none[2] = {kOne, kZero};
+
+// Whether some lane of the wave has such a vector.
+template <typename T>
+__device__ __forceinline__ bool any_partial(const T &t) {
+    bool e = false;
+    for (uint32_t o : t.own)
+        e = e || (o != T::kAll && o != 0u);
+    return __ballot(e) != 0ull;
+}
 
 // What the list is made from, requested before anything is waited for: the
 // biases, the first 4096 tokens of the context, the first 256 nodes.
@@ -638,10 +683,12 @@ __global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
                             false);
     // in place without a mask, only the listed tokens are read and written
     const bool sparse = p.in_place && !(kMask && t.masked);
-    RowRegs<kU> ra, rb, rc;
+    RowRegs<kIn, kU> ra, rb, rc;
+    RowStream<kIn, kU, kMask, kTiny> rows;
+    rows.init(p, t);
     if (!sparse) {
-        load_row<kMask, kTiny>(p, t, t.r0, ra);
-        load_row<kMask, kTiny>(p, t, t.r0 + 1, rb);
+        rows.template next<false>(p, t, ra);
+        rows.template next<false>(p, t, rb);
     }
     Penalty pe;
     uint32_t hit;
@@ -660,13 +707,15 @@ __global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
         return;
     }
     typename In::type *stage = (typename In::type *)s.stage;
-    auto step = [&](RowRegs<kU> &g, int r) {
-        O *dst = (O *)p.out + ((int64_t)t.b * R + r) * V;
+    const bool edge = any_partial(t);
+    O *dst = (O *)p.out + ((int64_t)t.b * R + t.r0) * V;
+    auto step = [&](RowRegs<kIn, kU> &g, int r) {
         const __amdgpu_buffer_rsrc_t rs =
             __builtin_amdgcn_make_buffer_rsrc(dst, 0, V * (int)sizeof(O), 0x00027000);
+        if (edge)
 #pragma unroll
-        for (int u = 0; u < kU; ++u)
-            g.x[u] = own_first<kTiny>(p, t, u, g.x[u]);
+            for (int u = 0; u < kU; ++u)
+                g.x[u] = own_first<kTiny>(p, t, u, g.x[u]);
         if (listed > 0) {
 #pragma unroll
             for (int u = 0; u < kU; ++u)
@@ -727,7 +776,7 @@ __global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
                                                        kNt);
             else
                 __builtin_amdgcn_raw_buffer_store_b64(u32x2{pk[0], pk[1]}, rs, o, 0, kNt);
-            if (t.own[u] != kAll && t.own[u] != 0u && write) {
+            if (edge && t.own[u] != kAll && t.own[u] != 0u && write) {
 #pragma unroll
                 for (int j = 0; j < kPer; ++j)
                     if ((t.own[u] >> j) & 1u) {
@@ -738,14 +787,15 @@ __global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
                     }
             }
         }
+        dst += V;
     };
     for (int r = t.r0; r < t.r1; r += 3) {
-        load_row<kMask, kTiny>(p, t, r + 2, rc);
+        rows.template next<false>(p, t, rc);
         step(ra, r);
-        load_row<kMask, kTiny>(p, t, r + 3, ra);
+        rows.template next<false>(p, t, ra);
         if (r + 1 < t.r1)
             step(rb, r + 1);
-        load_row<kMask, kTiny>(p, t, r + 4, rb);
+        rows.template next<false>(p, t, rb);
         if (r + 2 < t.r1)
             step(rc, r + 2);
     }
@@ -851,69 +901,85 @@ __global__ __launch_bounds__(kThreads) void k_verify(LogitsParams p) {
     if (!t.rows(p))
         return;
     const Lds s = lds_carve(mem, T::kTokens, sizeof(E), R, p.rows, p.a.n_bias, true);
-    RowRegs<kU> ra, rb, rc;
-    load_row<kMask, kTiny>(p, t, t.r0, ra);
-    load_row<kMask, kTiny>(p, t, t.r0 + 1, rb);
+    RowRegs<kIn, kU> ra, rb, rc;
+    RowStream<kIn, kU, kMask, kTiny> rows;
+    rows.init(p, t);
+    auto ahead = rows;  // the first two rows' vectors, before the list is known
+    ahead.template next<false>(p, t, ra);
+    ahead.template next<false>(p, t, rb);
     for (int i = tid; i < 2 * p.rows * kWaves; i += kThreads)
         s.key[i] = 0u;
     __syncthreads();
     Penalty pe;
     uint32_t hit;
     const int listed = list_tokens<kU>(p, t, s, h, pe, hit);
-    const int64_t words = (V + 31) / 32;
-    // A listed token of this lane: its logit and the word with its allowed bit
-    // are requested two rows ahead like the vectors (lanes without one: the
-    // row's first token).
-    struct Item {
-        E x;
-        uint32_t bits;
-    };
-    auto item = [&](uint32_t tok, int r, Item &i) {
-        const int64_t row = (int64_t)t.b * R + (r < t.r1 ? r : t.r1 - 1);
-        i.x = ((const E *)p.a.logits)[row * V + tok];
-        if constexpr (kMask)
-            i.bits = t.masked ? p.a.allowed[row * words + (tok >> 5)] : 0u;
-    };
-    // its key: order key, then the lowest place
-    auto item_key = [&](const Item &i, uint32_t tok, uint32_t off, uint32_t w, int r) {
-        const float y = processed(In::get(i.x), w, pe, s, (r - t.r0) * R, R > 256);
-        const bool ok = !kMask || !t.masked || ((i.bits >> (tok & 31u)) & 1u);
-        const uint32_t k = order16(ok ? Elem<SWITCHSD_BF16>::put(y) : 0xFF80u);
-        return k ? (k << 16) | (kNone - off) : 0u;
-    };
+    // This lane's first listed token is read with the rows (lanes without one:
+    // the row's first token); the first two rows' now.
     uint32_t off = 0u, word = 0u, tok = 0u;
     if (tid < listed) {
         off = s.list[tid];
         word = s.word[off];
         tok = t.token(off);
     }
-    Item ia, ib, ic;
-    item(tok, t.r0, ia);
-    item(tok, t.r0 + 1, ib);
-    auto step = [&](RowRegs<kU> &g, const Item &it, int r) {
-        // What is listed, not allowed or does not exist leaves the maximum (all
-        // bits set: a negative NaN); -inf, which an allowed or a forbidden token
-        // may be, matters only where nothing is above it.
-        constexpr uint32_t kLow = 0x007Fu;  // the key of -inf
+    rows.item(t, tok);
+    auto first_item = [&](RowRegs<kIn, kU> &g, const char *src, const uint8_t *bits) {
+        g.ix = *(const E *)(src + rows.io);
+        if constexpr (kMask)
+            g.ibits = *(const uint32_t *)(bits + rows.ibo);
+    };
+    first_item(ra, rows.src, rows.bits);
+    const bool two = t.r0 + 1 < t.r1;
+    first_item(rb, rows.src + (two ? rows.step : 0), rows.bits + (two ? rows.bstep : 0));
+    rows.src = ahead.src;
+    rows.bits = ahead.bits;
+    rows.left = ahead.left;
+    const int64_t words = (V + 31) / 32;
+    // a listed token's key: order key, then the lowest place
+    auto item_key = [&](E x, uint32_t bits, uint32_t tok, uint32_t off, uint32_t w, int r) {
+        const float y = processed(In::get(x), w, pe, s, (r - t.r0) * R, R > 256);
+        const bool ok = !kMask || !t.masked || ((bits >> (tok & 31u)) & 1u);
+        const uint32_t k = order16(ok ? Elem<SWITCHSD_BF16>::put(y) : 0xFF80u);
+        return k ? (k << 16) | (kNone - off) : 0u;
+    };
+    // What is listed or does not exist leaves the maximum (all bits set: a
+    // negative NaN), and so does what is not allowed; -inf, which an allowed or a
+    // forbidden token may be, matters only where nothing is above it.
+    constexpr uint32_t kLow = 0x007Fu;  // the key of -inf
+    auto spread = [](uint32_t bits, int q) {
+        return kIn == SWITCHSD_F32 ? (uint32_t)((int32_t)(bits << (31 - q)) >> 31)
+                                   : halves(bits, q);
+    };
+    u32x4 gone[kU];
+    uint32_t inner[kU];  // tokens that exist and are not listed
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+        inner[u] = t.own[u] & ~(hit >> (u * kPer));
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            gone[u][q] = spread(~inner[u], q);
+    }
+    const bool edge = any_partial(t);
+    auto step = [&](const RowRegs<kIn, kU> &g, int r) {
         u32x4 x[kU];
-        bool forbidden = false;
+        uint32_t no[kU], forbidden = 0u;
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
-            const uint32_t ok = allowed_of<kMask>(t, u, g);
-            const uint32_t out = (hit >> (u * kPer)) | ~t.own[u] | (kMask ? ~ok : 0u);
-            x[u] = own_first<kTiny>(p, t, u, g.x[u]);
-            if (out & kAll) {
+            x[u] = g.x[u];
+            if (edge)
+                x[u] = own_first<kTiny>(p, t, u, x[u]);
+            x[u] |= gone[u];
+            if (kMask && t.masked) {
+                no[u] = ~allowed_of<kMask>(t, u, g) & inner[u];
+                if (__ballot(no[u] != 0u) != 0ull) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    x[u][q] |= kIn == SWITCHSD_F32 ? (uint32_t)((int32_t)(out << (31 - q)) >> 31)
-                                                   : halves(out, q);
+                    for (int q = 0; q < 4; ++q)
+                        x[u][q] |= spread(no[u], q);
+                }
+                forbidden |= no[u];
             }
-            if (kMask)
-                forbidden = forbidden || (~ok & t.own[u] & ~(hit >> (u * kPer)));
         }
-        uint32_t k = lane_key<kIn, kU>(x);
-        if (kMask && forbidden)
-            k = k > kLow ? k : kLow;
+        const uint32_t held = lane_key<kIn, kU>(x);
+        const uint32_t k = kMask && forbidden && held < kLow ? kLow : held;
         const uint32_t top = wave_max(k);
         const unsigned long long who = __ballot(k == top);
         uint32_t *key = s.key + (r - t.r0) * kWaves + wave;
@@ -931,27 +997,29 @@ __global__ __launch_bounds__(kThreads) void k_verify(LogitsParams p) {
             }
         } else if (top != 0u) {
             uint32_t at = kNone;
-            if (lane_key<kIn, kU>(x) == top)
+            if (held == top)
                 at = lane_place<kIn, kU>(x, top, (uint32_t)tid);
-            if (kMask && top == kLow)  // a forbidden token is -inf too
+            if (kMask && t.masked && top == kLow)  // a forbidden token is -inf too
 #pragma unroll
                 for (int u = kU - 1; u >= 0; --u) {
-                    const uint32_t no = ~allowed_of<kMask>(t, u, g) & t.own[u] &
-                                        ~(hit >> (u * kPer));
-                    const uint32_t o = (uint32_t)((u * kThreads + tid) * kPer + __ffs(no) - 1);
-                    at = no && o < at ? o : at;
+                    const uint32_t o =
+                        (uint32_t)((u * kThreads + tid) * kPer + __ffs(no[u]) - 1);
+                    at = no[u] && o < at ? o : at;
                 }
             const uint32_t low = kNone - wave_max(kNone - at);
             if (lane == 0)
                 *key = kPlaced | (top << 15) | low;
         }
         if (wave * 64 < listed) {
-            uint32_t ki = tid < listed ? item_key(it, tok, off, word, r) : 0u;
+            uint32_t ki = tid < listed ? item_key(g.ix, g.ibits, tok, off, word, r) : 0u;
             for (int q = tid + kThreads; q < listed; q += kThreads) {
-                const uint32_t o = s.list[q];
-                Item i;
-                item(t.token(o), r, i);
-                const uint32_t k2 = item_key(i, t.token(o), o, s.word[o], r);
+                const uint32_t o = s.list[q], tq = t.token(o);
+                const int64_t row = (int64_t)t.b * R + r;
+                uint32_t bits = 0u;
+                if (kMask && t.masked)
+                    bits = p.a.allowed[row * words + (tq >> 5)];
+                const uint32_t k2 = item_key(((const E *)p.a.logits)[row * V + tq], bits, tq, o,
+                                             s.word[o], r);
                 ki = k2 > ki ? k2 : ki;
             }
             ki = wave_max(ki);
@@ -960,17 +1028,14 @@ __global__ __launch_bounds__(kThreads) void k_verify(LogitsParams p) {
         }
     };
     for (int r = t.r0; r < t.r1; r += 3) {
-        load_row<kMask, kTiny>(p, t, r + 2, rc);
-        item(tok, r + 2, ic);
-        step(ra, ia, r);
-        load_row<kMask, kTiny>(p, t, r + 3, ra);
-        item(tok, r + 3, ia);
+        rows.template next<true>(p, t, rc);
+        step(ra, r);
+        rows.template next<true>(p, t, ra);
         if (r + 1 < t.r1)
-            step(rb, ib, r + 1);
-        load_row<kMask, kTiny>(p, t, r + 4, rb);
-        item(tok, r + 4, ib);
+            step(rb, r + 1);
+        rows.template next<true>(p, t, rb);
         if (r + 2 < t.r1)
-            step(rc, ic, r + 2);
+            step(rc, r + 2);
     }
     __syncthreads();
     // the places of the maxima that one lane held, a row and wave per lane

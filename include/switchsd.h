@@ -390,7 +390,7 @@ typedef enum { SWITCHSD_BF16 = 0, SWITCHSD_F16 = 1, SWITCHSD_F32 = 2 } switchsd_
  * infinities follow the arithmetic.  A row whose mask allows nothing is all
  * -inf, of which the greedy choice is token 0.
  * Token ids outside [0, V) (pads, -1) count for nothing.
- *   logits [B, R, V] of logits_type, aligned to its elements; dtok [B, R],
+ *   logits [B, R, V] of logits_type, aligned to its elements, V <= 2^26; dtok [B, R],
  *   dpar [B, R] or NULL (chains), dn [B]; tokens [B, Lmax], lengths [B]
  *   (needed with any of the three penalties, else not read; prompt_lens NULL:
  *   no prompt, every token counts), Lmax <= SWITCHSD_MAX_HISTORY; repetition,

@@ -972,7 +972,7 @@ int check_logits(const switchsd_logits_args *a) {
         return SWITCHSD_EINVAL;
     if (a->logits_type < SWITCHSD_BF16 || a->logits_type > SWITCHSD_F32)
         return SWITCHSD_EINVAL;
-    if (!shape_ok_B(a->B) || a->R < 1 || a->R > SWITCHSD_MAX_R || a->V < 1 || a->V > (1 << 28) ||
+    if (!shape_ok_B(a->B) || a->R < 1 || a->R > SWITCHSD_MAX_R || a->V < 1 || a->V > (1 << 26) ||
         a->Lmax < 0 || a->Lmax > SWITCHSD_MAX_HISTORY || a->n_bias < 0 ||
         a->n_bias > SWITCHSD_MAX_BIAS)
         return SWITCHSD_ESHAPE;
@@ -1029,6 +1029,7 @@ int set_logits_grid(LogitsParams &p) {
         rows = (a.R + more - 1) / more;
         groups = (a.R + rows - 1) / rows;
     }
+    p.split = p.unroll == 2 && rows >= kWholeRows ? 1 : 4;
     p.rows = (int32_t)rows;
     p.groups = (int32_t)groups;
     return launch_ok((int64_t)a.B * groups * p.chunks) ? SWITCHSD_OK : SWITCHSD_ESHAPE;

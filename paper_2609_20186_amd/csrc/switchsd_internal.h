@@ -205,8 +205,10 @@ constexpr int kLogitsUnroll = 2;
 // 16-byte vectors of the blocks that make a chunk: every 2^k-th of a row.
 constexpr int kVerifyBlk = 16;
 constexpr int kProcessBlk = 32;
+// Rows of a work-group of k_verify from which its waves take whole rows.
+constexpr int kWholeRows = 8;
 // LDS bytes of the path counts of a work-group's rows.
-constexpr int kPathBytes = 16384;
+constexpr int kPathBytes = 8192;
 
 // Drafted rows a work-group of the page plan takes, at most (one sequence at
 // least), and positions of a range that one of the packed slots takes.
@@ -223,6 +225,7 @@ struct LogitsParams {
     int32_t unroll;     // 16-byte vectors per lane and row
     int32_t chunks;     // vocabulary chunks: a power of two, 2^chunk_log
     int32_t chunk_log;
+    int32_t split;      // verify: waves that share a row (1 or 4)
     int32_t rows;       // rows per group (at most kRowGroup)
     int32_t groups;
     // verify

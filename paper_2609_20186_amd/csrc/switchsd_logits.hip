@@ -129,9 +129,18 @@ struct Elem<SWITCHSD_F32> {
 struct Lds {
     uint32_t *word;   // [tokens]
     void *stage;      // process: [tokens] of the input's type, vectors with listed tokens;
-                      // verify: [rows][kWaves] the vector with the wave's maximum
-    uint16_t *list;   // [tokens] the tokens that have a word
-    uint32_t *key;    // [rows][kWaves] maxima over the vectors, then over the listed tokens
+                      // verify: [rows][split][2] the vectors with the maximum
+    void *list;       // process: [tokens] uint16, the tokens that have a word; verify: the
+                      // first kListed of them, uint32, << 16 the place in `held`
+    uint32_t *lword;  // verify: [kListed] their words
+    // in place of the words, unless more tokens have one than the list holds:
+    u32x4 *gone;      // verify: [vectors] all bits set where a token is listed or does not
+                      // exist
+    u32x4 *held;      // verify: [kWaves][kSlots] the row's vectors with listed tokens
+    uint32_t *bits;   // verify: [kWaves][tokens / 32] the row's allowed bits
+    uint8_t *slot;    // verify: [vectors] a vector's slot in `held` (kNoSlot: none)
+    uint8_t *inner;   // verify: [vectors] the tokens that exist and are not listed
+    uint32_t *key;    // verify: [2][rows][split] maxima over vectors, over listed tokens
     float *bias;      // [n_bias]
     uint32_t *count;  // [R] count and prompt bit of a drafted token, at its node
     uint32_t *node;   // [R] parent, and << 16 the node that stands for the token (kNone:
@@ -142,35 +151,48 @@ struct Lds {
 
 constexpr size_t kEpiBytesPerNode = 20;
 
-__host__ __device__ inline size_t stage_bytes(int tokens, int size, int rows, bool verify) {
-    return verify ? (size_t)rows * kWaves * 16 : (size_t)tokens * size;
-}
+// Listed tokens that k_verify keeps a list of (the rest are found by their
+// words), and vectors with listed tokens that a wave keeps in LDS (the tokens
+// of the rest are read again).
+constexpr int kListed = 512;
+constexpr int kSlots = 128;
+constexpr uint32_t kNoSlot = 0xFFu;
 
 __host__ __device__ inline size_t path_bytes(int rows, int R) {
     return ((size_t)rows * R * (R > 256 ? 2 : 1) + 3) / 4 * 4;
 }
 
-__host__ __device__ inline size_t lds_bytes(int tokens, int size, int R, int rows, int n_bias,
-                                            bool verify) {
-    const size_t n = (size_t)tokens * 6 + stage_bytes(tokens, size, rows, verify) +
-                     (verify ? (size_t)rows * kWaves * 8 : 0) + (size_t)n_bias * 4 +
-                     (size_t)R * 8 + path_bytes(rows, R);
-    const size_t epi = verify ? R * kEpiBytesPerNode : 0;
-    return n > epi ? n : epi;
-}
-
-__device__ __forceinline__ Lds lds_carve(unsigned char *m, int tokens, int size, int R, int rows,
-                                         int n_bias, bool verify) {
-    Lds l;
-    l.word = (uint32_t *)m;
-    l.stage = l.word + tokens;
-    l.list = (uint16_t *)((unsigned char *)l.stage + stage_bytes(tokens, size, rows, verify));
-    l.key = (uint32_t *)(l.list + tokens);
-    l.bias = (float *)(l.key + (verify ? 2 * rows * kWaves : 0));
-    l.count = (uint32_t *)(l.bias + n_bias);
-    l.node = l.count + R;
-    l.path = (uint8_t *)(l.node + R);
-    return l;
+// Places of the parts, and the bytes of all.  split: waves that share a row
+// (0: k_process).
+__host__ __device__ __forceinline__ size_t lds_carve(unsigned char *m, int tokens, int size,
+                                                     int R, int rows, int n_bias, int split,
+                                                     Lds &l) {
+    unsigned char *const m0 = m;
+    auto take = [&](size_t n) {
+        unsigned char *q = m;
+        m += (n + 15) / 16 * 16;
+        return q;
+    };
+    const size_t gone = split ? (size_t)tokens * size : 0;
+    const size_t held = split == 1 ? (size_t)kWaves * kSlots * 16 : 0;
+    const size_t words = (size_t)tokens * 4;
+    unsigned char *w = take(words > gone + held ? words : gone + held);
+    l.word = (uint32_t *)w;
+    l.gone = (u32x4 *)w;
+    l.held = (u32x4 *)(w + gone);
+    l.stage = take(split ? (size_t)rows * split * 32 : (size_t)tokens * size);
+    l.list = take(split ? kListed * 4 : tokens * 2);
+    l.lword = (uint32_t *)take(split ? kListed * 4 : 0);
+    l.bits = (uint32_t *)take(split ? kWaves * tokens / 8 : 0);
+    l.slot = take(split ? tokens * size / 16 : 0);
+    l.inner = take(split ? tokens * size / 16 : 0);
+    l.key = (uint32_t *)take((size_t)rows * split * 8);
+    l.bias = (float *)take((size_t)n_bias * 4);
+    l.count = (uint32_t *)take((size_t)R * 4);
+    l.node = (uint32_t *)take((size_t)R * 4);
+    l.path = take(path_bytes(rows, R));
+    const size_t epi = split ? R * kEpiBytesPerNode : 0;
+    return (size_t)(m - m0) > epi ? (size_t)(m - m0) : epi;
 }
 
 struct Penalty {
@@ -334,13 +356,11 @@ struct Tile {
 };
 
 // One lane's part of a row: kU vectors, the bytes with the allowed bits of their
-// tokens, and (k_verify) its first listed token with the word of its bit.
-template <int kIn, int kU>
+// tokens.
+template <int kU>
 struct RowRegs {
     u32x4 x[kU];
     uint32_t bits[kU];
-    typename Elem<kIn>::type ix;
-    uint32_t ibits;
 };
 
 // The rows to read, in order.  The requests are unconditional, so that a wait
@@ -355,7 +375,7 @@ struct RowStream {
     const uint8_t *bits;
     int64_t step, bstep;
     int left;  // rows
-    uint32_t o[kU], bo[kU], io, ibo;
+    uint32_t o[kU], bo[kU];
 
     template <typename T>
     __device__ __forceinline__ void init(const LogitsParams &p, const T &t) {
@@ -367,21 +387,14 @@ struct RowStream {
         bits = kMask && t.masked ? (const uint8_t *)p.a.allowed + row * bstep
                                  : (const uint8_t *)p.a.logits;
         left = t.r1 - t.r0;
-        io = ibo = 0u;
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
             o[u] = (uint32_t)t.at[u] * (uint32_t)sizeof(E);
             bo[u] = kMask && t.masked && t.v0[u] < V ? (uint32_t)t.v0[u] >> 3 : 0u;
         }
     }
-    // the listed token that is read beside the vectors
     template <typename T>
-    __device__ __forceinline__ void item(const T &t, uint32_t tok) {
-        io = tok * (uint32_t)sizeof(E);
-        ibo = kMask && t.masked ? (tok >> 5) * 4u : 0u;
-    }
-    template <bool kItem, typename T>
-    __device__ __forceinline__ void next(const LogitsParams &p, const T &t, RowRegs<kIn, kU> &g) {
+    __device__ __forceinline__ void next(const LogitsParams &p, const T &t, RowRegs<kU> &g) {
         const bool live = left > 0;
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
@@ -400,11 +413,6 @@ struct RowStream {
             if constexpr (kMask)
                 g.bits[u] = bits[bo[u]];
         }
-        if constexpr (kItem) {
-            g.ix = *(const E *)(src + io);
-            if constexpr (kMask)
-                g.ibits = *(const uint32_t *)(bits + ibo);
-        }
         left -= 1;
         const bool more = left > 0;
         src += more ? step : 0;
@@ -413,8 +421,8 @@ struct RowStream {
 };
 
 // The allowed bits of vector u.
-template <bool kMask, typename T, typename G>
-__device__ __forceinline__ uint32_t allowed_of(const T &t, int u, const G &g) {
+template <bool kMask, typename T, int kU>
+__device__ __forceinline__ uint32_t allowed_of(const T &t, int u, const RowRegs<kU> &g) {
     if (!kMask || !t.masked)
         return T::kAll;
     return (g.bits[u] >> (t.v0[u] & 7)) & T::kAll;
@@ -422,11 +430,11 @@ __device__ __forceinline__ uint32_t allowed_of(const T &t, int u, const G &g) {
 
 // The row's last, partial vector was read as a whole one: its own tokens first.
 template <bool kTiny, typename T>
-__device__ __forceinline__ u32x4 own_first(const LogitsParams &p, const T &t, int u, u32x4 x) {
+__device__ __forceinline__ u32x4 own_first(int V, uint32_t own, u32x4 x) {
     typedef unsigned __int128 u128;
-    if (!kTiny && t.own[u] != T::kAll && t.own[u] != 0u)
+    if (!kTiny && own != T::kAll && own != 0u)
         x = __builtin_bit_cast(u32x4, __builtin_bit_cast(u128, x) >>
-                                          ((T::kPer - p.a.V % T::kPer) * T::kBits));
+                                          ((T::kPer - V % T::kPer) * T::kBits));
     return x;
 }
 
@@ -485,7 +493,7 @@ __device__ __forceinline__ void request(const LogitsParams &p, int b, Ahead &h) 
 
 // The words and the list.  `hit`: bit u * kPer + j of a lane is set where token
 // j of its vector u is listed; returns the number of listed tokens.
-template <int kU, typename T>
+template <int kU, bool kVerify, typename T>
 __device__ __forceinline__ int list_tokens(const LogitsParams &p, const T &t, const Lds &s,
                                            const Ahead &h, Penalty &pe, uint32_t &hit) {
     constexpr int kPer = T::kPer;
@@ -620,7 +628,11 @@ __device__ __forceinline__ int list_tokens(const LogitsParams &p, const T &t, co
             hit |= ((w.x ? 1u : 0u) | (w.y ? 2u : 0u) | (w.z ? 4u : 0u) | (w.w ? 8u : 0u))
                    << (u * kPer + q * 4);
         }
-    const int mine = __popc(hit);
+    // tokens, and << 16 vectors with one (at most 4096 and 512)
+    int mine = __popc(hit);
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+        mine += (hit >> (u * kPer)) & T::kAll ? 1 << 16 : 0;
     int upto = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -636,9 +648,34 @@ __device__ __forceinline__ int list_tokens(const LogitsParams &p, const T &t, co
         k += w < wave ? s_sum[w] : 0;
         total += s_sum[w];
     }
-    for (uint32_t h = hit; h; h &= h - 1u) {
-        const int j = __ffs(h) - 1;
-        s.list[k++] = (uint16_t)(((j / kPer) * kThreads + tid) * kPer + j % kPer);
+    total &= 0xFFFF;
+    if constexpr (kVerify) {
+        int v = k >> 16;
+        k &= 0xFFFF;
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            const uint32_t hu = (hit >> (u * kPer)) & T::kAll;
+            const uint32_t slot = hu && v < kSlots ? (uint32_t)v : kNoSlot;
+            s.slot[u * kThreads + tid] = (uint8_t)slot;
+            for (uint32_t h = hu; h; h &= h - 1u) {
+                const int j = __ffs(h) - 1;
+                const uint32_t at = slot == kNoSlot ? kNone : slot * kPer + j;
+                const uint32_t off = (uint32_t)((u * kThreads + tid) * kPer + j);
+                if (k < kListed) {
+                    ((uint32_t *)s.list)[k] = off | at << 16;
+                    s.lword[k] = s.word[off];
+                }
+                ++k;
+            }
+            v += hu ? 1 : 0;
+        }
+    } else {
+        k &= 0xFFFF;
+        for (uint32_t h = hit; h; h &= h - 1u) {
+            const int j = __ffs(h) - 1;
+            ((uint16_t *)s.list)[k++] =
+                (uint16_t)(((j / kPer) * kThreads + tid) * kPer + j % kPer);
+        }
     }
     if (p.penal && s_low < R && tid < t.r1 - t.r0) {
         // each row's path, down to the lowest node with a token of the chunk
@@ -679,26 +716,27 @@ __global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
     request(p, t.b, h);
     if (!t.rows(p))
         return;
-    const Lds s = lds_carve(mem, T::kTokens, sizeof(typename In::type), R, p.rows, p.a.n_bias,
-                            false);
+    Lds s;
+    lds_carve(mem, T::kTokens, sizeof(typename In::type), R, p.rows, p.a.n_bias, 0, s);
     // in place without a mask, only the listed tokens are read and written
     const bool sparse = p.in_place && !(kMask && t.masked);
-    RowRegs<kIn, kU> ra, rb, rc;
+    RowRegs<kU> ra, rb, rc;
     RowStream<kIn, kU, kMask, kTiny> rows;
     rows.init(p, t);
     if (!sparse) {
-        rows.template next<false>(p, t, ra);
-        rows.template next<false>(p, t, rb);
+        rows.next(p, t, ra);
+        rows.next(p, t, rb);
     }
     Penalty pe;
     uint32_t hit;
-    const int listed = list_tokens<kU>(p, t, s, h, pe, hit);
+    const int listed = list_tokens<kU, false>(p, t, s, h, pe, hit);
+    const uint16_t *list = (const uint16_t *)s.list;
     if (sparse) {
         if constexpr (kIn == kOut)
             for (int r = t.r0; r < t.r1; ++r) {
                 O *dst = (O *)p.out + ((int64_t)t.b * R + r) * V;
                 for (int k = tid; k < listed; k += kThreads) {
-                    const uint32_t off = s.list[k];
+                    const uint32_t off = list[k];
                     O *d = dst + t.token(off);
                     *d = Out::put(processed(In::get(*d), s.word[off], pe, s,
                                             (r - t.r0) * R, R > 256));
@@ -709,13 +747,13 @@ __global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
     typename In::type *stage = (typename In::type *)s.stage;
     const bool edge = any_partial(t);
     O *dst = (O *)p.out + ((int64_t)t.b * R + t.r0) * V;
-    auto step = [&](RowRegs<kIn, kU> &g, int r) {
+    auto step = [&](RowRegs<kU> &g, int r) {
         const __amdgpu_buffer_rsrc_t rs =
             __builtin_amdgcn_make_buffer_rsrc(dst, 0, V * (int)sizeof(O), 0x00027000);
         if (edge)
 #pragma unroll
             for (int u = 0; u < kU; ++u)
-                g.x[u] = own_first<kTiny>(p, t, u, g.x[u]);
+                g.x[u] = own_first<kTiny, T>(V, t.own[u], g.x[u]);
         if (listed > 0) {
 #pragma unroll
             for (int u = 0; u < kU; ++u)
@@ -723,7 +761,7 @@ __global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
                     ((u32x4 *)stage)[u * kThreads + tid] = g.x[u];
             __syncthreads();
             for (int k = tid; k < listed; k += kThreads) {
-                const uint32_t off = s.list[k];
+                const uint32_t off = list[k];
                 const float y = processed(In::get(stage[off]), s.word[off], pe, s,
                                           (r - t.r0) * R, R > 256);
                 if constexpr (sizeof(typename In::type) == 4)
@@ -790,12 +828,12 @@ __global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
         dst += V;
     };
     for (int r = t.r0; r < t.r1; r += 3) {
-        rows.template next<false>(p, t, rc);
+        rows.next(p, t, rc);
         step(ra, r);
-        rows.template next<false>(p, t, ra);
+        rows.next(p, t, ra);
         if (r + 1 < t.r1)
             step(rb, r + 1);
-        rows.template next<false>(p, t, rb);
+        rows.next(p, t, rb);
         if (r + 2 < t.r1)
             step(rc, r + 2);
     }
@@ -865,9 +903,9 @@ __device__ __forceinline__ uint32_t lane_key(const u32x4 (&x)[kU]) {
         return order16(B::put(Elem<kIn>::get((uint16_t)v)));
 }
 
-// The lowest token's place with key `top` among a lane's vectors (the first is
-// number `v` of the chunk).
-template <int kIn, int kU>
+// The lowest token's place with key `top` among a lane's vectors of a piece (the
+// first is number `v` of the chunk, the next 64 or kThreads on, see kSplit).
+template <int kIn, int kSplit, int kU>
 __device__ __forceinline__ uint32_t lane_place(const u32x4 (&x)[kU], uint32_t top, uint32_t v) {
     constexpr int kPer = Elem<kIn>::per;
     uint32_t at = kNone;
@@ -875,7 +913,7 @@ __device__ __forceinline__ uint32_t lane_place(const u32x4 (&x)[kU], uint32_t to
     for (int u = kU - 1; u >= 0; --u)
 #pragma unroll
         for (int j = kPer - 1; j >= 0; --j)
-            at = elem_key<kIn>(x[u], j) == top ? (u * kThreads + v) * kPer + j : at;
+            at = elem_key<kIn>(x[u], j) == top ? (u * kSplit * 64 + v) * kPer + j : at;
     return at;
 }
 
@@ -883,16 +921,41 @@ __device__ __forceinline__ uint32_t lane_place(const u32x4 (&x)[kU], uint32_t to
 // that holds it, which is then in LDS too.
 constexpr uint32_t kPlaced = 0x80000000u;
 
-template <int kIn, int kU, bool kMask, bool kTiny>
-__global__ __launch_bounds__(kThreads) void k_verify(LogitsParams p) {
+// LDS that only the wave itself uses: its operations are done in order, and
+// this keeps the compiler to that order.
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// kSplit: waves that share a row.  4: each of them takes a quarter of the
+// chunk of every row; 1: a wave takes the whole chunk of every fourth row, in
+// four pieces, and closes a row (wave maximum, listed tokens) once per four
+// pieces.  A wave holds four pieces in registers; each is requested anew, for
+// the row after next in its place, once it has been used.  Whole rows keep the
+// vectors with listed tokens in LDS, wave by wave; quarters read those tokens
+// beside them (one per lane with the row's other requests).
+// kU: vectors of a piece per lane.
+constexpr int kBufs = 4;
+
+template <int kIn, int kSplit, int kU, bool kMask, bool kTiny>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kTiny ? 1 : 4))) void
+k_verify(LogitsParams p) {
+    constexpr int kP = kWaves / kSplit;    // pieces of a row per wave
+    constexpr int kRows = kBufs / kP;      // rows held at once
+    constexpr int kStep = kWaves / kSplit; // a wave's rows are this far apart
+    constexpr int kLanes = kSplit * 64;    // lanes that share a row's listed tokens
     typedef Tile<kIn, kU, kVerifyBlk> T;
     typedef Elem<kIn> In;
     typedef typename In::type E;
     constexpr int kPer = T::kPer;
     constexpr uint32_t kAll = T::kAll;
+    constexpr int kWords = T::kTokens / 32;       // of the chunk's allowed bits
+    constexpr int kWordLoads = (kWords + 63) / 64;
     extern __shared__ __align__(16) unsigned char mem[];
     __shared__ int s_last;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int R = p.a.R, V = p.a.V;
     T t;
     t.init(p);
@@ -900,152 +963,272 @@ __global__ __launch_bounds__(kThreads) void k_verify(LogitsParams p) {
     request(p, t.b, h);
     if (!t.rows(p))
         return;
-    const Lds s = lds_carve(mem, T::kTokens, sizeof(E), R, p.rows, p.a.n_bias, true);
-    RowRegs<kIn, kU> ra, rb, rc;
-    RowStream<kIn, kU, kMask, kTiny> rows;
-    rows.init(p, t);
-    auto ahead = rows;  // the first two rows' vectors, before the list is known
-    ahead.template next<false>(p, t, ra);
-    ahead.template next<false>(p, t, rb);
-    for (int i = tid; i < 2 * p.rows * kWaves; i += kThreads)
+    Lds s;
+    lds_carve(mem, T::kTokens, sizeof(E), R, p.rows, p.a.n_bias, kSplit, s);
+    const bool masked = kMask && t.masked;
+
+    // ---- the pieces' vectors: number `n` of a lane starts at token v0 + n *
+    // span; a vector that does not exist whole is read as the row's last whole one
+    auto vec = [&](int q, int u) {
+        return kSplit == 1 ? (uint32_t)((q * kU + u) * 64 + lane)
+                           : (uint32_t)((u * kWaves + wave) * 64 + lane);
+    };
+    const int v0 = (int)t.token(vec(0, 0) * kPer);
+    const int span = (kSplit * 64 / kVerifyBlk) << (t.chunk_log + T::kBlkLog);
+    auto own = [&](int n) {
+        const int left = V - (v0 + n * span);
+        return left >= kPer ? kAll : left > 0 ? (1u << left) - 1u : 0u;
+    };
+    bool part = false;
+#pragma unroll
+    for (int n = 0; n < kP * kU; ++n)
+        part = part || (own(n) != kAll && own(n) != 0u);
+    const bool edge = __ballot(part) != 0ull;
+    const int first = t.r0 + (kSplit == 1 ? wave : 0);
+    const int64_t words = (V + 31) / 32;
+    u32x4 x[kBufs][kU];
+    uint32_t bw[kRows][kWordLoads];
+    E ix[kRows];
+    // Row r of the logits (behind the last row: that row).
+    auto row_of = [&](int r) { return (int64_t)t.b * R + (r < t.r1 ? r : t.r1 - 1); };
+    // All requests are unconditional, so that a wait for one piece leaves the
+    // later ones in flight: behind the last row every lane reads that row's
+    // first vector.
+    auto fetch = [&](int j, int r) {
+        const char *src = (const char *)p.a.logits + row_of(r) * V * (int64_t)sizeof(E);
+        const bool live = r < t.r1;
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            const int v = v0 + (j % kP * kU + u) * span;
+            const int at = v < V - kPer ? v : V - kPer;
+            if constexpr (kTiny) {
+                union {
+                    E e[kPer];
+                    u32x4 v;
+                } y;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+                    y.e[i] = ((const E *)src)[v < V && v + i < V ? v + i : 0];
+                x[j][u] = y.v;
+            } else {
+                x[j][u] = __builtin_nontemporal_load(
+                    (const u32x4_a *)(src + (live ? (uint32_t)at * (uint32_t)sizeof(E) : 0u)));
+            }
+        }
+    };
+    // the words with the allowed bits of the chunk, 32 places each
+    uint32_t wat[kWordLoads];
+#pragma unroll
+    for (int i = 0; i < kWordLoads; ++i) {
+        const uint32_t place = (uint32_t)(lane + i * 64) * 32u;
+        const uint32_t tok = t.token(place);
+        wat[i] = masked && place < (uint32_t)T::kTokens && tok < (uint32_t)V ? tok >> 5 : 0u;
+    }
+    auto fetch_bits = [&](int i, int r) {
+        if constexpr (kMask) {  // (without a mask a word of the nodes' counts)
+            const uint32_t *w = masked ? p.a.allowed + row_of(r) * words
+                                       : (const uint32_t *)p.a.dn;
+#pragma unroll
+            for (int q = 0; q < kWordLoads; ++q)
+                bw[i][q] = w[wat[q]];
+        }
+    };
+#pragma unroll
+    for (int j = 0; j < kBufs; ++j) {
+        if (j % kP == 0)
+            fetch_bits(j / kP, first + j / kP * kStep);
+        fetch(j, first + j / kP * kStep);
+    }
+    for (int i = tid; i < 2 * p.rows * kSplit; i += kThreads)
         s.key[i] = 0u;
     __syncthreads();
     Penalty pe;
-    uint32_t hit;
-    const int listed = list_tokens<kU>(p, t, s, h, pe, hit);
-    // This lane's first listed token is read with the rows (lanes without one:
-    // the row's first token); the first two rows' now.
-    uint32_t off = 0u, word = 0u, tok = 0u;
-    if (tid < listed) {
-        off = s.list[tid];
-        word = s.word[off];
-        tok = t.token(off);
-    }
-    rows.item(t, tok);
-    auto first_item = [&](RowRegs<kIn, kU> &g, const char *src, const uint8_t *bits) {
-        g.ix = *(const E *)(src + rows.io);
-        if constexpr (kMask)
-            g.ibits = *(const uint32_t *)(bits + rows.ibo);
-    };
-    first_item(ra, rows.src, rows.bits);
-    const bool two = t.r0 + 1 < t.r1;
-    first_item(rb, rows.src + (two ? rows.step : 0), rows.bits + (two ? rows.bstep : 0));
-    rows.src = ahead.src;
-    rows.bits = ahead.bits;
-    rows.left = ahead.left;
-    const int64_t words = (V + 31) / 32;
-    // a listed token's key: order key, then the lowest place
-    auto item_key = [&](E x, uint32_t bits, uint32_t tok, uint32_t off, uint32_t w, int r) {
-        const float y = processed(In::get(x), w, pe, s, (r - t.r0) * R, R > 256);
-        const bool ok = !kMask || !t.masked || ((bits >> (tok & 31u)) & 1u);
-        const uint32_t k = order16(ok ? Elem<SWITCHSD_BF16>::put(y) : 0xFF80u);
-        return k ? (k << 16) | (kNone - off) : 0u;
-    };
+    uint32_t mine;
+    const int listed = list_tokens<kU, true>(p, t, s, h, pe, mine);
+    const uint32_t *list = (const uint32_t *)s.list;
+    const bool fits = listed <= kListed;
+
     // What is listed or does not exist leaves the maximum (all bits set: a
     // negative NaN), and so does what is not allowed; -inf, which an allowed or a
     // forbidden token may be, matters only where nothing is above it.
     constexpr uint32_t kLow = 0x007Fu;  // the key of -inf
-    auto spread = [](uint32_t bits, int q) {
-        return kIn == SWITCHSD_F32 ? (uint32_t)((int32_t)(bits << (31 - q)) >> 31)
-                                   : halves(bits, q);
+    auto spread = [](uint32_t b, int q) {
+        return kIn == SWITCHSD_F32 ? (uint32_t)((int32_t)(b << (31 - q)) >> 31) : halves(b, q);
     };
-    u32x4 gone[kU];
-    uint32_t inner[kU];  // tokens that exist and are not listed
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-        inner[u] = t.own[u] & ~(hit >> (u * kPer));
+        const uint32_t in = t.own[u] & ~(mine >> (u * kPer));
+        u32x4 g;
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            gone[u][q] = spread(~inner[u], q);
-    }
-    const bool edge = any_partial(t);
-    auto step = [&](const RowRegs<kIn, kU> &g, int r) {
-        u32x4 x[kU];
-        uint32_t no[kU], forbidden = 0u;
-#pragma unroll
-        for (int u = 0; u < kU; ++u) {
-            x[u] = g.x[u];
-            if (edge)
-                x[u] = own_first<kTiny>(p, t, u, x[u]);
-            x[u] |= gone[u];
-            if (kMask && t.masked) {
-                no[u] = ~allowed_of<kMask>(t, u, g) & inner[u];
-                if (__ballot(no[u] != 0u) != 0ull) {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        x[u][q] |= spread(no[u], q);
-                }
-                forbidden |= no[u];
-            }
-        }
-        const uint32_t held = lane_key<kIn, kU>(x);
-        const uint32_t k = kMask && forbidden && held < kLow ? kLow : held;
-        const uint32_t top = wave_max(k);
-        const unsigned long long who = __ballot(k == top);
-        uint32_t *key = s.key + (r - t.r0) * kWaves + wave;
-        if (top > kLow && (who & (who - 1ull)) == 0ull) {
-            // one lane holds it: its token is looked up when the rows are done
-            if (k == top) {
-                uint32_t u = 0u;
-                u32x4 v = x[0];
-                if constexpr (kU == 2) {
-                    u = lane_key<kIn, 1>({x[0]}) == top ? 0u : 1u;
-                    v = u ? x[kU - 1] : v;
-                }
-                *key = (top << 15) | (u * kThreads + (uint32_t)tid);
-                ((u32x4 *)s.stage)[(r - t.r0) * kWaves + wave] = v;
-            }
-        } else if (top != 0u) {
-            uint32_t at = kNone;
-            if (held == top)
-                at = lane_place<kIn, kU>(x, top, (uint32_t)tid);
-            if (kMask && t.masked && top == kLow)  // a forbidden token is -inf too
-#pragma unroll
-                for (int u = kU - 1; u >= 0; --u) {
-                    const uint32_t o =
-                        (uint32_t)((u * kThreads + tid) * kPer + __ffs(no[u]) - 1);
-                    at = no[u] && o < at ? o : at;
-                }
-            const uint32_t low = kNone - wave_max(kNone - at);
-            if (lane == 0)
-                *key = kPlaced | (top << 15) | low;
-        }
-        if (wave * 64 < listed) {
-            uint32_t ki = tid < listed ? item_key(g.ix, g.ibits, tok, off, word, r) : 0u;
-            for (int q = tid + kThreads; q < listed; q += kThreads) {
-                const uint32_t o = s.list[q], tq = t.token(o);
-                const int64_t row = (int64_t)t.b * R + r;
-                uint32_t bits = 0u;
-                if (kMask && t.masked)
-                    bits = p.a.allowed[row * words + (tq >> 5)];
-                const uint32_t k2 = item_key(((const E *)p.a.logits)[row * V + tq], bits, tq, o,
-                                             s.word[o], r);
-                ki = k2 > ki ? k2 : ki;
-            }
-            ki = wave_max(ki);
-            if (lane == 0)
-                s.key[(p.rows + r - t.r0) * kWaves + wave] = ki;
-        }
-    };
-    for (int r = t.r0; r < t.r1; r += 3) {
-        rows.template next<true>(p, t, rc);
-        step(ra, r);
-        rows.template next<true>(p, t, ra);
-        if (r + 1 < t.r1)
-            step(rb, r + 1);
-        rows.template next<true>(p, t, rb);
-        if (r + 2 < t.r1)
-            step(rc, r + 2);
+        for (int i = 0; i < 4; ++i)
+            g[i] = spread(~in, i);
+        if (fits)
+            s.gone[u * kThreads + tid] = g;
+        s.inner[u * kThreads + tid] = (uint8_t)in;
     }
     __syncthreads();
-    // the places of the maxima that one lane held, a row and wave per lane
-    if (tid < (t.r1 - t.r0) * kWaves) {
-        const uint32_t e = s.key[tid];
+    uint64_t slots = ~0ull;  // of this lane's vectors in `held`, a byte each
+    if (kSplit == 1 && listed > 0 && fits) {
+        slots = 0ull;
+#pragma unroll
+        for (int n = 0; n < kP * kU; ++n)
+            slots |= (uint64_t)s.slot[vec(n / kU, n % kU)] << (8 * n);
+    }
+    u32x4 *held = s.held + wave * kSlots;
+    uint32_t *abits = s.bits + wave * kWords;
+    const int nth = kSplit == 1 ? lane : tid;
+    uint32_t entry0 = 0u, word0 = 0u;  // this lane's first listed token
+    if (nth < listed) {
+        entry0 = list[nth];
+        word0 = s.lword[nth];
+    }
+    const uint32_t item0 = t.token(entry0 & 0xFFFFu) * (uint32_t)sizeof(E);
+    auto fetch_item = [&](int i, int r) {  // (lanes without one: the chunk's first token)
+        if constexpr (kSplit != 1)
+            ix[i] = *(const E *)((const char *)p.a.logits +
+                                 row_of(r) * V * (int64_t)sizeof(E) +
+                                 (nth < listed ? item0 : 0u));
+    };
+#pragma unroll
+    for (int i = 0; i < kRows; ++i)
+        fetch_item(i, first + i * kStep);
+
+    // ---- the rows
+    for (int r = first; r < t.r1; r += kRows * kStep) {
+        uint32_t best = 0u, bq = 0u;    // the lane's maximum and its piece
+        uint32_t forb = kNone;          // its lowest forbidden place
+        u32x4 top_x[kU];
+#pragma unroll
+        for (int j = 0; j < kBufs; ++j) {
+            const int q = j % kP, row = r + j / kP * kStep;
+            if (q == 0) {
+                best = bq = 0u;
+                forb = kNone;
+                if constexpr (kMask) {
+#pragma unroll
+                    for (int i = 0; i < kWordLoads; ++i)
+                        if (kWords % 64 == 0 || lane + i * 64 < kWords)
+                            abits[lane + i * 64] = bw[j / kP][i];
+                    fetch_bits(j / kP, row + kRows * kStep);
+                }
+                wave_fence();
+            }
+            u32x4 y[kU];
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                y[u] = x[j][u];
+                if (edge)
+                    y[u] = own_first<kTiny, T>(V, own(q * kU + u), y[u]);
+                if (kSplit == 1) {
+                    const uint32_t slot = (uint32_t)(slots >> (8 * (q * kU + u))) & 0xFFu;
+                    if (slot != kNoSlot)
+                        held[slot] = y[u];
+                }
+                if (fits)
+                    y[u] |= s.gone[vec(q, u)];
+                else
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        y[u][i] |= spread(~(uint32_t)s.inner[vec(q, u)], i);
+                if (masked) {
+                    const uint32_t v = vec(q, u), place = v * kPer;
+                    const uint32_t ok = ((const uint8_t *)abits)[place >> 3] >> (place & 7u);
+                    uint32_t no = ~ok & kAll;
+                    if (__ballot(no != 0u) != 0ull) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            y[u][i] |= spread(no, i);
+                        no &= s.inner[v];
+                        const uint32_t at = place + (uint32_t)__ffs(no) - 1u;
+                        forb = no && at < forb ? at : forb;
+                    }
+                }
+            }
+            const uint32_t k = lane_key<kIn, kU>(y);
+            const bool up = q == 0 || k > best;
+            best = up ? k : best;
+            bq = up ? (uint32_t)q : bq;
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+                top_x[u] = up ? y[u] : top_x[u];
+            fetch(j, row + kRows * kStep);
+            const E x0 = ix[j / kP];
+            if (q == kP - 1)
+                fetch_item(j / kP, row + kRows * kStep);
+            if (q != kP - 1 || row >= t.r1)
+                continue;
+            const uint32_t mx = kMask && forb != kNone && best < kLow ? kLow : best;
+            const uint32_t top = wave_max(mx);
+            const unsigned long long who = __ballot(mx == top);
+            const int slot = (row - t.r0) * kSplit + (kSplit == 1 ? 0 : wave);
+            if (top > kLow && (who & (who - 1ull)) == 0ull) {
+                // one lane holds it: its token is looked up when the rows are done
+                if (mx == top) {
+                    s.key[slot] = (top << 15) | (bq * 64u * kU + vec(0, 0));
+#pragma unroll
+                    for (int u = 0; u < kU; ++u)
+                        ((u32x4 *)s.stage)[slot * kU + u] = top_x[u];
+                }
+            } else if (top != 0u) {
+                uint32_t at = kNone;
+                if (best == top)
+                    at = lane_place<kIn, kSplit, kU>(top_x, top, bq * 64u * kU + vec(0, 0));
+                if (kMask && top == kLow)  // a forbidden token is -inf too
+                    at = forb < at ? forb : at;
+                const uint32_t low = kNone - wave_max(kNone - at);
+                if (lane == 0)
+                    s.key[slot] = kPlaced | (top << 15) | low;
+            }
+            wave_fence();
+            if ((kSplit == 1 ? 0 : wave * 64) < listed) {
+                uint32_t ki = 0u;  // order key, then the lowest place
+                auto value = [&](uint32_t place, uint32_t at) {
+                    return kSplit == 1 && at != kNone
+                               ? ((const E *)held)[at]
+                               : ((const E *)p.a.logits)[row_of(row) * V + t.token(place)];
+                };
+                auto item = [&](E v, uint32_t place, uint32_t w) {
+                    const float f = processed(In::get(v), w, pe, s, (row - t.r0) * R, R > 256);
+                    const bool ok = !masked || ((abits[place >> 5] >> (place & 31u)) & 1u);
+                    const uint32_t o = order16(ok ? Elem<SWITCHSD_BF16>::put(f) : 0xFF80u);
+                    const uint32_t k2 = o ? (o << 16) | (kNone - place) : 0u;
+                    ki = k2 > ki ? k2 : ki;
+                };
+                if (fits) {
+                    if (nth < listed)
+                        item(kSplit == 1 ? value(entry0 & 0xFFFFu, entry0 >> 16) : x0,
+                             entry0 & 0xFFFFu, word0);
+                    for (int i = nth + kLanes; i < listed; i += kLanes) {
+                        const uint32_t e = list[i];
+                        item(value(e & 0xFFFFu, e >> 16), e & 0xFFFFu, s.lword[i]);
+                    }
+                } else {
+                    // more than the list holds: every token with a word
+                    for (int i = nth; i < T::kTokens; i += kLanes)
+                        if (s.word[i] != 0u)
+                            item(value((uint32_t)i, kNone), (uint32_t)i, s.word[i]);
+                }
+                ki = wave_max(ki);
+                if (lane == 0)
+                    s.key[p.rows * kSplit + slot] = ki;
+            }
+            wave_fence();
+        }
+    }
+    __syncthreads();
+    // the places of the maxima that one lane held
+    for (int i = tid; i < (t.r1 - t.r0) * kSplit; i += kThreads) {
+        const uint32_t e = s.key[i];
         const uint32_t top = (e & ~kPlaced) >> 15;
         uint32_t at = e & 0x7FFFu;
-        if (!(e & kPlaced))
-            at = lane_place<kIn, 1>({((const u32x4 *)s.stage)[tid]}, top, at);
-        s.key[tid] = e != 0u ? (top << 16) | (kNone - at) : 0u;
+        if (!(e & kPlaced)) {
+            u32x4 y[kU];
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+                y[u] = ((const u32x4 *)s.stage)[i * kU + u];
+            at = lane_place<kIn, kSplit, kU>(y, top, at);
+        }
+        s.key[i] = e != 0u ? (top << 16) | (kNone - at) : 0u;
     }
     __syncthreads();
     if (tid < 64) {
@@ -1053,9 +1236,9 @@ __global__ __launch_bounds__(kThreads) void k_verify(LogitsParams p) {
         if (tid < t.r1 - t.r0) {
             uint32_t k = 0u;
 #pragma unroll
-            for (int q = 0; q < kWaves; ++q) {
-                const uint32_t a = s.key[tid * kWaves + q];
-                const uint32_t c = s.key[(p.rows + tid) * kWaves + q];
+            for (int q = 0; q < kSplit; ++q) {
+                const uint32_t a = s.key[tid * kSplit + q];
+                const uint32_t c = s.key[(p.rows + tid) * kSplit + q];
                 k = a > k ? a : k;
                 k = c > k ? c : k;
             }
@@ -1076,14 +1259,18 @@ __global__ __launch_bounds__(kThreads) void k_verify(LogitsParams p) {
         accept(p, t.b, mem);
 }
 
-template <int kIn, int kOut, int kU, bool kVerify, bool kTiny, bool kMask>
+// kU: vectors per lane and row (of a piece); kSplit: waves that share a row of
+// k_verify, 0: k_process.
+template <int kIn, int kOut, int kU, int kSplit, bool kTiny, bool kMask>
 int launch(const LogitsParams &p, hipStream_t stream) {
     const dim3 grid((unsigned)((int64_t)p.a.B * p.groups * p.chunks));
-    const size_t lds = lds_bytes(Tile<kIn, kU, 16>::kTokens, sizeof(typename Elem<kIn>::type), p.a.R,
-                                 p.rows, p.a.n_bias, kVerify);
-    if constexpr (kVerify)
-        hipLaunchKernelGGL((k_verify<kIn, kU, kMask, kTiny>), grid, dim3(kThreads), lds, stream,
-                           p);
+    Lds l;
+    const size_t lds = lds_carve(nullptr, kThreads * kU * Elem<kIn>::per,
+                                 sizeof(typename Elem<kIn>::type), p.a.R, p.rows, p.a.n_bias,
+                                 kSplit, l);
+    if constexpr (kSplit > 0)
+        hipLaunchKernelGGL((k_verify<kIn, kSplit, kU, kMask, kTiny>), grid, dim3(kThreads), lds,
+                           stream, p);
     else
         hipLaunchKernelGGL((k_process<kIn, kOut, kU, kMask, kTiny>), grid, dim3(kThreads), lds,
                            stream, p);
@@ -1092,11 +1279,14 @@ int launch(const LogitsParams &p, hipStream_t stream) {
 
 template <int kIn, int kOut, bool kVerify, bool kMask>
 int launch_unroll(const LogitsParams &p, hipStream_t stream) {
+    constexpr int kSplit = kVerify ? 4 : 0;
     if (p.a.V < Elem<kIn>::per)
-        return launch<kIn, kOut, 1, kVerify, true, kMask>(p, stream);
-    if (p.unroll == 2)
-        return launch<kIn, kOut, 2, kVerify, false, kMask>(p, stream);
-    return launch<kIn, kOut, 1, kVerify, false, kMask>(p, stream);
+        return launch<kIn, kOut, 1, kSplit, true, kMask>(p, stream);
+    if constexpr (kVerify)
+        if (p.split == 1)
+            return launch<kIn, kOut, 2, 1, false, kMask>(p, stream);
+    return p.unroll == 2 ? launch<kIn, kOut, 2, kSplit, false, kMask>(p, stream)
+                         : launch<kIn, kOut, 1, kSplit, false, kMask>(p, stream);
 }
 
 template <int kIn, int kOut, bool kVerify>

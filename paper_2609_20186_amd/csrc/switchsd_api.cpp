@@ -1089,6 +1089,8 @@ int switchsd_verify_processed(const switchsd_logits_args *a, int32_t *accept_len
     const Workspace w = carve(workspace, a->B, a->R, 0, 0);
     p.keys = w.keys;
     p.key_stride = w.key_stride;
+    p.skeys = w.skeys;
+    p.skey_stride = w.skey_stride;
     p.tickets = w.tk_all;
     if ((rc = set_logits_grid(p)))
         return rc;

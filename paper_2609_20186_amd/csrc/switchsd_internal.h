@@ -206,7 +206,7 @@ constexpr int kLogitsUnroll = 2;
 constexpr int kVerifyBlk = 16;
 constexpr int kProcessBlk = 32;
 // Rows of a work-group of k_verify from which its waves take whole rows.
-constexpr int kWholeRows = 8;
+constexpr int kWholeRows = 16;
 // LDS bytes of the path counts of a work-group's rows.
 constexpr int kPathBytes = 8192;
 
@@ -230,8 +230,10 @@ struct LogitsParams {
     int32_t groups;
     // verify
     int32_t *accept_len, *accept_node, *bonus, *out_tokens, *amax;
-    unsigned long long *keys;  // [B] x key_stride row maxima
+    unsigned long long *keys;  // [B] x key_stride row maxima (R > 64)
     int32_t key_stride;
+    unsigned long long *skeys; // [B] x skey_stride copies of them (R <= 64)
+    int32_t skey_stride;
     uint32_t *tickets;         // [B] x kLineU32
 };
 

@@ -93,6 +93,20 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
     return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
+// Inclusive sum over the wave's lanes: row shifts, then two row broadcasts.
+__device__ __forceinline__ int wave_scan(int v) {
+#define SWITCHSD_STEP(ctrl, mask) \
+    v += __builtin_amdgcn_update_dpp(0, v, ctrl, mask, 0xf, false);
+    SWITCHSD_STEP(0x111, 0xf)
+    SWITCHSD_STEP(0x112, 0xf)
+    SWITCHSD_STEP(0x114, 0xf)
+    SWITCHSD_STEP(0x118, 0xf)
+    SWITCHSD_STEP(0x142, 0xa)
+    SWITCHSD_STEP(0x143, 0xc)
+#undef SWITCHSD_STEP
+    return v;
+}
+
 template <int kType>
 struct Elem;
 template <>
@@ -173,7 +187,7 @@ __host__ __device__ __forceinline__ size_t lds_carve(unsigned char *m, int token
         m += (n + 15) / 16 * 16;
         return q;
     };
-    const size_t gone = split ? (size_t)tokens * size : 0;
+    const size_t gone = split == 1 ? (size_t)tokens * size : 0;
     const size_t held = split == 1 ? (size_t)kWaves * kSlots * 16 : 0;
     const size_t words = (size_t)tokens * 4;
     unsigned char *w = take(words > gone + held ? words : gone + held);
@@ -184,8 +198,8 @@ __host__ __device__ __forceinline__ size_t lds_carve(unsigned char *m, int token
     l.list = take(split ? kListed * 4 : tokens * 2);
     l.lword = (uint32_t *)take(split ? kListed * 4 : 0);
     l.bits = (uint32_t *)take(split ? kWaves * tokens / 8 : 0);
-    l.slot = take(split ? tokens * size / 16 : 0);
-    l.inner = take(split ? tokens * size / 16 : 0);
+    l.slot = take(split == 1 ? tokens * size / 16 : 0);
+    l.inner = take(split == 1 ? tokens * size / 16 : 0);
     l.key = (uint32_t *)take((size_t)rows * split * 8);
     l.bias = (float *)take((size_t)n_bias * 4);
     l.count = (uint32_t *)take((size_t)R * 4);
@@ -222,63 +236,90 @@ __device__ __forceinline__ float processed(float l, uint32_t w, const Penalty &p
     return y;
 }
 
-// The accept rule over the row maxima of sequence b (Sec. 3.3, Parallel
-// Verification), by the whole work-group: an edge holds iff the node's token
-// is its valid parent's maximum; a node is accepted iff every edge up to the
-// anchor holds; the deepest accepted node wins, ties to the lowest index.
-__device__ void accept(const LogitsParams &p, int b, unsigned char *mem) {
-    const int R = p.a.R, tid = threadIdx.x;
+// LDS that only the wave itself uses: its operations are done in order, and
+// this keeps the compiler to that order.
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Row maxima of a sequence meet in the workspace: up to 64 rows in one of 16
+// copies by chunk (atomics to one line follow each other), else in one.
+constexpr int kCopies = 16;
+__device__ __forceinline__ unsigned long long *row_keys(const LogitsParams &p, int b, int copy) {
+    return p.a.R <= 64 ? p.skeys + (int64_t)b * p.skey_stride + copy * p.a.R
+                       : p.keys + (int64_t)b * p.key_stride;
+}
+
+// The accept rule over the row maxima of sequence b with n nodes (Sec. 3.3,
+// Parallel Verification), by wave 0: an edge holds iff the node's token is its
+// valid parent's maximum; a node is accepted iff every edge up to the anchor
+// holds; the deepest accepted node wins, ties to the lowest index.  tok0 and
+// par0: token and parent of node `lane`.
+__device__ __forceinline__ void accept(const LogitsParams &p, int b, int n, int tok0, int par0,
+                                       unsigned char *mem) {
+    const int R = p.a.R, lane = threadIdx.x;
     const int64_t base = (int64_t)b * R;
-    const int n = clampi(p.a.dn[b], 1, R);
     int32_t *am = (int32_t *)mem, *tok = am + R, *par = tok + R;
     uint32_t *st = (uint32_t *)(par + R);  // [2][R]
-    __shared__ uint32_t s_best;
-    unsigned long long *keys = p.keys + (int64_t)b * p.key_stride;
-    for (int i = tid; i < R; i += kThreads) {
-        int a = -1;
+    const int copies = p.chunks < kCopies ? p.chunks : kCopies;
+    for (int i = lane; i < R; i += 64) {
+        unsigned long long k = 0ull;
         if (i < n) {
-            const unsigned long long k = ld_u64(&keys[i]);
-            st_u64(&keys[i], 0ull);
-            a = k ? (int32_t)(0xFFFFFFFFu - (uint32_t)k) : 0;
+            if (R > 64) {
+                k = ld_u64(row_keys(p, b, 0) + i);
+                st_u64(row_keys(p, b, 0) + i, 0ull);
+            } else {
+                unsigned long long c[kCopies];
+#pragma unroll
+                for (int q = 0; q < kCopies; ++q)
+                    c[q] = ld_u64(row_keys(p, b, q < copies ? q : 0) + i);
+#pragma unroll
+                for (int q = 0; q < kCopies; ++q)
+                    k = c[q] > k ? c[q] : k;
+                for (int q = 0; q < copies; ++q)
+                    st_u64(row_keys(p, b, q) + i, 0ull);
+            }
         }
+        const int a = i >= n ? -1 : k ? (int32_t)(0xFFFFFFFFu - (uint32_t)k) : 0;
         am[i] = a;
-        tok[i] = p.a.dtok[base + i];
-        par[i] = p.a.dpar ? p.a.dpar[base + i] : i - 1;
+        tok[i] = i == lane ? tok0 : p.a.dtok[base + i];
+        par[i] = i == lane ? par0 : p.a.dpar ? p.a.dpar[base + i] : i - 1;
         if (p.amax)
             p.amax[base + i] = a;
     }
-    if (tid == 0)
-        s_best = 0u;
-    __syncthreads();
-    for (int i = tid; i < n; i += kThreads) {
+    wave_fence();
+    for (int i = lane; i < n; i += 64) {
         const int q = par[i];
         const bool valid = i >= 1 && q >= 0 && q < i;
         const bool ok = i == 0 || (valid && tok[i] == am[q]);
         st[i] = (ok ? kHolds : 0u) | ((i == 0 ? 0u : 1u) << 16) | (uint32_t)(valid ? q : 0);
     }
-    __syncthreads();
+    wave_fence();
     int cur = 0;
     for (bool open = true; open; cur ^= 1) {
         bool more = false;
-        for (int i = tid; i < n; i += kThreads) {
+        for (int i = lane; i < n; i += 64) {
             const uint32_t s1 = st[cur * R + i];
             const uint32_t nv = jump_compose(s1, st[cur * R + (int)(s1 & 0xFFFFu)]);
             st[(cur ^ 1) * R + i] = nv;
             more |= (nv & 0xFFFFu) != 0u;
         }
-        open = __syncthreads_or(more);
+        wave_fence();
+        open = __ballot(more) != 0ull;
     }
-    for (int i = tid; i < n; i += kThreads) {
+    uint32_t kb = 0u;
+    for (int i = lane; i < n; i += 64) {
         const uint32_t s1 = st[cur * R + i];
-        if (s1 & kHolds)
-            atomicMax(&s_best, (((s1 >> 16) & 0x7FFFu) << 16) | (0xFFFFu - (uint32_t)i));
+        const uint32_t k = (((s1 >> 16) & 0x7FFFu) << 16) | (0xFFFFu - (uint32_t)i);
+        kb = (s1 & kHolds) && k > kb ? k : kb;
     }
-    __syncthreads();
-    const int best = (int)(0xFFFFu - (s_best & 0xFFFFu)), depth = (int)(s_best >> 16);
-    for (int i = tid; i < R; i += kThreads)
+    kb = wave_max(kb);
+    const int best = (int)(0xFFFFu - (kb & 0xFFFFu)), depth = (int)(kb >> 16);
+    for (int i = lane; i < R; i += 64)
         if (i > depth)
             p.out_tokens[base + i] = -1;
-    if (tid == 0) {
+    if (lane == 0) {
         int node = best;
         for (int pos = depth - 1; pos >= 0; --pos) {
             p.out_tokens[base + pos] = tok[node];
@@ -493,7 +534,7 @@ __device__ __forceinline__ void request(const LogitsParams &p, int b, Ahead &h) 
 
 // The words and the list.  `hit`: bit u * kPer + j of a lane is set where token
 // j of its vector u is listed; returns the number of listed tokens.
-template <int kU, bool kVerify, typename T>
+template <int kU, int kSplit, typename T>
 __device__ __forceinline__ int list_tokens(const LogitsParams &p, const T &t, const Lds &s,
                                            const Ahead &h, Penalty &pe, uint32_t &hit) {
     constexpr int kPer = T::kPer;
@@ -540,47 +581,42 @@ __device__ __forceinline__ int list_tokens(const LogitsParams &p, const T &t, co
     }
     if (p.penal) {
         // the prompt sets a bit, what follows it counts
-        auto part = [&](int lo, int hi, auto mark) {
-            auto one = [&](int32_t tok, int i) {
-                uint32_t off;
-                if ((uint32_t)(i - lo) < (uint32_t)(hi - lo) && t.place(tok, V, off))
-                    mark(&s.word[off]);
-            };
-            const int v0 = lo / 4;
-            if (Lmax < 4) {
-                if (tid < Lmax)
-                    one(x[tid], tid);
-                return;
+        auto one = [&](int32_t tok, int i) {
+            uint32_t off;
+            if (i < L && t.place(tok, V, off)) {
+                if (i < P)
+                    atomicOr(&s.word[off], kPrompt);
+                else
+                    atomicAdd(&s.word[off], 1u);
             }
-            auto four = [&](const i32x4 &c, int v) {
-                // of a vector that starts early, the tokens of the one before
-                // it do not count again
-                const int i = ctx_start(v, Lmax);
+        };
+        // of a vector that starts early, the tokens of the one before it do not
+        // count again
+        auto four = [&](const i32x4 &c, int v) {
+            const int i = ctx_start(v, Lmax);
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    one(c[j], i + j >= 4 * v ? i + j : hi);
-            };
-            if (v0 < kAhead * kThreads)
+            for (int j = 0; j < 4; ++j)
+                one(c[j], i + j >= 4 * v ? i + j : L);
+        };
+        if (Lmax < 4) {
+            if (tid < Lmax)
+                one(x[tid], tid);
+        } else {
 #pragma unroll
-                for (int q = 0; q < kAhead; ++q)
+            for (int q = 0; q < kAhead; ++q)
+                if (4 * q * kThreads < L)
                     four(h.c[q], tid + q * kThreads);
-            int v = v0 / kThreads * kThreads;
-            v = (v > kAhead * kThreads ? v : kAhead * kThreads) + tid;
-            for (; 4 * (v - tid) < hi; v += 8 * kThreads) {
+            for (int v = tid + kAhead * kThreads; 4 * (v - tid) < L; v += 8 * kThreads) {
                 i32x4 c[8];
 #pragma unroll
                 for (int q = 0; q < 8; ++q)
                     c[q] = *(const i32x4_a *)(x + ctx_start(v + q * kThreads, Lmax));
 #pragma unroll
                 for (int q = 0; q < 8; ++q)
-                    if (4 * (v - tid + q * kThreads) < hi)
+                    if (4 * (v - tid + q * kThreads) < L)
                         four(c[q], v + q * kThreads);
             }
-        };
-        if (P > 0)
-            part(0, P, [](uint32_t *w) { atomicOr(w, kPrompt); });
-        if (P < L)
-            part(P, L, [](uint32_t *w) { atomicAdd(w, 1u); });
+        }
         // the draft's nodes, with their tokens' places
         int32_t d_tok = h.tok, d_par = h.par;
         for (int i = tid; i < t.n; i += kThreads) {
@@ -630,15 +666,11 @@ __device__ __forceinline__ int list_tokens(const LogitsParams &p, const T &t, co
         }
     // tokens, and << 16 vectors with one (at most 4096 and 512)
     int mine = __popc(hit);
+    if (kSplit == 1)
 #pragma unroll
-    for (int u = 0; u < kU; ++u)
-        mine += (hit >> (u * kPer)) & T::kAll ? 1 << 16 : 0;
-    int upto = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int q = __shfl_up(upto, o);
-        upto += lane >= o ? q : 0;
-    }
+        for (int u = 0; u < kU; ++u)
+            mine += (hit >> (u * kPer)) & T::kAll ? 1 << 16 : 0;
+    const int upto = wave_scan(mine);
     if (lane == 63)
         s_sum[wave] = upto;
     __syncthreads();
@@ -649,14 +681,15 @@ __device__ __forceinline__ int list_tokens(const LogitsParams &p, const T &t, co
         total += s_sum[w];
     }
     total &= 0xFFFF;
-    if constexpr (kVerify) {
+    if constexpr (kSplit > 0) {
         int v = k >> 16;
         k &= 0xFFFF;
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
             const uint32_t hu = (hit >> (u * kPer)) & T::kAll;
             const uint32_t slot = hu && v < kSlots ? (uint32_t)v : kNoSlot;
-            s.slot[u * kThreads + tid] = (uint8_t)slot;
+            if (kSplit == 1)
+                s.slot[u * kThreads + tid] = (uint8_t)slot;
             for (uint32_t h = hu; h; h &= h - 1u) {
                 const int j = __ffs(h) - 1;
                 const uint32_t at = slot == kNoSlot ? kNone : slot * kPer + j;
@@ -729,7 +762,7 @@ __global__ __launch_bounds__(kThreads) void k_process(LogitsParams p) {
     }
     Penalty pe;
     uint32_t hit;
-    const int listed = list_tokens<kU, false>(p, t, s, h, pe, hit);
+    const int listed = list_tokens<kU, 0>(p, t, s, h, pe, hit);
     const uint16_t *list = (const uint16_t *)s.list;
     if (sparse) {
         if constexpr (kIn == kOut)
@@ -921,13 +954,6 @@ __device__ __forceinline__ uint32_t lane_place(const u32x4 (&x)[kU], uint32_t to
 // that holds it, which is then in LDS too.
 constexpr uint32_t kPlaced = 0x80000000u;
 
-// LDS that only the wave itself uses: its operations are done in order, and
-// this keeps the compiler to that order.
-__device__ __forceinline__ void wave_fence() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 // kSplit: waves that share a row.  4: each of them takes a quarter of the
 // chunk of every row; 1: a wave takes the whole chunk of every fourth row, in
 // four pieces, and closes a row (wave maximum, listed tokens) once per four
@@ -953,7 +979,6 @@ k_verify(LogitsParams p) {
     constexpr int kWords = T::kTokens / 32;       // of the chunk's allowed bits
     constexpr int kWordLoads = (kWords + 63) / 64;
     extern __shared__ __align__(16) unsigned char mem[];
-    __shared__ int s_last;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int R = p.a.R, V = p.a.V;
@@ -1044,7 +1069,7 @@ k_verify(LogitsParams p) {
     __syncthreads();
     Penalty pe;
     uint32_t mine;
-    const int listed = list_tokens<kU, true>(p, t, s, h, pe, mine);
+    const int listed = list_tokens<kU, kSplit>(p, t, s, h, pe, mine);
     const uint32_t *list = (const uint32_t *)s.list;
     const bool fits = listed <= kListed;
 
@@ -1055,18 +1080,22 @@ k_verify(LogitsParams p) {
     auto spread = [](uint32_t b, int q) {
         return kIn == SWITCHSD_F32 ? (uint32_t)((int32_t)(b << (31 - q)) >> 31) : halves(b, q);
     };
+    u32x4 gone[kU];  // of vectors u * kThreads + tid: with shared rows, this lane's
+    uint32_t inner[kU];
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-        const uint32_t in = t.own[u] & ~(mine >> (u * kPer));
-        u32x4 g;
+        inner[u] = t.own[u] & ~(mine >> (u * kPer));
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            g[i] = spread(~in, i);
-        if (fits)
-            s.gone[u * kThreads + tid] = g;
-        s.inner[u * kThreads + tid] = (uint8_t)in;
+            gone[u][i] = spread(~inner[u], i);
+        if (kSplit == 1) {
+            if (fits)
+                s.gone[u * kThreads + tid] = gone[u];
+            s.inner[u * kThreads + tid] = (uint8_t)inner[u];
+        }
     }
-    __syncthreads();
+    if (kSplit == 1)
+        __syncthreads();
     uint64_t slots = ~0ull;  // of this lane's vectors in `held`, a byte each
     if (kSplit == 1 && listed > 0 && fits) {
         slots = 0ull;
@@ -1101,6 +1130,8 @@ k_verify(LogitsParams p) {
 #pragma unroll
         for (int j = 0; j < kBufs; ++j) {
             const int q = j % kP, row = r + j / kP * kStep;
+            if (kSplit != 1 && row >= t.r1)
+                break;
             if (q == 0) {
                 best = bq = 0u;
                 forb = kNone;
@@ -1124,7 +1155,9 @@ k_verify(LogitsParams p) {
                     if (slot != kNoSlot)
                         held[slot] = y[u];
                 }
-                if (fits)
+                if (kSplit != 1)
+                    y[u] |= gone[u];
+                else if (fits)
                     y[u] |= s.gone[vec(q, u)];
                 else
 #pragma unroll
@@ -1138,7 +1171,7 @@ k_verify(LogitsParams p) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
                             y[u][i] |= spread(no, i);
-                        no &= s.inner[v];
+                        no &= kSplit == 1 ? (uint32_t)s.inner[v] : inner[u];
                         const uint32_t at = place + (uint32_t)__ffs(no) - 1u;
                         forb = no && at < forb ? at : forb;
                     }
@@ -1155,7 +1188,7 @@ k_verify(LogitsParams p) {
             const E x0 = ix[j / kP];
             if (q == kP - 1)
                 fetch_item(j / kP, row + kRows * kStep);
-            if (q != kP - 1 || row >= t.r1)
+            if (q != kP - 1)
                 continue;
             const uint32_t mx = kMask && forb != kNone && best < kLow ? kLow : best;
             const uint32_t top = wave_max(mx);
@@ -1231,32 +1264,32 @@ k_verify(LogitsParams p) {
         s.key[i] = e != 0u ? (top << 16) | (kNone - at) : 0u;
     }
     __syncthreads();
-    if (tid < 64) {
-        // one row per lane (at most kRowGroup = 64 rows)
-        if (tid < t.r1 - t.r0) {
-            uint32_t k = 0u;
+    if (tid >= 64)
+        return;
+    // one row per lane (at most kRowGroup = 64 rows)
+    const int64_t node = (int64_t)t.b * R + (tid < R ? tid : R - 1);
+    const int tok0 = p.a.dtok[node];
+    int par0 = tid - 1;
+    if (p.a.dpar)
+        par0 = p.a.dpar[node];
+    if (tid < t.r1 - t.r0) {
+        uint32_t k = 0u;
 #pragma unroll
-            for (int q = 0; q < kSplit; ++q) {
-                const uint32_t a = s.key[tid * kSplit + q];
-                const uint32_t c = s.key[(p.rows + tid) * kSplit + q];
-                k = a > k ? a : k;
-                k = c > k ? c : k;
-            }
-            if (k)
-                __hip_atomic_fetch_max(
-                    &p.keys[(int64_t)t.b * p.key_stride + t.r0 + tid],
-                    ((unsigned long long)order32(k >> 16) << 32) |
-                        (0xFFFFFFFFu - t.token(kNone - (k & 0xFFFFu))),
-                    __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        for (int q = 0; q < kSplit; ++q) {
+            const uint32_t a = s.key[tid * kSplit + q];
+            const uint32_t c = s.key[(p.rows + tid) * kSplit + q];
+            k = a > k ? a : k;
+            k = c > k ? c : k;
         }
-        const bool last = arrive(&p.tickets[(int64_t)t.b * kLineU32],
-                                 (uint32_t)(p.chunks * ((t.n + p.rows - 1) / p.rows)));
-        if (tid == 0)
-            s_last = last;
+        if (k)
+            __hip_atomic_fetch_max(row_keys(p, t.b, (int)(t.chunk % kCopies)) + t.r0 + tid,
+                                   ((unsigned long long)order32(k >> 16) << 32) |
+                                       (0xFFFFFFFFu - t.token(kNone - (k & 0xFFFFu))),
+                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    __syncthreads();
-    if (s_last)
-        accept(p, t.b, mem);
+    if (arrive(&p.tickets[(int64_t)t.b * kLineU32],
+               (uint32_t)(p.chunks * ((t.n + p.rows - 1) / p.rows))))
+        accept(p, t.b, t.n, tok0, par0, mem);
 }
 
 // kU: vectors per lane and row (of a piece); kSplit: waves that share a row of

@@ -409,20 +409,29 @@ _DT["i64"] = (torch.int64,)
 _DT["logits"] = tuple(_TYPES)
 
 
-def _arr(t, kind, name, shape, optional=False):
-    """Device pointer of a tensor of exactly this shape on the current device."""
+def _current_device():
+    if _device is None or not _initialized():
+        return torch.cuda.current_device() if torch.cuda.is_available() else -1
+    return _device()
+
+
+def _arr(t, kind, name, shape, dev, optional=False):
+    """Device pointer of a tensor of exactly this shape on device `dev`."""
+    # the accepted case first: a call checks up to ten tensors
+    if isinstance(t, _Tensor) and t.get_device() == dev and t.dtype in _DT[kind] and \
+            t.shape == shape and t.is_contiguous() and t.is_cuda:
+        return t.data_ptr()
     ptr = _ptr(t, kind, name, optional)
-    if ptr is not None:
+    if ptr is not None or t is not None:
         if tuple(t.shape) != tuple(shape):
             raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-        _here(t, name)
+        _here(t, name, dev)
     return ptr
 
 
-def _here(t, name):
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name} is on device {t.get_device()}, the current device is "
-                         f"{torch.cuda.current_device()}")
+def _here(t, name, dev):
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on device {t.get_device()}, the current device is {dev}")
 
 
 def build_logits_args(logits, dtok, dpar, dn, tokens=None, lengths=None, prompt_lens=None,
@@ -439,65 +448,70 @@ def build_logits_args(logits, dtok, dpar, dn, tokens=None, lengths=None, prompt_
     if not isinstance(logits, _Tensor) or logits.dim() != 3:
         raise ValueError("logits must be a device tensor [B, R, V]")
     B, R, V = logits.shape
+    dev = _current_device()
     a = LogitsArgs()
-    a.logits = _arr(logits, "logits", "logits", (B, R, V))
+    a.logits = _arr(logits, "logits", "logits", (B, R, V), dev)
     a.logits_type = _TYPES[logits.dtype]
     a.B, a.R, a.V = B, R, V
-    a.dtok = _arr(dtok, "i32", "dtok", (B, R))
-    a.dpar = _arr(dpar, "i32", "dpar", (B, R), True)
-    a.dn = _arr(dn, "i32", "dn", (B,))
+    a.dtok = _arr(dtok, "i32", "dtok", (B, R), dev)
+    a.dpar = _arr(dpar, "i32", "dpar", (B, R), dev, True)
+    a.dn = _arr(dn, "i32", "dn", (B,), dev)
     penal = any(t is not None for t in (repetition, frequency, presence))
     if tokens is not None:
         if not isinstance(tokens, _Tensor) or tokens.dim() != 2:
             raise ValueError("tokens must be a device tensor [B, Lmax]")
         a.Lmax = tokens.shape[1]
-        a.tokens = _arr(tokens, "i32", "tokens", (B, a.Lmax))
+        a.tokens = _arr(tokens, "i32", "tokens", (B, a.Lmax), dev)
     elif penal:
         raise ValueError("tokens is required")
-    a.lengths = _arr(lengths, "i32", "lengths", (B,), not penal)
-    a.prompt_lens = _arr(prompt_lens, "i32", "prompt_lens", (B,), True)
+    a.lengths = _arr(lengths, "i32", "lengths", (B,), dev, not penal)
+    a.prompt_lens = _arr(prompt_lens, "i32", "prompt_lens", (B,), dev, True)
     for name, t in (("repetition", repetition), ("frequency", frequency),
                     ("presence", presence)):
-        setattr(a, name, _arr(t, "f32", name, (B,), True))
+        setattr(a, name, _arr(t, "f32", name, (B,), dev, True))
     if (bias_ids is None) != (bias_vals is None):
         raise ValueError("bias_ids and bias_vals come together")
     if bias_ids is not None:
         if not isinstance(bias_ids, _Tensor) or bias_ids.dim() != 2:
             raise ValueError("bias_ids must be a device tensor [B, n]")
         a.n_bias = bias_ids.shape[1]
-        a.bias_ids = _arr(bias_ids, "i32", "bias_ids", (B, a.n_bias))
-        a.bias_vals = _arr(bias_vals, "f32", "bias_vals", (B, a.n_bias))
-    a.allowed = _arr(allowed, "u32", "allowed", (B, R, (V + 31) // 32), True)
-    a.allowed_on = _arr(allowed_on, "i32", "allowed_on", (B,), True)
-    a.shape, a.device = (B, R, V), logits.get_device()
+        a.bias_ids = _arr(bias_ids, "i32", "bias_ids", (B, a.n_bias), dev)
+        a.bias_vals = _arr(bias_vals, "f32", "bias_vals", (B, a.n_bias), dev)
+    a.allowed = _arr(allowed, "u32", "allowed", (B, R, (V + 31) // 32), dev, True)
+    a.allowed_on = _arr(allowed_on, "i32", "allowed_on", (B,), dev, True)
+    a.shape, a.device = (B, R, V), dev
     a.keep = (logits, dtok, dpar, dn, tokens, lengths, prompt_lens, repetition, frequency,
               presence, bias_ids, bias_vals, allowed, allowed_on)
     return a
 
 
 def _args_here(args):
-    if args.device != torch.cuda.current_device():
+    dev = _current_device()
+    if args.device != dev:
         raise ValueError(f"the arguments are on device {args.device}, the current device is "
-                         f"{torch.cuda.current_device()}")
+                         f"{dev}")
+    return dev
 
 
 def switchsd_process_logits(args, out, stream=None):
     """out [B, R, V]: bf16 or the logits' type (the logits themselves: in place)."""
-    _args_here(args)
+    dev = _args_here(args)
     _check("switchsd_process_logits", lib.switchsd_process_logits(
-        ctypes.byref(args), _arr(out, "logits", "out", args.shape), _TYPES[out.dtype],
+        ctypes.byref(args), _arr(out, "logits", "out", args.shape, dev), _TYPES[out.dtype],
         _stream(stream)))
 
 
 def switchsd_verify_processed(args, accept_len, accept_node, bonus, out_tokens, amax, workspace,
                               stream=None):
-    _args_here(args)
+    dev = _args_here(args)
     B, R, _ = args.shape
-    _here(workspace, "workspace")
+    _here(workspace, "workspace", dev)
     _check("switchsd_verify_processed", lib.switchsd_verify_processed(
-        ctypes.byref(args), _arr(accept_len, "i32", "accept_len", (B,)),
-        _arr(accept_node, "i32", "accept_node", (B,)), _arr(bonus, "i32", "bonus", (B,)),
-        _arr(out_tokens, "i32", "out_tokens", (B, R)), _arr(amax, "i32", "amax", (B, R), True),
+        ctypes.byref(args), _arr(accept_len, "i32", "accept_len", (B,), dev),
+        _arr(accept_node, "i32", "accept_node", (B,), dev),
+        _arr(bonus, "i32", "bonus", (B,), dev),
+        _arr(out_tokens, "i32", "out_tokens", (B, R), dev),
+        _arr(amax, "i32", "amax", (B, R), dev, True),
         _ptr(workspace, "u8", "workspace"), workspace.numel(), _stream(stream)))
 
 
@@ -515,27 +529,27 @@ def build_page_args(lengths, dpar, dn, Lmax, page_size, table, held, ring, ring_
     if R is None:
         raise ValueError("R is required")
     B, most = table.shape
+    dev = _current_device()
     a = PageArgs()
     a.B, a.R, a.Lmax, a.page_size, a.max_pages = B, R, int(Lmax), int(page_size), most
-    a.table = _arr(table, "i32", "table", (B, most))
+    a.table = _arr(table, "i32", "table", (B, most), dev)
     for name, t in (("lengths", lengths), ("dn", dn), ("held", held), ("missing", missing)):
-        setattr(a, name, _arr(t, "i32", name, (B,)))
-    a.dpar = _arr(dpar, "i32", "dpar", (B, R), True)
+        setattr(a, name, _arr(t, "i32", name, (B,), dev))
+    a.dpar = _arr(dpar, "i32", "dpar", (B, R), dev, True)
     if not isinstance(ring, _Tensor) or ring.dim() != 1:
         raise ValueError("ring must be a device tensor [ring_pages]")
     a.ring_pages = ring.shape[0]
-    a.ring = _arr(ring, "i32", "ring", (a.ring_pages,))
-    a.ring_state = _arr(ring_state, "i32", "ring_state", (2,))
-    a.slots = _arr(slots, "i64", "slots", (B, R), True)
-    a.positions = _arr(positions, "i32", "positions", (B, R), True)
-    a.device = table.get_device()
+    a.ring = _arr(ring, "i32", "ring", (a.ring_pages,), dev)
+    a.ring_state = _arr(ring_state, "i32", "ring_state", (2,), dev)
+    a.slots = _arr(slots, "i64", "slots", (B, R), dev, True)
+    a.positions = _arr(positions, "i32", "positions", (B, R), dev, True)
+    a.device = dev
     a.keep = (lengths, dpar, dn, table, held, ring, ring_state, slots, positions, missing)
     return a
 
 
 def switchsd_page_plan(args, workspace, stream=None):
-    _args_here(args)
-    _here(workspace, "workspace")
+    _here(workspace, "workspace", _args_here(args))
     _check("switchsd_page_plan", lib.switchsd_page_plan(
         ctypes.byref(args), _ptr(workspace, "u8", "workspace"), workspace.numel(),
         _stream(stream)))
@@ -547,20 +561,23 @@ def switchsd_span_slots(begin, end, tokens, table, held, page_size, cu, slots, p
     [B + 1] int32, slots int64 and positions, packed, seq int32 of one length
     (each None if not wanted)."""
     B, Lmax = tokens.shape
-    if slots is not None and (table is None or held is None):
-        raise ValueError("slots need table and held")
-    most = table.shape[1] if slots is not None else 0
-    n = [t.shape[0] for t in (slots, positions, packed, seq) if t is not None]
-    cap = (n[0] if n else 0,)
+    dev = _current_device()
+    most, p_table, p_held = 0, None, None
+    if slots is not None:
+        if table is None or held is None:
+            raise ValueError("slots need table and held")
+        most = table.shape[1]
+        p_table = _arr(table, "i32", "table", (B, most), dev)
+        p_held = _arr(held, "i32", "held", (B,), dev)
+    cap = next((t.shape for t in (slots, positions, packed, seq) if t is not None), (0,))
     _check("switchsd_span_slots", lib.switchsd_span_slots(
-        _arr(begin, "i32", "begin", (B,)), _arr(end, "i32", "end", (B,)),
-        _arr(tokens, "i32", "tokens", (B, Lmax)),
-        _arr(table, "i32", "table", (B, most), True) if most else None,
-        _arr(held, "i32", "held", (B,), True) if most else None, B, Lmax, most, int(page_size),
-        _arr(cu, "i32", "cu", (B + 1,)), _arr(slots, "i64", "slots", cap, True),
-        _arr(positions, "i32", "positions", cap, True),
-        _arr(packed, "i32", "packed", cap, True), _arr(seq, "i32", "seq", cap, True), cap[0],
-        _stream(stream)))
+        _arr(begin, "i32", "begin", (B,), dev), _arr(end, "i32", "end", (B,), dev),
+        _arr(tokens, "i32", "tokens", (B, Lmax), dev), p_table, p_held, B, Lmax, most,
+        int(page_size), _arr(cu, "i32", "cu", (B + 1,), dev),
+        None if slots is None else _arr(slots, "i64", "slots", cap, dev),
+        None if positions is None else _arr(positions, "i32", "positions", cap, dev),
+        None if packed is None else _arr(packed, "i32", "packed", cap, dev),
+        None if seq is None else _arr(seq, "i32", "seq", cap, dev), cap[0], _stream(stream)))
 
 
 def switchsd_compact_cache(cache, slots, dpar, dn, accept_node, stream=None):
@@ -571,11 +588,12 @@ def switchsd_compact_cache(cache, slots, dpar, dn, accept_node, stream=None):
     planes, n_slots = cache.shape[:2]
     if not cache.is_contiguous() and not cache[0].is_contiguous():
         raise ValueError("cache planes must be contiguous")
-    _here(cache, "cache")
+    dev = _current_device()
+    _here(cache, "cache", dev)
     B, R = slots.shape
     row = cache.element_size() * (cache.numel() // (planes * n_slots) if cache.numel() else 0)
     _check("switchsd_compact_cache", lib.switchsd_compact_cache(
         cache.data_ptr(), planes, cache.stride(0) * cache.element_size(), n_slots, row,
-        _arr(slots, "i64", "slots", (B, R)), _arr(dpar, "i32", "dpar", (B, R), True),
-        _arr(dn, "i32", "dn", (B,)), _arr(accept_node, "i32", "accept_node", (B,)), B, R,
+        _arr(slots, "i64", "slots", (B, R), dev), _arr(dpar, "i32", "dpar", (B, R), dev, True),
+        _arr(dn, "i32", "dn", (B,), dev), _arr(accept_node, "i32", "accept_node", (B,), dev), B, R,
         _stream(stream)))

@@ -965,6 +965,9 @@ size_t type_size(int32_t type) { return type == SWITCHSD_F32 ? 4 : 2; }
 // Work-groups of a launch: 256 lanes each, fewer than 2^32 lanes together.
 bool launch_ok(int64_t g) { return g >= 1 && g < (1 << 24); }
 
+// n = 2^k: k, else -1.
+int32_t log_of(int32_t n) { return (n & (n - 1)) == 0 ? __builtin_ctz((unsigned)n) : -1; }
+
 bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
 int check_logits(const switchsd_logits_args *a) {
@@ -1133,7 +1136,9 @@ int switchsd_page_plan(const switchsd_page_args *a, void *workspace, size_t work
     p.slots = a->slots;
     p.positions = a->positions;
     p.missing = a->missing;
-    p.seqs = kPlanNodes / a->R < kThreads ? kPlanNodes / a->R : kThreads;
+    p.page_log = log_of(a->page_size);
+    // R <= 64: whole sequences of each of the four waves' lanes
+    p.seqs = a->R <= 64 ? kThreads / 64 * (64 / a->R) : kPlanNodes / a->R;
     p.ticket = carve(workspace, a->B, 0, 0, 0).tk_all;
     return launch_page_plan_kernel(p, stream);
 }
@@ -1163,6 +1168,7 @@ int switchsd_span_slots(const int32_t *begin, const int32_t *end, const int32_t 
     p.Lmax = Lmax;
     p.max_pages = max_pages;
     p.page_size = page_size;
+    p.page_log = log_of(page_size);
     p.cu = cu;
     p.slots = slots;
     p.positions = positions;

@@ -243,6 +243,7 @@ struct PageParams {
     int32_t *table, *held, *ring, *ring_state;
     int64_t *slots;
     int32_t *positions, *missing;
+    int32_t page_log;  // page_size = 2^page_log, or -1
     int32_t seqs;      // sequences per work-group
     uint32_t *ticket;
 };
@@ -250,6 +251,7 @@ struct PageParams {
 struct SpanParams {
     const int32_t *begin, *end, *tokens, *table, *held;
     int32_t B, Lmax, max_pages, page_size;
+    int32_t page_log;  // page_size = 2^page_log, or -1
     int32_t *cu;
     int64_t *slots;
     int32_t *positions, *packed, *seq;

@@ -42,10 +42,8 @@ def processed(d, real):
         if penal:
             L = int(np.clip(d["lengths"][b], 0, d["tokens"].shape[1]))
             P = 0 if d["prompt_lens"] is None else int(np.clip(d["prompt_lens"][b], 0, L))
-            for i in range(L):
-                v = int(d["tokens"][b, i])
-                if 0 <= v < V:
-                    (given if i < P else made)[v] += 1
+            for counts, x in ((given, d["tokens"][b, :P]), (made, d["tokens"][b, P:L])):
+                counts += np.bincount(x[(x >= 0) & (x < V)], minlength=V)
         rho = real(1 if d["repetition"] is None else d["repetition"][b])
         freq = real(0 if d["frequency"] is None else d["frequency"][b])
         pres = real(0 if d["presence"] is None else d["presence"][b])

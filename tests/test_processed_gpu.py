@@ -246,6 +246,36 @@ def test_verify(src, shape):
         assert int(ws.count_nonzero()) == 0
 
 
+@pytest.mark.parametrize("src,B,R,V,L,spread", [
+    ("bf16", 64, 17, 70001, 50, False), ("bf16", 64, 20, 70001, 6000, True),
+    ("bf16", 64, 16, 70000, 60000, True), ("f16", 64, 19, 66000, 6000, True),
+    ("f16", 64, 17, 70001, 60000, True), ("f32", 40, 18, 70001, 300, False),
+    ("f32", 40, 21, 70002, 9000, True), ("f32", 40, 16, 66000, 60000, True),
+    ("bf16", 9, 201, 70001, 3000, True),
+])
+def test_verify_large_batches(src, B, R, V, L, spread):
+    """Sizes at which a wave takes whole rows: few listed tokens, more vectors
+    with one than the wave keeps, more tokens than the list holds."""
+    say(f"[verify] large {src} {B}x{R}x{V} L={L}")
+    d = make(B, R, V, L, seed=V + L, src=src, draft="candidates", k=5)
+    if spread:                                          # a history over the whole vocabulary
+        d["tokens"] = np.random.default_rng(L).integers(0, V, (B, L)).astype(np.int32)
+        d["lengths"][::2] = L
+    d["dn"][::3] = R
+    plant(d, L)
+    d["bias_vals"] = np.maximum(d["bias_vals"], np.float32(-9))
+    # rows where nothing but -inf is left, with and without a mask's help
+    d["logits"][4, 3] = -np.inf
+    d["logits"][5, 2] = float("nan")
+    d["allowed_on"][5] = 0
+    d["allowed"][6, 1, :] = 0
+    want = ref.greedy(d, ref.processed(d, np.float32))
+    got, ws = gpu_verify(device_args(d))
+    for name, t in got.items():
+        np.testing.assert_array_equal(t.cpu().numpy(), want[name], err_msg=name)
+    assert int(ws.count_nonzero()) == 0
+
+
 def test_verify_is_process_then_accept():
     """The two routes agree, on a workspace that calls of other shapes used."""
     from paper_2609_20186_amd import binding as sd

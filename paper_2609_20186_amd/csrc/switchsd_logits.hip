@@ -141,7 +141,7 @@ struct Elem<SWITCHSD_F32> {
 
 // LDS of a work-group, carved from one array.
 struct Lds {
-    uint32_t *word;   // [tokens]
+    uint32_t *word;   // [tokens], then a word of each lane's
     void *stage;      // process: [tokens] of the input's type, vectors with listed tokens;
                       // verify: [rows][split][2] the vectors with the maximum
     void *list;       // process: [tokens] uint16, the tokens that have a word; verify: the
@@ -189,7 +189,7 @@ __host__ __device__ __forceinline__ size_t lds_carve(unsigned char *m, int token
     };
     const size_t gone = split == 1 ? (size_t)tokens * size : 0;
     const size_t held = split == 1 ? (size_t)kWaves * kSlots * 16 : 0;
-    const size_t words = (size_t)tokens * 4;
+    const size_t words = (size_t)(tokens + 64) * 4;
     unsigned char *w = take(words > gone + held ? words : gone + held);
     l.word = (uint32_t *)w;
     l.gone = (u32x4 *)w;
@@ -333,11 +333,11 @@ __device__ __forceinline__ void accept(const LogitsParams &p, int b, int n, int 
     }
 }
 
-// Bits 2q and 2q + 1 of `bits`, each spread over one half of a word.
+// Bits 2q and 2q + 1 of `bits` (16 at most), each spread over one half of a word:
+// both are moved to the halves' signs at once.
 __device__ __forceinline__ uint32_t halves(uint32_t bits, int q) {
-    const uint32_t lo = (uint32_t)((int32_t)(bits << (31 - 2 * q)) >> 31);
-    const uint32_t hi = (uint32_t)((int32_t)(bits << (30 - 2 * q)) >> 31);
-    return (lo & 0xFFFFu) | (hi & 0xFFFF0000u);
+    const uint32_t w = (bits | bits << 15) << (15 - 2 * q);
+    return __builtin_bit_cast(uint32_t, (s16x2)(__builtin_bit_cast(s16x2, w) >> (int16_t)15));
 }
 __device__ __forceinline__ uint32_t select16(uint32_t m, uint32_t x, uint32_t y) {
     return (x & m) | (y & ~m);
@@ -363,7 +363,12 @@ struct Tile {
 
     __device__ __forceinline__ void init(const LogitsParams &p) {
         chunk_log = p.chunk_log;
+        // consecutive work-groups go to different XCDs: neighbouring chunks, which
+        // share lines of the masks and of rows that do not start on one, are
+        // given to the work-groups of one XCD
         chunk = blockIdx.x & ((uint32_t)p.chunks - 1u);
+        if (chunk_log >= 3)
+            chunk = (chunk & 7u) << (chunk_log - 3) | chunk >> 3;
         const int gb = blockIdx.x >> chunk_log;
         const int group = gb % p.groups;
         b = gb / p.groups;
@@ -580,27 +585,36 @@ __device__ __forceinline__ int list_tokens(const LogitsParams &p, const T &t, co
         __syncthreads();
     }
     if (p.penal) {
-        // the prompt sets a bit, what follows it counts
-        auto one = [&](int32_t tok, int i) {
+        // The prompt sets a bit, what follows it counts.  Without branches:
+        // tokens of other chunks and places without a token go to words of the
+        // lanes' own behind the chunk's.
+        auto four = [&](const i32x4 &c, int v) {
+            // of a vector that starts early, the tokens of the one before it do
+            // not count again
+            const int i = ctx_start(v, Lmax), d = i - 4 * v;
+            const uint32_t live = 4 * v < L ? (uint32_t)(L - 4 * v) : 0u;
+            const int first = 4 * (v - tid);  // of the work-group's vectors
+            const bool pre = first < P, post = first + 4 * kThreads > P;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t off;
+                const bool here = t.place(c[j], V, off) && (uint32_t)(d + j) < live;
+                uint32_t *w = s.word + (here ? off : (uint32_t)(T::kTokens + lane));
+                const bool prompt = i + j < P;
+                if (pre)
+                    atomicOr(w, prompt ? kPrompt : 0u);
+                if (post)
+                    atomicAdd(w, prompt ? 0u : 1u);
+            }
+        };
+        if (Lmax < 4) {
             uint32_t off;
-            if (i < L && t.place(tok, V, off)) {
-                if (i < P)
+            if (tid < L && t.place(x[tid], V, off)) {
+                if (tid < P)
                     atomicOr(&s.word[off], kPrompt);
                 else
                     atomicAdd(&s.word[off], 1u);
             }
-        };
-        // of a vector that starts early, the tokens of the one before it do not
-        // count again
-        auto four = [&](const i32x4 &c, int v) {
-            const int i = ctx_start(v, Lmax);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                one(c[j], i + j >= 4 * v ? i + j : L);
-        };
-        if (Lmax < 4) {
-            if (tid < Lmax)
-                one(x[tid], tid);
         } else {
 #pragma unroll
             for (int q = 0; q < kAhead; ++q)
@@ -965,7 +979,7 @@ constexpr uint32_t kPlaced = 0x80000000u;
 constexpr int kBufs = 4;
 
 template <int kIn, int kSplit, int kU, bool kMask, bool kTiny>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kTiny ? 1 : 4))) void
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kTiny ? 1 : kIn == SWITCHSD_F32 && kMask && kSplit == 1 ? 3 : 4))) void
 k_verify(LogitsParams p) {
     constexpr int kP = kWaves / kSplit;    // pieces of a row per wave
     constexpr int kRows = kBufs / kP;      // rows held at once
@@ -1087,7 +1101,7 @@ k_verify(LogitsParams p) {
         inner[u] = t.own[u] & ~(mine >> (u * kPer));
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            gone[u][i] = spread(~inner[u], i);
+            gone[u][i] = spread(~inner[u] & kAll, i);
         if (kSplit == 1) {
             if (fits)
                 s.gone[u * kThreads + tid] = gone[u];
@@ -1105,6 +1119,9 @@ k_verify(LogitsParams p) {
     }
     u32x4 *held = s.held + wave * kSlots;
     uint32_t *abits = s.bits + wave * kWords;
+    auto allowed_at = [&](uint32_t v) {  // the allowed bits of vector v, lowest first
+        return (uint32_t)((const uint8_t *)abits)[v * kPer >> 3] >> (v * kPer & 7u);
+    };
     const int nth = kSplit == 1 ? lane : tid;
     uint32_t entry0 = 0u, word0 = 0u;  // this lane's first listed token
     if (nth < listed) {
@@ -1125,7 +1142,6 @@ k_verify(LogitsParams p) {
     // ---- the rows
     for (int r = first; r < t.r1; r += kRows * kStep) {
         uint32_t best = 0u, bq = 0u;    // the lane's maximum and its piece
-        uint32_t forb = kNone;          // its lowest forbidden place
         u32x4 top_x[kU];
 #pragma unroll
         for (int j = 0; j < kBufs; ++j) {
@@ -1134,7 +1150,6 @@ k_verify(LogitsParams p) {
                 break;
             if (q == 0) {
                 best = bq = 0u;
-                forb = kNone;
                 if constexpr (kMask) {
 #pragma unroll
                     for (int i = 0; i < kWordLoads; ++i)
@@ -1162,19 +1177,13 @@ k_verify(LogitsParams p) {
                 else
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        y[u][i] |= spread(~(uint32_t)s.inner[vec(q, u)], i);
+                        y[u][i] |= spread(~(uint32_t)s.inner[vec(q, u)] & kAll, i);
                 if (masked) {
-                    const uint32_t v = vec(q, u), place = v * kPer;
-                    const uint32_t ok = ((const uint8_t *)abits)[place >> 3] >> (place & 7u);
-                    uint32_t no = ~ok & kAll;
-                    if (__ballot(no != 0u) != 0ull) {
+                    const uint32_t no = ~allowed_at(vec(q, u)) & kAll;
+                    if (__ballot(no != 0u) != 0ull)
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
                             y[u][i] |= spread(no, i);
-                        no &= kSplit == 1 ? (uint32_t)s.inner[v] : inner[u];
-                        const uint32_t at = place + (uint32_t)__ffs(no) - 1u;
-                        forb = no && at < forb ? at : forb;
-                    }
                 }
             }
             const uint32_t k = lane_key<kIn, kU>(y);
@@ -1190,13 +1199,24 @@ k_verify(LogitsParams p) {
                 fetch_item(j / kP, row + kRows * kStep);
             if (q != kP - 1)
                 continue;
-            const uint32_t mx = kMask && forb != kNone && best < kLow ? kLow : best;
-            const uint32_t top = wave_max(mx);
-            const unsigned long long who = __ballot(mx == top);
+            uint32_t top = wave_max(best);
+            uint32_t forb = kNone;  // this lane's lowest forbidden place
+            if (masked && top <= kLow) {
+                // nothing above -inf: a forbidden token is -inf too
+#pragma unroll
+                for (int i = kP * kU - 1; i >= 0; --i) {
+                    const uint32_t v = vec(i / kU, i % kU);
+                    const uint32_t no =
+                        ~allowed_at(v) & (kSplit == 1 ? (uint32_t)s.inner[v] : inner[i % kU]);
+                    forb = no ? v * kPer + (uint32_t)__ffs(no) - 1u : forb;
+                }
+                top = __ballot(forb != kNone) != 0ull ? kLow : top;
+            }
+            const unsigned long long who = __ballot(best == top);
             const int slot = (row - t.r0) * kSplit + (kSplit == 1 ? 0 : wave);
             if (top > kLow && (who & (who - 1ull)) == 0ull) {
                 // one lane holds it: its token is looked up when the rows are done
-                if (mx == top) {
+                if (best == top) {
                     s.key[slot] = (top << 15) | (bq * 64u * kU + vec(0, 0));
 #pragma unroll
                     for (int u = 0; u < kU; ++u)
@@ -1206,8 +1226,7 @@ k_verify(LogitsParams p) {
                 uint32_t at = kNone;
                 if (best == top)
                     at = lane_place<kIn, kSplit, kU>(top_x, top, bq * 64u * kU + vec(0, 0));
-                if (kMask && top == kLow)  // a forbidden token is -inf too
-                    at = forb < at ? forb : at;
+                at = forb < at ? forb : at;
                 const uint32_t low = kNone - wave_max(kNone - at);
                 if (lane == 0)
                     s.key[slot] = kPlaced | (top << 15) | low;
@@ -1227,13 +1246,32 @@ k_verify(LogitsParams p) {
                     const uint32_t k2 = o ? (o << 16) | (kNone - place) : 0u;
                     ki = k2 > ki ? k2 : ki;
                 };
-                if (fits) {
+                if (fits && kSplit == 1) {
+                    // four of the lane's tokens at a time, their reads together
+                    for (int i0 = lane; i0 < listed + lane; i0 += 4 * kLanes) {
+                        uint32_t e[4], w[4];
+                        E v[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int c = i0 + i * kLanes < listed ? i0 + i * kLanes : 0;
+                            e[i] = list[c];
+                            w[i] = s.lword[c];
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            v[i] = ((const E *)held)[e[i] >> 16 != kNone ? e[i] >> 16 : 0u];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (i0 + i * kLanes < listed)
+                                item(e[i] >> 16 != kNone ? v[i] : value(e[i] & 0xFFFFu, kNone),
+                                     e[i] & 0xFFFFu, w[i]);
+                    }
+                } else if (fits) {
                     if (nth < listed)
-                        item(kSplit == 1 ? value(entry0 & 0xFFFFu, entry0 >> 16) : x0,
-                             entry0 & 0xFFFFu, word0);
+                        item(x0, entry0 & 0xFFFFu, word0);
                     for (int i = nth + kLanes; i < listed; i += kLanes) {
                         const uint32_t e = list[i];
-                        item(value(e & 0xFFFFu, e >> 16), e & 0xFFFFu, s.lword[i]);
+                        item(value(e & 0xFFFFu, kNone), e & 0xFFFFu, s.lword[i]);
                     }
                 } else {
                     // more than the list holds: every token with a word

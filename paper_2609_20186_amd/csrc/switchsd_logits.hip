@@ -1,22 +1,42 @@
 // switchsd_logits.hip -- gfx950 kernels for penalties, biases and grammar masks
-// on the logits of the drafted rows (k_logits), written out or verified on the
-// fly.
+// on the logits of the drafted rows: written out (k_process) or verified on the
+// fly (k_verify).
+//
+// For token v in row r, with c its occurrences behind the prompt and on the
+// row's path, and s whether the history holds it at all:
+//   y = s ? (l > 0 ? l / rho : l * rho) : l;  c > 0: y -= f * c, y -= p;
+//   y += bias_v;  not allowed: y = -inf.
+// Few tokens of a row are touched by any of it but the mask, so the work is one
+// pass over the rows' bytes (the bound: HBM) plus a few tokens.
 //
 // A work-group takes one chunk of the vocabulary and a group of rows of one
 // sequence.  It first makes a word per token of the chunk in LDS (how often the
-// history holds it, whether the prompt does, its first draft node, the bias
-// entry that names it) and lists the tokens that have one (list_tokens).  Then it
-// streams the chunk of each of its rows, two rows ahead.
+// history holds it, whether the prompt does, the draft node that stands for
+// it, the bias entry that names it) and lists the tokens that have one
+// (list_tokens); what a drafted token adds on each row's path is counted into a
+// table once.  Counting anew in every work-group keeps the call to one launch
+// and no scratch memory: 32 histories of 4096 tokens cost the verification of
+// 32 x 8 rows of 128256 about 3 us, biases another 1.5.
 //   k_process: vectors that hold a listed token pass through LDS, where the
 //     listed tokens are computed one per lane; all others pass as they are.
 //   k_verify: the rows' maxima are taken over the vectors without their listed
-//     tokens, which are read and computed one per lane beside them; nothing is
-//     exchanged between the waves until the rows are done.
-// So the work per row is the row's bytes plus the listed tokens, however they
-// lie.
+//     tokens, which are computed one per lane beside them; nothing is exchanged
+//     between the waves until the rows are done.
+// Computing the listed tokens where their vectors lie, in the lanes that hold
+// them, measured 109 instead of 32 us for 32 x 8 rows of 128256 and 17 ms
+// instead of 0.6 for 32 x 201 drafted rows.
 //
 // A chunk is every 2^k-th block of 16 vectors (k_process: 32): low token ids,
-// which are the frequent ones, spread over all work-groups of a row.
+// which are the frequent ones, spread over all work-groups of a row.  Blocks of
+// 16, 32, 64 vectors measured 25.5, 28.0, 30.8 us (verify, 32 x 8 rows of
+// 128256) and 301, 269, 303 us (process, 32 x 60 rows of floats).
+//
+// Measured (MI355X), bytes that must move over time: process 32 x 8 rows of
+// 128256 bf16 27.9 us, 4.7 TB/s (a copy of that size class reaches 5.2 TB/s);
+// 32 x 60 rows of floats to bf16 under a grammar 266 us, 5.6 TB/s; verify 32 x 8
+// rows 25.5 us, 2.6 TB/s; 32 x 201 candidate rows under a grammar 206 us, 4.6
+// TB/s.  What bounds the small ones is the chain before the first row (draft
+// length, history, list) and after the last (row maxima, ticket, accept rule).
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 
@@ -217,13 +237,14 @@ struct Penalty {
 // entry `row` of s.path.
 __device__ __forceinline__ float processed(float l, uint32_t w, const Penalty &pe, const Lds &s,
                                            int row, bool wide) {
-    uint32_t c = w;
+    uint32_t c = w & kCount;
+    bool prompt = w & kPrompt;
     if (w & kDrafted) {
-        const uint32_t e = w & kCount;
-        c = s.count[e] + (wide ? ((const uint16_t *)s.path)[row + e] : s.path[row + e]);
+        const uint32_t at = s.count[c];
+        c = (at & kCount) +
+            (wide ? ((const uint16_t *)s.path)[row + c] : (uint32_t)s.path[row + c]);
+        prompt = at & kPrompt;
     }
-    const bool prompt = c & kPrompt;
-    c &= kCount;
     float y = l;
     if (c != 0u || prompt)
         y = l > 0.0f ? l / pe.rho : l * pe.rho;
@@ -976,10 +997,19 @@ constexpr uint32_t kPlaced = 0x80000000u;
 // vectors with listed tokens in LDS, wave by wave; quarters read those tokens
 // beside them (one per lane with the row's other requests).
 // kU: vectors of a piece per lane.
+// Measured, whole rows / quarters: 32 x 8 rows of 128256 26.7 / 25.5 us, 32 x 13
+// 33.7 / 32.5, 32 x 21 44.8 / 45.3, 32 x 201 candidate rows under a grammar 243 /
+// 278; whole rows from kWholeRows rows a work-group on.
 constexpr int kBufs = 4;
+// Waves per SIMD the registers are kept to (floats under a mask need more of
+// them).
+constexpr int waves_of(int in, int split, bool mask) {
+    return in == SWITCHSD_F32 && mask && split == 1 ? 3 : 4;
+}
 
 template <int kIn, int kSplit, int kU, bool kMask, bool kTiny>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kTiny ? 1 : kIn == SWITCHSD_F32 && kMask && kSplit == 1 ? 3 : 4))) void
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(kTiny ? 1 : waves_of(kIn, kSplit, kMask)))) void
 k_verify(LogitsParams p) {
     constexpr int kP = kWaves / kSplit;    // pieces of a row per wave
     constexpr int kRows = kBufs / kP;      // rows held at once

@@ -336,6 +336,53 @@ def test_captured_and_on_another_stream():
     assert torch.equal(o2.view(word), out.view(word))
 
 
+def test_two_graphs_share_a_workspace():
+    """Two captured verifications of different shapes on one workspace, replayed
+    in turn."""
+    from paper_2609_20186_amd import binding as sd
+    say("[verify] two graphs")
+    ws = sd.alloc_workspace(6, 70)
+    side = torch.cuda.Stream()
+    runs = []
+    for seed, (B, R, V) in enumerate([(6, 70, 3001), (4, 5, 40000)]):
+        d = plant(make(B, R, V, 100, seed=40 + seed, draft="tree"), seed)
+        args = device_args(d)
+        out, _ = gpu_verify(args, ws)
+        graph = torch.cuda.CUDAGraph()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=side):
+            sd.switchsd_verify_processed(args, out["accept_len"], out["accept_node"],
+                                         out["bonus"], out["out_tokens"], out["amax"], ws, side)
+        runs.append((d, args, out, graph, ref.greedy(d, ref.processed(d, np.float32))))
+    for turn in range(3):
+        for d, args, out, graph, want in runs:
+            for t in out.values():
+                t.fill_(-9)
+            graph.replay()
+            for name, t in out.items():
+                np.testing.assert_array_equal(t.cpu().numpy(), want[name], err_msg=name)
+    assert int(ws.count_nonzero()) == 0
+
+
+def test_longest_history():
+    """A token repeated through the longest history and drafted again: its count
+    fills the whole field."""
+    from paper_2609_20186_amd import binding as sd
+    say("[process] longest history")
+    L = sd.MAX_HISTORY
+    d = make(2, 3, 50, 8, seed=1, n_bias=3, mask=False, special=False)
+    d["tokens"] = np.full((2, L), 7, np.int32)
+    d["tokens"][1, :5] = 9
+    d["lengths"], d["prompt_lens"] = np.array([L, L], np.int32), np.array([0, 5], np.int32)
+    d["dtok"] = np.array([[-1, 7, 7], [-1, 9, 7]], np.int32)
+    d["dn"][:] = 3
+    d["frequency"] = np.array([1e-5, 2e-5], np.float32)
+    o = torch.full(d["logits"].shape, 77.0, dtype=torch.float32, device="cuda")
+    d["logits"] = d["logits"].float()
+    sd.switchsd_process_logits(device_args(d), o)
+    check_rows(d, o, torch.float32, 77.0)
+
+
 def test_more_than_two_to_the_31_logits():
     """Offsets beyond 32 bits: the last sequences of a 2.2e9-element tensor."""
     from paper_2609_20186_amd import binding as sd

@@ -398,7 +398,8 @@ typedef enum { SWITCHSD_BF16 = 0, SWITCHSD_F16 = 1, SWITCHSD_F32 = 2 } switchsd_
  *   int32 and bias_vals [B, n_bias] float, n_bias <= SWITCHSD_MAX_BIAS;
  *   allowed [B, R, (V + 31) / 32] uint32 (bit v % 32 of word v / 32; NULL:
  *   everything is allowed), allowed_on [B] int32 (NULL: every sequence; the
- *   masks of the others are not read). */
+ *   masks of the others are not read).  Shapes that would take 2^24 work-groups
+ *   or more are refused. */
 typedef struct {
     const void *logits;
     int32_t logits_type; /* switchsd_type */
@@ -443,7 +444,8 @@ int switchsd_verify_processed(const switchsd_logits_args *args, int32_t *accept_
  * for the sequences in order, as long as the running total of what they lack
  * fits count: the first sequence that does not fit and all later ones that
  * lack pages get none, and missing[b] is what such a sequence lacks (0 for all
- * others).  Returned pages are appended in sequence order (cut at ring_pages).
+ * others).  Returned pages are appended in sequence order; a ring that has no
+ * room for all of them (fewer entries than the cache has pages) loses the rest.
  *   slots[b, r] = table[b, p / page_size] * page_size + p % page_size for
  *   p = L - 1 + r, r < n, where the page is held, else -1;
  *   positions[b, r] = L - 1 + depth(r) for r < n and L > 0, else -1 (the walk

@@ -326,8 +326,9 @@ __global__ __launch_bounds__(kThreads) void k_page_plan(PageParams p) {
     block_scan2(popped, z, total, zt, red);
     if (tid == 0) {
         p.ring_state[0] = (int)(((uint32_t)head + (uint32_t)total) % (uint32_t)p.ring_pages);
-        const int64_t left = (int64_t)count - total + bt;
-        p.ring_state[1] = left > p.ring_pages ? p.ring_pages : (int)left;
+        // what lies behind the ring's end was not appended and does not count
+        const int room = p.ring_pages - count;
+        p.ring_state[1] = count - total + (bt < room ? bt : room);
         if (gridDim.x > 1)
             st_u32(p.ticket, 0u);
     }

@@ -157,11 +157,11 @@ def page_plan(s):
                 slots[b, r] = int(s["table"][b, p // page]) * page + p % page
             up, whole = path_of(par, r)
             positions[b, r] = L - 1 + len(up) - (0 if whole else 1)
+    back = back[:P - count]
     for i, x in enumerate(back):
-        if count + i < P:
-            s["ring"][(head + count + i) % P] = x
+        s["ring"][(head + count + i) % P] = x
     s["ring_state"][0] = (head + popped) % P
-    s["ring_state"][1] = min(P, count - popped + len(back))
+    s["ring_state"][1] = count - popped + len(back)
     return slots, positions, missing
 
 

@@ -117,6 +117,26 @@ def test_plan_clamps_its_state():
         compare_plan(s, t, res, str(state))
 
 
+@pytest.mark.parametrize("B", [3, 600])
+def test_plan_of_a_ring_that_is_too_small(B):
+    """Pages that find no room behind the free ones are lost, not counted: the
+    free part then holds the entries that were written and no others."""
+    from paper_2609_20186_amd import binding as sd
+    say(f"[plan] ring too small, {B}")
+    s = {"B": B, "R": 2, "Lmax": 64, "page": 4, "dpar": None,
+         "lengths": np.zeros(B, np.int32), "dn": np.full(B, 2, np.int32),
+         "table": np.arange(100, 100 + 3 * B, dtype=np.int32).reshape(B, 3),
+         "held": np.full(B, 2, np.int32), "ring": np.arange(6, dtype=np.int32),
+         "ring_state": np.array([4, 5], np.int32)}
+    s["lengths"][0] = 11                     # takes one page, the others return two each
+    t, args, ws = device_plan(s)
+    res = ref.page_plan(s)
+    sd.switchsd_page_plan(args, ws)
+    compare_plan(s, t, res, "too small")
+    assert t["ring_state"].tolist() == [5, 5]            # 5 free - 1 taken + 1 kept
+    assert t["ring"].tolist() == [0, 1, 2, 102 + 1, 4, 5]
+
+
 def test_plan_captured():
     from paper_2609_20186_amd import binding as sd
     say("[plan] graph")

@@ -416,9 +416,10 @@ struct Tile {
     }
     // a token's place in the chunk, if it has one
     __device__ __forceinline__ bool place(int32_t t, int V, uint32_t &off) const {
-        const uint32_t blk = (uint32_t)t >> kBlkLog;
-        off = ((blk >> chunk_log) << kBlkLog) | ((uint32_t)t & ((1u << kBlkLog) - 1u));
-        return (uint32_t)t < (uint32_t)V && ((blk ^ chunk) & ((1u << chunk_log) - 1u)) == 0u;
+        const uint32_t u = (uint32_t)t, low = (1u << kBlkLog) - 1u;
+        off = ((u >> chunk_log) & ~low) | (u & low);
+        return u < (uint32_t)V &&
+               (u & (((1u << chunk_log) - 1u) << kBlkLog)) == (uint32_t)chunk << kBlkLog;
     }
 };
 
@@ -616,6 +617,21 @@ __device__ __forceinline__ int list_tokens(const LogitsParams &p, const T &t, co
             const uint32_t live = 4 * v < L ? (uint32_t)(L - 4 * v) : 0u;
             const int first = 4 * (v - tid);  // of the work-group's vectors
             const bool pre = first < P, post = first + 4 * kThreads > P;
+            if (first + 4 * kThreads <= L && pre != post) {
+                // all of them tokens, on one side of the prompt's end: half the
+                // instructions (7 x 11 rows behind 32768 tokens: 32.8 to 30.1 us)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t off;
+                    const bool here = t.place(c[j], V, off);
+                    uint32_t *w = s.word + (here ? off : (uint32_t)(T::kTokens + lane));
+                    if (pre)
+                        atomicOr(w, kPrompt);
+                    else
+                        atomicAdd(w, 1u);
+                }
+                return;
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 uint32_t off;
@@ -642,7 +658,8 @@ __device__ __forceinline__ int list_tokens(const LogitsParams &p, const T &t, co
                 if (4 * q * kThreads < L)
                     four(h.c[q], tid + q * kThreads);
             for (int v = tid + kAhead * kThreads; 4 * (v - tid) < L; v += 8 * kThreads) {
-                i32x4 c[8];
+                i32x4 c[8];  // 16 took 1 us off 32768 tokens, and waves off the CUs: 206 to 220 us
+                             // for 32 x 201 drafted rows
 #pragma unroll
                 for (int q = 0; q < 8; ++q)
                     c[q] = *(const i32x4_a *)(x + ctx_start(v + q * kThreads, Lmax));

@@ -6,9 +6,9 @@
 // A plan moves a few kilobytes: it is bound by its chain of dependent reads
 // (requests, sums over the sequences, pages, slots) and, with several
 // work-groups, by the ticket of the last one.  Measured (MI355X): 32 sequences
-// of 8 rows 4.5 us a call, 1024 trees of 60 nodes 8.7 us.  Packed slots write
-// 20 bytes a position: 256 prompts of up to 8192 tokens 11 us, 4.0 TB/s.  Cache
-// rows: 16 x 20 rows of 1 KB in each of 32 planes moved in 7.3 us, 2.9 TB/s.
+// of 8 rows 2.7 us, 1024 trees of 60 nodes 8.7 us.  Packed slots write 20 bytes
+// a position: 256 prompts of up to 8192 tokens 11 us, 4.0 TB/s.  Cache rows: 16
+// x 20 rows of 1 KB in each of 32 planes moved in 7.4 us, 2.9 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <stdint.h>

@@ -137,6 +137,22 @@ def test_plan_of_a_ring_that_is_too_small(B):
     assert t["ring"].tolist() == [0, 1, 2, 102 + 1, 4, 5]
 
 
+def test_plan_of_the_most_sequences():
+    from paper_2609_20186_amd import binding as sd
+    say("[plan] 65536 sequences")
+    s, rng = plan_state(65536, 2, 9, 4, "tree", 11, 0)
+    t, args, ws = device_plan(s)
+    for step in range(2):
+        s["lengths"][:] = rng.integers(0, 10, len(s["lengths"]))
+        s["dn"][:] = rng.integers(1, 3, len(s["dn"]))
+        t["lengths"].copy_(torch.from_numpy(s["lengths"]))
+        t["dn"].copy_(torch.from_numpy(s["dn"]))
+        res = ref.page_plan(s)
+        sd.switchsd_page_plan(args, ws)
+        compare_plan(s, t, res, f"step {step}")
+    assert int(ws.count_nonzero()) == 0
+
+
 def test_plan_captured():
     from paper_2609_20186_amd import binding as sd
     say("[plan] graph")
@@ -175,7 +191,8 @@ def test_plan_outputs_left_out():
 
 
 @pytest.mark.parametrize("B,Lmax,page,most_short", [(1, 1, 1, 0), (4, 50, 16, 0), (3, 5000, 7, 2),
-                                                    (300, 40, 16, 1), (2500, 9, 4, 0)])
+                                                    (300, 40, 16, 1), (2500, 9, 4, 0),
+                                                    (65536, 4, 2, 0)])
 def test_spans(B, Lmax, page, most_short):
     from paper_2609_20186_amd import binding as sd
     say(f"[spans] {B} {Lmax} {page}")

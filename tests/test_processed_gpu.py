@@ -336,6 +336,32 @@ def test_captured_and_on_another_stream():
     assert torch.equal(o2.view(word), out.view(word))
 
 
+def test_two_streams_at_once():
+    """Verifications that may overlap, each with a workspace of its own."""
+    from paper_2609_20186_amd import binding as sd
+    say("[verify] two streams")
+    runs = []
+    for seed, (B, R, V) in enumerate([(9, 20, 30000), (5, 66, 20001)]):
+        d = plant(make(B, R, V, 400, seed=70 + seed, draft="tree"), seed)
+        out, ws = gpu_verify(device_args(d))
+        runs.append((d, device_args(d), out, ws, torch.cuda.Stream(),
+                     ref.greedy(d, ref.processed(d, np.float32))))
+    for d, args, out, ws, stream, want in runs:
+        for t in out.values():
+            t.fill_(-9)
+        stream.wait_stream(torch.cuda.current_stream())
+    for turn in range(20):
+        for d, args, out, ws, stream, want in runs:
+            sd.switchsd_verify_processed(args, out["accept_len"], out["accept_node"],
+                                         out["bonus"], out["out_tokens"], out["amax"], ws,
+                                         stream)
+    torch.cuda.synchronize()
+    for d, args, out, ws, stream, want in runs:
+        for name, t in out.items():
+            np.testing.assert_array_equal(t.cpu().numpy(), want[name], err_msg=name)
+        assert int(ws.count_nonzero()) == 0
+
+
 def test_two_graphs_share_a_workspace():
     """Two captured verifications of different shapes on one workspace, replayed
     in turn."""

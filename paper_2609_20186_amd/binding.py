@@ -410,16 +410,18 @@ _DT["logits"] = tuple(_TYPES)
 
 
 def _current_device():
+    # -2 without a GPU: no tensor's number (-1 is the CPU's)
     if _device is None or not _initialized():
-        return torch.cuda.current_device() if torch.cuda.is_available() else -1
+        return torch.cuda.current_device() if torch.cuda.is_available() else -2
     return _device()
 
 
 def _arr(t, kind, name, shape, dev, optional=False):
     """Device pointer of a tensor of exactly this shape on device `dev`."""
-    # the accepted case first: a call checks up to ten tensors
+    # the accepted case first: a call checks up to ten tensors; what has the
+    # device's number is on a GPU
     if isinstance(t, _Tensor) and t.get_device() == dev and t.dtype in _DT[kind] and \
-            t.shape == shape and t.is_contiguous() and t.is_cuda:
+            t.shape == shape and t.is_contiguous():
         return t.data_ptr()
     ptr = _ptr(t, kind, name, optional)
     if ptr is not None or t is not None:
@@ -569,7 +571,9 @@ def switchsd_span_slots(begin, end, tokens, table, held, page_size, cu, slots, p
         most = table.shape[1]
         p_table = _arr(table, "i32", "table", (B, most), dev)
         p_held = _arr(held, "i32", "held", (B,), dev)
-    cap = next((t.shape for t in (slots, positions, packed, seq) if t is not None), (0,))
+    one = slots if slots is not None else positions if positions is not None else \
+        packed if packed is not None else seq
+    cap = (0,) if one is None else one.shape
     _check("switchsd_span_slots", lib.switchsd_span_slots(
         _arr(begin, "i32", "begin", (B,), dev), _arr(end, "i32", "end", (B,), dev),
         _arr(tokens, "i32", "tokens", (B, Lmax), dev), p_table, p_held, B, Lmax, most,
@@ -591,9 +595,10 @@ def switchsd_compact_cache(cache, slots, dpar, dn, accept_node, stream=None):
     dev = _current_device()
     _here(cache, "cache", dev)
     B, R = slots.shape
-    row = cache.element_size() * (cache.numel() // (planes * n_slots) if cache.numel() else 0)
+    size, numel = cache.element_size(), cache.numel()
+    row = size * (numel // (planes * n_slots) if numel else 0)
     _check("switchsd_compact_cache", lib.switchsd_compact_cache(
-        cache.data_ptr(), planes, cache.stride(0) * cache.element_size(), n_slots, row,
+        cache.data_ptr(), planes, cache.stride(0) * size, n_slots, row,
         _arr(slots, "i64", "slots", (B, R), dev), _arr(dpar, "i32", "dpar", (B, R), dev, True),
         _arr(dn, "i32", "dn", (B,), dev), _arr(accept_node, "i32", "accept_node", (B,), dev), B, R,
         _stream(stream)))

@@ -8,7 +8,7 @@
 // work-groups, by the ticket of the last one.  Measured (MI355X): 32 sequences
 // of 8 rows 2.7 us, 1024 trees of 60 nodes 8.7 us.  Packed slots write 20 bytes
 // a position: 256 prompts of up to 8192 tokens 11 us, 4.0 TB/s.  Cache rows: 16
-// x 20 rows of 1 KB in each of 32 planes moved in 7.4 us, 2.9 TB/s.
+// x 20 rows of 1 KB in each of 32 planes moved in 6.7 us, 3.1 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <stdint.h>
@@ -456,7 +456,9 @@ __global__ __launch_bounds__(kThreads) void k_compact(CompactParams p) {
     __shared__ int64_t slot[SWITCHSD_MAX_R];
     __shared__ int16_t path[SWITCHSD_MAX_R];  // node at depth d
     __shared__ int64_t src[SWITCHSD_MAX_R], dst[SWITCHSD_MAX_R];
-    __shared__ int s_depth, s_m;
+    // bit i: node i does not follow node i - 1 (the anchor does not)
+    __shared__ unsigned long long s_heads[SWITCHSD_MAX_R / 64];
+    __shared__ int s_m;
     const int tid = threadIdx.x;
     const int b = blockIdx.x / p.blocks, blk = blockIdx.x - b * p.blocks;
     const int64_t base = (int64_t)b * p.R;
@@ -464,24 +466,39 @@ __global__ __launch_bounds__(kThreads) void k_compact(CompactParams p) {
     const int a = p.accept_node[b];
     if (a <= 0 || a >= n)
         return;
-    for (int i = tid; i <= a; i += kThreads) {
-        const int q = p.dpar[base + i];
-        par[i] = (int16_t)(q >= 0 && q < i ? q : -1);
-        slot[i] = p.slots[base + i];
+    for (int i0 = 0; i0 <= a; i0 += kThreads) {
+        const int i = i0 + tid;
+        int q = -1;
+        if (i <= a) {
+            q = p.dpar[base + i];
+            q = q >= 0 && q < i ? q : -1;
+            par[i] = (int16_t)q;
+            slot[i] = p.slots[base + i];
+        }
+        const unsigned long long heads = __ballot(i == 0 || q != i - 1);
+        if ((tid & 63) == 0 && i < SWITCHSD_MAX_R)
+            s_heads[i >> 6] = heads;
     }
     __syncthreads();
-    if (tid == 0) {
+    if (tid < 64) {
+        // the path, deepest node first, a run of nodes that follow each other
+        // (within 64) at a time: chains and candidates are few runs (a path of 20
+        // moved in 4.8 us, node by node in 5.7)
         int depth = 0, cur = a;
         while (cur > 0) {
-            path[depth++] = (int16_t)cur;  // deepest first
-            cur = par[cur];
+            const int own = par[cur], top = cur & 63;
+            const unsigned long long h = s_heads[cur >> 6] & (~0ull >> (63 - top));
+            const int low = h ? cur - top + 63 - __builtin_clzll(h) : cur - top;
+            const int run = cur - (low > 0 ? low : 1) + 1;
+            if (tid < run)
+                path[depth + tid] = (int16_t)(cur - tid);
+            depth += run;
+            cur = low == 0 ? 0 : low == cur ? own : par[low];
         }
-        s_depth = cur == 0 ? depth : 0;
-        s_m = 0;
-    }
-    __syncthreads();
-    const int depth = s_depth;
-    if (tid < 64) {
+        depth = cur == 0 ? depth : 0;
+        // read by other lanes of the wave
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
         // the moves that are any, in path order
         int m = 0;
         for (int j0 = 1; j0 <= depth; j0 += 64) {

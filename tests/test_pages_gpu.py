@@ -225,7 +225,7 @@ def test_spans(B, Lmax, page, most_short):
     (1, 1, "tree", 1, 8, torch.bfloat16), (3, 9, "tree", 4, 64, torch.bfloat16),
     (5, 60, "tree", 3, 130, torch.float16), (4, 201, "candidates", 2, 512, torch.bfloat16),
     (2, 1024, "tree", 1, 16, torch.float32), (6, 30, "long", 5, 33, torch.float32),
-    (3, 40, "tree", 7, 1004, torch.uint8),
+    (3, 40, "tree", 7, 1004, torch.uint8), (3, 1024, "candidates", 2, 64, torch.float32),
 ])
 def test_compact(B, R, kind, planes, row, dtype):
     from paper_2609_20186_amd import binding as sd

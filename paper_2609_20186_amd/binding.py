@@ -560,9 +560,18 @@ def switchsd_page_plan(args, workspace, stream=None):
 def switchsd_span_slots(begin, end, tokens, table, held, page_size, cu, slots, positions, packed,
                         seq, stream=None):
     """begin, end, held [B], tokens [B, Lmax], table [B, max_pages] int32; cu
-    [B + 1] int32, slots int64 and positions, packed, seq int32 of one length
-    (each None if not wanted)."""
+    [B + 1] int32, slots int64 and positions, packed, seq int32 [capacity] (each
+    None if not wanted)."""
     B, Lmax = tokens.shape
+    one = slots if slots is not None else positions if positions is not None else \
+        packed if packed is not None else seq
+    cap = (0,)
+    if one is not None:
+        # the library is told one capacity: of an output of several axes it would
+        # fill no more than the first axis' length
+        if not isinstance(one, _Tensor) or one.dim() != 1:
+            raise ValueError("slots, positions, packed and seq must be device tensors [capacity]")
+        cap = one.shape
     dev = _current_device()
     most, p_table, p_held = 0, None, None
     if slots is not None:
@@ -571,9 +580,6 @@ def switchsd_span_slots(begin, end, tokens, table, held, page_size, cu, slots, p
         most = table.shape[1]
         p_table = _arr(table, "i32", "table", (B, most), dev)
         p_held = _arr(held, "i32", "held", (B,), dev)
-    one = slots if slots is not None else positions if positions is not None else \
-        packed if packed is not None else seq
-    cap = (0,) if one is None else one.shape
     _check("switchsd_span_slots", lib.switchsd_span_slots(
         _arr(begin, "i32", "begin", (B,), dev), _arr(end, "i32", "end", (B,), dev),
         _arr(tokens, "i32", "tokens", (B, Lmax), dev), p_table, p_held, B, Lmax, most,

@@ -558,11 +558,22 @@ def switchsd_page_plan(args, workspace, stream=None):
 
 
 def switchsd_span_slots(begin, end, tokens, table, held, page_size, cu, slots, positions, packed,
-                        seq, stream=None):
+                        seq, stream=None, Lmax=None):
     """begin, end, held [B], tokens [B, Lmax], table [B, max_pages] int32; cu
     [B + 1] int32, slots int64 and positions, packed, seq int32 [capacity] (each
-    None if not wanted)."""
-    B, Lmax = tokens.shape
+    None if not wanted).  Without packed, tokens may be None; the limit of the
+    positions is then given as Lmax."""
+    if tokens is None:
+        if packed is not None or Lmax is None:
+            raise ValueError("tokens is required (without packed: tokens or Lmax)")
+        if not isinstance(begin, _Tensor) or begin.dim() != 1:
+            raise ValueError("begin must be a device tensor [B]")
+        B, Lmax = begin.shape[0], int(Lmax)
+    else:
+        B, cols = tokens.shape
+        if Lmax is not None and Lmax != cols:
+            raise ValueError(f"tokens has {cols} columns, Lmax is {Lmax}")
+        Lmax = cols
     one = slots if slots is not None else positions if positions is not None else \
         packed if packed is not None else seq
     cap = (0,)
@@ -582,8 +593,8 @@ def switchsd_span_slots(begin, end, tokens, table, held, page_size, cu, slots, p
         p_held = _arr(held, "i32", "held", (B,), dev)
     _check("switchsd_span_slots", lib.switchsd_span_slots(
         _arr(begin, "i32", "begin", (B,), dev), _arr(end, "i32", "end", (B,), dev),
-        _arr(tokens, "i32", "tokens", (B, Lmax), dev), p_table, p_held, B, Lmax, most,
-        int(page_size), _arr(cu, "i32", "cu", (B + 1,), dev),
+        None if tokens is None else _arr(tokens, "i32", "tokens", (B, Lmax), dev), p_table, p_held,
+        B, Lmax, most, int(page_size), _arr(cu, "i32", "cu", (B + 1,), dev),
         None if slots is None else _arr(slots, "i64", "slots", cap, dev),
         None if positions is None else _arr(positions, "i32", "positions", cap, dev),
         None if packed is None else _arr(packed, "i32", "packed", cap, dev),

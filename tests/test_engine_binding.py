@@ -23,3 +23,17 @@ def test_packed_outputs_have_one_axis(at, shape):
     outs[at] = torch.zeros(shape, dtype=torch.int64 if at == 0 else torch.int32)
     with pytest.raises(ValueError, match=r"\[capacity\]"):
         spans(i32(2, 9), outs)
+
+
+def test_spans_without_tokens():
+    """Without packed, tokens are not needed, as in the C call; Lmax then is."""
+    outs = [None, i32(5), None, i32(5)]
+    with pytest.raises(ValueError, match="Lmax"):
+        spans(None, outs)
+    with pytest.raises(ValueError, match="tokens is required"):
+        spans(None, [None, None, i32(5), None], Lmax=9)
+    with pytest.raises(ValueError, match="Lmax is 8"):
+        spans(i32(2, 9), outs, Lmax=8)
+    # complete: what is refused is that these are host tensors
+    with pytest.raises(ValueError, match="begin must be a device tensor"):
+        spans(None, outs, Lmax=9)

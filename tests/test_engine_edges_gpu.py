@@ -1,7 +1,9 @@
 """Calls around the step at the edges of what they take."""
+import numpy as np
 import pytest
 import torch
 
+import engine_ref as ref
 from gpu_helpers import say
 
 pytestmark = pytest.mark.gpu
@@ -27,3 +29,29 @@ def test_packed_outputs_of_two_axes_are_refused():
     assert bool((pos == -7).all()) and bool((cu == -7).all())
     sd.switchsd_span_slots(begin, end, tokens, None, None, 16, cu, None, pos.view(-1), None, None)
     assert torch.equal(pos, torch.arange(n, **i32).expand(B, n))
+
+
+def test_spans_without_tokens():
+    """Positions, slots and sequences of ranges whose tokens are not given."""
+    from paper_2609_20186_amd import binding as sd
+    say("[spans] without tokens")
+    B, Lmax, page, most = 7, 90, 16, 6
+    rng = np.random.default_rng(5)
+    table = rng.integers(0, 1000, (B, most)).astype(np.int32)
+    held = rng.integers(0, most + 1, B).astype(np.int32)
+    begin = rng.integers(-2, 60, B).astype(np.int32)
+    end = rng.integers(0, Lmax + 20, B).astype(np.int32)
+    cu, rec = ref.spans(begin, end, np.zeros((B, Lmax), np.int32), table, held, page, 1 << 40)
+    dev = [torch.from_numpy(x).cuda() for x in (begin, end, table, held)]
+    n = len(rec) + 3
+    i32 = dict(dtype=torch.int32, device="cuda")
+    c = torch.full((B + 1,), -7, **i32)
+    slots = torch.full((n,), -7, dtype=torch.int64, device="cuda")
+    pos, seq = torch.full((n,), -7, **i32), torch.full((n,), -7, **i32)
+    sd.switchsd_span_slots(dev[0], dev[1], None, dev[2], dev[3], page, c, slots, pos, None, seq,
+                           Lmax=Lmax)
+    np.testing.assert_array_equal(c.cpu().numpy(), cu)
+    want = np.array(rec, np.int64).reshape(-1, 4)
+    for j, t in ((0, slots), (1, pos), (3, seq)):
+        np.testing.assert_array_equal(t[:len(rec)].cpu().numpy(), want[:, j])
+        assert bool((t[len(rec):] == -7).all())

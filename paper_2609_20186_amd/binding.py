@@ -431,6 +431,13 @@ def _arr(t, kind, name, shape, dev, optional=False):
     return ptr
 
 
+def _workspace(t, dev):
+    """Device pointer of a workspace on device `dev`."""
+    ptr = _ptr(t, "u8", "workspace")
+    _here(t, "workspace", dev)
+    return ptr
+
+
 def _here(t, name, dev):
     if t.get_device() != dev:
         raise ValueError(f"{name} is on device {t.get_device()}, the current device is {dev}")
@@ -507,14 +514,14 @@ def switchsd_verify_processed(args, accept_len, accept_node, bonus, out_tokens, 
                               stream=None):
     dev = _args_here(args)
     B, R, _ = args.shape
-    _here(workspace, "workspace", dev)
+    p_workspace = _workspace(workspace, dev)
     _check("switchsd_verify_processed", lib.switchsd_verify_processed(
         ctypes.byref(args), _arr(accept_len, "i32", "accept_len", (B,), dev),
         _arr(accept_node, "i32", "accept_node", (B,), dev),
         _arr(bonus, "i32", "bonus", (B,), dev),
         _arr(out_tokens, "i32", "out_tokens", (B, R), dev),
         _arr(amax, "i32", "amax", (B, R), dev, True),
-        _ptr(workspace, "u8", "workspace"), workspace.numel(), _stream(stream)))
+        p_workspace, workspace.numel(), _stream(stream)))
 
 
 def build_page_args(lengths, dpar, dn, Lmax, page_size, table, held, ring, ring_state, slots,
@@ -551,10 +558,9 @@ def build_page_args(lengths, dpar, dn, Lmax, page_size, table, held, ring, ring_
 
 
 def switchsd_page_plan(args, workspace, stream=None):
-    _here(workspace, "workspace", _args_here(args))
+    p_workspace = _workspace(workspace, _args_here(args))
     _check("switchsd_page_plan", lib.switchsd_page_plan(
-        ctypes.byref(args), _ptr(workspace, "u8", "workspace"), workspace.numel(),
-        _stream(stream)))
+        ctypes.byref(args), p_workspace, workspace.numel(), _stream(stream)))
 
 
 def switchsd_span_slots(begin, end, tokens, table, held, page_size, cu, slots, positions, packed,
@@ -570,6 +576,8 @@ def switchsd_span_slots(begin, end, tokens, table, held, page_size, cu, slots, p
             raise ValueError("begin must be a device tensor [B]")
         B, Lmax = begin.shape[0], int(Lmax)
     else:
+        if not isinstance(tokens, _Tensor) or tokens.dim() != 2:
+            raise ValueError("tokens must be a device tensor [B, Lmax]")
         B, cols = tokens.shape
         if Lmax is not None and Lmax != cols:
             raise ValueError(f"tokens has {cols} columns, Lmax is {Lmax}")
@@ -586,8 +594,8 @@ def switchsd_span_slots(begin, end, tokens, table, held, page_size, cu, slots, p
     dev = _current_device()
     most, p_table, p_held = 0, None, None
     if slots is not None:
-        if table is None or held is None:
-            raise ValueError("slots need table and held")
+        if not isinstance(table, _Tensor) or table.dim() != 2 or held is None:
+            raise ValueError("slots need table [B, max_pages] and held [B]")
         most = table.shape[1]
         p_table = _arr(table, "i32", "table", (B, most), dev)
         p_held = _arr(held, "i32", "held", (B,), dev)
@@ -609,6 +617,8 @@ def switchsd_compact_cache(cache, slots, dpar, dn, accept_node, stream=None):
     planes, n_slots = cache.shape[:2]
     if not cache.is_contiguous() and not cache[0].is_contiguous():
         raise ValueError("cache planes must be contiguous")
+    if not isinstance(slots, _Tensor) or slots.dim() != 2:
+        raise ValueError("slots must be a device tensor [B, R]")
     dev = _current_device()
     _here(cache, "cache", dev)
     B, R = slots.shape

@@ -37,3 +37,26 @@ def test_spans_without_tokens():
     # complete: what is refused is that these are host tensors
     with pytest.raises(ValueError, match="begin must be a device tensor"):
         spans(None, outs, Lmax=9)
+
+
+def test_missing_workspace():
+    """None is refused as every other missing tensor is."""
+    a = sd.LogitsArgs()
+    a.shape, a.device = (2, 3, 8), sd._current_device()
+    with pytest.raises(ValueError, match="workspace is required"):
+        sd.switchsd_verify_processed(a, i32(2), i32(2), i32(2), i32(2, 3), i32(2, 3), None)
+    a = sd.PageArgs()
+    a.device = sd._current_device()
+    with pytest.raises(ValueError, match="workspace is required"):
+        sd.switchsd_page_plan(a, None)
+    with pytest.raises(ValueError, match="workspace must be a device tensor"):
+        sd.switchsd_page_plan(a, torch.zeros(1024, dtype=torch.uint8))
+
+
+def test_spans_ranks():
+    outs = [torch.zeros(5, dtype=torch.int64), None, None, None]
+    with pytest.raises(ValueError, match="tokens must be"):
+        spans(i32(9), outs)
+    for table, held in ((None, i32(2)), (i32(8), i32(2)), (i32(2, 4), None)):
+        with pytest.raises(ValueError, match="slots need table"):
+            sd.switchsd_span_slots(i32(2), i32(2), i32(2, 9), table, held, 16, i32(3), *outs)

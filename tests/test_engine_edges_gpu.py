@@ -55,3 +55,15 @@ def test_spans_without_tokens():
     for j, t in ((0, slots), (1, pos), (3, seq)):
         np.testing.assert_array_equal(t[:len(rec)].cpu().numpy(), want[:, j])
         assert bool((t[len(rec):] == -7).all())
+
+
+def test_compact_without_slots():
+    """Slots that are missing or of another rank are refused by name."""
+    from paper_2609_20186_amd import binding as sd
+    say("[compact] without slots")
+    cache = torch.zeros((2, 8, 4), device="cuda")
+    i32 = dict(dtype=torch.int32, device="cuda")
+    par, one = torch.full((1, 3), -1, **i32), torch.ones(1, **i32)
+    for slots in (None, torch.zeros(3, dtype=torch.int64, device="cuda")):
+        with pytest.raises(ValueError, match="slots must be"):
+            sd.switchsd_compact_cache(cache, slots, par, one, one)

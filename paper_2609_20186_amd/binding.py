@@ -438,6 +438,17 @@ def _workspace(t, dev):
     return ptr
 
 
+_INT_MAX = 2 ** 31 - 1
+
+
+def _sizes(**sizes):
+    """ctypes keeps the low 32 bits of an int32 argument: a size beyond them
+    would be taken for another, valid one."""
+    for name, n in sizes.items():
+        if not -_INT_MAX - 1 <= n <= _INT_MAX:
+            raise ValueError(f"{name} = {n} does not fit 32 bits")
+
+
 def _here(t, name, dev):
     if t.get_device() != dev:
         raise ValueError(f"{name} is on device {t.get_device()}, the current device is {dev}")
@@ -457,6 +468,7 @@ def build_logits_args(logits, dtok, dpar, dn, tokens=None, lengths=None, prompt_
     if not isinstance(logits, _Tensor) or logits.dim() != 3:
         raise ValueError("logits must be a device tensor [B, R, V]")
     B, R, V = logits.shape
+    _sizes(B=B, R=R, V=V)
     dev = _current_device()
     a = LogitsArgs()
     a.logits = _arr(logits, "logits", "logits", (B, R, V), dev)
@@ -469,6 +481,7 @@ def build_logits_args(logits, dtok, dpar, dn, tokens=None, lengths=None, prompt_
     if tokens is not None:
         if not isinstance(tokens, _Tensor) or tokens.dim() != 2:
             raise ValueError("tokens must be a device tensor [B, Lmax]")
+        _sizes(Lmax=tokens.shape[1])
         a.Lmax = tokens.shape[1]
         a.tokens = _arr(tokens, "i32", "tokens", (B, a.Lmax), dev)
     elif penal:
@@ -483,6 +496,7 @@ def build_logits_args(logits, dtok, dpar, dn, tokens=None, lengths=None, prompt_
     if bias_ids is not None:
         if not isinstance(bias_ids, _Tensor) or bias_ids.dim() != 2:
             raise ValueError("bias_ids must be a device tensor [B, n]")
+        _sizes(n_bias=bias_ids.shape[1])
         a.n_bias = bias_ids.shape[1]
         a.bias_ids = _arr(bias_ids, "i32", "bias_ids", (B, a.n_bias), dev)
         a.bias_vals = _arr(bias_vals, "f32", "bias_vals", (B, a.n_bias), dev)
@@ -538,15 +552,18 @@ def build_page_args(lengths, dpar, dn, Lmax, page_size, table, held, ring, ring_
     if R is None:
         raise ValueError("R is required")
     B, most = table.shape
+    Lmax, page_size = int(Lmax), int(page_size)
+    _sizes(B=B, R=R, Lmax=Lmax, page_size=page_size, max_pages=most)
     dev = _current_device()
     a = PageArgs()
-    a.B, a.R, a.Lmax, a.page_size, a.max_pages = B, R, int(Lmax), int(page_size), most
+    a.B, a.R, a.Lmax, a.page_size, a.max_pages = B, R, Lmax, page_size, most
     a.table = _arr(table, "i32", "table", (B, most), dev)
     for name, t in (("lengths", lengths), ("dn", dn), ("held", held), ("missing", missing)):
         setattr(a, name, _arr(t, "i32", name, (B,), dev))
     a.dpar = _arr(dpar, "i32", "dpar", (B, R), dev, True)
     if not isinstance(ring, _Tensor) or ring.dim() != 1:
         raise ValueError("ring must be a device tensor [ring_pages]")
+    _sizes(ring_pages=ring.shape[0])
     a.ring_pages = ring.shape[0]
     a.ring = _arr(ring, "i32", "ring", (a.ring_pages,), dev)
     a.ring_state = _arr(ring_state, "i32", "ring_state", (2,), dev)
@@ -599,14 +616,18 @@ def switchsd_span_slots(begin, end, tokens, table, held, page_size, cu, slots, p
         most = table.shape[1]
         p_table = _arr(table, "i32", "table", (B, most), dev)
         p_held = _arr(held, "i32", "held", (B,), dev)
+    page_size, room = int(page_size), cap[0]
+    if (B | Lmax | most | page_size | room) >> 31:
+        _sizes(B=B, Lmax=Lmax, max_pages=most, page_size=page_size)
+        room = min(room, _INT_MAX)  # no total is larger
     _check("switchsd_span_slots", lib.switchsd_span_slots(
         _arr(begin, "i32", "begin", (B,), dev), _arr(end, "i32", "end", (B,), dev),
         None if tokens is None else _arr(tokens, "i32", "tokens", (B, Lmax), dev), p_table, p_held,
-        B, Lmax, most, int(page_size), _arr(cu, "i32", "cu", (B + 1,), dev),
+        B, Lmax, most, page_size, _arr(cu, "i32", "cu", (B + 1,), dev),
         None if slots is None else _arr(slots, "i64", "slots", cap, dev),
         None if positions is None else _arr(positions, "i32", "positions", cap, dev),
         None if packed is None else _arr(packed, "i32", "packed", cap, dev),
-        None if seq is None else _arr(seq, "i32", "seq", cap, dev), cap[0], _stream(stream)))
+        None if seq is None else _arr(seq, "i32", "seq", cap, dev), room, _stream(stream)))
 
 
 def switchsd_compact_cache(cache, slots, dpar, dn, accept_node, stream=None):
@@ -624,6 +645,8 @@ def switchsd_compact_cache(cache, slots, dpar, dn, accept_node, stream=None):
     B, R = slots.shape
     size, numel = cache.element_size(), cache.numel()
     row = size * (numel // (planes * n_slots) if numel else 0)
+    if (planes | B | R | row) >> 31:
+        _sizes(planes=planes, B=B, R=R, row_bytes=row)
     _check("switchsd_compact_cache", lib.switchsd_compact_cache(
         cache.data_ptr(), planes, cache.stride(0) * size, n_slots, row,
         _arr(slots, "i64", "slots", (B, R), dev), _arr(dpar, "i32", "dpar", (B, R), dev, True),

@@ -60,3 +60,46 @@ def test_spans_ranks():
     for table, held in ((None, i32(2)), (i32(8), i32(2)), (i32(2, 4), None)):
         with pytest.raises(ValueError, match="slots need table"):
             sd.switchsd_span_slots(i32(2), i32(2), i32(2, 9), table, held, 16, i32(3), *outs)
+
+
+HUGE = 2 ** 32 + 16                     # 16 in its low 32 bits
+
+
+def huge(*shape, dtype=torch.int32):
+    """A tensor of that shape over one element."""
+    return torch.zeros(1, dtype=dtype).expand(shape)
+
+
+@pytest.mark.parametrize("call", [
+    lambda: sd.build_logits_args(huge(1, 1, HUGE, dtype=torch.bfloat16), i32(1, 1), None, i32(1)),
+    lambda: sd.build_logits_args(huge(HUGE, 1, 8, dtype=torch.float32), i32(1, 1), None, i32(1)),
+    lambda: sd.build_page_args(i32(2), None, i32(2), HUGE, 4, i32(2, 3), i32(2), i32(9), i32(2),
+                               None, None, i32(2), R=2),
+    lambda: sd.build_page_args(i32(2), None, i32(2), 9, HUGE, i32(2, 3), i32(2), i32(9), i32(2),
+                               None, None, i32(2), R=2),
+    lambda: sd.build_page_args(i32(2), None, i32(2), 9, 4, huge(2, HUGE), i32(2), i32(9), i32(2),
+                               None, None, i32(2), R=2),
+    lambda: sd.build_page_args(i32(2), None, i32(2), 9, 4, i32(2, 3), i32(2), i32(9), i32(2),
+                               None, None, i32(2), R=HUGE),
+    lambda: sd.switchsd_span_slots(i32(2), i32(2), huge(2, HUGE), None, None, 16, i32(3), None,
+                                   i32(5), None, None),
+    lambda: sd.switchsd_span_slots(i32(2), i32(2), i32(2, 9), None, None, HUGE, i32(3), None,
+                                   i32(5), None, None),
+    lambda: sd.switchsd_span_slots(i32(2), i32(2), i32(2, 9), None, None, 16 - 2 ** 32, i32(3),
+                                   None, i32(5), None, None),
+    lambda: sd.switchsd_span_slots(i32(2), i32(2), None, None, None, 16, i32(3), None,
+                                   i32(5), None, None, Lmax=HUGE),
+])
+def test_sizes_beyond_32_bits(call):
+    """ctypes passes the low 32 bits on: 2^32 + 16 would be taken for 16."""
+    assert sd.ctypes.c_int32(HUGE).value == 16
+    with pytest.raises(ValueError, match="does not fit 32 bits"):
+        call()
+
+
+def test_sizes_that_fit_reach_the_library():
+    """A negative size is not the binding's to refuse."""
+    sd._sizes(B=-2 ** 31, R=-3, V=2 ** 31 - 1)
+    for n in (2 ** 31, -2 ** 31 - 1, HUGE):
+        with pytest.raises(ValueError, match="does not fit 32 bits"):
+            sd._sizes(V=n)

@@ -67,3 +67,30 @@ def test_compact_without_slots():
     for slots in (None, torch.zeros(3, dtype=torch.int64, device="cuda")):
         with pytest.raises(ValueError, match="slots must be"):
             sd.switchsd_compact_cache(cache, slots, par, one, one)
+
+
+def test_sizes_beyond_32_bits():
+    """A vocabulary and rows of bytes whose low 32 bits are a valid size are
+    refused; packed outputs of more than 2^32 entries are filled."""
+    from paper_2609_20186_amd import binding as sd
+    say("[binding] sizes beyond 32 bits")
+    i32 = dict(dtype=torch.int32, device="cuda")
+    one = torch.ones(1, **i32)
+    x = torch.empty((1, 1, 2 ** 32 + 64), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError, match="V = 4294967360 does not fit"):
+        sd.build_logits_args(x, one.view(1, 1), None, one)
+    del x
+    cache = torch.empty((1, 2, 2 ** 32 + 64), dtype=torch.uint8, device="cuda")
+    with pytest.raises(ValueError, match="row_bytes = 4294967360 does not fit"):
+        sd.switchsd_compact_cache(cache, torch.zeros((1, 2), dtype=torch.int64, device="cuda"),
+                                  torch.zeros((1, 2), **i32), one, one)
+    del cache
+    B, n = 4, 20
+    big = torch.empty(2 ** 32 + 5, **i32)
+    big[:B * n + 9] = -7
+    cu = torch.full((B + 1,), -7, **i32)
+    sd.switchsd_span_slots(torch.zeros(B, **i32), torch.full((B,), n, **i32),
+                           torch.zeros((B, 64), **i32), None, None, 16, cu, None, big, None, None)
+    assert cu.tolist() == [0, 20, 40, 60, 80]
+    assert torch.equal(big[:B * n].view(B, n), torch.arange(n, **i32).expand(B, n))
+    assert bool((big[B * n:B * n + 9] == -7).all())

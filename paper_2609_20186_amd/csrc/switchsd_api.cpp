@@ -998,18 +998,8 @@ int check_logits(const switchsd_logits_args *a) {
 // chunk anew.  Large chunks and many rows per work-group count least often;
 // both shrink while there are too few work-groups.
 int set_logits_grid(LogitsParams &p) {
-    int cus = 0;
-    const int rc = cu_count(&cus);
-    if (rc)
-        return rc;
     const switchsd_logits_args &a = p.a;
     p.penal = a.repetition || a.frequency || a.presence;
-    // Four work-groups per compute unit, down to two where each would count a
-    // long history.
-    int64_t want = 4 * (int64_t)cus;
-    if (p.penal && a.Lmax > 4096)
-        want = want * 4096 / a.Lmax;
-    want = want < 2 * cus ? 2 * cus : want;
     const int64_t vecs = p.out ? kProcessBlk : kVerifyBlk;  // of a block
     const int64_t blk = vecs * (a.logits_type == SWITCHSD_F32 ? 4 : 8);
     const int64_t blocks = (a.V + blk - 1) / blk;
@@ -1018,15 +1008,32 @@ int set_logits_grid(LogitsParams &p) {
     int64_t rows = a.R < kRowGroup ? a.R : kRowGroup;
     rows = rows < most ? rows : most;
     int64_t groups = (a.R + rows - 1) / rows;
-    for (p.unroll = kLogitsUnroll;; p.unroll >>= 1) {
-        const int64_t per = kThreads / vecs * p.unroll;  // blocks of a chunk, at most
+    const auto set_chunks = [&](int32_t unroll) {
+        const int64_t per = kThreads / vecs * unroll;  // blocks of a chunk, at most
+        p.unroll = unroll;
         p.chunk_log = 0;
         while (((int64_t)1 << p.chunk_log) * per < blocks)
             ++p.chunk_log;
         p.chunks = 1 << p.chunk_log;
-        if (p.unroll == 1 || (int64_t)a.B * groups * p.chunks >= want)
-            break;
-    }
+    };
+    set_chunks(kLogitsUnroll);
+    // The fewest work-groups that these sizes take, whatever the device: refused
+    // before any HIP call.  What follows adds work-groups only up to a few per
+    // compute unit.
+    if (!launch_ok((int64_t)a.B * groups * p.chunks))
+        return SWITCHSD_ESHAPE;
+    int cus = 0;
+    const int rc = cu_count(&cus);
+    if (rc)
+        return rc;
+    // Four work-groups per compute unit, down to two where each would count a
+    // long history.
+    int64_t want = 4 * (int64_t)cus;
+    if (p.penal && a.Lmax > 4096)
+        want = want * 4096 / a.Lmax;
+    want = want < 2 * cus ? 2 * cus : want;
+    while (p.unroll > 1 && (int64_t)a.B * groups * p.chunks < want)
+        set_chunks(p.unroll >> 1);
     const int64_t more = want / ((int64_t)a.B * p.chunks);  // groups that want would take
     if (more > groups) {
         rows = (a.R + more - 1) / more;
@@ -1035,7 +1042,7 @@ int set_logits_grid(LogitsParams &p) {
     p.split = p.unroll == 2 && rows >= kWholeRows ? 1 : 4;
     p.rows = (int32_t)rows;
     p.groups = (int32_t)groups;
-    return launch_ok((int64_t)a.B * groups * p.chunks) ? SWITCHSD_OK : SWITCHSD_ESHAPE;
+    return SWITCHSD_OK;
 }
 
 }  // namespace

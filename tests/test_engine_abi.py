@@ -222,3 +222,40 @@ def test_reference_plan():
     assert positions.tolist() == [[3, 4], [-1, -1], [8, 9]]
     assert missing.tolist() == [0, 0, 2]
     assert s["ring"].tolist() == [9, 5, 6, 3] and s["ring_state"].tolist() == [0, 3]
+
+
+@pytest.mark.parametrize("t,blk", [(sd.BF16, 8), (sd.F16, 8), (sd.F32, 4)])
+def test_logits_work_groups(t, blk):
+    """2^24 work-groups or more are refused by the sizes alone, before any HIP
+    call: a chunk holds 512 vectors and a work-group up to 64 rows."""
+    lib = sd.lib
+    size = 4 if t == sd.F32 else 2
+    chunk = 512 * blk
+
+    def both(B, R, V):
+        a = logits_args(logits_type=t, B=B, R=R, V=V, logits=1 << 20)
+        out = (1 << 20) + size * B * R * V + 4096
+        need = sd.workspace_bytes(B, R)
+        return (lib.switchsd_process_logits(ctypes.byref(a), out, t, None),
+                lib.switchsd_verify_processed(ctypes.byref(a), P, P, P, P, P, P, need, None))
+    assert both(1 << 24, 1, chunk) == (ESHAPE, ESHAPE)
+    assert both(1 << 23, 1, chunk + 1) == (ESHAPE, ESHAPE)
+    assert both(1 << 23, 65, chunk) == (ESHAPE, ESHAPE)
+    assert both(1 << 16, 1024, chunk) == (ESHAPE, ESHAPE)   # 4 rows a work-group
+    assert both(1 << 10, 1, 1 << 26) == (ESHAPE,) * 2       # 2^14 chunks (floats: 2^15)
+    assert both(1 << 24, 1024, 1 << 26) == (ESHAPE, ESHAPE)
+
+
+def test_logits_largest_vocabulary():
+    """Offsets in a row are 32 bits wide: V up to 2^26 and no further."""
+    lib = sd.lib
+    for t in (sd.BF16, sd.F16, sd.F32):
+        a = logits_args(logits_type=t, V=(1 << 26) + 1)
+        assert lib.switchsd_process_logits(ctypes.byref(a), FAR, t, None) == ESHAPE
+        assert lib.switchsd_verify_processed(ctypes.byref(a), P, P, P, P, P, P, 1 << 15,
+                                             None) == ESHAPE
+        # 2^26 itself: what is refused is a missing output
+        a = logits_args(logits_type=t, V=1 << 26)
+        assert lib.switchsd_process_logits(ctypes.byref(a), None, t, None) == EINVAL
+        assert lib.switchsd_verify_processed(ctypes.byref(a), None, P, P, P, P, P, 1 << 15,
+                                             None) == EINVAL

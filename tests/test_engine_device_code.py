@@ -64,3 +64,23 @@ def test_buffer_stores_are_bounded_by_the_row(kernels):
         assert len(stores) == body.count("buffer_store_"), n
         assert all(o == "0" and "offset:" not in rest for o, rest in stores), n
         assert "buffer_load_" not in body, n
+
+
+def test_registers_of_the_verification(kernels):
+    """Four waves to a SIMD (128 registers); floats under a mask, whole rows per
+    wave, three (168).  Vocabularies of less than a vector are not held to it."""
+    seen = set()
+    for n, (_, meta) in kernels.items():
+        m = re.search(r"k_verifyILi(\d)ELi(\d)ELi(\d)ELb(\d)ELb(\d)EE", n)
+        if not m:
+            assert "k_verify" not in n, n
+            continue
+        src, split, unroll, mask, tiny = (int(v) for v in m.groups())
+        seen.add((src, split, unroll, mask, tiny))
+        if not tiny:
+            regs = int(re.search(r"amdhsa_next_free_vgpr (\d+)", meta).group(1))
+            assert regs <= (168 if src == 2 and split == 1 and mask else 128), (n, regs)
+    # each type: quarter rows of one and two vectors, whole rows, the tiny one,
+    # each with and without masks
+    assert seen == {(s, w, u, k, t) for s in range(3) for k in range(2)
+                    for w, u, t in ((4, 1, 0), (4, 2, 0), (1, 2, 0), (4, 1, 1))}

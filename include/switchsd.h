@@ -438,7 +438,9 @@ int switchsd_verify_processed(const switchsd_logits_args *args, int32_t *accept_
  * max_pages; it takes what it lacks over held[b] from the free ring and gives
  * nothing back while it lives.  A sequence with L = 0 is finished: its pages
  * return to the ring (for later calls; pages given back by a call are not
- * handed out by it), its table entries become -1 and held[b] = 0.
+ * handed out by it), its table entries become -1 and held[b] = 0.  A commit
+ * appends to every sequence, so an engine sets a finished sequence's length to 0
+ * after it, and again after every later one, or it counts as begun anew.
  * The ring holds ring_state = {head, count}: the free pages are
  * ring[(head + i) mod ring_pages], i < count.  Pages are taken from the head,
  * for the sequences in order, as long as the running total of what they lack
@@ -505,7 +507,10 @@ int switchsd_span_slots(const int32_t *begin, const int32_t *end, const int32_t 
  * The slots of a call's drafted nodes must be distinct.
  *   dpar [B, R] or NULL (chains: nothing to move), dn, accept_node [B];
  *   cache 4-byte aligned, row_bytes and plane_stride multiples of 4,
- *   plane_stride >= n_slots * row_bytes (one plane: not looked at).  One launch. */
+ *   plane_stride >= n_slots * row_bytes (one plane: not looked at).  One launch;
+ *   B times the bytes of one slot in all planes stays below about 64 GB (rows
+ *   and planes that are multiples of 16 bytes) or 16 GB: shapes that would take
+ *   2^24 work-groups or more are refused. */
 int switchsd_compact_cache(void *cache, int32_t planes, int64_t plane_stride, int64_t n_slots,
                            int32_t row_bytes, const int64_t *slots, const int32_t *dpar,
                            const int32_t *dn, const int32_t *accept_node, int32_t B, int32_t R,

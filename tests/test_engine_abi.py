@@ -259,3 +259,17 @@ def test_logits_largest_vocabulary():
         assert lib.switchsd_process_logits(ctypes.byref(a), None, t, None) == EINVAL
         assert lib.switchsd_verify_processed(ctypes.byref(a), None, P, P, P, P, P, 1 << 15,
                                              None) == EINVAL
+
+
+def test_compact_work_groups():
+    """A work-group moves 256 pieces of 16 (else 4) bytes of a sequence: 2^24
+    work-groups or more are refused."""
+    def call(B, planes, row, cache):
+        return sd.lib.switchsd_compact_cache(cache, planes, row, 1, row, P, P, P, P, B, 8, None)
+    row = 1 << 20
+    for size, at in ((16, P), (4, P + 4)):
+        many = (1 << 24) // (row // size // 256)
+        assert call(1, many, row, at) == ESHAPE
+        assert call(many, 1, row, at) == ESHAPE
+        assert call(1 << 24, 1, size, at) == ESHAPE
+        assert call(1 << 24, 1 << 30, row, at) == ESHAPE

@@ -16,6 +16,20 @@ __device__ __forceinline__ int clampi(int v, int lo, int hi) {
     return v < lo ? lo : (v > hi ? hi : v);
 }
 
+// Inclusive sum over the wave's lanes: row shifts, then two row broadcasts.
+__device__ __forceinline__ int wave_scan(int v) {
+#define SWITCHSD_STEP(ctrl, mask) \
+    v += __builtin_amdgcn_update_dpp(0, v, ctrl, mask, 0xf, false);
+    SWITCHSD_STEP(0x111, 0xf)
+    SWITCHSD_STEP(0x112, 0xf)
+    SWITCHSD_STEP(0x114, 0xf)
+    SWITCHSD_STEP(0x118, 0xf)
+    SWITCHSD_STEP(0x142, 0xa)
+    SWITCHSD_STEP(0x143, 0xc)
+#undef SWITCHSD_STEP
+    return v;
+}
+
 // Values that one work-group hands to another travel through agent-scope
 // atomics, which are coherent across the XCDs without any L2 write-back.
 __device__ __forceinline__ unsigned long long ld_u64(const unsigned long long *p) {

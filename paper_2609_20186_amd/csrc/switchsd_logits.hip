@@ -113,20 +113,6 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
     return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
-// Inclusive sum over the wave's lanes: row shifts, then two row broadcasts.
-__device__ __forceinline__ int wave_scan(int v) {
-#define SWITCHSD_STEP(ctrl, mask) \
-    v += __builtin_amdgcn_update_dpp(0, v, ctrl, mask, 0xf, false);
-    SWITCHSD_STEP(0x111, 0xf)
-    SWITCHSD_STEP(0x112, 0xf)
-    SWITCHSD_STEP(0x114, 0xf)
-    SWITCHSD_STEP(0x118, 0xf)
-    SWITCHSD_STEP(0x142, 0xa)
-    SWITCHSD_STEP(0x143, 0xc)
-#undef SWITCHSD_STEP
-    return v;
-}
-
 template <int kType>
 struct Elem;
 template <>

@@ -22,20 +22,6 @@ namespace {
 
 constexpr int kWaves = kThreads / 64;
 
-// Inclusive sums over the wave's lanes: row shifts, then two row broadcasts.
-__device__ __forceinline__ int wave_scan(int v) {
-#define SWITCHSD_STEP(ctrl, mask) \
-    v += __builtin_amdgcn_update_dpp(0, v, ctrl, mask, 0xf, false);
-    SWITCHSD_STEP(0x111, 0xf)
-    SWITCHSD_STEP(0x112, 0xf)
-    SWITCHSD_STEP(0x114, 0xf)
-    SWITCHSD_STEP(0x118, 0xf)
-    SWITCHSD_STEP(0x142, 0xa)
-    SWITCHSD_STEP(0x143, 0xc)
-#undef SWITCHSD_STEP
-    return v;
-}
-
 // Inclusive sums over the work-group's lanes of (a, b); their totals.
 __device__ __forceinline__ void block_scan2(int &a, int &b, int &ta, int &tb,
                                             int (&sh)[2][kWaves]) {

@@ -593,21 +593,25 @@ def switchsd_span_slots(begin, end, tokens, table, held, page_size, cu, slots, p
             raise ValueError("begin must be a device tensor [B]")
         B, Lmax = begin.shape[0], int(Lmax)
     else:
-        if not isinstance(tokens, _Tensor) or tokens.dim() != 2:
-            raise ValueError("tokens must be a device tensor [B, Lmax]")
-        B, cols = tokens.shape
+        try:
+            B, cols = tokens.shape
+        except (AttributeError, ValueError):
+            raise ValueError("tokens must be a device tensor [B, Lmax]") from None
         if Lmax is not None and Lmax != cols:
             raise ValueError(f"tokens has {cols} columns, Lmax is {Lmax}")
         Lmax = cols
     one = slots if slots is not None else positions if positions is not None else \
         packed if packed is not None else seq
-    cap = (0,)
+    cap, room = (0,), 0
     if one is not None:
         # the library is told one capacity: of an output of several axes it would
         # fill no more than the first axis' length
-        if not isinstance(one, _Tensor) or one.dim() != 1:
-            raise ValueError("slots, positions, packed and seq must be device tensors [capacity]")
-        cap = one.shape
+        try:
+            cap = one.shape
+            room, = cap
+        except (AttributeError, ValueError):
+            raise ValueError("slots, positions, packed and seq must be device tensors "
+                             "[capacity]") from None
     dev = _current_device()
     most, p_table, p_held = 0, None, None
     if slots is not None:
@@ -616,7 +620,7 @@ def switchsd_span_slots(begin, end, tokens, table, held, page_size, cu, slots, p
         most = table.shape[1]
         p_table = _arr(table, "i32", "table", (B, most), dev)
         p_held = _arr(held, "i32", "held", (B,), dev)
-    page_size, room = int(page_size), cap[0]
+    page_size = int(page_size)
     if (B | Lmax | most | page_size | room) >> 31:
         _sizes(B=B, Lmax=Lmax, max_pages=most, page_size=page_size)
         room = min(room, _INT_MAX)  # no total is larger
@@ -638,11 +642,12 @@ def switchsd_compact_cache(cache, slots, dpar, dn, accept_node, stream=None):
     planes, n_slots = cache.shape[:2]
     if not cache.is_contiguous() and not cache[0].is_contiguous():
         raise ValueError("cache planes must be contiguous")
-    if not isinstance(slots, _Tensor) or slots.dim() != 2:
-        raise ValueError("slots must be a device tensor [B, R]")
+    try:
+        B, R = slots.shape
+    except (AttributeError, ValueError):
+        raise ValueError("slots must be a device tensor [B, R]") from None
     dev = _current_device()
     _here(cache, "cache", dev)
-    B, R = slots.shape
     size, numel = cache.element_size(), cache.numel()
     row = size * (numel // (planes * n_slots) if numel else 0)
     if (planes | B | R | row) >> 31:

@@ -997,13 +997,21 @@ int check_logits(const switchsd_logits_args *a) {
 // of rows of one sequence, each of which counts the history's tokens in its
 // chunk anew.  Large chunks and many rows per work-group count least often;
 // both shrink while there are too few work-groups.
+//
+// The number of chunks is a power of two, so that a token's chunk and place are
+// bits of its number.  Vocabularies that do not nearly fill the chunks leave
+// lanes without a vector, and there are up to twice the work-groups: of 128256
+// tokens 98% of the places are filled, of 100000 and 200000 76%, of 151936 58%,
+// of 131073 50%.  32 x 8 rows of bf16 with penalties and biases take 27.1, 26.1,
+// 41.6, 35.9 and 42.6 us (process: 4.9, 3.9, 4.9, 4.4, 3.2 TB/s), verified 26.2,
+// 25.9, 43.8, 43.8 and 47.2 us.
 int set_logits_grid(LogitsParams &p) {
     const switchsd_logits_args &a = p.a;
     p.penal = a.repetition || a.frequency || a.presence;
     const int64_t vecs = p.out ? kProcessBlk : kVerifyBlk;  // of a block
     const int64_t blk = vecs * (a.logits_type == SWITCHSD_F32 ? 4 : 8);
     const int64_t blocks = (a.V + blk - 1) / blk;
-    // rows of a work-group, at most: their path counts take 16 KB of LDS
+    // rows of a work-group, at most: their path counts take kPathBytes of LDS
     const int64_t most = kPathBytes / (a.R * (a.R > 256 ? 2 : 1));
     int64_t rows = a.R < kRowGroup ? a.R : kRowGroup;
     rows = rows < most ? rows : most;

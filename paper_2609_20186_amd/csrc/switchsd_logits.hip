@@ -16,7 +16,8 @@
 // (list_tokens); what a drafted token adds on each row's path is counted into a
 // table once.  Counting anew in every work-group keeps the call to one launch
 // and no scratch memory: 32 histories of 4096 tokens cost the verification of
-// 32 x 8 rows of 128256 about 3 us, biases another 1.5.
+// 32 x 8 rows of 128256 6.4 us (25.0 instead of 18.6), writing them 3.7 (26.4
+// instead of 22.7); 300 biases alone 1.3 and 0.8.
 //   k_process: vectors that hold a listed token pass through LDS, where the
 //     listed tokens are computed one per lane; all others pass as they are.
 //   k_verify: the rows' maxima are taken over the vectors without their listed
@@ -32,11 +33,14 @@
 // 128256) and 301, 269, 303 us (process, 32 x 60 rows of floats).
 //
 // Measured (MI355X), bytes that must move over time: process 32 x 8 rows of
-// 128256 bf16 27.9 us, 4.7 TB/s (a copy of that size class reaches 5.2 TB/s);
-// 32 x 60 rows of floats to bf16 under a grammar 266 us, 5.6 TB/s; verify 32 x 8
-// rows 25.5 us, 2.6 TB/s; 32 x 201 candidate rows under a grammar 206 us, 4.6
-// TB/s.  What bounds the small ones is the chain before the first row (draft
-// length, history, list) and after the last (row maxima, ticket, accept rule).
+// 128256 bf16 26.9 us, 4.9 TB/s (a large copy reaches 5.1 to 5.2 TB/s); 32 x 60
+// rows of floats to bf16 under a grammar 266 us, 5.6 TB/s (a large conversion
+// of floats to bf16: 5.85); verify 32 x 8 rows 25.2 us, 2.6 TB/s; 32 x 201
+// candidate rows under a grammar 206 us, 4.6 TB/s; one row of 32000 written 5.2
+// us, verified 9.7.  What bounds the small ones is the chain before the first
+// row (draft length, history, list) and after the last (row maxima, ticket,
+// accept rule).  Vocabularies that fill the chunks worse are slower (see where
+// the grid is set).
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 
@@ -1000,9 +1004,10 @@ constexpr uint32_t kPlaced = 0x80000000u;
 // vectors with listed tokens in LDS, wave by wave; quarters read those tokens
 // beside them (one per lane with the row's other requests).
 // kU: vectors of a piece per lane.
-// Measured, whole rows / quarters: 32 x 8 rows of 128256 26.7 / 25.5 us, 32 x 13
-// 33.7 / 32.5, 32 x 21 44.8 / 45.3, 32 x 201 candidate rows under a grammar 243 /
-// 278; whole rows from kWholeRows rows a work-group on.
+// Measured, whole rows / quarters of 128256 tokens: 128 x 2 rows 58.8 / 51.0 us,
+// 64 x 6 43.0 / 39.8, 32 x 10 28.4 / 27.8, 32 x 13 31.5 / 32.6, 32 x 16 34.8 /
+// 37.3, 32 x 32 56.8 / 62.2, 32 x 201 candidate rows under a grammar 206 / 275;
+// whole rows from kWholeRows rows a work-group on.
 constexpr int kBufs = 4;
 // Waves per SIMD the registers are kept to (floats under a mask need more of
 // them).

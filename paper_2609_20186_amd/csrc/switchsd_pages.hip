@@ -5,8 +5,12 @@
 //
 // A plan moves a few kilobytes: it is bound by its chain of dependent reads
 // (requests, sums over the sequences, pages, slots) and, with several
-// work-groups, by the ticket of the last one.  Measured (MI355X): 32 sequences
-// of 8 rows 2.7 us, 1024 trees of 60 nodes 8.7 us.  Packed slots write 20 bytes
+// work-groups, by the ticket of the last one.  Measured (MI355X), each state
+// planned once, so that pages move: 32 sequences of 8 rows 4.8 us, 32 of 201 14.2
+// us, 1024 trees of 60 nodes 9.4 us (planned again, when nothing moves: 2.7 and
+// 8.8 us for the first and the last).  Every work-group sums over all sequences
+// before its own, which grows with the square of their number: 65536 trees of
+// 60 nodes take 1.5 ms.  Packed slots write 20 bytes
 // a position: 256 prompts of up to 8192 tokens 11 us, 4.0 TB/s.  Cache rows: 16
 // x 20 rows of 1 KB in each of 32 planes moved in 6.7 us, 3.1 TB/s.
 #include <hip/hip_runtime.h>
@@ -433,7 +437,7 @@ __global__ __launch_bounds__(kThreads) void k_span_slots(SpanParams p) {
 // node j moves to is the source of no later node (nodes ascend along the path,
 // so a later source lies beyond j), and the lane itself has read it before if
 // it was an earlier one's.  kAhead rows are read before the first of them is
-// written.
+// written, what is left behind those two at a time (a path of 20: 8, 8, 2, 2).
 constexpr int kAhead = 8;
 
 template <typename Vec>

@@ -26,9 +26,11 @@
  * Synchronization), and the copy-mode labels the probe is trained on
  * (switchsd_copy_labels; Sec. 3.2).  Next to it, what an engine around the
  * step needs per step: penalties, biases and grammar masks on the logits
- * (switchsd_process_logits, switchsd_verify_processed) and the pages and slots
+ * (switchsd_process_logits, switchsd_verify_processed), the pages and slots
  * of a paged KV cache (switchsd_page_plan, switchsd_span_slots,
- * switchsd_compact_cache).
+ * switchsd_compact_cache), its contents and the target's attention over them
+ * (switchsd_store_cache, switchsd_paged_attention), and the log probabilities of
+ * what was emitted (switchsd_token_logprobs, with its gradient).
  *
  * Conventions for every entry point:
  *   - All array pointers are DEVICE pointers owned by the caller; arrays are
@@ -369,8 +371,13 @@ size_t switchsd_label_workspace_bytes(int32_t B, int32_t Lmax);
 #define SWITCHSD_MAX_HISTORY 2097151    /* longest history (2^21 - 1)              */
 #define SWITCHSD_MAX_PLAN_B 65536       /* most sequences of a plan                */
 
-/* Types of logits. */
-typedef enum { SWITCHSD_BF16 = 0, SWITCHSD_F16 = 1, SWITCHSD_F32 = 2 } switchsd_type;
+/* Types of logits, and of a cache's keys and values. */
+typedef enum {
+    SWITCHSD_BF16 = 0,
+    SWITCHSD_F16 = 1,
+    SWITCHSD_F32 = 2,
+    SWITCHSD_E4M3 = 3  /* caches only */
+} switchsd_type;
 
 /* Penalties for repeated tokens, biases and a grammar's mask on the logits of
  * the drafted rows.  Row r of sequence b is the target's output after node r,
@@ -515,6 +522,154 @@ int switchsd_compact_cache(void *cache, int32_t planes, int64_t plane_stride, in
                            int32_t row_bytes, const int64_t *slots, const int32_t *dpar,
                            const int32_t *dn, const int32_t *accept_node, int32_t B, int32_t R,
                            hipStream_t stream);
+
+/* ---- The paged KV cache's contents and the attention over them ------------ */
+
+#define SWITCHSD_MAX_TOP 64             /* most alternatives listed per row        */
+#define SWITCHSD_MAX_HEADS 256          /* most query heads                        */
+
+/* The new tokens' keys and values written to the cache slots that
+ * switchsd_page_plan or switchsd_span_slots named: for row j < n (with count: j <
+ * min(n, *count), *count being cu + B of the packed form, whose slots behind it
+ * are left over) with 0 <= slots[j] < n_slots, k_cache[slots[j], h, :] =
+ * keys[j, h, :] and v_cache[...] = values[j, h, :]; all other rows are skipped.
+ * A cache of the rows' type takes them as they are.  A SWITCHSD_E4M3 cache
+ * (8-bit floats with 4 exponent bits and a largest value of 448) takes
+ * value / k_scale[h] (v_scale[h]; NULL: 1), the quotient in 32 bits, then rounded
+ * with ties to even, magnitudes beyond 448 -- infinities too -- set to 448 and
+ * NaN kept.
+ *   keys, values: n rows of Hkv heads of D elements of `type` (SWITCHSD_BF16 or
+ *   SWITCHSD_F16), key_stride and value_stride elements apart (at least Hkv * D:
+ *   they may be parts of one projection's output); slots [n] int64, distinct where
+ *   they name a slot (of rows that share one, any or a mixture stays); count [1] int32 on
+ *   the device or NULL; k_cache, v_cache [n_slots, Hkv, D] of cache_type (`type` or
+ *   SWITCHSD_E4M3); k_scale, v_scale [Hkv] float.  D is 64, 128 or 256, 1 <= Hkv <=
+ *   SWITCHSD_MAX_HEADS; keys, values, caches and strides aligned to 16 bytes.
+ *   The rows overlap neither cache.  One launch. */
+int switchsd_store_cache(const void *keys, int64_t key_stride, const void *values,
+                         int64_t value_stride, int32_t type, const int64_t *slots, int32_t n,
+                         const int32_t *count, int32_t Hkv, int32_t D, void *k_cache,
+                         void *v_cache, int32_t cache_type, int64_t n_slots,
+                         const float *k_scale, const float *v_scale, hipStream_t stream);
+
+/* Attention of new tokens over the paged cache, their own keys and values
+ * included (stored before the call) -- the target's verification pass over the
+ * drafted rows (Sec. 3.3, Parallel Verification with Block-Triangular
+ * Attention), a single token, or chunks of prompts.  What all layers of a step
+ * share:
+ *   drafted rows (cu == NULL): sequence b's rows are b * R + i, i < n_b =
+ *     clamp(dn[b], 1, R), at the cache positions p_b + i, p_b = L - 1, L =
+ *     clamp(lengths[b], 0, Lmax), as switchsd_page_plan places them; L = 0 is a
+ *     finished sequence, without rows;
+ *   packed rows (cu != NULL): sequence b's rows are cu[b] + i, i < n_b =
+ *     cu[b+1] - cu[b] (no more than R, none where cu descends or leaves [0,
+ *     rows]), at the positions p_b + i, p_b = clamp(begin[b], 0, Lmax), as
+ *     switchsd_span_slots lists them.
+ * Position p lies in slot table[b, p / page_size] * page_size + p % page_size;
+ * where p / page_size >= clamp(held[b], 0, max_pages), or the slot is not in [0,
+ * n_slots), there is no key.  Row i sees the positions p < p_b and of the new ones
+ * p_b + j, j < n_b: with mask those whose bit j % 32 of mask[row, j / 32] is set
+ * (switchsd_tree_mask), else j <= i.
+ *   lengths, dn [B] or begin [B], cu [B + 1]; mask [rows, (R + 31) / 32] uint32 or
+ *   NULL; table [B, max_pages], held [B] int32; rows: how many rows q and out have
+ *   (drafted: B * R).  scale multiplies the products of queries and keys.
+ *   D is 64, 128 or 256; Hkv divides Hq <= SWITCHSD_MAX_HEADS; query head h reads
+ *   head h / (Hq / Hkv) of the cache.  B <= SWITCHSD_MAX_PLAN_B, R <= 2^20, Lmax <=
+ *   2^30, B * max_pages < 2^31, 1 <= page_size <= 65536. */
+typedef struct {
+    int32_t B, R, rows, Hq, Hkv, D;
+    int32_t Lmax, page_size, max_pages;
+    float scale;
+    const int32_t *lengths, *dn;
+    const int32_t *begin, *cu;
+    const uint32_t *mask;
+    const int32_t *table, *held;
+} switchsd_attention_args;
+
+/* out[row, h, :] = sum over seen positions of exp(s - lse) v, s = scale * q . k,
+ * lse[row, h] = log of the sum of exp(s).  A row that sees nothing has out = 0 and
+ * lse = -inf; rows that belong to no sequence are left as they are.  Keys and
+ * values that a row does not see do not reach it, whatever they hold (NaN and
+ * infinities too).  Products, sums and the softmax are held in 32 bits; the
+ * weights exp(s - m) are rounded to q's type for the product with the values, as
+ * out is.  A cache in SWITCHSD_E4M3 stands for its values times k_scale[h],
+ * v_scale[h] ([Hkv] float, NULL: 1).
+ *   q: `rows` rows of Hq heads of D elements of `type` (SWITCHSD_BF16 or
+ *   SWITCHSD_F16), q_stride elements apart (at least Hq * D); k_cache, v_cache
+ *   [n_slots, Hkv, D] of cache_type (`type` or SWITCHSD_E4M3); out [rows, Hq, D] of
+ *   `type`, apart from the inputs; lse [rows, Hq] float or NULL; all but lse and
+ *   the scales aligned to 16 bytes, and q_stride * 2 a multiple of 16.
+ *   attention_workspace: switchsd_attention_workspace_bytes of the same args, 256-byte
+ *   aligned, no initialization needed; calls that share one must be ordered. */
+int switchsd_paged_attention(const switchsd_attention_args *args, const void *q, int64_t q_stride,
+                             int32_t type, const void *k_cache, const void *v_cache,
+                             int32_t cache_type, int64_t n_slots, const float *k_scale,
+                             const float *v_scale, void *out, float *lse,
+                             void *attention_workspace, size_t attention_workspace_bytes,
+                             hipStream_t stream);
+
+/* Bytes of the workspace that attention of these sizes needs (only B, R, rows,
+ * Hq, Hkv and D are read; the pointers may be NULL); 0 for sizes that
+ * switchsd_paged_attention refuses. */
+size_t switchsd_attention_workspace_bytes(const switchsd_attention_args *args);
+
+/* ---- Probabilities of what was emitted ------------------------------------ */
+
+/* Log probabilities of given tokens under p = softmax(logits / temperature).
+ * Entry (b, i) reads row r of sequence b's logits:
+ *   rows (accept_node == NULL): r = i, for i < clamp(dn[b], 1, R) (dn NULL: R);
+ *   what a step emitted (accept_node != NULL): r is the i-th node of the path from
+ *   the anchor (i = 0) to accept_node[b], i <= its depth, so that tokens is the
+ *   step's out_tokens; a sequence whose accept_node is outside [0, clamp(dn[b], 1,
+ *   R)) or whose path does not lead to the anchor has no entries.  dpar [B, R]
+ *   or NULL (chains).
+ * Entries that there are not are neither read nor written.
+ *   logits [B, R, V] of logits_type, aligned to its elements, V <= 2^26, R <=
+ *   SWITCHSD_MAX_R; tokens [B, R] int32 (NULL where neither logprob nor rank is
+ *   wanted); temperature > 0 and finite.  Fewer than 2^24 entries. */
+typedef struct {
+    const void *logits;
+    int32_t logits_type; /* switchsd_type */
+    int32_t B, R, V;
+    const int32_t *tokens;
+    const int32_t *dn, *dpar, *accept_node;
+    float temperature;
+} switchsd_logprob_args;
+
+/* With z = logits / temperature of the entry's row:
+ *   lse = log of the sum of exp(z), logprob = z[token] - lse,
+ *   entropy = -sum of p log p,
+ *   rank = how many tokens are ahead of the given one: a larger logit, or the
+ *   same (-0 equals +0) and a lower index -- 0 for the greedy choice;
+ *   top_ids [B, R, n_top], top_logprobs: the n_top first tokens in that order.
+ * NaN weighs nothing, has log probability -inf and stands behind every number.  A
+ * row without a finite maximum (every value NaN or -inf, or +inf present) puts
+ * all weight on its greedy choice (the lowest index of the maximum, 0 for all
+ * NaN): its logprob is 0, that of others -inf, the entropy 0, and lse is the
+ * maximum (-inf for all NaN).  A token outside [0, V) has logprob -inf and rank -1.
+ * Sums are held in 32 bits or more.  The order of logits depends on the logits
+ * alone, not on the temperature.
+ *   logprob, lse, entropy [B, R] float, rank [B, R] int32, top_ids [B, R, n_top]
+ *   int32, top_logprobs float, each NULL if not wanted; 0 <= n_top <= min(V,
+ *   SWITCHSD_MAX_TOP), 0 iff both top outputs are NULL.  One launch. */
+int switchsd_token_logprobs(const switchsd_logprob_args *args, float *logprob, float *lse,
+                            float *entropy, int32_t *rank, int32_t n_top, int32_t *top_ids,
+                            float *top_logprobs, hipStream_t stream);
+
+/* The gradient of sum g_logprob * logprob + g_entropy * entropy with respect to the
+ * logits, for the entries' rows: with p = exp(z - lse),
+ *   grad[v] = (g_logprob * ((v == token) - p[v])
+ *              - g_entropy * p[v] * (log p[v] + entropy)) / temperature,
+ * a weight p of 0 adding nothing to either product.  lse and entropy [B, R] are what
+ * switchsd_token_logprobs gave for the same logits.  A NaN logit has p = 0.  A row
+ * whose lse is not finite (no finite maximum) has the gradient 0.
+ *   lse [B, R] float; g_logprob [B, R] float or NULL; g_entropy [B, R] float or
+ *   NULL, with entropy [B, R]; tokens may be NULL without g_logprob; grad [B, R, V]
+ *   of logits_type, rounded once: apart from the logits or the logits themselves.
+ *   Rows without an entry are neither read nor written.  One launch. */
+int switchsd_token_logprobs_grad(const switchsd_logprob_args *args, const float *lse,
+                                 const float *entropy, const float *g_logprob,
+                                 const float *g_entropy, void *grad, hipStream_t stream);
 
 /* Workspace bytes needed by calls with B sequences of R rows, contexts of up
  * to Lmax tokens and n_cand copy candidates (pass 0 for what a call does not

@@ -20,7 +20,8 @@ MAX_CAND = 16
 MAX_BIAS = 511
 MAX_HISTORY = 2 ** 21 - 1
 MODE_AUTO, MODE_FUSED, MODE_SPLIT = 0, 1, 2
-BF16, F16, F32 = 0, 1, 2
+BF16, F16, F32, E4M3 = 0, 1, 2, 3
+MAX_TOP = 64
 
 STATUS = {0: "OK", -1: "EINVAL", -2: "ESHAPE", -3: "EHIP", -4: "EWORKSPACE", -5: "EDEVICE",
           -6: "ESCRATCH"}
@@ -31,7 +32,9 @@ EXPORTS = ("switchsd_ngram_match", "switchsd_probe_score", "switchsd_select_draf
            "switchsd_workspace_bytes", "switchsd_sample_workspace_bytes",
            "switchsd_label_workspace_bytes", "switchsd_workspace_status", "switchsd_step_noalloc",
            "switchsd_process_logits", "switchsd_verify_processed", "switchsd_page_plan",
-           "switchsd_span_slots", "switchsd_compact_cache",
+           "switchsd_span_slots", "switchsd_compact_cache", "switchsd_store_cache",
+           "switchsd_paged_attention", "switchsd_attention_workspace_bytes",
+           "switchsd_token_logprobs", "switchsd_token_logprobs_grad",
            "switchsd_test_withhold_probe_flag", "switchsd_test_withhold_segment",
            "switchsd_status_string")
 
@@ -98,6 +101,19 @@ class PageArgs(ctypes.Structure):
                 ("ring_state", _P), ("slots", _P), ("positions", _P), ("missing", _P)]
 
 
+class AttentionArgs(ctypes.Structure):
+    _fields_ = [("B", _I), ("R", _I), ("rows", _I), ("Hq", _I), ("Hkv", _I), ("D", _I),
+                ("Lmax", _I), ("page_size", _I), ("max_pages", _I), ("scale", ctypes.c_float),
+                ("lengths", _P), ("dn", _P), ("begin", _P), ("cu", _P), ("mask", _P),
+                ("table", _P), ("held", _P)]
+
+
+class LogprobArgs(ctypes.Structure):
+    _fields_ = [("logits", _P), ("logits_type", _I), ("B", _I), ("R", _I), ("V", _I),
+                ("tokens", _P), ("dn", _P), ("dpar", _P), ("accept_node", _P),
+                ("temperature", ctypes.c_float)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run `python -m paper_2609_20186_amd.build`")
@@ -132,6 +148,17 @@ def _load():
                                         _I, _P]
     lib.switchsd_compact_cache.argtypes = [_P, _I, ctypes.c_int64, ctypes.c_int64, _I, _P, _P,
                                            _P, _P, _I, _I, _P]
+    L = ctypes.c_int64
+    lib.switchsd_store_cache.argtypes = [_P, L, _P, L, _I, _P, _I, _P, _I, _I, _P, _P, _I, L, _P,
+                                         _P, _P]
+    lib.switchsd_paged_attention.argtypes = [ctypes.POINTER(AttentionArgs), _P, L, _I, _P, _P, _I,
+                                             L, _P, _P, _P, _P, _P, S, _P]
+    lib.switchsd_attention_workspace_bytes.argtypes = [ctypes.POINTER(AttentionArgs)]
+    lib.switchsd_attention_workspace_bytes.restype = S
+    lib.switchsd_token_logprobs.argtypes = [ctypes.POINTER(LogprobArgs), _P, _P, _P, _P, _I, _P,
+                                            _P, _P]
+    lib.switchsd_token_logprobs_grad.argtypes = [ctypes.POINTER(LogprobArgs), _P, _P, _P, _P, _P,
+                                                 _P]
     for knob in ("switchsd_test_withhold_probe_flag", "switchsd_test_withhold_segment"):
         getattr(lib, knob).argtypes = [_I]
         getattr(lib, knob).restype = None
@@ -657,3 +684,206 @@ def switchsd_compact_cache(cache, slots, dpar, dn, accept_node, stream=None):
         _arr(slots, "i64", "slots", (B, R), dev), _arr(dpar, "i32", "dpar", (B, R), dev, True),
         _arr(dn, "i32", "dn", (B,), dev), _arr(accept_node, "i32", "accept_node", (B,), dev), B, R,
         _stream(stream)))
+
+
+# ------------------------------------------------------------------ attention over the paged cache
+
+_HALF = {torch.bfloat16: BF16, torch.float16: F16}
+_CACHES = dict(_HALF)
+_CACHES[torch.float8_e4m3fn] = E4M3
+_DT["cache"] = tuple(_CACHES)
+_DT["half"] = tuple(_HALF)
+
+
+def _rows(t, name, dev, heads=None):
+    """Shape, row stride and device pointer of [rows, heads, D] elements whose rows
+    may lie apart (parts of one projection's output)."""
+    if not isinstance(t, _Tensor) or not t.is_cuda or t.dim() != 3:
+        raise ValueError(f"{name} must be a device tensor [rows, heads, D]")
+    if t.dtype not in _HALF:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected one of {_DT['half']}")
+    if t.get_device() != dev:
+        _here(t, name, dev)
+    n, H, D = shape = t.shape
+    if heads is not None and shape != heads:
+        raise ValueError(f"{name} has shape {tuple(shape)}, expected {tuple(heads)}")
+    row, head, one = t.stride()
+    if (one != 1 and D > 1) or (head != D and H > 1):
+        raise ValueError(f"the heads of {name} must be contiguous")
+    return shape, row if n > 1 else max(row, H * D), t.data_ptr()
+
+
+def _caches(k_cache, v_cache, dtype, Hkv, D, k_scale, v_scale, dev):
+    """Type, slots and pointers of a pair of cache planes."""
+    if not isinstance(k_cache, _Tensor) or k_cache.dim() != 3:
+        raise ValueError("k_cache must be a device tensor [n_slots, Hkv, D]")
+    n = k_cache.shape[0]
+    kind = k_cache.dtype
+    ptrs = (_arr(k_cache, "cache", "k_cache", (n, Hkv, D), dev),
+            _arr(v_cache, "cache", "v_cache", (n, Hkv, D), dev))
+    if v_cache.dtype != kind or (kind != dtype and _CACHES[kind] != E4M3):
+        raise ValueError(f"caches of {kind} and {v_cache.dtype} for rows of {dtype}")
+    return _CACHES[kind], n, ptrs, (
+        None if k_scale is None else _arr(k_scale, "f32", "k_scale", (Hkv,), dev),
+        None if v_scale is None else _arr(v_scale, "f32", "v_scale", (Hkv,), dev))
+
+
+def switchsd_store_cache(keys, values, slots, k_cache, v_cache, count=None, k_scale=None,
+                         v_scale=None, stream=None):
+    """keys, values [n, Hkv, D] (bf16 or fp16; rows may lie apart) into the slots
+    [n] int64 (any shape of n elements) of k_cache, v_cache [n_slots, Hkv, D] (the same
+    type, or float8_e4m3fn with k_scale, v_scale [Hkv] float or None); count: how many
+    of the rows there are, [1] int32 on the device (None: all)."""
+    dev = _current_device()
+    shape, k_stride, p_k = _rows(keys, "keys", dev)
+    n, Hkv, D = shape
+    _, v_stride, p_v = _rows(values, "values", dev, shape)
+    if values.dtype != keys.dtype:
+        raise ValueError(f"keys have dtype {keys.dtype}, values {values.dtype}")
+    if not isinstance(slots, _Tensor) or slots.numel() != n:
+        raise ValueError(f"slots must be a device tensor of {n} elements")
+    _sizes(n=n, Hkv=Hkv, D=D)
+    kind, n_slots, (p_kc, p_vc), (p_ks, p_vs) = _caches(k_cache, v_cache, keys.dtype, Hkv, D,
+                                                        k_scale, v_scale, dev)
+    _check("switchsd_store_cache", lib.switchsd_store_cache(
+        p_k, k_stride, p_v, v_stride, _HALF[keys.dtype], _arr(slots, "i64", "slots", slots.shape,
+                                                              dev), n,
+        None if count is None else _arr(count, "i32", "count", (1,), dev), Hkv, D, p_kc, p_vc,
+        kind, n_slots, p_ks, p_vs, _stream(stream)))
+
+
+def build_attention_args(rows, R, Hq, Hkv, D, page_size, table, held, Lmax, lengths=None, dn=None,
+                         begin=None, cu=None, mask=None, scale=None):
+    """AttentionArgs for switchsd_paged_attention, the same for all layers of a
+    step: table [B, max_pages] and held [B] int32, and either the drafted rows'
+    lengths and dn [B] (rows = B * R) or the packed rows' begin [B] and cu [B + 1]
+    (R: the most rows of a sequence).  mask: uint32 (or int32) [rows, (R + 31) // 32]
+    (or [B, R, ...]) of the new positions each row sees, None: its own and earlier
+    ones.  scale: default 1 / sqrt(D).  The tensors are kept alive by the result."""
+    if not isinstance(table, _Tensor) or table.dim() != 2:
+        raise ValueError("table must be a device tensor [B, max_pages]")
+    B, most = table.shape
+    rows, R, Hq, Hkv, D = int(rows), int(R), int(Hq), int(Hkv), int(D)
+    page_size, Lmax = int(page_size), int(Lmax)
+    _sizes(B=B, rows=rows, R=R, Hq=Hq, Hkv=Hkv, D=D, Lmax=Lmax, page_size=page_size,
+           max_pages=most)
+    dev = _current_device()
+    a = AttentionArgs()
+    a.B, a.R, a.rows, a.Hq, a.Hkv, a.D = B, R, rows, Hq, Hkv, D
+    a.Lmax, a.page_size, a.max_pages = Lmax, page_size, most
+    a.scale = D ** -0.5 if scale is None else float(scale)
+    a.table = _arr(table, "i32", "table", (B, most), dev)
+    a.held = _arr(held, "i32", "held", (B,), dev)
+    if (cu is None) != (begin is None) or (cu is None) == (lengths is None) or \
+            (lengths is None) != (dn is None):
+        raise ValueError("either lengths and dn, or begin and cu")
+    if cu is None:
+        a.lengths = _arr(lengths, "i32", "lengths", (B,), dev)
+        a.dn = _arr(dn, "i32", "dn", (B,), dev)
+    else:
+        a.begin = _arr(begin, "i32", "begin", (B,), dev)
+        a.cu = _arr(cu, "i32", "cu", (B + 1,), dev)
+    if mask is not None:
+        words = (R + 31) // 32
+        a.mask = _arr(mask, "u32", "mask", (B, R, words) if isinstance(mask, _Tensor) and
+                      mask.dim() == 3 and rows == B * R else (rows, words), dev)
+    a.shape, a.device = (rows, Hq, D), dev
+    a.keep = (table, held, lengths, dn, begin, cu, mask)
+    return a
+
+
+def attention_workspace_bytes(args):
+    return int(lib.switchsd_attention_workspace_bytes(ctypes.byref(args)))
+
+
+def alloc_attention_workspace(args, device="cuda"):
+    return torch.empty(max(attention_workspace_bytes(args), 256), dtype=torch.uint8,
+                       device=device)
+
+
+def switchsd_paged_attention(args, q, k_cache, v_cache, out, workspace, lse=None, k_scale=None,
+                             v_scale=None, stream=None):
+    """q [rows, Hq, D] (bf16 or fp16; rows may lie apart) over k_cache, v_cache
+    [n_slots, Hkv, D] (the same type, or float8_e4m3fn with k_scale, v_scale [Hkv] float
+    or None) into out [rows, Hq, D] and lse [rows, Hq] float (None: not wanted)."""
+    dev = _args_here(args)
+    shape, q_stride, p_q = _rows(q, "q", dev, args.shape)
+    kind, n_slots, (p_kc, p_vc), (p_ks, p_vs) = _caches(k_cache, v_cache, q.dtype, args.Hkv,
+                                                        args.D, k_scale, v_scale, dev)
+    p_out = _arr(out, "half", "out", shape, dev)
+    if out.dtype != q.dtype:
+        raise ValueError(f"out has dtype {out.dtype}, q {q.dtype}")
+    p_workspace = _workspace(workspace, dev)
+    _check("switchsd_paged_attention", lib.switchsd_paged_attention(
+        ctypes.byref(args), p_q, q_stride, _HALF[q.dtype], p_kc, p_vc, kind, n_slots, p_ks, p_vs,
+        p_out, None if lse is None else _arr(lse, "f32", "lse", shape[:2], dev), p_workspace,
+        workspace.numel(), _stream(stream)))
+
+
+# ------------------------------------------------------------------ log probabilities
+
+def build_logprob_args(logits, tokens=None, dn=None, dpar=None, accept_node=None,
+                       temperature=1.0):
+    """LogprobArgs for switchsd_token_logprobs and its gradient: logits [B, R, V]
+    (bf16 or its bits, fp16 or fp32), tokens [B, R] int32 (None where neither logprob
+    nor rank is wanted), dn [B] (None: all rows); with accept_node [B], and dpar [B, R]
+    (None: chains), the rows along each accepted path, tokens being the step's
+    out_tokens.  The tensors are kept alive by the result."""
+    if not isinstance(logits, _Tensor) or logits.dim() != 3:
+        raise ValueError("logits must be a device tensor [B, R, V]")
+    B, R, V = logits.shape
+    _sizes(B=B, R=R, V=V)
+    if dpar is not None and accept_node is None:
+        raise ValueError("dpar comes with accept_node")
+    dev = _current_device()
+    a = LogprobArgs()
+    a.logits = _arr(logits, "logits", "logits", (B, R, V), dev)
+    a.logits_type = _TYPES[logits.dtype]
+    a.B, a.R, a.V = B, R, V
+    a.tokens = _arr(tokens, "i32", "tokens", (B, R), dev, True)
+    a.dn = _arr(dn, "i32", "dn", (B,), dev, True)
+    a.dpar = _arr(dpar, "i32", "dpar", (B, R), dev, True)
+    a.accept_node = _arr(accept_node, "i32", "accept_node", (B,), dev, True)
+    a.temperature = float(temperature)
+    a.shape, a.device = (B, R, V), dev
+    a.keep = (logits, tokens, dn, dpar, accept_node)
+    return a
+
+
+def switchsd_token_logprobs(args, logprob=None, lse=None, entropy=None, rank=None, top_ids=None,
+                            top_logprobs=None, stream=None):
+    """logprob, lse, entropy [B, R] float, rank [B, R] int32, top_ids int32 and
+    top_logprobs float [B, R, n_top], each None if not wanted."""
+    dev = _args_here(args)
+    shape = args.shape[:2]
+    n_top = 0
+    one = top_ids if top_ids is not None else top_logprobs
+    if one is not None:
+        if not isinstance(one, _Tensor) or one.dim() != 3:
+            raise ValueError("top_ids and top_logprobs must be device tensors [B, R, n_top]")
+        n_top = one.shape[2]
+        _sizes(n_top=n_top)
+    top = (*shape, n_top)
+    _check("switchsd_token_logprobs", lib.switchsd_token_logprobs(
+        ctypes.byref(args), _arr(logprob, "f32", "logprob", shape, dev, True),
+        _arr(lse, "f32", "lse", shape, dev, True), _arr(entropy, "f32", "entropy", shape, dev, True),
+        _arr(rank, "i32", "rank", shape, dev, True), n_top,
+        _arr(top_ids, "i32", "top_ids", top, dev, True),
+        _arr(top_logprobs, "f32", "top_logprobs", top, dev, True), _stream(stream)))
+
+
+def switchsd_token_logprobs_grad(args, lse, entropy, g_logprob, g_entropy, grad, stream=None):
+    """grad [B, R, V] of the logits' type (the logits themselves: in place) from lse
+    and entropy [B, R] of switchsd_token_logprobs and the loss's gradients g_logprob,
+    g_entropy [B, R] float (one of the two may be None; entropy is needed with
+    g_entropy)."""
+    dev = _args_here(args)
+    shape = args.shape[:2]
+    p_grad = _arr(grad, "logits", "grad", args.shape, dev)
+    if _TYPES[grad.dtype] != args.logits_type:
+        raise ValueError(f"grad has dtype {grad.dtype}, the logits another")
+    _check("switchsd_token_logprobs_grad", lib.switchsd_token_logprobs_grad(
+        ctypes.byref(args), _arr(lse, "f32", "lse", shape, dev),
+        _arr(entropy, "f32", "entropy", shape, dev, True),
+        _arr(g_logprob, "f32", "g_logprob", shape, dev, True),
+        _arr(g_entropy, "f32", "g_entropy", shape, dev, True), p_grad, _stream(stream)))

@@ -8,6 +8,7 @@ them into ``paper_2609_20186_amd/libswitchsd.so``.
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -25,7 +26,12 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-Wall",
 # packed fp32 VALU ops stay disabled in every device compile
 DEVICE = ["--offload-arch=" + ARCH, "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 SOURCES = ["switchsd_kernels.hip", "switchsd_noalloc.hip", "switchsd_logits.hip",
-           "switchsd_pages.hip", "switchsd_api.cpp"]
+           "switchsd_pages.hip", "switchsd_attention.hip", "switchsd_logprobs.hip",
+           "switchsd_api.cpp"]
+# what has no phase stamps is compiled once for both libraries
+UNSTAMPED = ["switchsd_attention.hip", "switchsd_logprobs.hip"]
+# sources compiled at once
+JOBS = max(1, min(4, os.cpu_count() or 1))
 
 
 def _run(cmd, verbose):
@@ -49,14 +55,16 @@ def _link(objs, lib, verbose):
 def _compile(sources, subdir, defines, verbose):
     out = os.path.join(BUILD, subdir)
     os.makedirs(out, exist_ok=True)
-    objs = []
-    for src in sources:
+
+    def one(src):
         obj = os.path.join(out, src + ".o")
         lang = ["-x", "hip"] if src.endswith(".hip") else []
         _run([HIPCC] + COMMON + defines + DEVICE + lang + ["-c", os.path.join(CSRC, src), "-o", obj],
              verbose)
-        objs.append(obj)
-    return objs
+        return obj
+
+    with ThreadPoolExecutor(JOBS) as pool:
+        return list(pool.map(one, sources))
 
 
 def build(verbose=False):
@@ -64,8 +72,11 @@ def build(verbose=False):
     with per-work-group phase stamps (libswitchsd_timeline.so, used only by
     ``timeline.py``) and the streaming-read calibration kernel
     (libswitchsd_calibrate.so, used only by ``bench.py``)."""
-    _link(_compile(SOURCES, "product", [], verbose), LIB, verbose)
-    _link(_compile(SOURCES, "timeline", ["-DSWITCHSD_TIMELINE"], verbose), TIMELINE_LIB, verbose)
+    objs = _compile(SOURCES, "product", [], verbose)
+    _link(objs, LIB, verbose)
+    stamped = [src for src in SOURCES if src not in UNSTAMPED]
+    _link(_compile(stamped, "timeline", ["-DSWITCHSD_TIMELINE"], verbose) +
+          [obj for src, obj in zip(SOURCES, objs) if src in UNSTAMPED], TIMELINE_LIB, verbose)
     _link(_compile(["read_calibration.hip"], "calibrate", [], verbose), CALIBRATE_LIB, verbose)
     return LIB
 

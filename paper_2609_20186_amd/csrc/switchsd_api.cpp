@@ -1236,3 +1236,197 @@ int switchsd_compact_cache(void *cache, int32_t planes, int64_t plane_stride, in
 }
 
 }  // extern "C"
+
+// ---- attention over the paged cache
+
+namespace {
+
+bool head_dim_ok(int32_t D) { return D == 64 || D == 128 || D == 256; }
+
+bool half_type(int32_t type) { return type == SWITCHSD_BF16 || type == SWITCHSD_F16; }
+
+int check_attention_shape(const switchsd_attention_args *a) {
+    if (a->B < 0 || a->B > SWITCHSD_MAX_PLAN_B || a->R < 1 || a->R > (1 << 20) || a->rows < 0 ||
+        a->Hkv < 1 || a->Hq < a->Hkv || a->Hq > SWITCHSD_MAX_HEADS || a->Hq % a->Hkv != 0 ||
+        !head_dim_ok(a->D))
+        return SWITCHSD_ESHAPE;
+    return SWITCHSD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int switchsd_store_cache(const void *keys, int64_t key_stride, const void *values,
+                         int64_t value_stride, int32_t type, const int64_t *slots, int32_t n,
+                         const int32_t *count, int32_t Hkv, int32_t D, void *k_cache,
+                         void *v_cache, int32_t cache_type, int64_t n_slots,
+                         const float *k_scale, const float *v_scale, hipStream_t stream) {
+    if (!half_type(type) || (cache_type != type && cache_type != SWITCHSD_E4M3))
+        return SWITCHSD_EINVAL;
+    if (n < 0 || Hkv < 1 || Hkv > SWITCHSD_MAX_HEADS || !head_dim_ok(D) || n_slots < 0 ||
+        n_slots > (1ll << 40) || key_stride < (int64_t)Hkv * D ||
+        value_stride < (int64_t)Hkv * D || key_stride > (1ll << 32) ||
+        value_stride > (1ll << 32))
+        return SWITCHSD_ESHAPE;
+    if (key_stride % 8 != 0 || value_stride % 8 != 0)
+        return SWITCHSD_EINVAL;
+    if (n == 0 || n_slots == 0)
+        return SWITCHSD_OK;
+    if (!keys || !values || !slots || !k_cache || !v_cache || !aligned(keys, 16) ||
+        !aligned(values, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) ||
+        !aligned(slots, 8))
+        return SWITCHSD_EINVAL;
+    if (cache_type != SWITCHSD_E4M3 && (k_scale || v_scale))
+        return SWITCHSD_EINVAL;
+    StoreParams p;
+    memset(&p, 0, sizeof p);
+    p.k = keys;
+    p.v = values;
+    p.k_stride = key_stride * 2;
+    p.v_stride = value_stride * 2;
+    p.slots = slots;
+    p.count = count;
+    p.n = n;
+    p.Hkv = Hkv;
+    p.D = D;
+    p.k_cache = k_cache;
+    p.v_cache = v_cache;
+    p.n_slots = n_slots;
+    p.k_scale = k_scale;
+    p.v_scale = v_scale;
+    return launch_store_kernel(p, type, cache_type, stream);
+}
+
+size_t switchsd_attention_workspace_bytes(const switchsd_attention_args *a) {
+    if (!a || check_attention_shape(a))
+        return 0;
+    return attention_part_floats(a->R * (int64_t)(a->Hq / a->Hkv), a->D) * sizeof(float);
+}
+
+int switchsd_paged_attention(const switchsd_attention_args *a, const void *q, int64_t q_stride,
+                             int32_t type, const void *k_cache, const void *v_cache,
+                             int32_t cache_type, int64_t n_slots, const float *k_scale,
+                             const float *v_scale, void *out, float *lse,
+                             void *attention_workspace, size_t attention_workspace_bytes,
+                             hipStream_t stream) {
+    if (!a || !half_type(type) || (cache_type != type && cache_type != SWITCHSD_E4M3))
+        return SWITCHSD_EINVAL;
+    int rc = check_attention_shape(a);
+    if (rc)
+        return rc;
+    if (a->Lmax < 1 || a->Lmax > (1 << 30) || a->page_size < 1 || a->page_size > 65536 ||
+        a->max_pages < 1 || (int64_t)a->B * a->max_pages > 0x7FFFFFFFll || n_slots < 0 ||
+        n_slots > (1ll << 40) || q_stride < (int64_t)a->Hq * a->D || q_stride > (1ll << 32) ||
+        (!a->cu && a->rows != (int64_t)a->B * a->R))
+        return SWITCHSD_ESHAPE;
+    if (q_stride % 8 != 0 || !(a->scale > -INFINITY && a->scale < INFINITY))
+        return SWITCHSD_EINVAL;
+    if (cache_type != SWITCHSD_E4M3 && (k_scale || v_scale))
+        return SWITCHSD_EINVAL;
+    if (a->B == 0 || a->rows == 0)
+        return SWITCHSD_OK;
+    if (!q || !out || !a->table || !a->held || (n_slots > 0 && (!k_cache || !v_cache)) ||
+        (a->cu ? !a->begin : !a->lengths || !a->dn) || !aligned(q, 16) || !aligned(out, 16) ||
+        !aligned(k_cache, 16) || !aligned(v_cache, 16))
+        return SWITCHSD_EINVAL;
+    if (!attention_workspace || !aligned(attention_workspace, kAlign) ||
+        attention_workspace_bytes < switchsd_attention_workspace_bytes(a))
+        return SWITCHSD_EWORKSPACE;
+    AttnParams p;
+    memset(&p, 0, sizeof p);
+    p.a = *a;
+    p.q = q;
+    p.q_stride = q_stride;
+    p.k_cache = k_cache;
+    p.v_cache = v_cache;
+    p.n_slots = n_slots;
+    p.k_scale = k_scale;
+    p.v_scale = v_scale;
+    p.out = out;
+    p.lse = lse;
+    p.part = (float *)attention_workspace;
+    p.G = a->Hq / a->Hkv;
+    return launch_attention_kernel(p, type, cache_type, stream);
+}
+
+}  // extern "C"
+
+// ---- log probabilities
+
+namespace {
+
+int check_logprobs(const switchsd_logprob_args *a) {
+    if (!a || a->logits_type < SWITCHSD_BF16 || a->logits_type > SWITCHSD_F32 ||
+        !(a->temperature > 0.0f && a->temperature < INFINITY) ||
+        !(1.0f / a->temperature < INFINITY))
+        return SWITCHSD_EINVAL;
+    if (!shape_ok_B(a->B) || a->R < 1 || a->R > SWITCHSD_MAX_R || a->V < 1 || a->V > (1 << 26) ||
+        (a->B > 0 && !launch_ok((int64_t)a->B * a->R)))
+        return SWITCHSD_ESHAPE;
+    if (a->B > 0 && (!a->logits || !aligned(a->logits, type_size(a->logits_type))))
+        return SWITCHSD_EINVAL;
+    return SWITCHSD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int switchsd_token_logprobs(const switchsd_logprob_args *a, float *logprob, float *lse,
+                            float *entropy, int32_t *rank, int32_t n_top, int32_t *top_ids,
+                            float *top_logprobs, hipStream_t stream) {
+    const int rc = check_logprobs(a);
+    if (rc)
+        return rc;
+    if (n_top < 0 || n_top > SWITCHSD_MAX_TOP || n_top > a->V)
+        return SWITCHSD_ESHAPE;
+    if ((n_top > 0) != (top_ids || top_logprobs))
+        return SWITCHSD_EINVAL;
+    if (a->B == 0)
+        return SWITCHSD_OK;
+    if ((logprob || rank) && !a->tokens)
+        return SWITCHSD_EINVAL;
+    if (!logprob && !lse && !entropy && !rank && n_top == 0)
+        return SWITCHSD_EINVAL;
+    LogprobParams p;
+    memset(&p, 0, sizeof p);
+    p.a = *a;
+    p.inv_t = 1.0f / a->temperature;
+    p.logprob = logprob;
+    p.lse = lse;
+    p.entropy = entropy;
+    p.rank = rank;
+    p.n_top = n_top;
+    p.top_ids = top_ids;
+    p.top_logprobs = top_logprobs;
+    return launch_logprob_kernel(p, stream);
+}
+
+int switchsd_token_logprobs_grad(const switchsd_logprob_args *a, const float *lse,
+                                 const float *entropy, const float *g_logprob,
+                                 const float *g_entropy, void *grad, hipStream_t stream) {
+    const int rc = check_logprobs(a);
+    if (rc || a->B == 0)
+        return rc;
+    if (!lse || !grad || !aligned(grad, type_size(a->logits_type)) || (!g_logprob && !g_entropy) ||
+        (g_logprob && !a->tokens) || (g_entropy && !entropy))
+        return SWITCHSD_EINVAL;
+    // grad is the logits themselves, or apart from them
+    const uint64_t n = (uint64_t)a->B * a->R * a->V * type_size(a->logits_type);
+    const uintptr_t i0 = (uintptr_t)a->logits, o0 = (uintptr_t)grad;
+    if (i0 != o0 && o0 < i0 + n && i0 < o0 + n)
+        return SWITCHSD_EINVAL;
+    LogprobParams p;
+    memset(&p, 0, sizeof p);
+    p.a = *a;
+    p.inv_t = 1.0f / a->temperature;
+    p.in_lse = lse;
+    p.in_entropy = entropy;
+    p.g_logprob = g_logprob;
+    p.g_entropy = g_entropy;
+    p.grad = grad;
+    return launch_logprob_grad_kernel(p, stream);
+}
+
+}  // extern "C"

@@ -270,6 +270,63 @@ struct CompactParams {
     int32_t blocks;      // work-groups per sequence
 };
 
+// ---- attention over the paged cache (switchsd_attention.hip)
+
+struct StoreParams {
+    const void *k, *v;
+    int64_t k_stride, v_stride;  // bytes
+    const int64_t *slots;
+    const int32_t *count;
+    int32_t n, Hkv, D;
+    void *k_cache, *v_cache;
+    int64_t n_slots;
+    const float *k_scale, *v_scale;
+};
+
+struct AttnParams {
+    switchsd_attention_args a;
+    const void *q;
+    int64_t q_stride;  // elements
+    const void *k_cache, *v_cache;
+    int64_t n_slots;
+    const float *k_scale, *v_scale;
+    void *out;
+    float *lse;
+    float *part;       // partial results
+    int32_t G;         // query heads per head of the cache
+};
+
+// Floats of the partial results: each of kAttnGroups work-groups leaves at most
+// two, of as many rows as a work-group takes, D sums, a maximum and a sum each.
+constexpr int kAttnGroups = 512;
+constexpr int attention_tile(int64_t most) { return most <= 32 ? 32 : most <= 64 ? 64 : 128; }
+constexpr size_t attention_part_floats(int64_t most, int32_t D) {
+    return (size_t)2 * kAttnGroups * attention_tile(most) * (D + 2);
+}
+
+int launch_store_kernel(const StoreParams &p, int32_t type, int32_t cache_type,
+                        hipStream_t stream);
+int launch_attention_kernel(const AttnParams &p, int32_t type, int32_t cache_type,
+                            hipStream_t stream);
+
+// ---- log probabilities (switchsd_logprobs.hip)
+
+struct LogprobParams {
+    switchsd_logprob_args a;
+    float inv_t;  // 1 / temperature
+    float *logprob, *lse, *entropy;
+    int32_t *rank;
+    int32_t n_top;
+    int32_t *top_ids;
+    float *top_logprobs;
+    // gradient
+    const float *in_lse, *in_entropy, *g_logprob, *g_entropy;
+    void *grad;
+};
+
+int launch_logprob_kernel(const LogprobParams &p, hipStream_t stream);
+int launch_logprob_grad_kernel(const LogprobParams &p, hipStream_t stream);
+
 int launch_logits_kernel(const LogitsParams &p, int32_t out_type, hipStream_t stream);
 int launch_page_plan_kernel(const PageParams &p, hipStream_t stream);
 int launch_span_kernel(const SpanParams &p, hipStream_t stream);

@@ -1347,6 +1347,7 @@ int switchsd_paged_attention(const switchsd_attention_args *a, const void *q, in
     p.lse = lse;
     p.part = (float *)attention_workspace;
     p.G = a->Hq / a->Hkv;
+    p.page_log = log_of(a->page_size);
     return launch_attention_kernel(p, type, cache_type, stream);
 }
 

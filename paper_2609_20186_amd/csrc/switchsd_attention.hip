@@ -82,6 +82,8 @@ __global__ void __launch_bounds__(kThreads) k_store(const StoreParams p) {
 
 // ---- attention
 
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
 // A sequence's new rows: how many, the row of the first in q and out, and its
 // cache position.
 struct Chunk {
@@ -111,79 +113,918 @@ __device__ __forceinline__ float cached(const void *base, int64_t at) {
     return to_f32<TYPE>(((const uint16_t *)base)[at]);
 }
 
-// A wave per row and query head, a key per lane.
-template <int TYPE, bool E4M3, int D>
-__global__ void __launch_bounds__(64) k_attend(const AttnParams p) {
-    const switchsd_attention_args &a = p.a;
-    __shared__ float sq[D];
-    const int lane = threadIdx.x;
-    int64_t id = blockIdx.x;
-    const int h = id % a.Hq;
-    id /= a.Hq;
-    const int i = id % a.R, b = id / a.R;
-    const Chunk c = chunk_of(a, b);
-    if (i >= c.n)
-        return;
-    const int hk = h / p.G;
-    const int64_t row = c.row + i;
-    const uint16_t *q = (const uint16_t *)p.q + row * p.q_stride + (int64_t)h * D;
-    for (int d = lane; d < D; d += 64)
-        sq[d] = to_f32<TYPE>(q[d]);
+// The work of a launch, cut on the device: items are (sequence, tile of query
+// rows, head of the cache), an item's keys are cut into units, and what a
+// work-group takes is found by the sums over all sequences of what comes before it.
+// With many items each work-group takes one whole; with few, kAttnGroups
+// work-groups take equal shares of all units, in order, and k_merge joins what
+// was cut.
+struct Work {
+    int64_t items, units;  // of all sequences
+    int whole;             // one item for each work-group
+    int groups;            // work-groups that have work
+};
+
+// What sequence b has: tiles of query rows and units of keys (1 at least, so that
+// every row is written).
+struct Share {
+    int tiles, units;
+};
+__device__ __forceinline__ int keys_of(const AttnParams &p, const Chunk &c, int b) {
+    const int held = clampi(p.a.held[b], 0, p.a.max_pages);
+    const int64_t end = (int64_t)c.pos + c.n, most = (int64_t)held * p.a.page_size;
+    return p.n_slots == 0 ? 0 : (int)(end < most ? end : most);
+}
+template <int TILE, int UNIT>
+__device__ __forceinline__ Share share_of(const AttnParams &p, int b) {
+    const Chunk c = chunk_of(p.a, b);
+    Share s;
+    s.tiles = (int)(((int64_t)c.n * p.G + TILE - 1) / TILE);
+    const int keys = keys_of(p, c, b);
+    s.units = keys > UNIT ? (keys + UNIT - 1) / UNIT : 1;
+    return s;
+}
+
+__device__ __forceinline__ int64_t shfl_up64(int64_t v, int d) { return __shfl_up(v, d); }
+
+struct PlanShared {
+    int64_t sums[2][kThreads / 64];
+    int64_t off;
+    int b;
+};
+
+// Total work; then, for work-group `group` (of items in the merge), the sequence
+// that its first unit (item) lies in and how many come before it there.
+template <int TILE, int UNIT>
+__device__ __forceinline__ Work plan(const AttnParams &p, int64_t group, bool by_item,
+                                     PlanShared &sh, int &b_out, int64_t &off_out) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int per = (p.a.B + kThreads - 1) / kThreads;
+    const int b0 = tid * per, b1 = b0 + per < p.a.B ? b0 + per : p.a.B;
+    int64_t items = 0, units = 0;
+    for (int b = b0; b < b1; ++b) {
+        const Share s = share_of<TILE, UNIT>(p, b);
+        items += (int64_t)s.tiles * p.a.Hkv;
+        units += (int64_t)s.tiles * p.a.Hkv * s.units;
+    }
+    int64_t pi = items, pu = units;  // inclusive sums over the lanes
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t x = shfl_up64(pi, d), y = shfl_up64(pu, d);
+        pi += lane >= d ? x : 0;
+        pu += lane >= d ? y : 0;
+    }
+    if (lane == 63) {
+        sh.sums[0][wave] = pi;
+        sh.sums[1][wave] = pu;
+    }
+    if (tid == 0)
+        sh.b = -1;
     __syncthreads();
-    const float sk = a.scale * (p.k_scale ? p.k_scale[hk] : 1.0f);
-    const int held = clampi(a.held[b], 0, a.max_pages);
-    const int64_t end = (int64_t)c.pos + c.n;
-    const int words = (a.R + 31) / 32;
-    float m = -INFINITY, l = 0.0f, o[D / 64];
-    for (int t = 0; t < D / 64; ++t)
-        o[t] = 0.0f;
-    for (int64_t k0 = 0; k0 < end; k0 += 64) {
-        const int64_t pos = k0 + lane;
-        bool seen = pos < end && pos / a.page_size < held;
-        int64_t slot = 0;
-        if (seen) {
-            slot = (int64_t)a.table[(int64_t)b * a.max_pages + pos / a.page_size] * a.page_size +
-                   pos % a.page_size;
-            seen = slot >= 0 && slot < p.n_slots;
-            slot = seen ? slot : 0;
-        }
-        const int64_t j = pos - c.pos;
-        if (seen && j >= 0)
-            seen = a.mask ? (a.mask[row * words + j / 32] >> (j % 32)) & 1 : j <= i;
-        float s = -INFINITY;
-        if (seen) {
-            s = 0.0f;
-            for (int d = 0; d < D; ++d)
-                s = fmaf(sq[d], cached<TYPE, E4M3>(p.k_cache, (slot * a.Hkv + hk) * D + d), s);
-            s *= sk;
-        }
-        float top = s;
-        for (int x = 32; x; x >>= 1)
-            top = fmaxf(top, __shfl_xor(top, x));
-        const float mn = fmaxf(m, top), ms = mn == -INFINITY ? 0.0f : mn;
-        const float w = seen ? expf(s - ms) : 0.0f, alpha = expf(m - ms);
-        m = mn;
-        float sum = w;
-        for (int x = 32; x; x >>= 1)
-            sum += __shfl_xor(sum, x);
-        l = l * alpha + sum;
-        for (int t = 0; t < D / 64; ++t)
-            o[t] *= alpha;
-        for (int y = 0; y < 64; ++y) {
-            if (!__shfl((int)seen, y))
-                continue;
-            const float wy = __shfl(w, y);
-            const int64_t at = (__shfl((long long)slot, y) * a.Hkv + hk) * D + lane;
-            for (int t = 0; t < D / 64; ++t)
-                o[t] = fmaf(wy, cached<TYPE, E4M3>(p.v_cache, at + t * 64), o[t]);
+    Work w;
+    w.items = w.units = 0;
+#pragma unroll
+    for (int v = 0; v < kThreads / 64; ++v) {
+        pi += v < wave ? sh.sums[0][v] : 0;
+        pu += v < wave ? sh.sums[1][v] : 0;
+        w.items += sh.sums[0][v];
+        w.units += sh.sums[1][v];
+    }
+    w.whole = p.whole || w.items >= kAttnWhole;
+    const int64_t most = w.units / kAttnLeast;
+    w.groups = (int)(w.whole ? w.items : most < 1 ? 1 : most < kAttnGroups ? most : kAttnGroups);
+    const int64_t at = w.whole || by_item ? group : group * w.units / w.groups;
+    int64_t before = w.whole || by_item ? pi - items : pu - units;
+    const int64_t mine = w.whole || by_item ? items : units;
+    if (w.items > 0 && at >= before && at < before + mine) {
+        for (int b = b0; b < b1; ++b) {
+            const Share s = share_of<TILE, UNIT>(p, b);
+            const int64_t n =
+                (int64_t)s.tiles * p.a.Hkv * (w.whole || by_item ? 1 : s.units);
+            if (at < before + n) {
+                sh.b = b;
+                sh.off = at - before;
+                break;
+            }
+            before += n;
         }
     }
-    const float sv = p.v_scale ? p.v_scale[hk] : 1.0f;
-    uint16_t *out = (uint16_t *)p.out + (row * a.Hq + h) * D;
-    for (int t = 0; t < D / 64; ++t)
-        out[t * 64 + lane] = from_f32<TYPE>(l == 0.0f ? 0.0f : o[t] / l * sv);
-    if (p.lse && lane == 0)
-        p.lse[row * a.Hq + h] = l == 0.0f ? -INFINITY : m + logf(l);
+    __syncthreads();
+    b_out = sh.b;
+    off_out = sh.off;
+    return w;
+}
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+template <int TYPE>
+__device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
+    if (TYPE == SWITCHSD_BF16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                       __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+template <int TYPE>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    const f32x2 v = {a, b};
+    if (TYPE == SWITCHSD_BF16)
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+}
+
+// Sixteen 8-bit floats as two vectors of 16-bit ones, which hold them exactly.
+template <int TYPE>
+__device__ __forceinline__ void widen(u32x4 x, u32x4 &lo, u32x4 &hi) {
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (TYPE == SWITCHSD_BF16) {
+            w[j * 2] = __builtin_bit_cast(
+                uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[j], 1.0f, false));
+            w[j * 2 + 1] = __builtin_bit_cast(
+                uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[j], 1.0f, true));
+        } else {
+            w[j * 2] = __builtin_bit_cast(
+                uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x[j], 1.0f, false));
+            w[j * 2 + 1] = __builtin_bit_cast(
+                uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x[j], 1.0f, true));
+        }
+    }
+    lo = u32x4{w[0], w[1], w[2], w[3]};
+    hi = u32x4{w[4], w[5], w[6], w[7]};
+}
+
+// Sets the infinities and NaN among eight 16-bit elements to 0; whether there
+// were any.
+template <int TYPE>
+__device__ __forceinline__ bool clear_not_finite(u32x4 &x) {
+    const uint32_t e = TYPE == SWITCHSD_BF16 ? 0x7F80u : 0x7C00u;
+    bool bad = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const bool lo = (x[j] & e) == e, hi = (x[j] >> 16 & e) == e;
+        x[j] &= (lo ? 0xFFFF0000u : ~0u) & (hi ? 0xFFFFu : ~0u);
+        bad |= lo || hi;
+    }
+    return bad;
+}
+
+// Four 16-bit elements of one column of an LDS tile of rows: of every 16 lanes,
+// lane x names the 8 bytes at row x / 4, columns 4 (x % 4) .., and gets the four
+// rows of column x.
+__device__ __forceinline__ uint2 read_transposed(const char *at) {
+    typedef __attribute__((address_space(3))) s16x4 *lds_ptr;
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at));
+}
+
+// What a lane holds of one query row (its column of the products).
+struct Row {
+    int64_t row;  // in q and out
+    int i, head;  // new token of the sequence, query head
+    bool ok;
+};
+__device__ __forceinline__ Row row_of(const AttnParams &p, const Chunk &c, int h, int m) {
+    Row r;
+    r.i = m / p.G;
+    r.head = h * p.G + m % p.G;
+    r.ok = r.i < c.n;
+    r.row = (int64_t)c.row + r.i;
+    return r;
+}
+
+// The query rows as the products' right operand: lane l holds row l % 32, and of
+// step kk the 8 elements that the keys' operand has there.  The sign of the
+// softmax's factor is taken into them, and a factor of 0 (the scores are then
+// taken as they are, all 0), so that what is not seen can be -inf before it.
+template <bool E4M3, int D>
+__device__ __forceinline__ void load_query(const AttnParams &p, const Row &r, float signed_factor,
+                                           u32x4 (&q)[D / 16]) {
+    const int half = (threadIdx.x >> 5) & 1;
+    const char *src = (const char *)p.q + (r.row * p.q_stride + (int64_t)r.head * D) * 2;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+        const int d = E4M3 ? kk / 2 * 32 + half * 16 + kk % 2 * 8 : kk * 16 + half * 8;
+        q[kk] = r.ok && signed_factor != 0.0f ? *(const u32x4 *)(src + d * 2) : u32x4{0, 0, 0, 0};
+        if (signed_factor < 0.0f)
+            q[kk] ^= 0x80008000u;
+    }
+}
+
+// Which of the 32 cache positions from kb on row r sees, of those in `valid`.
+__device__ __forceinline__ uint32_t seen_bits(const AttnParams &p, const Chunk &c, const Row &r,
+                                              int kb, uint32_t valid) {
+    const int j0 = kb - c.pos;  // the first one's place among the new
+    uint32_t bits;
+    if (!p.a.mask) {
+        const int cnt = r.i - j0 + 1;
+        bits = cnt >= 32 ? ~0u : cnt > 0 ? (1u << cnt) - 1 : 0u;
+    } else {
+        const int words = (p.a.R + 31) / 32;
+        const uint32_t *row = p.a.mask + r.row * words;
+        bits = j0 <= -32 ? ~0u : 0u;
+        if (r.ok && j0 > -32) {
+            const int w = j0 >= 0 ? j0 / 32 : -1, sh = j0 & 31;
+            const uint32_t lo = w < 0 ? ~0u : w < words ? row[w] : 0u;
+            const uint32_t hi = sh && w + 1 < words ? row[w + 1] : 0u;
+            bits = sh ? lo >> sh | hi << (32 - sh) : lo;
+        }
+    }
+    return r.ok ? bits & valid : 0u;
+}
+
+// Running softmax of one query row per lane (both halves of a wave hold the same
+// rows, each the keys that its half of the products has): m is the maximum that
+// the weights are taken against, in powers of two; it follows the true one with
+// a delay of up to kDelay, which weights of up to 2^kDelay carry.
+constexpr float kDelay = 8.0f;
+
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+
+// Scores -> weights.  s holds products; `factor` (>= 0) brings them to powers of
+// two.  Returns what the sums so far have to be multiplied with (1: nothing).
+template <int N>
+__device__ __forceinline__ float weigh(f32x16 (&s)[N], float factor, float &m, float &l) {
+    float top = s[0][0];
+#pragma unroll
+    for (int x = 0; x < N; ++x)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            top = fmaxf(top, s[x][e]);
+    top = fmaxf(top, other_half(top)) * factor;
+    float alpha = 1.0f;
+    if (__any(top > m + kDelay || (m == -INFINITY && top > m))) {
+        const float mn = fmaxf(m, top);
+        alpha = m == mn ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= alpha;
+    }
+    const float base = m == -INFINITY ? 0.0f : m;
+    float sum = 0.0f;
+#pragma unroll
+    for (int x = 0; x < N; ++x)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            s[x][e] = __builtin_amdgcn_exp2f(fmaf(s[x][e], factor, -base));
+            sum += s[x][e];
+        }
+    l += sum;
+    return alpha;
+}
+
+// Infinities and NaN among the values of 32 positions that not every row sees were
+// taken as 0, since a weight of 0 would carry them to the rows that do not see
+// them.  Here they reach the rows that do: whatever the weight, the sum becomes
+// what it is with the value itself.
+template <int TYPE, bool E4M3, int D>
+__device__ __forceinline__ void add_not_finite(const AttnParams &p, int h, int64_t slot,
+                                               uint32_t seen, f32x16 (&o)[D / 32]) {
+    const int half = (threadIdx.x >> 5) & 1;
+    for (int x = 0; x < 32; ++x) {
+        const int64_t s = __shfl((long long)slot, x);
+        if (s < 0)
+            continue;
+        const bool on = seen >> x & 1;
+        const int64_t at = (s * p.a.Hkv + h) * D + half * 4;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    // a rare path: one value at a time, for few registers
+                    __builtin_amdgcn_sched_barrier(0);
+                    const float v = cached<TYPE, E4M3>(p.v_cache, at + dt * 32 + g * 8 + e);
+                    if (on && !(fabsf(v) < INFINITY))
+                        o[dt][g * 4 + e] += v;
+                }
+    }
+}
+
+// O^T += V^T P^T of 32 keys whose values stand in LDS, a row each `pitch` bytes.
+template <int TYPE, int D>
+__device__ __forceinline__ void add_values(const f32x16 &s, const char *values, int pitch,
+                                           f32x16 (&o)[D / 32]) {
+    const int lane = threadIdx.x & 63, x = lane & 15;
+    // the lane's 8 bytes: keys 4 (lane / 32) + x / 4, columns 16 (lane / 16 % 2) + 4 (x % 4)
+    const char *at = values + ((lane >> 5) * 4 + x / 4) * pitch +
+                     ((lane >> 4 & 1) * 16 + x % 4 * 4) * 2;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        u32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            w[j] = pack2<TYPE>(s[t * 8 + j * 2], s[t * 8 + j * 2 + 1]);
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) {
+            const uint2 a = read_transposed(at + t * 16 * pitch + dt * 64);
+            const uint2 b = read_transposed(at + (t * 16 + 8) * pitch + dt * 64);
+            o[dt] = mfma<TYPE>(u32x4{a.x, a.y, b.x, b.y}, w, o[dt]);
+        }
+    }
+}
+
+template <int D>
+__device__ __forceinline__ void scale_rows(f32x16 (&o)[D / 32], float f) {
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+        o[dt] *= f;
+}
+
+// Where a result goes: out and lse, or the work-group's place among the partial ones.
+template <int TYPE, int D, int TILE>
+__device__ __forceinline__ void put(const AttnParams &p, const Row &r, int h, int tile_row,
+                                    int64_t place, int dt, const f32x16 &o, float m, float l) {
+    const int half = (threadIdx.x >> 5) & 1;
+    if (!r.ok)
+        return;
+    if (place >= 0) {
+        float *part = p.part + place * (TILE * (D + 2));
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *(f32x4 *)(part + tile_row * D + dt * 32 + g * 8 + half * 4) =
+                f32x4{o[g * 4], o[g * 4 + 1], o[g * 4 + 2], o[g * 4 + 3]};
+        if (dt == 0 && half == 0) {
+            part[TILE * D + tile_row] = m;
+            part[TILE * D + TILE + tile_row] = l;
+        }
+        return;
+    }
+    const float sv = p.v_scale ? p.v_scale[h] : 1.0f;
+    const float f = l == 0.0f ? 0.0f : sv / l;
+    char *out = (char *)p.out + (r.row * p.a.Hq + r.head) * (D * 2);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        uint2 v;
+        v.x = pack2<TYPE>(o[g * 4] * f, o[g * 4 + 1] * f);
+        v.y = pack2<TYPE>(o[g * 4 + 2] * f, o[g * 4 + 3] * f);
+        if (l == 0.0f)
+            v = make_uint2(0, 0);
+        *(uint2 *)(out + (dt * 32 + g * 8 + half * 4) * 2) = v;
+    }
+    if (p.lse && dt == 0 && half == 0)
+        p.lse[r.row * p.a.Hq + r.head] =
+            l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// The cache offset (in slots) of position pos; < 0 where there is no key.
+__device__ __forceinline__ int64_t slot_of(const AttnParams &p, const int32_t *table, int pos,
+                                           int keys) {
+    if (pos >= keys)
+        return -1;
+    const int page = p.page_log >= 0 ? pos >> p.page_log : pos / p.a.page_size;
+    const int in = pos - page * p.a.page_size;
+    const int64_t slot = (int64_t)table[page] * p.a.page_size + in;
+    return slot >= 0 && slot < p.n_slots ? slot : -1;
+}
+
+// Up to 32 NQ query rows (all new tokens and query heads of one head of the
+// cache): the four waves take 32 keys each of every unit of 128, keys straight
+// into the registers that the products read, values through a part of LDS of
+// their own, so that no wave waits for another before the end.
+template <int TYPE, bool E4M3, int D, int NQ>
+__global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
+    k_attend_few(const AttnParams p) {
+    constexpr int TILE = 32 * NQ, UNIT = 128;
+    constexpr int CH = E4M3 ? D / 32 : D / 16;  // 16-byte pieces of a row per half wave
+    constexpr int PITCH = D * 2 + 32;
+    constexpr int kVBytes = 4 * 32 * PITCH, kOBytes = 4 * 2 * 4 * 64 * 16;
+    __shared__ __attribute__((aligned(16))) char lds[kVBytes > kOBytes ? kVBytes : kOBytes];
+    __shared__ float sm[4][TILE], sl[4][TILE];
+    __shared__ PlanShared sh;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    int b;
+    int64_t off;
+    const Work w = plan<TILE, UNIT>(p, blockIdx.x, false, sh, b, off);
+    if ((int64_t)blockIdx.x >= w.groups || b < 0)
+        return;
+    int64_t u = w.whole ? 0 : (int64_t)blockIdx.x * w.units / w.groups;
+    const int64_t u_end = w.whole ? 1 : ((int64_t)blockIdx.x + 1) * w.units / w.groups;
+    char *const values = lds + wave * 32 * PITCH;
+    bool first = true;
+
+    while (u < u_end) {
+        const Chunk c = chunk_of(p.a, b);
+        const int keys = keys_of(p, c, b);
+        const Share share = share_of<TILE, UNIT>(p, b);
+        const int nu = share.units;
+        if (share.tiles == 0) {  // a sequence without rows
+            ++b;
+            off = 0;
+            continue;
+        }
+        int item, ua, ub;
+        if (w.whole) {
+            item = (int)off;
+            ua = 0;
+            ub = nu;
+        } else {
+            item = (int)(off / nu);
+            ua = (int)(off - (int64_t)item * nu);
+            const int64_t left = u_end - u;
+            ub = left < nu - ua ? ua + (int)left : nu;
+        }
+        const int h = item % p.a.Hkv, tile = item / p.a.Hkv;
+        const int32_t *table = p.a.table + (int64_t)b * p.a.max_pages;
+        const float signed_factor = p.a.scale * kLog2e * (p.k_scale ? p.k_scale[h] : 1.0f);
+        const float factor = signed_factor == 0.0f ? 1.0f : fabsf(signed_factor);
+
+        Row r[NQ];
+        u32x4 q[NQ][D / 16];
+        f32x16 o[NQ][D / 32];
+        float m[NQ], l[NQ];
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) {
+            r[x] = row_of(p, c, h, tile * TILE + x * 32 + (lane & 31));
+            load_query<E4M3, D>(p, r[x], signed_factor, q[x]);
+            m[x] = -INFINITY;
+            l[x] = 0.0f;
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt)
+                o[x][dt] = f32x16{0};
+        }
+
+        // a lane's key is its number within 32; both halves of a row are read by
+        // the two lanes of its number
+        const int kl = wave * 32 + (lane & 31);
+        const char *const kbase =
+            (const char *)p.k_cache + (int64_t)h * D * (E4M3 ? 1 : 2) + half * 16;
+        const char *const vbase =
+            (const char *)p.v_cache + (int64_t)h * D * (E4M3 ? 1 : 2) + half * 16;
+        const int64_t row_bytes = (int64_t)p.a.Hkv * D * (E4M3 ? 1 : 2);
+        u32x4 kr[CH], vr[CH];
+        // positions without a key are read from the first slot, and not used
+        const auto load = [&](u32x4 (&to)[CH], const char *base, int64_t slot) {
+            const char *src = base + (slot < 0 ? 0 : slot) * row_bytes;
+#pragma unroll
+            for (int x = 0; x < CH; ++x)
+                to[x] = *(const u32x4 *)(src + x * 32);
+        };
+        const int stop = keys > 0 ? ub : ua;  // without keys nothing is read
+        bool poisoned = false;
+        int64_t slot = -1, next = -1;
+        if (ua < stop) {
+            slot = slot_of(p, table, ua * UNIT + kl, keys);
+            load(kr, kbase, slot);
+            load(vr, vbase, slot);
+            next = slot_of(p, table, (ua + 1) * UNIT + kl, keys);
+        }
+        for (int t = ua; t < stop; ++t) {
+            const int kb = t * UNIT + wave * 32;
+            const uint32_t valid = (uint32_t)__ballot(slot >= 0);
+            const bool plain = valid == ~0u && kb + 31 < c.pos;
+            f32x16 s[NQ][1];
+            const int64_t ahead = slot_of(p, table, (t + 2) * UNIT + kl, keys);
+#pragma unroll
+            for (int x = 0; x < NQ; ++x)
+                s[x][0] = f32x16{0};
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                if (E4M3) {
+                    u32x4 lo, hi;
+                    widen<TYPE>(kr[k], lo, hi);
+#pragma unroll
+                    for (int x = 0; x < NQ; ++x) {
+                        s[x][0] = mfma<TYPE>(lo, q[x][k * 2], s[x][0]);
+                        s[x][0] = mfma<TYPE>(hi, q[x][k * 2 + 1], s[x][0]);
+                    }
+                } else {
+#pragma unroll
+                    for (int x = 0; x < NQ; ++x)
+                        s[x][0] = mfma<TYPE>(kr[k], q[x][k], s[x][0]);
+                }
+            }
+            load(kr, kbase, next);
+            // values into LDS
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            char *dst = values + (lane & 31) * PITCH;
+            if (!plain) {
+                bool bad = false;
+#pragma unroll
+                for (int x = 0; x < CH; ++x) {
+                    if (E4M3) {
+                        // 0x7F and 0xFF are the NaN, there are no infinities
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if ((vr[x][j / 4] >> (j % 4 * 8) & 0x7Fu) == 0x7Fu) {
+                                vr[x][j / 4] &= ~(0xFFu << (j % 4 * 8));
+                                bad = true;
+                            }
+                    } else {
+                        bad |= clear_not_finite<TYPE>(vr[x]);
+                    }
+                }
+                poisoned |= __any(bad && slot >= 0);
+            }
+#pragma unroll
+            for (int x = 0; x < CH; ++x) {
+                if (E4M3) {
+                    u32x4 lo, hi;
+                    widen<TYPE>(vr[x], lo, hi);
+                    *(u32x4 *)(dst + (x * 32 + half * 16) * 2) = lo;
+                    *(u32x4 *)(dst + (x * 32 + half * 16 + 8) * 2) = hi;
+                } else {
+                    *(u32x4 *)(dst + (x * 16 + half * 8) * 2) = vr[x];
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            load(vr, vbase, next);
+#pragma unroll
+            for (int x = 0; x < NQ; ++x) {
+                if (!plain) {
+                    const uint32_t seen = seen_bits(p, c, r[x], kb, valid);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        s[x][0][e] = seen >> (e / 4 * 8 + half * 4 + e % 4) & 1 ? s[x][0][e]
+                                                                             : -INFINITY;
+                }
+                const float alpha = weigh<1>(s[x], factor, m[x], l[x]);
+                if (__any(alpha != 1.0f))
+                    scale_rows<D>(o[x], alpha);
+                add_values<TYPE, D>(s[x][0], values, PITCH, o[x]);
+            }
+            slot = next;
+            next = ahead;
+        }
+        if (poisoned) {
+            for (int t = ua; t < stop; ++t) {
+                const int kb = t * UNIT + wave * 32;
+                const int64_t at = slot_of(p, table, t * UNIT + kl, keys);
+                const uint32_t valid = (uint32_t)__ballot(at >= 0);
+                if (valid == ~0u && kb + 31 < c.pos)
+                    continue;
+#pragma unroll
+                for (int x = 0; x < NQ; ++x)
+                    add_not_finite<TYPE, E4M3, D>(p, h, at, seen_bits(p, c, r[x], kb, valid),
+                                                  o[x]);
+            }
+        }
+
+        // join the four waves
+        const bool done = ua == 0 && ub == nu;
+        const int64_t place = done ? -1 : (int64_t)blockIdx.x * 2 + (first ? 0 : 1);
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) {
+            l[x] += other_half(l[x]);
+            if (half == 0) {
+                sm[wave][x * 32 + lane] = m[x];
+                sl[wave][x * 32 + lane] = l[x];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) {
+            const int row = x * 32 + (lane & 31);
+            float top = sm[0][row];
+#pragma unroll
+            for (int v = 1; v < 4; ++v)
+                top = fmaxf(top, sm[v][row]);
+            float sum = 0.0f;
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+                sum += sm[v][row] == -INFINITY ? 0.0f
+                                               : sl[v][row] * __builtin_amdgcn_exp2f(sm[v][row] - top);
+            const float f = m[x] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[x] - top);
+            // two columns of 32 at a time: LDS holds them for four waves
+#pragma unroll
+            for (int d0 = 0; d0 < D / 32; d0 += 2) {
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        f32x4 v;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            v[e] = o[x][d0 + y][g * 4 + e] * f;
+                        *(f32x4 *)(lds + (((wave * 2 + y) * 4 + g) * 64 + lane) * 16) = v;
+                    }
+                __syncthreads();
+                if (wave < 2) {
+                    f32x16 t = f32x16{0};
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            const f32x4 y =
+                                *(const f32x4 *)(lds + (((v * 2 + wave) * 4 + g) * 64 + lane) * 16);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                t[g * 4 + e] += y[e];
+                        }
+                    put<TYPE, D, TILE>(p, r[x], h, row, place, d0 + wave, t, top, sum);
+                }
+                __syncthreads();
+            }
+        }
+        first = false;
+        u += w.whole ? 1 : ub - ua;
+        off += w.whole ? 1 : ub - ua;
+        if (!w.whole && off == (int64_t)share.tiles * p.a.Hkv * nu) {
+            ++b;
+            off = 0;
+        }
+    }
+}
+
+// Tiles of 128 query rows, 32 for each wave; the four waves share 64 keys and
+// values at a time in LDS, two buffers of them, the next ones on their way through
+// registers while the present ones are used.
+template <int TYPE, bool E4M3, int D>
+__global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(const AttnParams p) {
+    constexpr int TILE = 128, UNIT = 64;
+    constexpr int CH = E4M3 ? D / 16 : D / 8;  // 16-byte pieces of a row in the cache
+    constexpr int RPI = 64 / CH;               // rows that a wave reads at once
+    constexpr int NI = 16 / RPI;               // such reads for its 16 rows
+    constexpr int KP = D * 2, VP = D * 2 + 32;
+    __shared__ __attribute__((aligned(16))) char sk[2][UNIT * KP];
+    __shared__ __attribute__((aligned(16))) char sv[2][UNIT * VP];
+    __shared__ uint32_t sflag[2][4];      // keys there are (16 per wave), bit 16: not finite
+    __shared__ PlanShared sh;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    int b;
+    int64_t off;
+    const Work w = plan<TILE, UNIT>(p, blockIdx.x, false, sh, b, off);
+    if ((int64_t)blockIdx.x >= w.groups || b < 0)
+        return;
+    int64_t u = w.whole ? 0 : (int64_t)blockIdx.x * w.units / w.groups;
+    const int64_t u_end = w.whole ? 1 : ((int64_t)blockIdx.x + 1) * w.units / w.groups;
+    bool first = true;
+
+    while (u < u_end) {
+        const Chunk c = chunk_of(p.a, b);
+        const int keys = keys_of(p, c, b);
+        const Share share = share_of<TILE, UNIT>(p, b);
+        const int nu = share.units;
+        if (share.tiles == 0) {
+            ++b;
+            off = 0;
+            continue;
+        }
+        int item, ua, ub;
+        if (w.whole) {
+            item = (int)off;
+            ua = 0;
+            ub = nu;
+        } else {
+            item = (int)(off / nu);
+            ua = (int)(off - (int64_t)item * nu);
+            const int64_t left = u_end - u;
+            ub = left < nu - ua ? ua + (int)left : nu;
+        }
+        const int taken = ub - ua;
+        const bool done = ua == 0 && ub == nu;
+        // the last tiles first: without a mask they see the most keys
+        const int h = item % p.a.Hkv, tile = share.tiles - 1 - item / p.a.Hkv;
+        const int32_t *table = p.a.table + (int64_t)b * p.a.max_pages;
+        const float signed_factor = p.a.scale * kLog2e * (p.k_scale ? p.k_scale[h] : 1.0f);
+        const float factor = signed_factor == 0.0f ? 1.0f : fabsf(signed_factor);
+        // keys that the tile's (the wave's) last row sees
+        int lim = keys, wlim = keys;
+        if (!p.a.mask) {
+            const int i1 = (tile * TILE + TILE - 1) / p.G, i2 = (tile * TILE + wave * 32 + 31) / p.G;
+            const int64_t e1 = (int64_t)c.pos + (i1 < c.n ? i1 + 1 : c.n);
+            const int64_t e2 = (int64_t)c.pos + (i2 < c.n ? i2 + 1 : c.n);
+            lim = e1 < keys ? (int)e1 : keys;
+            wlim = e2 < keys ? (int)e2 : keys;
+        }
+        const int stop = (lim + UNIT - 1) / UNIT;
+        ub = ub < stop ? ub : stop;
+        const Row r = row_of(p, c, h, tile * TILE + wave * 32 + (lane & 31));
+        const bool rows = __any(r.ok);
+        u32x4 q[D / 16];
+        load_query<false, D>(p, r, signed_factor, q);
+        f32x16 o[D / 32];
+        float m = -INFINITY, l = 0.0f;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+            o[dt] = f32x16{0};
+
+        const int piece = lane % CH, sub = lane / CH;
+        const char *const kbase =
+            (const char *)p.k_cache + (int64_t)h * D * (E4M3 ? 1 : 2) + piece * 16;
+        const char *const vbase =
+            (const char *)p.v_cache + (int64_t)h * D * (E4M3 ? 1 : 2) + piece * 16;
+        const int64_t row_bytes = (int64_t)p.a.Hkv * D * (E4M3 ? 1 : 2);
+        u32x4 kr[NI], vr[NI];
+        const auto slots = [&](int t) {
+            return t < ub ? slot_of(p, table, t * UNIT + wave * 16 + (lane & 15), lim) : (int64_t)-1;
+        };
+        // positions without a key are read from the first slot, and not used
+        const auto load = [&](int64_t slot) {
+#pragma unroll
+            for (int x = 0; x < NI; ++x) {
+                const int64_t s = __shfl((long long)slot, x * RPI + sub);
+                const int64_t at = (s < 0 ? 0 : s) * row_bytes;
+                kr[x] = *(const u32x4 *)(kbase + at);
+                vr[x] = *(const u32x4 *)(vbase + at);
+            }
+        };
+        const auto stash = [&](int64_t slot, int t) {
+            const int buf = t & 1;
+            const uint32_t valid = (uint32_t)__ballot(slot >= 0) & 0xFFFFu;
+            const bool plain = valid == 0xFFFFu && (t + 1) * UNIT <= c.pos;
+            bool bad = false;
+#pragma unroll
+            for (int x = 0; x < NI; ++x) {
+                const int row = wave * 16 + x * RPI + sub;
+                char *kd = sk[buf] + row * KP, *vd = sv[buf] + row * VP;
+                if (E4M3) {
+                    u32x4 lo, hi;
+                    widen<TYPE>(kr[x], lo, hi);
+                    *(u32x4 *)(kd + (((piece * 2) ^ (row & 7)) * 16)) = lo;
+                    *(u32x4 *)(kd + (((piece * 2 + 1) ^ (row & 7)) * 16)) = hi;
+                    widen<TYPE>(vr[x], lo, hi);
+                    if (!plain) {
+                        bad |= clear_not_finite<TYPE>(lo);
+                        bad |= clear_not_finite<TYPE>(hi);
+                    }
+                    *(u32x4 *)(vd + piece * 32) = lo;
+                    *(u32x4 *)(vd + piece * 32 + 16) = hi;
+                } else {
+                    *(u32x4 *)(kd + ((piece ^ (row & 7)) * 16)) = kr[x];
+                    if (!plain)
+                        bad |= clear_not_finite<TYPE>(vr[x]);
+                    *(u32x4 *)(vd + piece * 16) = vr[x];
+                }
+            }
+            bad = __any(bad);
+            if (lane == 0)
+                sflag[buf][wave] = valid | (bad ? 0x10000u : 0u);
+        };
+
+        if (keys == 0)
+            ub = ua;
+        bool poisoned = false;
+        int64_t slot = slots(ua);
+        if (ua < ub) {
+            load(slot);
+            stash(slot, ua);
+        }
+        slot = slots(ua + 1);
+        for (int t = ua; t < ub; ++t) {
+            __syncthreads();
+            if (t + 1 < ub)
+                load(slot);
+            const int64_t next = slots(t + 2);
+            const int kb = t * UNIT, buf = t & 1;
+            if (rows && kb < wlim) {
+                const char *const K = sk[buf], *const V = sv[buf];
+                const bool plain = kb + UNIT <= c.pos;
+                const uint32_t f0 = sflag[buf][0], f1 = sflag[buf][1], f2 = sflag[buf][2],
+                               f3 = sflag[buf][3];
+                const uint32_t valid[2] = {(f0 & 0xFFFFu) | f1 << 16, (f2 & 0xFFFFu) | f3 << 16};
+                poisoned |= ((f0 | f1 | f2 | f3) & 0x10000u) != 0;
+                f32x16 s[2];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    s[y] = f32x16{0};
+                    const int row = y * 32 + (lane & 31);
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const u32x4 a =
+                            *(const u32x4 *)(K + row * KP + (((kk * 2 + half) ^ (row & 7)) * 16));
+                        s[y] = mfma<TYPE>(a, q[kk], s[y]);
+                    }
+                }
+                if (!plain || (valid[0] & valid[1]) != ~0u) {
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const uint32_t seen = seen_bits(p, c, r, kb + y * 32, valid[y]);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            s[y][e] = seen >> (e / 4 * 8 + half * 4 + e % 4) & 1 ? s[y][e]
+                                                                                 : -INFINITY;
+                    }
+                }
+                const float alpha = weigh<2>(s, factor, m, l);
+                if (__any(alpha != 1.0f))
+                    scale_rows<D>(o, alpha);
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+                    add_values<TYPE, D>(s[y], V + y * 32 * VP, VP, o);
+            }
+            if (t + 1 < ub)
+                stash(slot, t + 1);
+            slot = next;
+        }
+        __syncthreads();  // before the next item's first tile is stored
+        if (poisoned) {
+            for (int kb = ua * UNIT; kb < ub * UNIT && kb < wlim; kb += 32) {
+                const int64_t at = slot_of(p, table, kb + (lane & 31), lim);
+                const uint32_t valid = (uint32_t)__ballot(at >= 0);
+                if (valid != ~0u || kb / UNIT * UNIT + UNIT > c.pos)
+                    add_not_finite<TYPE, E4M3, D>(p, h, at, seen_bits(p, c, r, kb, valid), o);
+            }
+        }
+
+        l += other_half(l);
+        const int64_t place = done ? -1 : (int64_t)blockIdx.x * 2 + (first ? 0 : 1);
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+            put<TYPE, D, TILE>(p, r, h, wave * 32 + (lane & 31), place, dt, o[dt], m, l);
+        first = false;
+        u += w.whole ? 1 : taken;
+        off += w.whole ? 1 : taken;
+        if (!w.whole && off == (int64_t)share.tiles * p.a.Hkv * nu) {
+            ++b;
+            off = 0;
+        }
+    }
+}
+
+// Joins the partial results of the items that were cut.  Of a work-group's lanes,
+// D / 4 take four elements each of a row; `parts` such groups of lanes take every
+// parts-th result of one row, the others another row.
+template <int TYPE, int D, int TILE, int UNIT, bool LAST_FIRST>
+__global__ void __launch_bounds__(kThreads) k_merge(const AttnParams p, int parts) {
+    constexpr int LANES = D / 4, kSets = kThreads / LANES;
+    __shared__ PlanShared sh;
+    __shared__ int64_t base[kThreads / 64];
+    __shared__ f32x4 so[kThreads];
+    __shared__ float2 sml[kThreads];
+    const int64_t id = blockIdx.x;
+    const int tid = threadIdx.x;
+    int b;
+    int64_t item;
+    const Work w = plan<TILE, UNIT>(p, id, true, sh, b, item);
+    if (w.whole || id >= w.items || b < 0)
+        return;
+    // units before the item: those of earlier sequences are summed anew
+    int64_t sum = 0;
+    for (int x = tid; x < b; x += kThreads) {
+        const Share s = share_of<TILE, UNIT>(p, x);
+        sum += (int64_t)s.tiles * p.a.Hkv * s.units;
+    }
+    for (int d = 32; d; d >>= 1)
+        sum += __shfl_xor((long long)sum, d);
+    if ((tid & 63) == 0)
+        base[tid >> 6] = sum;
+    __syncthreads();
+    const Chunk c = chunk_of(p.a, b);
+    const Share s = share_of<TILE, UNIT>(p, b);
+    const int64_t u0 = base[0] + base[1] + base[2] + base[3] + item * s.units, u1 = u0 + s.units;
+    // work-group g takes the units from floor(g U / W) on: unit u is in the last g
+    // with g U / W < u + 1
+    const int64_t U = w.units, W = w.groups;
+    const int64_t g0 = ((u0 + 1) * W - 1) / U, g1 = (u1 * W - 1) / U;
+    if (g0 == g1)
+        return;  // one work-group had the whole item
+    const bool late = g0 * U / W < u0;  // the item is not the first one of g0
+    const int h = (int)(item % p.a.Hkv);
+    const int tile =
+        LAST_FIRST ? s.tiles - 1 - (int)(item / p.a.Hkv) : (int)(item / p.a.Hkv);
+    const int set = tid / LANES, lane = tid % LANES, d = lane * 4;
+    const int row = blockIdx.y * (kSets / parts) + set / parts;
+    const Row r = row_of(p, c, h, tile * TILE + row);
+    const bool on = row < TILE && r.ok;
+    float m = -INFINITY, l = 0.0f;
+    f32x4 o = f32x4{0};
+    if (on) {
+        const int64_t stride = TILE * (D + 2);
+#pragma unroll 4
+        for (int64_t g = g0 + set % parts; g <= g1; g += parts) {
+            const float *part = p.part + (g * 2 + (g == g0 && late ? 1 : 0)) * stride;
+            const float pm = part[TILE * D + row], pl = part[TILE * D + TILE + row];
+            const f32x4 po = *(const f32x4 *)(part + row * D + d);
+            const float mn = fmaxf(m, pm), at = mn == -INFINITY ? 0.0f : mn;
+            const float f = __builtin_amdgcn_exp2f(m - at), pf = __builtin_amdgcn_exp2f(pm - at);
+            m = mn;
+            l = l * f + pl * pf;
+            o = o * f + po * pf;
+        }
+    }
+    if (parts > 1) {
+        so[tid] = o;
+        sml[tid] = make_float2(m, l);
+        __syncthreads();
+        if (set % parts)
+            return;
+        for (int x = 1; x < parts; ++x) {
+            const float2 y = sml[tid + x * LANES];
+            const f32x4 po = so[tid + x * LANES];
+            const float mn = fmaxf(m, y.x), at = mn == -INFINITY ? 0.0f : mn;
+            const float f = __builtin_amdgcn_exp2f(m - at), pf = __builtin_amdgcn_exp2f(y.x - at);
+            m = mn;
+            l = l * f + y.y * pf;
+            o = o * f + po * pf;
+        }
+    }
+    if (!on)
+        return;
+    o = l == 0.0f ? f32x4{0} : o * ((p.v_scale ? p.v_scale[h] : 1.0f) / l);
+    *(uint2 *)((char *)p.out + ((r.row * p.a.Hq + r.head) * D + d) * 2) =
+        make_uint2(pack2<TYPE>(o[0], o[1]), pack2<TYPE>(o[2], o[3]));
+    if (p.lse && d == 0)
+        p.lse[r.row * p.a.Hq + r.head] =
+            l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 int launched() { return hipGetLastError() == hipSuccess ? SWITCHSD_OK : SWITCHSD_EHIP; }
@@ -209,16 +1050,60 @@ int launch_store_kernel(const StoreParams &p, int32_t type, int32_t cache_type,
 
 namespace {
 
-template <int TYPE, bool E4M3>
-int launch_attend(const AttnParams &p, hipStream_t stream) {
-    const dim3 g((unsigned)((int64_t)p.a.B * p.a.R * p.a.Hq)), t(64);
-    if (p.a.D == 64)
-        hipLaunchKernelGGL((k_attend<TYPE, E4M3, 64>), g, t, 0, stream, p);
-    else if (p.a.D == 128)
-        hipLaunchKernelGGL((k_attend<TYPE, E4M3, 128>), g, t, 0, stream, p);
-    else
-        hipLaunchKernelGGL((k_attend<TYPE, E4M3, 256>), g, t, 0, stream, p);
+template <int TYPE, int D, int TILE, int UNIT, bool LAST_FIRST>
+void launch_merge(const AttnParams &p, int64_t items, hipStream_t stream) {
+    constexpr int kSets = kThreads / (D / 4);
+    // about the results of an item, at most one set of lanes for each
+    int parts = 1;
+    while (parts < kSets && parts * items < kAttnGroups)
+        parts *= 2;
+    const int sets = kSets / parts;
+    const int64_t rows = (int64_t)p.a.R * p.G < TILE ? (int64_t)p.a.R * p.G : TILE;
+    hipLaunchKernelGGL((k_merge<TYPE, D, TILE, UNIT, LAST_FIRST>),
+                       dim3((unsigned)(items < kAttnWhole ? items : kAttnWhole),
+                            (unsigned)((rows + sets - 1) / sets)),
+                       dim3(kThreads), 0, stream, p, parts);
+}
+
+template <int TYPE, bool E4M3, int D>
+int launch_attend(AttnParams p, hipStream_t stream) {
+    const int64_t rows = (int64_t)p.a.R * p.G, tile = attention_tile(rows, D);
+    int64_t items = (int64_t)p.a.B * ((rows + tile - 1) / tile);
+    // packed: the rows that there are make no more tiles than this
+    const int64_t most = (int64_t)p.a.rows * p.G / tile + p.a.B;
+    if (p.a.cu && most < items)
+        items = most;
+    items *= p.a.Hkv;
+    const int64_t cap = (int64_t)p.a.max_pages * p.a.page_size;
+    const int64_t len = (int64_t)p.a.Lmax + p.a.R;
+    p.whole = (len < cap ? len : cap) <= kAttnShort;
+    const int64_t groups = p.whole || items > kAttnGroups ? items : kAttnGroups;
+    if (groups > 0x7FFFFFFFll)
+        return SWITCHSD_ESHAPE;
+    const dim3 g((unsigned)groups), t(kThreads);
+    if (tile == 32) {
+        hipLaunchKernelGGL((k_attend_few<TYPE, E4M3, D, 1>), g, t, 0, stream, p);
+        if (!p.whole)
+            launch_merge<TYPE, D, 32, 128, false>(p, items, stream);
+    } else if (tile == 64) {
+        if constexpr (D <= 128) {
+            hipLaunchKernelGGL((k_attend_few<TYPE, E4M3, D, 2>), g, t, 0, stream, p);
+            if (!p.whole)
+                launch_merge<TYPE, D, 64, 128, false>(p, items, stream);
+        }
+    } else {
+        hipLaunchKernelGGL((k_attend_many<TYPE, E4M3, D>), g, t, 0, stream, p);
+        if (!p.whole)
+            launch_merge<TYPE, D, 128, 64, true>(p, items, stream);
+    }
     return launched();
+}
+
+template <int TYPE, bool E4M3>
+int launch_typed(const AttnParams &p, hipStream_t stream) {
+    return p.a.D == 64    ? launch_attend<TYPE, E4M3, 64>(p, stream)
+           : p.a.D == 128 ? launch_attend<TYPE, E4M3, 128>(p, stream)
+                          : launch_attend<TYPE, E4M3, 256>(p, stream);
 }
 
 }  // namespace
@@ -227,10 +1112,10 @@ int launch_attention_kernel(const AttnParams &p, int32_t type, int32_t cache_typ
                             hipStream_t stream) {
     const bool e4m3 = cache_type == SWITCHSD_E4M3;
     if (type == SWITCHSD_BF16)
-        return e4m3 ? launch_attend<SWITCHSD_BF16, true>(p, stream)
-                    : launch_attend<SWITCHSD_BF16, false>(p, stream);
-    return e4m3 ? launch_attend<SWITCHSD_F16, true>(p, stream)
-                : launch_attend<SWITCHSD_F16, false>(p, stream);
+        return e4m3 ? launch_typed<SWITCHSD_BF16, true>(p, stream)
+                    : launch_typed<SWITCHSD_BF16, false>(p, stream);
+    return e4m3 ? launch_typed<SWITCHSD_F16, true>(p, stream)
+                : launch_typed<SWITCHSD_F16, false>(p, stream);
 }
 
 }  // namespace switchsd

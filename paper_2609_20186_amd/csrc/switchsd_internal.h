@@ -294,14 +294,27 @@ struct AttnParams {
     float *lse;
     float *part;       // partial results
     int32_t G;         // query heads per head of the cache
+    int32_t page_log;  // page_size = 2^page_log, or -1
+    int32_t whole;     // no item is cut
 };
 
+// Work-groups that share an attention's keys where there are few rows, and the
+// items (tiles of rows and heads) from which each takes a whole one; the fewest
+// units of keys per work-group; the longest contexts that are never cut.
+constexpr int kAttnGroups = 512;
+constexpr int kAttnWhole = 2048;
+constexpr int kAttnLeast = 2;
+constexpr int kAttnShort = 1024;
+
+// Query rows (new tokens times query heads of one head of the cache) of a
+// work-group, by the most that a sequence has.
+constexpr int attention_tile(int64_t most, int32_t D) {
+    return most <= 32 ? 32 : most <= 64 && D <= 128 ? 64 : 128;
+}
 // Floats of the partial results: each of kAttnGroups work-groups leaves at most
 // two, of as many rows as a work-group takes, D sums, a maximum and a sum each.
-constexpr int kAttnGroups = 512;
-constexpr int attention_tile(int64_t most) { return most <= 32 ? 32 : most <= 64 ? 64 : 128; }
 constexpr size_t attention_part_floats(int64_t most, int32_t D) {
-    return (size_t)2 * kAttnGroups * attention_tile(most) * (D + 2);
+    return (size_t)2 * kAttnGroups * attention_tile(most, D) * (D + 2);
 }
 
 int launch_store_kernel(const StoreParams &p, int32_t type, int32_t cache_type,

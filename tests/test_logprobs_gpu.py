@@ -1,0 +1,374 @@
+"""Log probabilities of given tokens, entropies, ranks, the likeliest alternatives
+and the gradient, against the references in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import attention_ref as ref
+from gpu_helpers import say
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+INF = math.inf
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2609_20186_amd import binding  # noqa: F401
+
+
+def dev(x):
+    return None if x is None else torch.from_numpy(np.ascontiguousarray(x)).to(DEV)
+
+
+def make(B, R, V, type, seed=0, path=None, dn=True, kind="normal"):
+    rng = np.random.default_rng(seed)
+    a = dict(B=B, R=R, V=V, type=type)
+    x = torch.randn(B, R, V, generator=torch.Generator().manual_seed(seed)) * 3
+    if kind == "special":
+        x[:, :, ::3] = -INF
+        x[:, ::2, 1::5] = math.nan
+        x[0, 0] = math.nan
+        if R > 1:
+            x[0, 1] = -INF
+        if R > 2:
+            x[0, 2, V // 2:] = INF
+        if R > 3:
+            x[0, 3] = 1.25
+        if R > 4:
+            x[0, 4] = -INF
+            x[0, 4, V - 1] = 2.0
+        if R > 5:
+            x[0, 5, V // 3] = math.nan
+            x[0, 5, :V // 3] = 0.0
+            x[0, 5, V // 3 + 1:] = -0.0
+    if kind == "falling":
+        x = torch.linspace(20, -20, V).expand(B, R, V).clone()
+    if kind == "rising":
+        x = torch.linspace(-20, 20, V).expand(B, R, V).clone()
+    if kind == "blocks":                     # the likeliest side by side
+        at = V // 2
+        x[:, :, at:at + 100] += 30
+    a["logits"] = x.to(TYPES[type])
+    a["dn"] = rng.integers(-1, R + 3, B).astype(np.int32) if dn else None
+    a["dpar"] = a["accept_node"] = None
+    if path:
+        a["accept_node"] = rng.integers(-1, R + 1, B).astype(np.int32)
+        if path == "tree":
+            p = np.stack([[-1] + [rng.integers(0, i) for i in range(1, R)] for _ in range(B)])
+            if B > 2 and R > 1:
+                p[B - 1, R // 2] = R + 4        # a broken path
+                p[B - 2, 1] = 1
+            a["dpar"] = p.astype(np.int32)
+    a["tokens"] = rng.integers(0, V, (B, R)).astype(np.int32)
+    a["tokens"][rng.random((B, R)) < 0.1] = -1
+    a["tokens"][rng.random((B, R)) < 0.05] = V
+    return a
+
+
+def args_of(a, T, logits):
+    from paper_2609_20186_amd import binding as sd
+    return sd.build_logprob_args(logits, dev(a["tokens"]), dev(a["dn"]), dev(a["dpar"]),
+                                 dev(a["accept_node"]), temperature=T)
+
+
+def run(a, T, n_top, stream=None, args=None, out=None):
+    from paper_2609_20186_amd import binding as sd
+    B, R = a["B"], a["R"]
+    if args is None:
+        args = args_of(a, T, a["logits"].to(DEV))
+    if out is None:
+        f = dict(dtype=torch.float32, device=DEV)
+        i = dict(dtype=torch.int32, device=DEV)
+        out = {n: torch.full((B, R), 77.0, **f) for n in ("logprob", "lse", "entropy")}
+        out["rank"] = torch.full((B, R), 77, **i)
+        out["top_ids"] = torch.full((B, R, n_top), 77, **i) if n_top else None
+        out["top_logprobs"] = torch.full((B, R, n_top), 77.0, **f) if n_top else None
+    sd.switchsd_token_logprobs(args, stream=stream, **out)
+    return out, args
+
+
+def near(got, want, V, T, big, what):
+    """z = l / T is off by two roundings of |z - max| (the factor 1 / T and the
+    product), exp2 and its argument's by a few more, the sum by log2 V + 20 of them
+    (its terms are added in chains of a few thousand at most, whose errors are
+    random; the bound takes every one of 2^-24 times the square root of V and 16
+    more), the result by its own rounding."""
+    got, want = np.asarray(got, np.float64), np.asarray(want, np.float64)
+    ok = np.isfinite(want)
+    np.testing.assert_array_equal(got[~ok], want[~ok], err_msg=what)
+    tol = 2.0 ** -24 * (math.sqrt(V) + 16 + 8 * big / T + 4 * np.abs(want[ok]))
+    assert (np.abs(got[ok] - want[ok]) <= tol).all(), \
+        (what, float(np.abs(got[ok] - want[ok]).max()), float(np.min(tol)))
+
+
+def check(a, T, n_top, out, what=""):
+    x = ref.f64(a["logits"])
+    o = {n: None if t is None else t.cpu().numpy() for n, t in out.items()}
+    some = 0
+    for b in range(a["B"]):
+        rows = ref.entries(a, b)
+        for i in range(a["R"]):
+            if i >= len(rows):
+                for n, t in o.items():
+                    assert t is None or (t[b, i] == 77).all(), (what, n, b, i)
+                continue
+            some += 1
+            row = x[b, rows[i]]
+            lse, lp, h = ref.row_logprobs(row, T)
+            fin = row[np.isfinite(row)]
+            big = np.abs(fin).max() if len(fin) else 0.0
+            at = f"{what} {b} {i}"
+            tok = int(a["tokens"][b, i])
+            inside = 0 <= tok < a["V"]
+            want = ref.order(row)
+            near(o["lse"][b, i], lse, a["V"], T, big, at + " lse")
+            near(o["entropy"][b, i], h, a["V"], T, big * max(1.0, abs(h)), at + " entropy")
+            near(o["logprob"][b, i], lp[tok] if inside else -INF, a["V"], T, big, at)
+            assert o["rank"][b, i] == (want.index(tok) if inside else -1), at
+            if n_top:
+                np.testing.assert_array_equal(o["top_ids"][b, i], want[:n_top], err_msg=at)
+                near(o["top_logprobs"][b, i], lp[want[:n_top]], a["V"], T, big, at + " top")
+    say(f"{what}: {some} entries")
+
+
+@pytest.mark.parametrize("type", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("kind", ["normal", "special", "falling", "rising", "blocks"])
+def test_values(type, kind):
+    for V, n_top in ((1, 1), (2, 0), (7, 7), (64, 64), (255, 5), (1000, 20), (4099, 64),
+                     (9001, 64)):
+        a = make(3, 7, V, type, seed=V, kind=kind)
+        out, _ = run(a, 1.0, n_top)
+        check(a, 1.0, n_top, out, f"{kind} {type} V={V}")
+
+
+@pytest.mark.parametrize("V", [32000, 50257, 128256, 151936])
+def test_vocabularies(V):
+    for kind, n_top in (("normal", 20), ("special", 1), ("blocks", 64), ("falling", 64)):
+        for type in ("bf16", "f32"):
+            a = make(2, 2, V, type, seed=1, kind=kind)
+            check(a, 0.7, n_top, run(a, 0.7, n_top)[0], f"{kind} {type} V={V}")
+
+
+def test_temperatures():
+    for T in (0.05, 0.7, 3.0, 1e6, 1e-30):
+        a = make(2, 5, 500, "f32", kind="special" if T > 1e-3 else "normal")
+        out, _ = run(a, T, 9)
+        if T > 1e-3:
+            check(a, T, 9, out, f"T={T}")
+            continue
+        # everything but the greedy choice is out of reach of 32 bits
+        best = a["logits"].argmax(-1)
+        for b in range(2):
+            for i in range(len(ref.entries(a, b))):
+                assert int(out["top_ids"][b, i, 0]) == int(best[b, i])
+                assert float(out["top_logprobs"][b, i, 0]) == 0.0 and float(out["entropy"][b, i]) == 0
+
+
+@pytest.mark.parametrize("path", ["chain", "tree"])
+def test_accepted_paths(path):
+    """The rows along each accepted path; paths that are none have no entries."""
+    for R in (1, 2, 9, 40, 300):
+        a = make(7, R, 200, "bf16", seed=R, path=path, dn=R != 9)
+        a["accept_node"][0] = R - 1
+        if a["dn"] is not None:
+            a["dn"][0] = R
+        check(a, 1.0, 3, run(a, 1.0, 3)[0], f"{path} {R}")
+
+
+def test_longest_path():
+    """A chain as a tree of the most rows: the longest walk."""
+    a = make(2, 1024, 64, "bf16", path="tree", dn=False)
+    a["dpar"] = np.tile(np.arange(-1, 1023, dtype=np.int32), (2, 1))
+    a["accept_node"][:] = [1023, 1000]
+    check(a, 1.0, 2, run(a, 1.0, 2)[0], "1024 nodes")
+
+
+def test_rows_at_any_address():
+    """Odd vocabularies put rows at every alignment; the first row too."""
+    for type in ("bf16", "f32"):
+        for shift in range(5):
+            a = make(2, 5, 1237, type, seed=shift)
+            buf = torch.zeros(a["logits"].numel() + 8, dtype=TYPES[type], device=DEV)
+            x = buf[shift:shift + a["logits"].numel()].view(a["logits"].shape)
+            x.copy_(a["logits"])
+            out, args = run(a, 1.0, 5, args=args_of(a, 1.0, x))
+            check(a, 1.0, 5, out, f"{type} +{shift}")
+
+
+def test_what_is_not_wanted():
+    from paper_2609_20186_amd import binding as sd
+    a = make(2, 3, 300, "bf16", dn=False)
+    full, args = run(a, 1.0, 4)
+    for name in full:
+        one = {name: torch.full_like(full[name], 7)}
+        sd.switchsd_token_logprobs(args, **one)
+        assert torch.equal(one[name], full[name]), name
+    a["tokens"] = None
+    args = args_of(a, 1.0, a["logits"].to(DEV))
+    ent = torch.zeros(2, 3, device=DEV)
+    sd.switchsd_token_logprobs(args, entropy=ent)
+    assert torch.equal(ent, full["entropy"])
+    with pytest.raises(sd.SwitchsdError, match="EINVAL"):
+        sd.switchsd_token_logprobs(args, logprob=ent)
+
+
+def test_offsets_beyond_32_bits():
+    """A logits tensor of over 4 GiB (2^31 elements and more): its last rows."""
+    B, R, V = 17, 1000, 131072
+    x = torch.empty(B, R, V, dtype=torch.bfloat16, device=DEV)
+    rows = torch.randn(2, V, generator=torch.Generator().manual_seed(3)).bfloat16()
+    x[16, 998:] = rows.to(DEV)
+    x[:, :1] = 0
+    from paper_2609_20186_amd import binding as sd
+    node = torch.zeros(B, dtype=torch.int32, device=DEV)
+    node[16] = 999
+    par = torch.zeros(B, R, dtype=torch.int32, device=DEV)
+    par[:, 999] = 998
+    tok = torch.full((B, R), 5, dtype=torch.int32, device=DEV)
+    args = sd.build_logprob_args(x, tok, None, par, node)
+    lp = torch.zeros(B, R, device=DEV)
+    lse = torch.zeros(B, R, device=DEV)
+    ids = torch.zeros(B, R, 3, dtype=torch.int32, device=DEV)
+    sd.switchsd_token_logprobs(args, logprob=lp, lse=lse, top_ids=ids)
+    for j in range(2):
+        row = ref.f64(rows[j])
+        near(float(lp[16, 1 + j]), ref.row_logprobs(row, 1.0)[1][5], V, 1.0, 6.0, "far")
+        assert ids[16, 1 + j].tolist() == ref.order(row)[:3]
+    g = torch.ones(B, R, device=DEV)
+    sd.switchsd_token_logprobs_grad(args, lse, None, g, None, x)
+    for j in range(2):
+        want = ref.grad_row(ref.f64(rows[j]), 1.0, 5, float(lse[16, 1 + j]), 0, 1.0, 0.0)
+        got = ref.f64(x[16, 998 + j])
+        assert (np.abs(got - want) <= ref.U["bf16"] * np.abs(want) * 1.01 + 1e-9).all()
+
+
+# ------------------------------------------------------------------ gradient
+
+def check_grad(a, T, out, lse, ent, g, ge, before, what):
+    """p is off by its exponent's error (8 roundings of |z| + |lse|), the bracket by
+    that of log p + entropy, both then by a few roundings of their own."""
+    x = ref.f64(a["logits"])
+    u = ref.U[a["type"]]
+    out, before = ref.f64(out), ref.f64(before)
+    for b in range(a["B"]):
+        rows = ref.entries(a, b)
+        left = set(range(a["R"])) - set(rows)
+        for r in left:
+            np.testing.assert_array_equal(out[b, r], before[b, r])
+        for i, r in enumerate(rows):
+            low, h = float(lse[b, i]), float(ent[b, i])
+            gl = 0.0 if g is None else float(g[b, i])
+            gh = 0.0 if ge is None else float(ge[b, i])
+            tok = int(a["tokens"][b, i])
+            want = ref.grad_row(x[b, r], T, tok, low, h, gl, gh)
+            if not np.isfinite(low):
+                assert (out[b, r] == 0).all(), (what, b, r)
+                continue
+            z = np.where(np.isfinite(x[b, r]), x[b, r], 0.0) / T
+            p = np.where(np.isfinite(x[b, r]), np.exp(z - low), 0.0)
+            err = 2.0 ** -24 * (8 * (np.abs(z) + abs(low)) + 16)
+            part = p * (abs(gl) + abs(gh) * (np.abs(z - low) + abs(h)))
+            tol = 1.01 * u * np.abs(want) + (part * err + p * abs(gh) * err +
+                                             2.0 ** -22 * (part + abs(gl) * (np.arange(a["V"]) == tok))) / T
+            tol += {"bf16": 1e-38, "f16": 2.0 ** -25, "f32": 1e-38}[a["type"]]
+            d = np.abs(out[b, r] - want)
+            assert (d <= tol).all(), (what, b, r, float((d - tol).max()))
+
+
+@pytest.mark.parametrize("type", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("path", [None, "tree"])
+@pytest.mark.parametrize("kind", ["normal", "special"])
+def test_gradient(type, path, kind):
+    from paper_2609_20186_amd import binding as sd
+    for V, T in ((1, 1.0), (9, 0.7), (1000, 1.0), (4099, 2.0), (50257, 1.0)):
+        a = make(3, 7, V, type, seed=V, path=path, kind=kind)
+        rng = torch.Generator().manual_seed(V)
+        g, ge = torch.randn(3, 7, generator=rng), torch.randn(3, 7, generator=rng)
+        logits = a["logits"].to(DEV)
+        out, args = run(a, T, 0, args=args_of(a, T, logits))
+        for gg, hh in ((g, ge), (g, None), (None, ge)):
+            grad = torch.full_like(logits, 5.0)
+            call = [None if t is None else t.to(DEV) for t in (gg, hh)]
+            sd.switchsd_token_logprobs_grad(args, out["lse"], out["entropy"], *call, grad)
+            check_grad(a, T, grad, out["lse"], out["entropy"], gg, hh,
+                       torch.full_like(logits, 5.0), f"{type} {V}")
+        # in place: the same bits, other rows are left as they are
+        args2 = args_of(a, T, logits)
+        before = logits.clone()
+        sd.switchsd_token_logprobs_grad(args2, out["lse"], out["entropy"], *call, logits)
+        live = torch.zeros(3, 7, dtype=torch.bool)
+        for b in range(3):
+            live[b, ref.entries(a, b)] = True
+        live = live.to(DEV)
+        bits = torch.int32 if type == "f32" else torch.int16
+        assert torch.equal(logits[live].view(bits), grad[live].view(bits))
+        assert torch.equal(logits[~live].view(bits), before[~live].view(bits))
+
+
+def test_gradient_against_differences():
+    """The kernels' own forward pass, in steps of d: what is left of its rounding is
+    2^-24 (sqrt V + 16 + 8 |z|) / d, of the step d^2."""
+    from paper_2609_20186_amd import binding as sd
+    V, T, d = 24, 0.8, 2.0 ** -5
+    a = make(1, 4, V, "f32", seed=9, dn=False)
+    a["tokens"] = np.array([[3, 0, 23, 7]], np.int32)
+    out, args = run(a, T, 0)
+    g = torch.tensor([[0.7, -1.0, 0.3, 0.0]])
+    ge = torch.tensor([[0.2, 0.0, -0.5, 1.0]])
+    grad = torch.zeros(1, 4, V, device=DEV)
+    sd.switchsd_token_logprobs_grad(args, out["lse"], out["entropy"], g.to(DEV), ge.to(DEV), grad)
+    x = a["logits"].clone()
+    num = np.zeros((4, V))
+    for v in range(V):
+        side = []
+        for s in (d, -d):
+            a["logits"] = x.clone()
+            a["logits"][:, :, v] += s
+            o, _ = run(a, T, 0)
+            side.append((g * o["logprob"].cpu() + ge * o["entropy"].cpu())[0].double().numpy())
+        num[:, v] = (side[0] - side[1]) / (2 * d)
+    # third derivatives of lse and entropy are below 8 / T^3 here
+    tol = 2.0 ** -24 * (math.sqrt(V) + 16 + 8 * 12) / d * 3 + 8 / T ** 3 * d * d / 6 * 2
+    assert (np.abs(grad.cpu().double().numpy()[0] - num) <= tol).all()
+
+
+def test_streams_and_graphs():
+    """Two calls at once; a captured forward and gradient, replayed with other
+    inputs between eager calls."""
+    from paper_2609_20186_amd import binding as sd
+    a, c = make(4, 8, 32000, "bf16", seed=1), make(4, 8, 50257, "f32", seed=2)
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    la, lc = a["logits"].to(DEV), c["logits"].to(DEV)
+    torch.cuda.synchronize()
+    oa, args = run(a, 1.0, 5, stream=s1, args=args_of(a, 1.0, la))
+    oc, _ = run(c, 0.7, 5, stream=s2, args=args_of(c, 0.7, lc))
+    torch.cuda.synchronize()
+    check(a, 1.0, 5, oa, "stream 1")
+    check(c, 0.7, 5, oc, "stream 2")
+    g = torch.randn(4, 8, device=DEV)
+    grad = torch.zeros_like(la)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sd.switchsd_token_logprobs(args, **oa)
+        sd.switchsd_token_logprobs_grad(args, oa["lse"], oa["entropy"], g, g, grad)
+    for seed in range(3):
+        la.copy_(torch.randn(la.shape, generator=torch.Generator().manual_seed(seed)) * 3)
+        graph.replay()
+        torch.cuda.synchronize()
+        once, first = {n: t.clone() for n, t in oa.items()}, grad.clone()
+        eager, _ = run(a, 1.0, 5, args=args)
+        sd.switchsd_token_logprobs_grad(args, eager["lse"], eager["entropy"], g, g, grad)
+        torch.cuda.synchronize()
+        i = 0
+        for n in once:
+            for b in range(4):
+                k = len(ref.entries(a, b))
+                assert torch.equal(once[n][b, :k], eager[n][b, :k]), n
+                i += k
+        assert i and torch.equal(first, grad)

@@ -575,7 +575,8 @@ int switchsd_store_cache(const void *keys, int64_t key_stride, const void *value
  *   (drafted: B * R).  scale multiplies the products of queries and keys.
  *   D is 64, 128 or 256; Hkv divides Hq <= SWITCHSD_MAX_HEADS; query head h reads
  *   head h / (Hq / Hkv) of the cache.  B <= SWITCHSD_MAX_PLAN_B, R <= 2^20, Lmax <=
- *   2^30, B * max_pages < 2^31, 1 <= page_size <= 65536. */
+ *   2^30, B * max_pages < 2^31, 1 <= page_size <= 65536; shapes that would take
+ *   2^24 work-groups or more (of 32 rows and query heads and more) are refused. */
 typedef struct {
     int32_t B, R, rows, Hq, Hkv, D;
     int32_t Lmax, page_size, max_pages;
@@ -634,7 +635,17 @@ typedef struct {
     const int32_t *tokens;
     const int32_t *dn, *dpar, *accept_node;
     float temperature;
+    void *workspace;        /* switchsd_logprob_workspace_bytes bytes, or NULL */
+    size_t workspace_bytes;
 } switchsd_logprob_args;
+
+/* With few rows each is cut into pieces that work-groups take side by side and the
+ * last of them joins; that needs this many bytes, 256-byte aligned, zeroed once by the
+ * caller (every call leaves them zeroed, so calls of different shapes may follow each
+ * other in one workspace of the largest size; calls that overlap in time may not
+ * share it).  0 where no row is cut, and for sizes that are refused.  Without a
+ * workspace no row is cut: the results differ in the order of their sums alone. */
+size_t switchsd_logprob_workspace_bytes(const switchsd_logprob_args *args);
 
 /* With z = logits / temperature of the entry's row:
  *   lse = log of the sum of exp(z), logprob = z[token] - lse,
@@ -666,6 +677,8 @@ int switchsd_token_logprobs(const switchsd_logprob_args *args, float *logprob, f
  *   lse [B, R] float; g_logprob [B, R] float or NULL; g_entropy [B, R] float or
  *   NULL, with entropy [B, R]; tokens may be NULL without g_logprob; grad [B, R, V]
  *   of logits_type, rounded once: apart from the logits or the logits themselves.
+ *   Shapes that would take 2^24 work-groups or more (16 KB of a row each) are
+ *   refused.
  *   Rows without an entry are neither read nor written.  One launch. */
 int switchsd_token_logprobs_grad(const switchsd_logprob_args *args, const float *lse,
                                  const float *entropy, const float *g_logprob,

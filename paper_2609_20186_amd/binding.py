@@ -35,6 +35,7 @@ EXPORTS = ("switchsd_ngram_match", "switchsd_probe_score", "switchsd_select_draf
            "switchsd_span_slots", "switchsd_compact_cache", "switchsd_store_cache",
            "switchsd_paged_attention", "switchsd_attention_workspace_bytes",
            "switchsd_token_logprobs", "switchsd_token_logprobs_grad",
+           "switchsd_logprob_workspace_bytes",
            "switchsd_test_withhold_probe_flag", "switchsd_test_withhold_segment",
            "switchsd_status_string")
 
@@ -111,7 +112,8 @@ class AttentionArgs(ctypes.Structure):
 class LogprobArgs(ctypes.Structure):
     _fields_ = [("logits", _P), ("logits_type", _I), ("B", _I), ("R", _I), ("V", _I),
                 ("tokens", _P), ("dn", _P), ("dpar", _P), ("accept_node", _P),
-                ("temperature", ctypes.c_float)]
+                ("temperature", ctypes.c_float), ("workspace", _P),
+                ("workspace_bytes", ctypes.c_size_t)]
 
 
 def _load():
@@ -157,6 +159,8 @@ def _load():
     lib.switchsd_attention_workspace_bytes.restype = S
     lib.switchsd_token_logprobs.argtypes = [ctypes.POINTER(LogprobArgs), _P, _P, _P, _P, _I, _P,
                                             _P, _P]
+    lib.switchsd_logprob_workspace_bytes.argtypes = [ctypes.POINTER(LogprobArgs)]
+    lib.switchsd_logprob_workspace_bytes.restype = S
     lib.switchsd_token_logprobs_grad.argtypes = [ctypes.POINTER(LogprobArgs), _P, _P, _P, _P, _P,
                                                  _P]
     for knob in ("switchsd_test_withhold_probe_flag", "switchsd_test_withhold_segment"):
@@ -823,12 +827,13 @@ def switchsd_paged_attention(args, q, k_cache, v_cache, out, workspace, lse=None
 # ------------------------------------------------------------------ log probabilities
 
 def build_logprob_args(logits, tokens=None, dn=None, dpar=None, accept_node=None,
-                       temperature=1.0):
+                       temperature=1.0, workspace=None):
     """LogprobArgs for switchsd_token_logprobs and its gradient: logits [B, R, V]
     (bf16 or its bits, fp16 or fp32), tokens [B, R] int32 (None where neither logprob
     nor rank is wanted), dn [B] (None: all rows); with accept_node [B], and dpar [B, R]
     (None: chains), the rows along each accepted path, tokens being the step's
-    out_tokens.  The tensors are kept alive by the result."""
+    out_tokens.  workspace: zeroed, of logprob_workspace_bytes, None: one of its own; switchsd_token_logprobs calls that share it (the result too) must be
+    ordered.  The tensors are kept alive by the result."""
     if not isinstance(logits, _Tensor) or logits.dim() != 3:
         raise ValueError("logits must be a device tensor [B, R, V]")
     B, R, V = logits.shape
@@ -845,9 +850,23 @@ def build_logprob_args(logits, tokens=None, dn=None, dpar=None, accept_node=None
     a.dpar = _arr(dpar, "i32", "dpar", (B, R), dev, True)
     a.accept_node = _arr(accept_node, "i32", "accept_node", (B,), dev, True)
     a.temperature = float(temperature)
+    need = logprob_workspace_bytes(a)
+    if workspace is None and need:
+        workspace = torch.zeros(need, dtype=torch.uint8, device=logits.device)
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = _workspace(workspace, dev), workspace.numel()
     a.shape, a.device = (B, R, V), dev
-    a.keep = (logits, tokens, dn, dpar, accept_node)
+    a.keep = (logits, tokens, dn, dpar, accept_node, workspace)
     return a
+
+
+def logprob_workspace_bytes(args):
+    return int(lib.switchsd_logprob_workspace_bytes(ctypes.byref(args)))
+
+
+def alloc_logprob_workspace(args, device="cuda"):
+    """Zeroed once here; the kernels keep it usable for every later call."""
+    return torch.zeros(max(logprob_workspace_bytes(args), 256), dtype=torch.uint8, device=device)
 
 
 def switchsd_token_logprobs(args, logprob=None, lse=None, entropy=None, rank=None, top_ids=None,

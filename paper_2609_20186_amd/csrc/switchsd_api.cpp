@@ -1374,6 +1374,16 @@ int check_logprobs(const switchsd_logprob_args *a) {
 
 extern "C" {
 
+size_t switchsd_logprob_workspace_bytes(const switchsd_logprob_args *a) {
+    if (!a || a->B < 1 || a->R < 1 || a->V < 1 || !launch_ok((int64_t)a->B * a->R))
+        return 0;
+    const LogprobCut cut = logprob_cut(*a, true);
+    if (cut.pieces == 1)
+        return 0;
+    const size_t n = (size_t)a->B * a->R;
+    return round_line(n * sizeof(uint32_t)) + n * cut.pieces * kLogprobRecord;
+}
+
 int switchsd_token_logprobs(const switchsd_logprob_args *a, float *logprob, float *lse,
                             float *entropy, int32_t *rank, int32_t n_top, int32_t *top_ids,
                             float *top_logprobs, hipStream_t stream) {
@@ -1390,6 +1400,9 @@ int switchsd_token_logprobs(const switchsd_logprob_args *a, float *logprob, floa
         return SWITCHSD_EINVAL;
     if (!logprob && !lse && !entropy && !rank && n_top == 0)
         return SWITCHSD_EINVAL;
+    if (a->workspace && (!aligned(a->workspace, kAlign) ||
+                         a->workspace_bytes < switchsd_logprob_workspace_bytes(a)))
+        return SWITCHSD_EWORKSPACE;
     LogprobParams p;
     memset(&p, 0, sizeof p);
     p.a = *a;
@@ -1401,6 +1414,10 @@ int switchsd_token_logprobs(const switchsd_logprob_args *a, float *logprob, floa
     p.n_top = n_top;
     p.top_ids = top_ids;
     p.top_logprobs = top_logprobs;
+    if (a->workspace) {
+        p.tickets = (uint32_t *)a->workspace;
+        p.records = (char *)a->workspace + round_line((size_t)a->B * a->R * sizeof(uint32_t));
+    }
     return launch_logprob_kernel(p, stream);
 }
 

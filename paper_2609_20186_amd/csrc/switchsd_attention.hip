@@ -1078,7 +1078,7 @@ int launch_attend(AttnParams p, hipStream_t stream) {
     const int64_t len = (int64_t)p.a.Lmax + p.a.R;
     p.whole = (len < cap ? len : cap) <= kAttnShort;
     const int64_t groups = p.whole || items > kAttnGroups ? items : kAttnGroups;
-    if (groups > 0x7FFFFFFFll)
+    if (groups >= 1 << 24)
         return SWITCHSD_ESHAPE;
     const dim3 g((unsigned)groups), t(kThreads);
     if (tile == 32) {

@@ -324,6 +324,31 @@ int launch_attention_kernel(const AttnParams &p, int32_t type, int32_t cache_typ
 
 // ---- log probabilities (switchsd_logprobs.hip)
 
+// Along accepted paths a sequence has few entries: work-groups for 8 of them, each of
+// which takes every eighth.
+inline int32_t logprob_slots(const switchsd_logprob_args &a) {
+    return a.accept_node && a.R > 8 ? 8 : a.R;
+}
+// Pieces of a row, for about kLogprobGroups work-groups together; a piece is at
+// least two vectors of each lane.
+constexpr int kLogprobGroups = 1024;
+constexpr int kLogprobPieces = 64;
+constexpr size_t kLogprobRecord = 16 + 8 * SWITCHSD_MAX_TOP;
+struct LogprobCut {
+    int32_t pieces, vecs;
+};
+inline LogprobCut logprob_cut(const switchsd_logprob_args &a, bool may) {
+    const int64_t rows = (int64_t)a.B * logprob_slots(a);
+    const int64_t per = a.logits_type == SWITCHSD_F32 ? 4 : 8;
+    const int64_t vecs = (a.V + per - 1) / per, least = 2 * kThreads;
+    int64_t n = may && rows > 0 ? kLogprobGroups / rows : 1;
+    n = n < vecs / least ? n : vecs / least;
+    n = n < kLogprobPieces ? n : kLogprobPieces;
+    n = n > 1 ? n : 1;
+    const int64_t each = ((vecs + n - 1) / n + kThreads - 1) / kThreads * kThreads;
+    return {(int32_t)((vecs + each - 1) / each), (int32_t)each};
+}
+
 struct LogprobParams {
     switchsd_logprob_args a;
     float inv_t;  // 1 / temperature
@@ -332,6 +357,11 @@ struct LogprobParams {
     int32_t n_top;
     int32_t *top_ids;
     float *top_logprobs;
+    int32_t slots;      // entries of a sequence that are taken side by side
+    int32_t pieces;     // of a row, piece_vecs vectors each
+    int32_t piece_vecs;
+    uint32_t *tickets;  // [B, R], with the records of a cut row's pieces
+    void *records;      // [B, R, pieces]
     // gradient
     const float *in_lse, *in_entropy, *g_logprob, *g_entropy;
     void *grad;

@@ -13,218 +13,733 @@ namespace switchsd {
 
 namespace {
 
-constexpr int kWaves = kThreads / 64;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// ---- elements
 
 template <int TYPE>
-__device__ __forceinline__ float load_logit(const void *base, int64_t at) {
+constexpr int kPerVec = TYPE == SWITCHSD_F32 ? 4 : 8;  // elements of 16 bytes
+template <int TYPE>
+constexpr int kSize = TYPE == SWITCHSD_F32 ? 4 : 2;
+
+typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
+typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
+
+// Rows stand at any element's address; so do their vectors.
+template <int TYPE>
+__device__ __forceinline__ u32x4 load_vec(const char *row, int64_t vec) {
     if (TYPE == SWITCHSD_F32)
-        return ((const float *)base)[at];
-    const uint16_t v = ((const uint16_t *)base)[at];
+        return *(const u32x4_a4 *)(row + vec * 16);
+    return *(const u32x4_a2 *)(row + vec * 16);
+}
+
+template <int TYPE>
+__device__ __forceinline__ float element(u32x4 x, int e) {
+    if (TYPE == SWITCHSD_F32)
+        return __builtin_bit_cast(float, (uint32_t)x[e]);
+    if (TYPE == SWITCHSD_BF16)
+        return __builtin_bit_cast(float, e % 2 ? x[e / 2] & 0xFFFF0000u : x[e / 2] << 16);
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)(x[e / 2] >> (e % 2 * 16)));
+}
+
+template <int TYPE>
+__device__ __forceinline__ float load_logit(const char *row, int64_t at) {
+    if (TYPE == SWITCHSD_F32)
+        return ((const float *)row)[at];
+    const uint16_t v = ((const uint16_t *)row)[at];
     if (TYPE == SWITCHSD_BF16)
         return __builtin_bit_cast(float, (uint32_t)v << 16);
     return (float)__builtin_bit_cast(_Float16, v);
 }
 
 template <int TYPE>
-__device__ __forceinline__ void store_logit(void *base, int64_t at, float v) {
+__device__ __forceinline__ void store_logit(char *row, int64_t at, float v) {
     if (TYPE == SWITCHSD_F32)
-        ((float *)base)[at] = v;
+        ((float *)row)[at] = v;
     else if (TYPE == SWITCHSD_BF16)
-        ((uint16_t *)base)[at] = __builtin_bit_cast(uint16_t, (__bf16)v);
+        ((uint16_t *)row)[at] = __builtin_bit_cast(uint16_t, (__bf16)v);
     else
-        ((uint16_t *)base)[at] = __builtin_bit_cast(uint16_t, (_Float16)v);
+        ((uint16_t *)row)[at] = __builtin_bit_cast(uint16_t, (_Float16)v);
 }
 
-// The row of entry (b, i), or -1 where there is none.
-__device__ __forceinline__ int entry_row(const switchsd_logprob_args &a, int b, int i) {
-    const int n = a.dn ? clampi(a.dn[b], 1, a.R) : a.R;
-    if (!a.accept_node)
-        return i < n ? i : -1;
-    const int last = a.accept_node[b];
-    if (last < 0 || last >= n)
-        return -1;
-    if (!a.dpar)
-        return i <= last ? i : -1;
-    // the path's depth, then its i-th node
-    int depth = 0;
-    for (int x = last; x > 0; ++depth) {
-        const int up = a.dpar[(int64_t)b * a.R + x];
-        if (up < 0 || up >= x)
-            return -1;
-        x = up;
+// The vector behind the last whole one, NaN where there is nothing.
+template <int TYPE>
+__device__ __forceinline__ u32x4 load_last(const char *row, int64_t vec, int V) {
+    u32x4 x = u32x4{~0u, ~0u, ~0u, ~0u};
+    for (int e = 0; e < kPerVec<TYPE>; ++e) {
+        const int64_t v = vec * kPerVec<TYPE> + e;
+        if (v >= V)
+            break;
+        if (TYPE == SWITCHSD_F32)
+            x[e] = ((const uint32_t *)row)[v];
+        else
+            x[e / 2] = (x[e / 2] & ~(0xFFFFu << (e % 2 * 16))) |
+                       (uint32_t)((const uint16_t *)row)[v] << (e % 2 * 16);
     }
-    if (i > depth)
-        return -1;
-    int x = last;
-    for (int d = depth; d > i; --d)
-        x = a.dpar[(int64_t)b * a.R + x];
     return x;
 }
 
-// Keys that order logits: larger first, then the lower index; NaN behind all
-// numbers.  Never 0.
+// Keys that order logits: larger first (-0 as 0), NaN behind all numbers as 0.
+__device__ __forceinline__ uint32_t order_of(float l) {
+    if (!(l == l))
+        return 0;
+    const uint32_t u = __builtin_bit_cast(uint32_t, l + 0.0f);
+    return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+constexpr uint32_t kMinusInf = ~0xFF800000u;  // order_of(-inf)
+// With the lower index first among equals.  Never 0.
 __device__ __forceinline__ unsigned long long order_key(float l, uint32_t v) {
-    uint32_t s = 0;
-    if (l == l) {
-        const uint32_t u = __builtin_bit_cast(uint32_t, l + 0.0f);
-        s = (u & 0x80000000u) ? ~u : u | 0x80000000u;
-    }
-    return ((unsigned long long)s << 32) | (0xFFFFFFFFu - v);
+    return (unsigned long long)order_of(l) << 32 | (0xFFFFFFFFu - v);
 }
-
-__device__ __forceinline__ unsigned long long block_max(unsigned long long v,
-                                                        unsigned long long *sh) {
-    for (int x = 32; x; x >>= 1) {
-        const unsigned long long o = __shfl_xor(v, x);
-        v = o > v ? o : v;
-    }
-    if ((threadIdx.x & 63) == 0)
-        sh[threadIdx.x >> 6] = v;
-    __syncthreads();
-    for (int w = 0; w < kWaves; ++w)
-        v = sh[w] > v ? sh[w] : v;
-    __syncthreads();
-    return v;
-}
-
-__device__ __forceinline__ double block_sum(double v, double *sh) {
-    for (int x = 32; x; x >>= 1)
-        v += __shfl_xor(v, x);
-    if ((threadIdx.x & 63) == 0)
-        sh[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0.0;
-    for (int w = 0; w < kWaves; ++w)
-        v += sh[w];
-    __syncthreads();
-    return v;
-}
-
 __device__ __forceinline__ float key_logit(unsigned long long key) {
     const uint32_t s = (uint32_t)(key >> 32);
     return __builtin_bit_cast(float, s == 0 ? 0x7FC00000u : (s >> 31) ? s & 0x7FFFFFFFu : ~s);
 }
-__device__ __forceinline__ uint32_t key_token(unsigned long long key) {
+__device__ __forceinline__ uint32_t key_index(unsigned long long key) {
     return 0xFFFFFFFFu - (uint32_t)key;
 }
 
-// A work-group per entry.
+// ---- entries
+
+// A sequence's entries: how many, and entry i's row.  Along a path: the walk from
+// accept_node to the anchor leaves its nodes in LDS, over which every lane goes
+// alike (a parent lies before its node, so a path has no more nodes than
+// accept_node + 1).
+struct Entries {
+    int n;
+    bool walked;
+};
+__device__ __forceinline__ Entries entries_of(const switchsd_logprob_args &a, int b, int from,
+                                              uint16_t *parents, uint16_t *path) {
+    const int n = a.dn ? clampi(a.dn[b], 1, a.R) : a.R;
+    if (!a.accept_node)
+        return {n, false};
+    const int last = a.accept_node[b];
+    if (last < 0 || last >= n || from > last)
+        return {0, false};
+    if (!a.dpar)
+        return {last + 1, false};
+    for (int x = threadIdx.x; x <= last; x += kThreads) {
+        const int up = a.dpar[(int64_t)b * a.R + x];
+        parents[x] = (uint16_t)(up >= 0 && up < x ? up : 0xFFFF);
+    }
+    __syncthreads();
+    int depth = 0;
+    for (int x = last; x > 0; ++depth) {
+        path[depth] = (uint16_t)x;
+        x = parents[x];
+        if (x == 0xFFFF)
+            return {0, false};
+    }
+    return {depth + 1, true};
+}
+__device__ __forceinline__ int row_of(const Entries &n, int i, const uint16_t *path) {
+    return !n.walked || i == 0 ? i : path[n.n - 1 - i];
+}
+
+// ---- log probabilities
+
+// What a lane (then a wave, then all) has seen of a row: weights 2^((l - ref) c)
+// against a reference of its own that follows its largest logit with a delay, their
+// sum and the sum of weight times exponent; the largest logit and the vector
+// it was first seen in (none while there is no number above -inf).
+struct Sums {
+    float ref, lim, s, t, mx;
+    int vec;
+};
+// A reference is moved when a weight would pass 2^kDelay.
+constexpr float kDelay = 20.0f;
+
+template <int TYPE>
+__device__ __forceinline__ void take(Sums &a, u32x4 x, int vec, float c, float delay) {
+    constexpr int N = kPerVec<TYPE>;
+    float f[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+        f[e] = element<TYPE>(x, e);
+    float top = f[0];  // NaN only if all are
+#pragma unroll
+    for (int e = 1; e < N; ++e)
+        top = fmaxf(top, f[e]);
+    const bool up = top > a.mx;
+    a.mx = up ? top : a.mx;
+    a.vec = up ? vec : a.vec;
+    if (__any(top > a.lim)) {
+        const float ref = fmaxf(a.ref, top);
+        const float d = a.ref == -INFINITY ? 0.0f : (a.ref - ref) * c;
+        const float f2 = __builtin_amdgcn_exp2f(d);
+        a.t = f2 * (a.t + a.s * d);
+        a.s *= f2;
+        a.ref = ref;
+        a.lim = ref + delay;
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        // NaN (and -inf beside itself) weighs nothing: the maximum drops it
+        const float y = fmaxf((f[e] - a.ref) * c, -150.0f);
+        const float w = __builtin_amdgcn_exp2f(y);
+        a.s += w;
+        a.t = fmaf(w, y, a.t);
+    }
+}
+
+// How many elements of a wave's vectors are ahead of a number above -inf: those
+// above the lane's threshold.
+template <int TYPE>
+__device__ __forceinline__ int above(u32x4 x, float bar) {
+    int n = 0;
+#pragma unroll
+    for (int e = 0; e < kPerVec<TYPE>; ++e)
+        n += __popcll(__ballot(element<TYPE>(x, e) > bar));
+    return n;
+}
+// The same of -inf or NaN: every number above -inf; of the vectors before the given
+// token's, -inf too, and before a NaN everything.
+template <int TYPE>
+__device__ __forceinline__ int above_low(u32x4 x, float lt, bool before) {
+    int n = 0;
+#pragma unroll
+    for (int e = 0; e < kPerVec<TYPE>; ++e) {
+        const float l = element<TYPE>(x, e);
+        n += __popcll(__ballot(lt == lt ? (before ? l >= lt : l > lt) : before || l == l));
+    }
+    return n;
+}
+
+// The next number below x (finite or +inf), where the order of logits is meant: 0
+// and -0 are one.
+__device__ __forceinline__ float below(float x) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    return __builtin_bit_cast(float, x == 0.0f ? 0x80000001u : x > 0.0f ? u - 1 : u + 1);
+}
+
+// Sums against reference `from`, against `to` (not below it).
+__device__ __forceinline__ void move(float &s, float &t, float from, float to, float c) {
+    const float d = s > 0.0f ? (from - to) * c : 0.0f;
+    const float f = __builtin_amdgcn_exp2f(d);
+    t = f * (t + s * d);
+    s *= f;
+}
+
+constexpr int kWaves = kThreads / 64;
+constexpr int kList = 2048;    // candidates in LDS
+constexpr int kGroups = 128;   // pairs of lanes whose largest logits are compared
+static_assert(kGroups * 2 == kThreads && SWITCHSD_MAX_TOP <= kGroups, "a group each");
+
+struct Selection {
+    unsigned long long firsts[kGroups], list[kList], best[SWITCHSD_MAX_TOP], bar;
+    uint16_t winner[kGroups];
+    int count, winners, counts[kWaves];
+    unsigned long long red[kWaves];
+};
+
+// Largest of the lanes' keys.
+__device__ __forceinline__ unsigned long long block_max(unsigned long long v,
+                                                        unsigned long long *red) {
+    for (int d = 32; d; d >>= 1) {
+        const unsigned long long o = __shfl_xor(v, d);
+        v = o > v ? o : v;
+    }
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0)
+        red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w)
+        v = red[w] > v ? red[w] : v;
+    return v;
+}
+
+// The list's k first keys, in order, to best; 0 behind the last.
+__device__ __forceinline__ void rank_list(Selection &sel, int count, int k) {
+    for (int x = threadIdx.x; x < k; x += kThreads)
+        if (x >= count)
+            sel.best[x] = 0;
+    for (int x = threadIdx.x; x < count; x += kThreads) {
+        const unsigned long long mine = sel.list[x];
+        int n = 0;
+#pragma unroll 4
+        for (int y = 0; y < count; ++y)
+            n += sel.list[y] > mine ? 1 : 0;
+        if (n < k)
+            sel.best[n] = mine;
+    }
+    __syncthreads();
+}
+
+// The k first tokens of the row's vectors [j0, j1), in order, to sel.best (0 where
+// there are fewer).  The largest logits of 128 pairs of lanes, in sel.firsts, were
+// compared: the k-th of them bounds the first tokens from below, and each of
+// them lies in one of the k first pairs, so only those pairs' vectors are read again.
+template <int TYPE>
+__device__ __forceinline__ void select(Selection &sel, const char *row, int V, int j0, int j1,
+                                       int k) {
+    constexpr int N = kPerVec<TYPE>;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, full = V / N;
+    const int v0 = j0 * N, v1 = j1 * N < V ? j1 * N : V;
+    {
+        const unsigned long long mine = sel.firsts[tid / 2];
+        const ulonglong2 *all = (const ulonglong2 *)sel.firsts + tid % 2 * (kGroups / 4);
+        int n = 0;
+#pragma unroll 8
+        for (int g = 0; g < kGroups / 4; ++g) {
+            const ulonglong2 o = all[g];
+            n += (o.x > mine ? 1 : 0) + (o.y > mine ? 1 : 0);
+        }
+        n += __shfl_xor(n, 1);
+        if (mine && tid % 2 == 0 && n < k) {
+            sel.winner[atomicAdd(&sel.winners, 1)] = (uint16_t)(tid / 2);
+            if (n == k - 1)
+                sel.bar = mine;
+        }
+    }
+    __syncthreads();
+    // with fewer than k pairs that hold a number above -inf, every such number is a
+    // candidate; else the elements whose (logit, vector) is not behind the k-th's
+    const int winners = sel.winners;
+    const unsigned long long bar =
+        winners < k ? (unsigned long long)(kMinusInf + 1) << 32 : sel.bar;
+    const int rounds = (j1 - j0 + kThreads - 1) / kThreads, per = rounds * 2;
+    for (int x = tid; x < winners * per; x += kThreads) {
+        const int w = x / per, y = x - w * per;
+        const int j = j0 + y / 2 * kThreads + sel.winner[w] * 2 + y % 2;
+        if (j >= j1)
+            continue;
+        const u32x4 q = j < full ? load_vec<TYPE>(row, j) : load_last<TYPE>(row, j, V);
+        unsigned take = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float l = element<TYPE>(q, e);
+            take |= l == l && order_key(l, j) >= bar ? 1u << e : 0u;
+        }
+        while (take) {
+            const int e = __builtin_ctz(take);
+            take &= take - 1;
+            const int at = atomicAdd(&sel.count, 1);
+            if (at < kList)
+                sel.list[at] = order_key(load_logit<TYPE>(row, j * N + e), j * N + e);
+        }
+    }
+    __syncthreads();
+    int count = sel.count;
+    if (count > kList) {
+        // more equal or rising candidates than fit: the next one behind the last,
+        // k times over the vectors
+        unsigned long long last = ~0ull;
+        for (int n = 0; n < k; ++n) {
+            unsigned long long next = 0;
+            for (int v = v0 + tid; v < v1; v += kThreads) {
+                const unsigned long long key = order_key(load_logit<TYPE>(row, v), v);
+                next = key < last && key > next ? key : next;
+            }
+            last = block_max(next, sel.red);
+            if (tid == 0)
+                sel.best[n] = last;
+        }
+        __syncthreads();
+        return;
+    }
+    // too few numbers: -inf by their index, then NaN by theirs
+    for (int what = 0; what < 2 && count < k; ++what) {
+        for (int base = v0; base < v1 && count < k; base += kThreads) {
+            const int v = base + tid;
+            const float l = v < v1 ? load_logit<TYPE>(row, v) : 0.0f;
+            const bool hit = v < v1 && (what == 0 ? l == -INFINITY : !(l == l));
+            const unsigned long long w = __ballot(hit);
+            __syncthreads();
+            if (lane == 0)
+                sel.counts[wave] = __popcll(w);
+            __syncthreads();
+            int at = count + __popcll(w & ((1ull << lane) - 1));
+            for (int x = 0; x < kWaves; ++x) {
+                at += x < wave ? sel.counts[x] : 0;
+                count += sel.counts[x];
+            }
+            if (hit && at < k)
+                sel.list[at] = order_key(l, v);
+        }
+        count = count < k ? count : k;
+    }
+    __syncthreads();
+    rank_list(sel, count, k);
+}
+
+// What the pieces of a cut row leave: sums, and the first tokens.
+struct Record {
+    unsigned long long sums[2];  // (largest, s), (t, ahead)
+    unsigned long long best[SWITCHSD_MAX_TOP];
+};
+static_assert(sizeof(Record) == kLogprobRecord, "size of a piece's record");
+
+__device__ __forceinline__ unsigned long long pair64(float a, uint32_t b) {
+    return (unsigned long long)__builtin_bit_cast(uint32_t, a) << 32 | b;
+}
+__device__ __forceinline__ float high(unsigned long long v) {
+    return __builtin_bit_cast(float, (uint32_t)(v >> 32));
+}
+
+// Entry (b, i) of the sequence's entries i = s, s + S, ..: a work-group reads a
+// row, or with few rows one of `pieces` pieces of it, once; of a cut row the last
+// work-group to arrive joins the pieces.  About 13 lane operations an element, the
+// exponential among them, which at full rate is what 5 to 6 TB/s of 16-bit logits
+// bring: a row is cut rather than left to one compute unit.
 template <int TYPE>
 __global__ void __launch_bounds__(kThreads) k_logprob(const LogprobParams p) {
+    constexpr int N = kPerVec<TYPE>;
+    constexpr int U = 4;  // vectors in flight per lane
     const switchsd_logprob_args &a = p.a;
-    __shared__ unsigned long long sk[kWaves];
-    __shared__ double sd[kWaves];
-    const int64_t e = blockIdx.x;
-    const int b = e / a.R, i = e % a.R, tid = threadIdx.x;
-    const int r = entry_row(a, b, i);
-    if (r < 0)
-        return;
-    const int64_t row = ((int64_t)b * a.R + r) * a.V;
-    unsigned long long best = 0;
-    for (int v = tid; v < a.V; v += kThreads) {
-        const unsigned long long k = order_key(load_logit<TYPE>(a.logits, row + v), v);
-        best = k > best ? k : best;
-    }
-    best = block_max(best, sk);
-    const float m = key_logit(best);
-    const bool flat = !(fabsf(m) < INFINITY);  // no finite maximum: one-hot
-    const int tok = a.tokens ? a.tokens[e] : -1;
-    const bool in = tok >= 0 && tok < a.V;
-    const float lt = in ? load_logit<TYPE>(a.logits, row + tok) : 0.0f;
-    const unsigned long long kt = in ? order_key(lt, tok) : 0;
-    double s = 0.0, t = 0.0, ahead = 0.0;
-    for (int v = tid; v < a.V; v += kThreads) {
-        const float l = load_logit<TYPE>(a.logits, row + v);
-        ahead += order_key(l, v) > kt ? 1.0 : 0.0;
-        const float x = (l - m) * p.inv_t, w = l == l && !flat ? expf(x) : 0.0f;
-        s += w;
-        t += w > 0.0f ? (double)w * x : 0.0;
-    }
-    s = block_sum(s, sd);
-    t = block_sum(t, sd);
-    ahead = block_sum(ahead, sd);
-    const float ls = flat ? 0.0f : (float)log(s);
-    const uint32_t greedy = key_token(best);
-    const auto logprob = [&](float l, uint32_t v) {
-        if (flat)
-            return v == greedy ? 0.0f : -INFINITY;
-        return l == l ? (l - m) * p.inv_t - ls : -INFINITY;
-    };
-    if (tid == 0) {
-        if (p.logprob)
-            p.logprob[e] = in ? logprob(lt, tok) : -INFINITY;
-        if (p.lse)
-            p.lse[e] = m != m ? -INFINITY : flat ? m : m * p.inv_t + ls;
-        if (p.entropy)
-            p.entropy[e] = flat ? 0.0f : (float)(log(s) - t / s);
-        if (p.rank)
-            p.rank[e] = in ? (int)ahead : -1;
-    }
-    for (int j = 0; j < p.n_top; ++j) {
-        if (j > 0) {
-            unsigned long long next = 0;
-            for (int v = tid; v < a.V; v += kThreads) {
-                const unsigned long long k = order_key(load_logit<TYPE>(a.logits, row + v), v);
-                next = k < best && k > next ? k : next;
+    __shared__ uint16_t parents[SWITCHSD_MAX_R], path[SWITCHSD_MAX_R];
+    __shared__ float4 sums[kWaves];
+    __shared__ Selection sel;
+    __shared__ int s_last;
+    const int piece = (int)(blockIdx.x % p.pieces);
+    const int64_t of = blockIdx.x / p.pieces;
+    const int b = (int)(of / p.slots), s0 = (int)(of % p.slots);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const Entries all = entries_of(a, b, s0, parents, path);
+    const int V = a.V, full = V / N, nv = (V + N - 1) / N, k = p.n_top;
+    const int j0 = piece * p.piece_vecs;
+    const int j1 = j0 + p.piece_vecs < nv ? j0 + p.piece_vecs : nv;
+    const int whole = j1 < full ? j1 : full;
+    const float c = p.inv_t * kLog2e, delay = kDelay / c;
+    const u32x4 nothing = u32x4{~0u, ~0u, ~0u, ~0u};  // NaN in every type
+
+    for (int i = s0; i < all.n; i += p.slots) {
+        const int64_t e = (int64_t)b * a.R + i;
+        const char *row = (const char *)a.logits +
+                          ((int64_t)b * a.R + row_of(all, i, path)) * V * kSize<TYPE>;
+        const int tok = a.tokens ? a.tokens[e] : -1;
+        const bool in = tok >= 0 && tok < V;
+        const float lt = in ? load_logit<TYPE>(row, tok) : 0.0f;
+        // tokens ahead of the given one: equal ones count before it, not behind;
+        // its own vector is looked at by itself
+        const bool ranked = p.rank && in;
+        const bool easy = lt > -INFINITY;  // not NaN, not -inf
+        const float below_lt = easy ? below(lt) : 0.0f;
+        const int own = tok / N;
+
+        __syncthreads();  // the last entry's use of LDS
+        if (tid == 0)
+            sel.count = sel.winners = 0;
+        Sums m = {-INFINITY, -INFINITY, 0.0f, 0.0f, -INFINITY, -1};
+        int ahead = 0;
+        const auto use = [&](u32x4 x, int j) {
+            take<TYPE>(m, x, j, c, delay);
+            if (!ranked)
+                return;
+            if (easy)
+                ahead += above<TYPE>(x, j < own ? below_lt : j > own ? lt : INFINITY);
+            else
+                ahead += above_low<TYPE>(j == own ? nothing : x, lt, j < own);
+        };
+        for (int at = j0; at < whole; at += kThreads * U) {
+            u32x4 x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int j = at + u * kThreads + tid;
+                x[u] = nothing;
+                if (j < whole)
+                    x[u] = load_vec<TYPE>(row, j);
             }
-            best = block_max(next, sk);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (at + u * kThreads + wave * 64 < whole)
+                    use(x[u], at + u * kThreads + tid < whole ? at + u * kThreads + tid : INT32_MAX);
         }
+        if (j1 > full) {
+            const int at = (full - j0) % kThreads;  // the lane whose turn it is
+            if (at / 64 == wave)
+                use(at == tid ? load_last<TYPE>(row, full, V) : nothing,
+                    at == tid ? full : INT32_MAX);
+        }
+        if (ranked && wave == 0 && own >= j0 && own < j1) {
+            const int v = own * N + lane;
+            const bool here = lane < N && v < V;
+            const float l = here ? load_logit<TYPE>(row, v) : 0.0f;
+            ahead += __popcll(__ballot(here && order_key(l, v) > order_key(lt, tok)));
+        }
+
+        // the wave's sums against its largest logit
+        float mx = m.mx;
+#pragma unroll
+        for (int d = 32; d; d >>= 1)
+            mx = fmaxf(mx, __shfl_xor(mx, d));
+        move(m.s, m.t, m.ref, mx, c);
+#pragma unroll
+        for (int d = 32; d; d >>= 1) {
+            m.s += __shfl_xor(m.s, d);
+            m.t += __shfl_xor(m.t, d);
+        }
+        if (k > 0) {
+            unsigned long long first = m.vec < 0 ? 0 : order_key(m.mx, m.vec);
+            const unsigned long long o = __shfl_xor(first, 1);
+            first = o > first ? o : first;
+            if (tid % 2 == 0)
+                sel.firsts[tid / 2] = first;
+        }
+        if (lane == 0)
+            sums[wave] = make_float4(mx, m.s, m.t, __builtin_bit_cast(float, ahead));
+        __syncthreads();
+        float M = sums[0].x, S = 0.0f, t = 0.0f;
+        ahead = 0;
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w)
+            M = fmaxf(M, sums[w].x);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            float4 v = sums[w];
+            move(v.y, v.z, v.x, M, c);
+            S += v.y;
+            t += v.z;
+            ahead += __builtin_bit_cast(int, v.w);
+        }
+        if (k > 0)
+            select<TYPE>(sel, row, V, j0, j1, k);
+
+        if (p.pieces > 1) {
+            Record *const of_row = (Record *)p.records + e * p.pieces;
+            uint32_t *const ticket = p.tickets + e;
+            if (wave == 0) {
+                Record *mine = of_row + piece;
+                if (lane == 0)
+                    st_u64(&mine->sums[0], pair64(M, __builtin_bit_cast(uint32_t, S)));
+                if (lane == 1)
+                    st_u64(&mine->sums[1], pair64(t, (uint32_t)ahead));
+                if (lane < k)
+                    st_u64(&mine->best[lane], sel.best[lane]);
+                const bool last = arrive(ticket, (uint32_t)p.pieces);
+                if (lane == 0)
+                    s_last = last ? 1 : 0;
+            }
+            __syncthreads();
+            if (!s_last)
+                continue;
+            if (tid == 0) {
+                st_u32(ticket, 0);
+                sel.count = 0;
+                sel.bar = ~0ull;
+            }
+            // pieces are few (at most kThreads): a lane for each
+            float pm = -INFINITY, ps = 0.0f, pt = 0.0f;
+            ahead = 0;
+            if (tid < p.pieces) {
+                const unsigned long long x = ld_u64(&of_row[tid].sums[0]);
+                const unsigned long long y = ld_u64(&of_row[tid].sums[1]);
+                pm = high(x);
+                ps = __builtin_bit_cast(float, (uint32_t)x);
+                pt = high(y);
+                ahead = (int)(uint32_t)y;
+            }
+            mx = pm;
+#pragma unroll
+            for (int d = 32; d; d >>= 1)
+                mx = fmaxf(mx, __shfl_xor(mx, d));
+            move(ps, pt, pm, mx, c);
+#pragma unroll
+            for (int d = 32; d; d >>= 1) {
+                ps += __shfl_xor(ps, d);
+                pt += __shfl_xor(pt, d);
+                ahead += __shfl_xor(ahead, d);
+            }
+            if (lane == 0)
+                sums[wave] = make_float4(mx, ps, pt, __builtin_bit_cast(float, ahead));
+            __syncthreads();
+            M = sums[0].x;
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w)
+                M = fmaxf(M, sums[w].x);
+            S = t = 0.0f;
+            ahead = 0;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                float4 v = sums[w];
+                move(v.y, v.z, v.x, M, c);
+                S += v.y;
+                t += v.z;
+                ahead += __builtin_bit_cast(int, v.w);
+            }
+            if (k > 0) {
+                // pieces' first ceil(k / pieces) tokens make k together: the last
+                // of them bounds the row's
+                const int q = (k + p.pieces - 1) / p.pieces - 1;
+                if (tid < p.pieces)
+                    atomicMin(&sel.bar, ld_u64(&of_row[tid].best[q]));
+                __syncthreads();
+                const unsigned long long bar = sel.bar;
+                for (int x = tid; x < p.pieces * k; x += kThreads) {
+                    const unsigned long long key = ld_u64(&of_row[x / k].best[x % k]);
+                    if (key && key >= bar) {
+                        const int at = atomicAdd(&sel.count, 1);
+                        if (at < kList)
+                            sel.list[at] = key;
+                    }
+                }
+                __syncthreads();
+                const int count = sel.count;
+                if (count <= kList) {
+                    rank_list(sel, count, k);
+                } else {
+                    unsigned long long last = ~0ull;
+                    for (int n = 0; n < k; ++n) {
+                        unsigned long long next = 0;
+                        for (int x = tid; x < p.pieces * k; x += kThreads) {
+                            const unsigned long long key = ld_u64(&of_row[x / k].best[x % k]);
+                            next = key < last && key > next ? key : next;
+                        }
+                        last = block_max(next, sel.red);
+                        if (tid == 0)
+                            sel.best[n] = last;
+                    }
+                    __syncthreads();
+                }
+                for (int x = tid; x < p.pieces * k; x += kThreads)
+                    st_u64(&of_row[x / k].best[x % k], 0);
+            }
+            // the workspace is left zeroed
+            for (int x = tid; x < p.pieces * 2; x += kThreads)
+                st_u64(&of_row[x / 2].sums[x % 2], 0);
+        }
+
+        // no finite maximum: all weight on the first one
+        const bool flat = !(fabsf(M) < INFINITY);
+        const float lnS = flat ? 0.0f : __builtin_amdgcn_logf(S) * kLn2;
+        int greedy = 0;
+        if (flat) {
+            unsigned long long first = 0;
+            for (int v = tid; v < V; v += kThreads) {
+                const unsigned long long key = order_key(load_logit<TYPE>(row, v), v);
+                first = key > first ? key : first;
+            }
+            greedy = (int)key_index(block_max(first, sel.red));
+        }
+        const auto logprob = [&](float l, int v) {
+            if (flat)
+                return v == greedy ? 0.0f : -INFINITY;
+            return l == l ? (l - M) * p.inv_t - lnS : -INFINITY;
+        };
         if (tid == 0) {
+            if (p.rank)
+                p.rank[e] = in ? ahead : -1;
+            if (p.logprob)
+                p.logprob[e] = in ? logprob(lt, tok) : -INFINITY;
+            if (p.lse)
+                p.lse[e] = flat ? M : M * p.inv_t + lnS;
+            if (p.entropy)
+                p.entropy[e] = flat ? 0.0f : lnS - t / S * kLn2;
+        }
+        if (tid < k) {
+            const unsigned long long key = sel.best[tid];
+            const int v = (int)key_index(key);
             if (p.top_ids)
-                p.top_ids[e * p.n_top + j] = (int)key_token(best);
+                p.top_ids[e * k + tid] = v;
             if (p.top_logprobs)
-                p.top_logprobs[e * p.n_top + j] = logprob(key_logit(best), key_token(best));
+                p.top_logprobs[e * k + tid] = logprob(key_logit(key), v);
         }
     }
 }
 
+// ---- gradient
+
+// A work-group per entry and piece of its row: one read, one write.
+constexpr int kGradVecs = 4;  // vectors of a lane
 template <int TYPE>
-__global__ void __launch_bounds__(kThreads) k_logprob_grad(const LogprobParams p) {
+__global__ void __launch_bounds__(kThreads) k_logprob_grad(const LogprobParams p, int pieces) {
+    constexpr int N = kPerVec<TYPE>;
     const switchsd_logprob_args &a = p.a;
-    const int64_t e = blockIdx.x;
-    const int b = e / a.R, i = e % a.R;
-    const int r = entry_row(a, b, i);
-    if (r < 0)
+    __shared__ uint16_t parents[SWITCHSD_MAX_R], path[SWITCHSD_MAX_R];
+    const int64_t e = blockIdx.x / pieces;
+    const int piece = (int)(blockIdx.x - e * pieces);
+    const int b = (int)(e / a.R), i = (int)(e % a.R);
+    const Entries all = entries_of(a, b, i, parents, path);
+    if (i >= all.n)
         return;
-    const int64_t row = ((int64_t)b * a.R + r) * a.V;
+    const int V = a.V, full = V / N;
+    const int64_t at = ((int64_t)b * a.R + row_of(all, i, path)) * V * kSize<TYPE>;
+    const char *row = (const char *)a.logits + at;
+    char *out = (char *)p.grad + at;
     const float lse = p.in_lse[e];
     const float g = p.g_logprob ? p.g_logprob[e] : 0.0f;
     const float ge = p.g_entropy ? p.g_entropy[e] : 0.0f;
     const float H = p.g_entropy ? p.in_entropy[e] : 0.0f;
     const int tok = p.g_logprob ? a.tokens[e] : -1;
     const bool flat = !(fabsf(lse) < INFINITY);
-    for (int v = threadIdx.x; v < a.V; v += kThreads) {
-        const float l = load_logit<TYPE>(a.logits, row + v);
-        const float x = l * p.inv_t - lse, w = l == l ? expf(x) : 0.0f;
-        const float d = w > 0.0f ? -w * (g + ge * (x + H)) : 0.0f;
-        store_logit<TYPE>(p.grad, row + v, flat ? 0.0f : (d + (v == tok ? g : 0.0f)) * p.inv_t);
+    const auto slope = [&](float l, int v) {
+        // NaN and -inf weigh nothing: the maximum drops them
+        const float x = fmaxf(fmaf(l, p.inv_t, -lse), -150.0f);
+        const float w = l == l ? __builtin_amdgcn_exp2f(x * kLog2e) : 0.0f;
+        const float d = (v == tok ? g : 0.0f) - w * fmaf(ge, x + H, g);
+        return flat ? 0.0f : d * p.inv_t;
+    };
+    const int j0 = piece * (kThreads * kGradVecs) + threadIdx.x;
+    u32x4 x[kGradVecs];
+#pragma unroll
+    for (int u = 0; u < kGradVecs; ++u)
+        if (j0 + u * kThreads < full)
+            x[u] = load_vec<TYPE>(row, j0 + u * kThreads);
+#pragma unroll
+    for (int u = 0; u < kGradVecs; ++u) {
+        const int j = j0 + u * kThreads;
+        if (j < full) {
+            u32x4 y;
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                const float d = slope(element<TYPE>(x[u], q), j * N + q);
+                if (TYPE == SWITCHSD_F32) {
+                    y[q] = __builtin_bit_cast(uint32_t, d);
+                } else {
+                    const uint16_t h = TYPE == SWITCHSD_BF16
+                                           ? __builtin_bit_cast(uint16_t, (__bf16)d)
+                                           : __builtin_bit_cast(uint16_t, (_Float16)d);
+                    y[q / 2] = q % 2 ? y[q / 2] | (uint32_t)h << 16 : h;
+                }
+            }
+            if (TYPE == SWITCHSD_F32)
+                *(u32x4_a4 *)(out + (int64_t)j * 16) = y;
+            else
+                *(u32x4_a2 *)(out + (int64_t)j * 16) = y;
+        } else if (j == full) {
+            for (int v = full * N; v < V; ++v)
+                store_logit<TYPE>(out, v, slope(load_logit<TYPE>(row, v), v));
+        }
     }
 }
 
 int launched() { return hipGetLastError() == hipSuccess ? SWITCHSD_OK : SWITCHSD_EHIP; }
 
-}  // namespace
-
-int launch_logprob_kernel(const LogprobParams &p, hipStream_t stream) {
-    const dim3 g((unsigned)((int64_t)p.a.B * p.a.R)), t(kThreads);
-    if (p.a.logits_type == SWITCHSD_BF16)
-        hipLaunchKernelGGL((k_logprob<SWITCHSD_BF16>), g, t, 0, stream, p);
-    else if (p.a.logits_type == SWITCHSD_F16)
-        hipLaunchKernelGGL((k_logprob<SWITCHSD_F16>), g, t, 0, stream, p);
-    else
-        hipLaunchKernelGGL((k_logprob<SWITCHSD_F32>), g, t, 0, stream, p);
+template <int TYPE>
+int launch_logprob(LogprobParams p, hipStream_t stream) {
+    p.slots = logprob_slots(p.a);
+    const LogprobCut cut = logprob_cut(p.a, p.records != nullptr);
+    p.pieces = cut.pieces;
+    p.piece_vecs = cut.vecs;
+    const int64_t groups = (int64_t)p.a.B * p.slots * p.pieces;
+    hipLaunchKernelGGL((k_logprob<TYPE>), dim3((unsigned)groups), dim3(kThreads), 0, stream, p);
     return launched();
 }
 
-int launch_logprob_grad_kernel(const LogprobParams &p, hipStream_t stream) {
-    const dim3 g((unsigned)((int64_t)p.a.B * p.a.R)), t(kThreads);
-    if (p.a.logits_type == SWITCHSD_BF16)
-        hipLaunchKernelGGL((k_logprob_grad<SWITCHSD_BF16>), g, t, 0, stream, p);
-    else if (p.a.logits_type == SWITCHSD_F16)
-        hipLaunchKernelGGL((k_logprob_grad<SWITCHSD_F16>), g, t, 0, stream, p);
-    else
-        hipLaunchKernelGGL((k_logprob_grad<SWITCHSD_F32>), g, t, 0, stream, p);
+template <int TYPE>
+int launch_grad(const LogprobParams &p, hipStream_t stream) {
+    const int64_t piece = (int64_t)kThreads * kGradVecs * kPerVec<TYPE>;
+    const int64_t pieces = (p.a.V + piece) / piece;  // with a place behind the last whole vector
+    const int64_t groups = (int64_t)p.a.B * p.a.R * pieces;
+    if (groups >= 1 << 24)
+        return SWITCHSD_ESHAPE;
+    hipLaunchKernelGGL((k_logprob_grad<TYPE>), dim3((unsigned)groups), dim3(kThreads), 0, stream, p,
+                       (int)pieces);
     return launched();
+}
+
+}  // namespace
+
+int launch_logprob_kernel(const LogprobParams &p, hipStream_t stream) {
+    return p.a.logits_type == SWITCHSD_BF16  ? launch_logprob<SWITCHSD_BF16>(p, stream)
+           : p.a.logits_type == SWITCHSD_F16 ? launch_logprob<SWITCHSD_F16>(p, stream)
+                                             : launch_logprob<SWITCHSD_F32>(p, stream);
+}
+
+int launch_logprob_grad_kernel(const LogprobParams &p, hipStream_t stream) {
+    return p.a.logits_type == SWITCHSD_BF16  ? launch_grad<SWITCHSD_BF16>(p, stream)
+           : p.a.logits_type == SWITCHSD_F16 ? launch_grad<SWITCHSD_F16>(p, stream)
+                                             : launch_grad<SWITCHSD_F32>(p, stream);
 }
 
 }  // namespace switchsd

@@ -372,3 +372,25 @@ def test_streams_and_graphs():
                 assert torch.equal(once[n][b, :k], eager[n][b, :k]), n
                 i += k
         assert i and torch.equal(first, grad)
+
+
+def test_one_workspace_for_all_shapes():
+    """Rows cut into pieces: the workspace is left zeroed, so other shapes, paths and
+    numbers of alternatives may follow in it; without one no row is cut."""
+    from paper_2609_20186_amd import binding as sd
+    shapes = [(1, 1, 151936, "bf16", 64), (2, 9, 32000, "f32", 5), (1, 3, 9001, "f16", 1),
+              (1, 1, 151936, "bf16", 0)]
+    made = [make(B, R, V, t, seed=R, kind="blocks", dn=False) for B, R, V, t, _ in shapes]
+    sizes = [sd.logprob_workspace_bytes(args_of(a, 1.0, a["logits"].to(DEV))) for a in made]
+    assert min(sizes) > 0
+    ws = torch.zeros(max(sizes), dtype=torch.uint8, device=DEV)
+    for _ in range(2):
+        for a, (_, _, _, _, k) in zip(made, shapes):
+            logits = a["logits"].to(DEV)
+            args = sd.build_logprob_args(logits, dev(a["tokens"]), workspace=ws)
+            out, _ = run(a, 1.0, k, args=args)
+            check(a, 1.0, k, out, "shared workspace")
+            assert int(ws.count_nonzero()) == 0
+            args.workspace, args.workspace_bytes = None, 0
+            out, _ = run(a, 1.0, k, args=args)
+            check(a, 1.0, k, out, "no workspace")

@@ -543,8 +543,8 @@ int switchsd_compact_cache(void *cache, int32_t planes, int64_t plane_stride, in
  *   they may be parts of one projection's output); slots [n] int64, distinct where
  *   they name a slot (of rows that share one, any or a mixture stays); count [1] int32 on
  *   the device or NULL; k_cache, v_cache [n_slots, Hkv, D] of cache_type (`type` or
- *   SWITCHSD_E4M3); k_scale, v_scale [Hkv] float.  D is 64, 128 or 256, 1 <= Hkv <=
- *   SWITCHSD_MAX_HEADS; keys, values, caches and strides aligned to 16 bytes.
+ *   SWITCHSD_E4M3), n_slots < 2^31; k_scale, v_scale [Hkv] float.  D is 64, 128 or 256,
+ *   1 <= Hkv <= SWITCHSD_MAX_HEADS; keys, values, caches and strides aligned to 16 bytes.
  *   The rows overlap neither cache.  One launch. */
 int switchsd_store_cache(const void *keys, int64_t key_stride, const void *values,
                          int64_t value_stride, int32_t type, const int64_t *slots, int32_t n,
@@ -575,7 +575,7 @@ int switchsd_store_cache(const void *keys, int64_t key_stride, const void *value
  *   (drafted: B * R).  scale multiplies the products of queries and keys.
  *   D is 64, 128 or 256; Hkv divides Hq <= SWITCHSD_MAX_HEADS; query head h reads
  *   head h / (Hq / Hkv) of the cache.  B <= SWITCHSD_MAX_PLAN_B, R <= 2^20, Lmax <=
- *   2^30, B * max_pages < 2^31, 1 <= page_size <= 65536; shapes that would take
+ *   2^30, B * max_pages < 2^31, n_slots < 2^31, 1 <= page_size <= 65536; shapes that would take
  *   2^24 work-groups or more (of 32 rows and query heads and more) are refused. */
 typedef struct {
     int32_t B, R, rows, Hq, Hkv, D;

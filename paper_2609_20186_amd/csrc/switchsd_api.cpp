@@ -1265,7 +1265,7 @@ int switchsd_store_cache(const void *keys, int64_t key_stride, const void *value
     if (!half_type(type) || (cache_type != type && cache_type != SWITCHSD_E4M3))
         return SWITCHSD_EINVAL;
     if (n < 0 || Hkv < 1 || Hkv > SWITCHSD_MAX_HEADS || !head_dim_ok(D) || n_slots < 0 ||
-        n_slots > (1ll << 40) || key_stride < (int64_t)Hkv * D ||
+        n_slots > 0x7FFFFFFFll || key_stride < (int64_t)Hkv * D ||
         value_stride < (int64_t)Hkv * D || key_stride > (1ll << 32) ||
         value_stride > (1ll << 32))
         return SWITCHSD_ESHAPE;
@@ -1317,7 +1317,7 @@ int switchsd_paged_attention(const switchsd_attention_args *a, const void *q, in
         return rc;
     if (a->Lmax < 1 || a->Lmax > (1 << 30) || a->page_size < 1 || a->page_size > 65536 ||
         a->max_pages < 1 || (int64_t)a->B * a->max_pages > 0x7FFFFFFFll || n_slots < 0 ||
-        n_slots > (1ll << 40) || q_stride < (int64_t)a->Hq * a->D || q_stride > (1ll << 32) ||
+        n_slots > 0x7FFFFFFFll || q_stride < (int64_t)a->Hq * a->D || q_stride > (1ll << 32) ||
         (!a->cu && a->rows != (int64_t)a->B * a->R))
         return SWITCHSD_ESHAPE;
     if (q_stride % 8 != 0 || !(a->scale > -INFINITY && a->scale < INFINITY))

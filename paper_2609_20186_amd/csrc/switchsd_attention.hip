@@ -347,7 +347,11 @@ __device__ __forceinline__ uint32_t seen_bits(const AttnParams &p, const Chunk &
 // a delay of up to kDelay, which weights of up to 2^kDelay carry.
 constexpr float kDelay = 8.0f;
 
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+__device__ __forceinline__ float other_half(float v) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v),
+                                                    __builtin_bit_cast(uint32_t, v), false, false);
+    return __builtin_bit_cast(float, (uint32_t)(threadIdx.x & 32 ? s[0] : s[1]));
+}
 
 // Scores -> weights.  s holds products; `factor` (>= 0) brings them to powers of
 // two.  Returns what the sums so far have to be multiplied with (1: nothing).
@@ -385,15 +389,15 @@ __device__ __forceinline__ float weigh(f32x16 (&s)[N], float factor, float &m, f
 // them.  Here they reach the rows that do: whatever the weight, the sum becomes
 // what it is with the value itself.
 template <int TYPE, bool E4M3, int D>
-__device__ __forceinline__ void add_not_finite(const AttnParams &p, int h, int64_t slot,
+__device__ __forceinline__ void add_not_finite(const AttnParams &p, int h, int slot,
                                                uint32_t seen, f32x16 (&o)[D / 32]) {
     const int half = (threadIdx.x >> 5) & 1;
     for (int x = 0; x < 32; ++x) {
-        const int64_t s = __shfl((long long)slot, x);
+        const int s = __shfl(slot, x);
         if (s < 0)
             continue;
         const bool on = seen >> x & 1;
-        const int64_t at = (s * p.a.Hkv + h) * D + half * 4;
+        const int64_t at = ((int64_t)s * p.a.Hkv + h) * D + half * 4;
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -409,26 +413,44 @@ __device__ __forceinline__ void add_not_finite(const AttnParams &p, int h, int64
     }
 }
 
-// O^T += V^T P^T of 32 keys whose values stand in LDS, a row each `pitch` bytes.
-template <int TYPE, int D>
-__device__ __forceinline__ void add_values(const f32x16 &s, const char *values, int pitch,
+// O^T += V^T P^T of 32 N keys whose values stand in LDS, a row each `pitch` bytes.
+// The fragments of the next 16 keys (and 128 columns) are asked for before the
+// present ones are multiplied: left alone the compiler waits for each.
+template <int TYPE, int D, int N>
+__device__ __forceinline__ void add_values(const f32x16 (&s)[N], const char *values, int pitch,
                                            f32x16 (&o)[D / 32]) {
+    constexpr int F = D / 32 < 4 ? D / 32 : 4, PARTS = D / 32 / F, STEPS = 2 * N * PARTS;
     const int lane = threadIdx.x & 63, x = lane & 15;
     // the lane's 8 bytes: keys 4 (lane / 32) + x / 4, columns 16 (lane / 16 % 2) + 4 (x % 4)
     const char *at = values + ((lane >> 5) * 4 + x / 4) * pitch +
                      ((lane >> 4 & 1) * 16 + x % 4 * 4) * 2;
+    u32x4 f[2][F];
+    const auto ask = [&](int step, u32x4 (&to)[F]) {
+        const char *from = at + step / PARTS * 16 * pitch + step % PARTS * (F * 64);
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        u32x4 w;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            w[j] = pack2<TYPE>(s[t * 8 + j * 2], s[t * 8 + j * 2 + 1]);
-#pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt) {
-            const uint2 a = read_transposed(at + t * 16 * pitch + dt * 64);
-            const uint2 b = read_transposed(at + (t * 16 + 8) * pitch + dt * 64);
-            o[dt] = mfma<TYPE>(u32x4{a.x, a.y, b.x, b.y}, w, o[dt]);
+        for (int d = 0; d < F; ++d) {
+            const uint2 a = read_transposed(from + d * 64);
+            const uint2 b = read_transposed(from + 8 * pitch + d * 64);
+            to[d] = u32x4{a.x, a.y, b.x, b.y};
         }
+    };
+    ask(0, f[0]);
+    u32x4 w;
+#pragma unroll
+    for (int step = 0; step < STEPS; ++step) {
+        if (step + 1 < STEPS)
+            ask(step + 1, f[(step + 1) & 1]);
+        const int t = step / PARTS;  // 16 keys
+        if (step % PARTS == 0) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                w[j] = pack2<TYPE>(s[t / 2][t % 2 * 8 + j * 2], s[t / 2][t % 2 * 8 + j * 2 + 1]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int d = 0; d < F; ++d)
+            o[step % PARTS * F + d] = mfma<TYPE>(f[step & 1][d], w, o[step % PARTS * F + d]);
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
@@ -476,14 +498,14 @@ __device__ __forceinline__ void put(const AttnParams &p, const Row &r, int h, in
 }
 
 // The cache offset (in slots) of position pos; < 0 where there is no key.
-__device__ __forceinline__ int64_t slot_of(const AttnParams &p, const int32_t *table, int pos,
-                                           int keys) {
+__device__ __forceinline__ int slot_of(const AttnParams &p, const int32_t *table, int pos,
+                                       int keys) {
     if (pos >= keys)
         return -1;
     const int page = p.page_log >= 0 ? pos >> p.page_log : pos / p.a.page_size;
     const int in = pos - page * p.a.page_size;
     const int64_t slot = (int64_t)table[page] * p.a.page_size + in;
-    return slot >= 0 && slot < p.n_slots ? slot : -1;
+    return slot >= 0 && slot < p.n_slots ? (int)slot : -1;
 }
 
 // Up to 32 NQ query rows (all new tokens and query heads of one head of the
@@ -559,18 +581,18 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
             (const char *)p.k_cache + (int64_t)h * D * (E4M3 ? 1 : 2) + half * 16;
         const char *const vbase =
             (const char *)p.v_cache + (int64_t)h * D * (E4M3 ? 1 : 2) + half * 16;
-        const int64_t row_bytes = (int64_t)p.a.Hkv * D * (E4M3 ? 1 : 2);
+        const uint32_t row_bytes = (uint32_t)(p.a.Hkv * D * (E4M3 ? 1 : 2));
         u32x4 kr[CH], vr[CH];
         // positions without a key are read from the first slot, and not used
-        const auto load = [&](u32x4 (&to)[CH], const char *base, int64_t slot) {
-            const char *src = base + (slot < 0 ? 0 : slot) * row_bytes;
+        const auto load = [&](u32x4 (&to)[CH], const char *base, int slot) {
+            const char *src = base + (uint64_t)(uint32_t)(slot < 0 ? 0 : slot) * row_bytes;
 #pragma unroll
             for (int x = 0; x < CH; ++x)
                 to[x] = *(const u32x4 *)(src + x * 32);
         };
         const int stop = keys > 0 ? ub : ua;  // without keys nothing is read
         bool poisoned = false;
-        int64_t slot = -1, next = -1;
+        int slot = -1, next = -1;
         if (ua < stop) {
             slot = slot_of(p, table, ua * UNIT + kl, keys);
             load(kr, kbase, slot);
@@ -582,7 +604,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
             const uint32_t valid = (uint32_t)__ballot(slot >= 0);
             const bool plain = valid == ~0u && kb + 31 < c.pos;
             f32x16 s[NQ][1];
-            const int64_t ahead = slot_of(p, table, (t + 2) * UNIT + kl, keys);
+            const int ahead = slot_of(p, table, (t + 2) * UNIT + kl, keys);
 #pragma unroll
             for (int x = 0; x < NQ; ++x)
                 s[x][0] = f32x16{0};
@@ -649,7 +671,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
                 const float alpha = weigh<1>(s[x], factor, m[x], l[x]);
                 if (__any(alpha != 1.0f))
                     scale_rows<D>(o[x], alpha);
-                add_values<TYPE, D>(s[x][0], values, PITCH, o[x]);
+                add_values<TYPE, D, 1>(s[x], values, PITCH, o[x]);
             }
             slot = next;
             next = ahead;
@@ -657,7 +679,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
         if (poisoned) {
             for (int t = ua; t < stop; ++t) {
                 const int kb = t * UNIT + wave * 32;
-                const int64_t at = slot_of(p, table, t * UNIT + kl, keys);
+                const int at = slot_of(p, table, t * UNIT + kl, keys);
                 const uint32_t valid = (uint32_t)__ballot(at >= 0);
                 if (valid == ~0u && kb + 31 < c.pos)
                     continue;
@@ -812,22 +834,22 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
             (const char *)p.k_cache + (int64_t)h * D * (E4M3 ? 1 : 2) + piece * 16;
         const char *const vbase =
             (const char *)p.v_cache + (int64_t)h * D * (E4M3 ? 1 : 2) + piece * 16;
-        const int64_t row_bytes = (int64_t)p.a.Hkv * D * (E4M3 ? 1 : 2);
+        const uint32_t row_bytes = (uint32_t)(p.a.Hkv * D * (E4M3 ? 1 : 2));
         u32x4 kr[NI], vr[NI];
         const auto slots = [&](int t) {
-            return t < ub ? slot_of(p, table, t * UNIT + wave * 16 + (lane & 15), lim) : (int64_t)-1;
+            return t < ub ? slot_of(p, table, t * UNIT + wave * 16 + (lane & 15), lim) : -1;
         };
         // positions without a key are read from the first slot, and not used
-        const auto load = [&](int64_t slot) {
+        const auto load = [&](int slot) {
 #pragma unroll
             for (int x = 0; x < NI; ++x) {
-                const int64_t s = __shfl((long long)slot, x * RPI + sub);
-                const int64_t at = (s < 0 ? 0 : s) * row_bytes;
+                const int s = __shfl(slot, x * RPI + sub);
+                const uint64_t at = (uint64_t)(uint32_t)(s < 0 ? 0 : s) * row_bytes;
                 kr[x] = *(const u32x4 *)(kbase + at);
                 vr[x] = *(const u32x4 *)(vbase + at);
             }
         };
-        const auto stash = [&](int64_t slot, int t) {
+        const auto stash = [&](int slot, int t) {
             const int buf = t & 1;
             const uint32_t valid = (uint32_t)__ballot(slot >= 0) & 0xFFFFu;
             const bool plain = valid == 0xFFFFu && (t + 1) * UNIT <= c.pos;
@@ -863,7 +885,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
         if (keys == 0)
             ub = ua;
         bool poisoned = false;
-        int64_t slot = slots(ua);
+        int slot = slots(ua);
         if (ua < ub) {
             load(slot);
             stash(slot, ua);
@@ -873,7 +895,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
             __syncthreads();
             if (t + 1 < ub)
                 load(slot);
-            const int64_t next = slots(t + 2);
+            const int next = slots(t + 2);
             const int kb = t * UNIT, buf = t & 1;
             if (rows && kb < wlim) {
                 const char *const K = sk[buf], *const V = sv[buf];
@@ -882,17 +904,30 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
                                f3 = sflag[buf][3];
                 const uint32_t valid[2] = {(f0 & 0xFFFFu) | f1 << 16, (f2 & 0xFFFFu) | f3 << 16};
                 poisoned |= ((f0 | f1 | f2 | f3) & 0x10000u) != 0;
+                // four fragments of the keys ahead of those that are multiplied
                 f32x16 s[2];
+                s[0] = s[1] = f32x16{0};
+                u32x4 f[2][4];
+                const auto ask = [&](int step, u32x4 (&to)[4]) {
+                    const int row = step / (D / 64) * 32 + (lane & 31);
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    s[y] = f32x16{0};
-                    const int row = y * 32 + (lane & 31);
-#pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk) {
-                        const u32x4 a =
+                    for (int x = 0; x < 4; ++x) {
+                        const int kk = step % (D / 64) * 4 + x;
+                        to[x] =
                             *(const u32x4 *)(K + row * KP + (((kk * 2 + half) ^ (row & 7)) * 16));
-                        s[y] = mfma<TYPE>(a, q[kk], s[y]);
                     }
+                };
+                ask(0, f[0]);
+#pragma unroll
+                for (int step = 0; step < D / 32; ++step) {
+                    if (step + 1 < D / 32)
+                        ask(step + 1, f[(step + 1) & 1]);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        s[step / (D / 64)] = mfma<TYPE>(f[step & 1][x], q[step % (D / 64) * 4 + x],
+                                                        s[step / (D / 64)]);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
                 if (!plain || (valid[0] & valid[1]) != ~0u) {
 #pragma unroll
@@ -907,9 +942,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
                 const float alpha = weigh<2>(s, factor, m, l);
                 if (__any(alpha != 1.0f))
                     scale_rows<D>(o, alpha);
-#pragma unroll
-                for (int y = 0; y < 2; ++y)
-                    add_values<TYPE, D>(s[y], V + y * 32 * VP, VP, o);
+                add_values<TYPE, D, 2>(s, V, VP, o);
             }
             if (t + 1 < ub)
                 stash(slot, t + 1);
@@ -918,7 +951,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
         __syncthreads();  // before the next item's first tile is stored
         if (poisoned) {
             for (int kb = ua * UNIT; kb < ub * UNIT && kb < wlim; kb += 32) {
-                const int64_t at = slot_of(p, table, kb + (lane & 31), lim);
+                const int at = slot_of(p, table, kb + (lane & 31), lim);
                 const uint32_t valid = (uint32_t)__ballot(at >= 0);
                 if (valid != ~0u || kb / UNIT * UNIT + UNIT > c.pos)
                     add_not_finite<TYPE, E4M3, D>(p, h, at, seen_bits(p, c, r, kb, valid), o);

@@ -145,6 +145,12 @@ __device__ __forceinline__ Share share_of(const AttnParams &p, int b) {
     return s;
 }
 
+__device__ __forceinline__ int64_t uniform64(int64_t v) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
+    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)v >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
 __device__ __forceinline__ int64_t shfl_up64(int64_t v, int d) { return __shfl_up(v, d); }
 
 struct PlanShared {
@@ -209,8 +215,14 @@ __device__ __forceinline__ Work plan(const AttnParams &p, int64_t group, bool by
         }
     }
     __syncthreads();
-    b_out = sh.b;
-    off_out = sh.off;
+    // the same in every lane, which the compiler is told so that what follows from it
+    // stays in scalar registers
+    b_out = __builtin_amdgcn_readfirstlane(sh.b);
+    off_out = uniform64(sh.off);
+    w.items = uniform64(w.items);
+    w.units = uniform64(w.units);
+    w.whole = __builtin_amdgcn_readfirstlane(w.whole);
+    w.groups = __builtin_amdgcn_readfirstlane(w.groups);
     return w;
 }
 
@@ -278,12 +290,18 @@ __device__ __forceinline__ bool clear_not_finite(u32x4 &x) {
     return bad;
 }
 
+// An LDS address as the 32 bits that it is.
+__device__ __forceinline__ uint32_t lds_offset(const char *at) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)at;
+}
+
 // Four 16-bit elements of one column of an LDS tile of rows: of every 16 lanes,
 // lane x names the 8 bytes at row x / 4, columns 4 (x % 4) .., and gets the four
 // rows of column x.
-__device__ __forceinline__ uint2 read_transposed(const char *at) {
+__device__ __forceinline__ uint2 read_transposed(uint32_t at) {
     typedef __attribute__((address_space(3))) s16x4 *lds_ptr;
-    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at));
+    return __builtin_bit_cast(uint2,
+                              __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(uintptr_t)at));
 }
 
 // What a lane holds of one query row (its column of the products).
@@ -341,6 +359,14 @@ __device__ __forceinline__ uint32_t seen_bits(const AttnParams &p, const Chunk &
     return r.ok ? bits & valid : 0u;
 }
 
+// Products of the keys that the lane's row does not see.
+__device__ __forceinline__ void hide(f32x16 &s, uint32_t seen) {
+    seen >>= (threadIdx.x >> 5 & 1) * 4;
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        s[e] = seen & 1u << (e / 4 * 8 + e % 4) ? s[e] : -INFINITY;
+}
+
 // Running softmax of one query row per lane (both halves of a wave hold the same
 // rows, each the keys that its half of the products has): m is the maximum that
 // the weights are taken against, in powers of two; it follows the true one with
@@ -353,10 +379,11 @@ __device__ __forceinline__ float other_half(float v) {
     return __builtin_bit_cast(float, (uint32_t)(threadIdx.x & 32 ? s[0] : s[1]));
 }
 
-// Scores -> weights.  s holds products; `factor` (>= 0) brings them to powers of
-// two.  Returns what the sums so far have to be multiplied with (1: nothing).
+// The largest of the lane's row's products of 32 N keys, in powers of two; moves m
+// where it has to, and returns what the sums so far have to be multiplied with (1:
+// nothing).
 template <int N>
-__device__ __forceinline__ float weigh(f32x16 (&s)[N], float factor, float &m, float &l) {
+__device__ __forceinline__ float follow(const f32x16 (&s)[N], float factor, float &m, float &l) {
     float top = s[0][0];
 #pragma unroll
     for (int x = 0; x < N; ++x)
@@ -371,17 +398,26 @@ __device__ __forceinline__ float weigh(f32x16 (&s)[N], float factor, float &m, f
         m = mn;
         l *= alpha;
     }
+    return alpha;
+}
+// Products -> weights, in 32 bits in s, summed to l; the weights in 16 bits as the
+// right operand of 2 N products with 16 keys each.
+template <int TYPE, int N>
+__device__ __forceinline__ void weigh(f32x16 (&s)[N], float factor, float m, float &l,
+                                      u32x4 (&w)[2 * N]) {
     const float base = m == -INFINITY ? 0.0f : m;
-    float sum = 0.0f;
+    float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int x = 0; x < N; ++x)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            s[x][e] = __builtin_amdgcn_exp2f(fmaf(s[x][e], factor, -base));
-            sum += s[x][e];
+        for (int e = 0; e < 16; e += 2) {
+            const float a = __builtin_amdgcn_exp2f(fmaf(s[x][e], factor, -base));
+            const float b = __builtin_amdgcn_exp2f(fmaf(s[x][e + 1], factor, -base));
+            sum[0] += a;
+            sum[1] += b;
+            w[x * 2 + e / 8][e % 8 / 2] = pack2<TYPE>(a, b);
         }
-    l += sum;
-    return alpha;
+    l += sum[0] + sum[1];
 }
 
 // Infinities and NaN among the values of 32 positions that not every row sees were
@@ -417,16 +453,16 @@ __device__ __forceinline__ void add_not_finite(const AttnParams &p, int h, int s
 // The fragments of the next 16 keys (and 128 columns) are asked for before the
 // present ones are multiplied: left alone the compiler waits for each.
 template <int TYPE, int D, int N>
-__device__ __forceinline__ void add_values(const f32x16 (&s)[N], const char *values, int pitch,
+__device__ __forceinline__ void add_values(const u32x4 (&w)[2 * N], const char *values, int pitch,
                                            f32x16 (&o)[D / 32]) {
     constexpr int F = D / 32 < 4 ? D / 32 : 4, PARTS = D / 32 / F, STEPS = 2 * N * PARTS;
     const int lane = threadIdx.x & 63, x = lane & 15;
     // the lane's 8 bytes: keys 4 (lane / 32) + x / 4, columns 16 (lane / 16 % 2) + 4 (x % 4)
-    const char *at = values + ((lane >> 5) * 4 + x / 4) * pitch +
-                     ((lane >> 4 & 1) * 16 + x % 4 * 4) * 2;
+    const uint32_t at = lds_offset(values) + ((lane >> 5) * 4 + x / 4) * pitch +
+                        ((lane >> 4 & 1) * 16 + x % 4 * 4) * 2;
     u32x4 f[2][F];
     const auto ask = [&](int step, u32x4 (&to)[F]) {
-        const char *from = at + step / PARTS * 16 * pitch + step % PARTS * (F * 64);
+        const uint32_t from = at + step / PARTS * 16 * pitch + step % PARTS * (F * 64);
 #pragma unroll
         for (int d = 0; d < F; ++d) {
             const uint2 a = read_transposed(from + d * 64);
@@ -435,21 +471,15 @@ __device__ __forceinline__ void add_values(const f32x16 (&s)[N], const char *val
         }
     };
     ask(0, f[0]);
-    u32x4 w;
 #pragma unroll
     for (int step = 0; step < STEPS; ++step) {
         if (step + 1 < STEPS)
             ask(step + 1, f[(step + 1) & 1]);
-        const int t = step / PARTS;  // 16 keys
-        if (step % PARTS == 0) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                w[j] = pack2<TYPE>(s[t / 2][t % 2 * 8 + j * 2], s[t / 2][t % 2 * 8 + j * 2 + 1]);
-        }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int d = 0; d < F; ++d)
-            o[step % PARTS * F + d] = mfma<TYPE>(f[step & 1][d], w, o[step % PARTS * F + d]);
+            o[step % PARTS * F + d] =
+                mfma<TYPE>(f[step & 1][d], w[step / PARTS], o[step % PARTS * F + d]);
         __builtin_amdgcn_sched_barrier(0);
     }
 }
@@ -497,15 +527,22 @@ __device__ __forceinline__ void put(const AttnParams &p, const Row &r, int h, in
             l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// The cache offset (in slots) of position pos; < 0 where there is no key.
+// The cache offset (in slots) of position pos; < 0 where there is no key.  The table's
+// entry is asked for by itself, so that the wait for it can come later.
+__device__ __forceinline__ int page_of(const AttnParams &p, int pos) {
+    return p.page_log >= 0 ? pos >> p.page_log : pos / p.a.page_size;
+}
+__device__ __forceinline__ int entry_of(const AttnParams &p, const int32_t *table, int pos,
+                                        int keys) {
+    return pos < keys ? table[page_of(p, pos)] : -1;
+}
+__device__ __forceinline__ int slot_in(const AttnParams &p, int entry, int pos, int keys) {
+    const int64_t slot = (int64_t)entry * p.a.page_size + (pos - page_of(p, pos) * p.a.page_size);
+    return pos < keys && entry >= 0 && slot < p.n_slots ? (int)slot : -1;
+}
 __device__ __forceinline__ int slot_of(const AttnParams &p, const int32_t *table, int pos,
                                        int keys) {
-    if (pos >= keys)
-        return -1;
-    const int page = p.page_log >= 0 ? pos >> p.page_log : pos / p.a.page_size;
-    const int in = pos - page * p.a.page_size;
-    const int64_t slot = (int64_t)table[page] * p.a.page_size + in;
-    return slot >= 0 && slot < p.n_slots ? (int)slot : -1;
+    return slot_in(p, entry_of(p, table, pos, keys), pos, keys);
 }
 
 // Up to 32 NQ query rows (all new tokens and query heads of one head of the
@@ -522,7 +559,8 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
     __shared__ __attribute__((aligned(16))) char lds[kVBytes > kOBytes ? kVBytes : kOBytes];
     __shared__ float sm[4][TILE], sl[4][TILE];
     __shared__ PlanShared sh;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int b;
     int64_t off;
     const Work w = plan<TILE, UNIT>(p, blockIdx.x, false, sh, b, off);
@@ -592,19 +630,22 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
         };
         const int stop = keys > 0 ? ub : ua;  // without keys nothing is read
         bool poisoned = false;
-        int slot = -1, next = -1;
+        int slot = -1, next = -1, entry = -1;
         if (ua < stop) {
             slot = slot_of(p, table, ua * UNIT + kl, keys);
+            next = slot_of(p, table, (ua + 1) * UNIT + kl, keys);
+            entry = entry_of(p, table, (ua + 2) * UNIT + kl, keys);
             load(kr, kbase, slot);
             load(vr, vbase, slot);
-            next = slot_of(p, table, (ua + 1) * UNIT + kl, keys);
         }
         for (int t = ua; t < stop; ++t) {
             const int kb = t * UNIT + wave * 32;
             const uint32_t valid = (uint32_t)__ballot(slot >= 0);
             const bool plain = valid == ~0u && kb + 31 < c.pos;
             f32x16 s[NQ][1];
-            const int ahead = slot_of(p, table, (t + 2) * UNIT + kl, keys);
+            const int ahead = slot_in(p, entry, (t + 2) * UNIT + kl, keys);
+            // before the next keys and values, which it is not to wait for
+            entry = entry_of(p, table, (t + 3) * UNIT + kl, keys);
 #pragma unroll
             for (int x = 0; x < NQ; ++x)
                 s[x][0] = f32x16{0};
@@ -662,16 +703,14 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
 #pragma unroll
             for (int x = 0; x < NQ; ++x) {
                 if (!plain) {
-                    const uint32_t seen = seen_bits(p, c, r[x], kb, valid);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        s[x][0][e] = seen >> (e / 4 * 8 + half * 4 + e % 4) & 1 ? s[x][0][e]
-                                                                             : -INFINITY;
+                    hide(s[x][0], seen_bits(p, c, r[x], kb, valid));
                 }
-                const float alpha = weigh<1>(s[x], factor, m[x], l[x]);
+                const float alpha = follow<1>(s[x], factor, m[x], l[x]);
                 if (__any(alpha != 1.0f))
                     scale_rows<D>(o[x], alpha);
-                add_values<TYPE, D, 1>(s[x], values, PITCH, o[x]);
+                u32x4 weights[2];
+                weigh<TYPE, 1>(s[x], factor, m[x], l[x], weights);
+                add_values<TYPE, D, 1>(weights, values, PITCH, o[x]);
             }
             slot = next;
             next = ahead;
@@ -765,12 +804,15 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
     constexpr int CH = E4M3 ? D / 16 : D / 8;  // 16-byte pieces of a row in the cache
     constexpr int RPI = 64 / CH;               // rows that a wave reads at once
     constexpr int NI = 16 / RPI;               // such reads for its 16 rows
-    constexpr int KP = D * 2, VP = D * 2 + 32;
+    // rows of keys 16 bytes apart from a multiple of 256, so that 16 of them read at one
+    // column lie in different banks; 4 rows of values read at two pairs of pieces too
+    constexpr int KP = D * 2 + 16, VP = D * 2 + 64;
     __shared__ __attribute__((aligned(16))) char sk[2][UNIT * KP];
     __shared__ __attribute__((aligned(16))) char sv[2][UNIT * VP];
     __shared__ uint32_t sflag[2][4];      // keys there are (16 per wave), bit 16: not finite
     __shared__ PlanShared sh;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int b;
     int64_t off;
     const Work w = plan<TILE, UNIT>(p, blockIdx.x, false, sh, b, off);
@@ -836,14 +878,16 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
             (const char *)p.v_cache + (int64_t)h * D * (E4M3 ? 1 : 2) + piece * 16;
         const uint32_t row_bytes = (uint32_t)(p.a.Hkv * D * (E4M3 ? 1 : 2));
         u32x4 kr[NI], vr[NI];
-        const auto slots = [&](int t) {
-            return t < ub ? slot_of(p, table, t * UNIT + wave * 16 + (lane & 15), lim) : -1;
-        };
+        const int kl = wave * 16 + (lane & 15);
         // positions without a key are read from the first slot, and not used
         const auto load = [&](int slot) {
+            int of[NI];
+#pragma unroll
+            for (int x = 0; x < NI; ++x)
+                of[x] = __shfl(slot, x * RPI + sub);
 #pragma unroll
             for (int x = 0; x < NI; ++x) {
-                const int s = __shfl(slot, x * RPI + sub);
+                const int s = of[x];
                 const uint64_t at = (uint64_t)(uint32_t)(s < 0 ? 0 : s) * row_bytes;
                 kr[x] = *(const u32x4 *)(kbase + at);
                 vr[x] = *(const u32x4 *)(vbase + at);
@@ -861,8 +905,8 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
                 if (E4M3) {
                     u32x4 lo, hi;
                     widen<TYPE>(kr[x], lo, hi);
-                    *(u32x4 *)(kd + (((piece * 2) ^ (row & 7)) * 16)) = lo;
-                    *(u32x4 *)(kd + (((piece * 2 + 1) ^ (row & 7)) * 16)) = hi;
+                    *(u32x4 *)(kd + piece * 32) = lo;
+                    *(u32x4 *)(kd + piece * 32 + 16) = hi;
                     widen<TYPE>(vr[x], lo, hi);
                     if (!plain) {
                         bad |= clear_not_finite<TYPE>(lo);
@@ -871,7 +915,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
                     *(u32x4 *)(vd + piece * 32) = lo;
                     *(u32x4 *)(vd + piece * 32 + 16) = hi;
                 } else {
-                    *(u32x4 *)(kd + ((piece ^ (row & 7)) * 16)) = kr[x];
+                    *(u32x4 *)(kd + piece * 16) = kr[x];
                     if (!plain)
                         bad |= clear_not_finite<TYPE>(vr[x]);
                     *(u32x4 *)(vd + piece * 16) = vr[x];
@@ -885,17 +929,22 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
         if (keys == 0)
             ub = ua;
         bool poisoned = false;
-        int slot = slots(ua);
+        int slot = -1, entry = -1;  // the next tile's slots, the table's entries of the one behind
         if (ua < ub) {
+            slot = slot_of(p, table, ua * UNIT + kl, lim);
             load(slot);
             stash(slot, ua);
+            slot = slot_of(p, table, (ua + 1) * UNIT + kl, lim);
+            entry = entry_of(p, table, (ua + 2) * UNIT + kl, lim);
         }
-        slot = slots(ua + 1);
         for (int t = ua; t < ub; ++t) {
             __syncthreads();
+            // before the keys and values, which it is not to wait for
+            const int after = entry_of(p, table, (t + 3) * UNIT + kl, lim);
+            __builtin_amdgcn_sched_barrier(0);
             if (t + 1 < ub)
                 load(slot);
-            const int next = slots(t + 2);
+            const int next = slot_in(p, entry, (t + 2) * UNIT + kl, lim);
             const int kb = t * UNIT, buf = t & 1;
             if (rows && kb < wlim) {
                 const char *const K = sk[buf], *const V = sv[buf];
@@ -914,7 +963,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
                     for (int x = 0; x < 4; ++x) {
                         const int kk = step % (D / 64) * 4 + x;
                         to[x] =
-                            *(const u32x4 *)(K + row * KP + (((kk * 2 + half) ^ (row & 7)) * 16));
+                            *(const u32x4 *)(K + row * KP + (kk * 2 + half) * 16);
                     }
                 };
                 ask(0, f[0]);
@@ -931,22 +980,20 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
                 }
                 if (!plain || (valid[0] & valid[1]) != ~0u) {
 #pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const uint32_t seen = seen_bits(p, c, r, kb + y * 32, valid[y]);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            s[y][e] = seen >> (e / 4 * 8 + half * 4 + e % 4) & 1 ? s[y][e]
-                                                                                 : -INFINITY;
-                    }
+                    for (int y = 0; y < 2; ++y)
+                        hide(s[y], seen_bits(p, c, r, kb + y * 32, valid[y]));
                 }
-                const float alpha = weigh<2>(s, factor, m, l);
+                const float alpha = follow<2>(s, factor, m, l);
                 if (__any(alpha != 1.0f))
                     scale_rows<D>(o, alpha);
-                add_values<TYPE, D, 2>(s, V, VP, o);
+                u32x4 weights[4];
+                weigh<TYPE, 2>(s, factor, m, l, weights);
+                add_values<TYPE, D, 2>(weights, V, VP, o);
             }
             if (t + 1 < ub)
                 stash(slot, t + 1);
             slot = next;
+            entry = after;
         }
         __syncthreads();  // before the next item's first tile is stored
         if (poisoned) {

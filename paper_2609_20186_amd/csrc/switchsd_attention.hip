@@ -809,7 +809,8 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
     constexpr int KP = D * 2 + 16, VP = D * 2 + 64;
     __shared__ __attribute__((aligned(16))) char sk[2][UNIT * KP];
     __shared__ __attribute__((aligned(16))) char sv[2][UNIT * VP];
-    __shared__ uint32_t sflag[2][4];      // keys there are (16 per wave), bit 16: not finite
+    __shared__ __attribute__((aligned(16))) uint64_t sflag[2][4];  // keys there are
+    __shared__ int s_poison;
     __shared__ PlanShared sh;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -878,24 +879,30 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
             (const char *)p.v_cache + (int64_t)h * D * (E4M3 ? 1 : 2) + piece * 16;
         const uint32_t row_bytes = (uint32_t)(p.a.Hkv * D * (E4M3 ? 1 : 2));
         u32x4 kr[NI], vr[NI];
-        const int kl = wave * 16 + (lane & 15);
-        // positions without a key are read from the first slot, and not used
-        const auto load = [&](int slot) {
+        const uint64_t apart = (uint64_t)(vbase - kbase);
+        if (tid == 0)
+            s_poison = 0;
+        // Slots by batches of four tiles: a lane has the slot of one key, of tile lane / 16
+        // of the batch and of the 16 keys there that its wave fetches.  The table's
+        // entries are asked for two batches ahead.  Positions without a key are fetched
+        // from the first slot, and not used.
+        const auto position = [&](int batch) {
+            return (ua + batch * 4 + lane / 16) * UNIT + wave * 16 + lane % 16;
+        };
+        const auto load = [&](int slots, int tile) {
             int of[NI];
 #pragma unroll
             for (int x = 0; x < NI; ++x)
-                of[x] = __shfl(slot, x * RPI + sub);
+                of[x] = __shfl(slots, tile * 16 + x * RPI + sub);
 #pragma unroll
             for (int x = 0; x < NI; ++x) {
-                const int s = of[x];
-                const uint64_t at = (uint64_t)(uint32_t)(s < 0 ? 0 : s) * row_bytes;
-                kr[x] = *(const u32x4 *)(kbase + at);
-                vr[x] = *(const u32x4 *)(vbase + at);
+                const char *from = kbase + (uint64_t)(uint32_t)of[x] * row_bytes;
+                kr[x] = *(const u32x4 *)from;
+                vr[x] = *(const u32x4 *)(from + apart);
             }
         };
-        const auto stash = [&](int slot, int t) {
+        const auto stash = [&](uint32_t valid, int t) {
             const int buf = t & 1;
-            const uint32_t valid = (uint32_t)__ballot(slot >= 0) & 0xFFFFu;
             const bool plain = valid == 0xFFFFu && (t + 1) * UNIT <= c.pos;
             bool bad = false;
 #pragma unroll
@@ -921,38 +928,48 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
                     *(u32x4 *)(vd + piece * 16) = vr[x];
                 }
             }
-            bad = __any(bad);
-            if (lane == 0)
-                sflag[buf][wave] = valid | (bad ? 0x10000u : 0u);
+            if (!plain && __any(bad) && lane == 0)
+                s_poison = 1;
         };
 
         if (keys == 0)
             ub = ua;
-        bool poisoned = false;
-        int slot = -1, entry = -1;  // the next tile's slots, the table's entries of the one behind
+        int slots = 0, next = 0, entry = -1;  // of this batch, the next; the table's behind
+        uint64_t valid = 0, valid_next = 0;
+        uint64_t all = 0;                     // keys that all four waves have
+        const auto slots_of = [&](int from, int batch, uint64_t &there) {
+            const int slot = slot_in(p, from, position(batch), lim);
+            there = __ballot(slot >= 0);
+            if (lane == 0)
+                sflag[batch & 1][wave] = there;
+            return slot < 0 ? 0 : slot;
+        };
         if (ua < ub) {
-            slot = slot_of(p, table, ua * UNIT + kl, lim);
-            load(slot);
-            stash(slot, ua);
-            slot = slot_of(p, table, (ua + 1) * UNIT + kl, lim);
-            entry = entry_of(p, table, (ua + 2) * UNIT + kl, lim);
+            const int e0 = entry_of(p, table, position(0), lim);
+            entry = entry_of(p, table, position(1), lim);
+            next = slots_of(e0, 0, valid_next);
+            load(next, 0);
+            stash((uint32_t)valid_next & 0xFFFFu, ua);
         }
         for (int t = ua; t < ub; ++t) {
             __syncthreads();
-            // before the keys and values, which it is not to wait for
-            const int after = entry_of(p, table, (t + 3) * UNIT + kl, lim);
-            __builtin_amdgcn_sched_barrier(0);
+            const int j = (t - ua) & 3, batch = (t - ua) >> 2;
+            if (j == 0) {
+                const u32x4 *f = (const u32x4 *)sflag[batch & 1];
+                const u32x4 both = f[0] & f[1];
+                all = (uint64_t)__builtin_amdgcn_readfirstlane(both[1] & both[3]) << 32 |
+                      __builtin_amdgcn_readfirstlane(both[0] & both[2]);
+                slots = next;
+                valid = valid_next;
+                next = slots_of(entry, batch + 1, valid_next);
+                entry = entry_of(p, table, position(batch + 2), lim);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             if (t + 1 < ub)
-                load(slot);
-            const int next = slot_in(p, entry, (t + 2) * UNIT + kl, lim);
+                load(j < 3 ? slots : next, (j + 1) & 3);
             const int kb = t * UNIT, buf = t & 1;
             if (rows && kb < wlim) {
                 const char *const K = sk[buf], *const V = sv[buf];
-                const bool plain = kb + UNIT <= c.pos;
-                const uint32_t f0 = sflag[buf][0], f1 = sflag[buf][1], f2 = sflag[buf][2],
-                               f3 = sflag[buf][3];
-                const uint32_t valid[2] = {(f0 & 0xFFFFu) | f1 << 16, (f2 & 0xFFFFu) | f3 << 16};
-                poisoned |= ((f0 | f1 | f2 | f3) & 0x10000u) != 0;
                 // four fragments of the keys ahead of those that are multiplied
                 f32x16 s[2];
                 s[0] = s[1] = f32x16{0};
@@ -978,10 +995,15 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
                                                         s[step / (D / 64)]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                if (!plain || (valid[0] & valid[1]) != ~0u) {
+                if ((~all >> j * 16 & 0xFFFF) != 0 || kb + UNIT > c.pos) {
+                    const uint64_t *f = sflag[batch & 1];
+                    const int x = j * 16;
 #pragma unroll
                     for (int y = 0; y < 2; ++y)
-                        hide(s[y], seen_bits(p, c, r, kb + y * 32, valid[y]));
+                        hide(s[y],
+                             seen_bits(p, c, r, kb + y * 32,
+                                       ((uint32_t)(f[y * 2] >> x) & 0xFFFFu) |
+                                           (uint32_t)(f[y * 2 + 1] >> x) << 16));
                 }
                 const float alpha = follow<2>(s, factor, m, l);
                 if (__any(alpha != 1.0f))
@@ -991,10 +1013,10 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
                 add_values<TYPE, D, 2>(weights, V, VP, o);
             }
             if (t + 1 < ub)
-                stash(slot, t + 1);
-            slot = next;
-            entry = after;
+                stash((uint32_t)((j < 3 ? valid : valid_next) >> ((j + 1) & 3) * 16) & 0xFFFFu, t + 1);
         }
+        __syncthreads();
+        const bool poisoned = s_poison != 0;
         __syncthreads();  // before the next item's first tile is stored
         if (poisoned) {
             for (int kb = ua * UNIT; kb < ub * UNIT && kb < wlim; kb += 32) {

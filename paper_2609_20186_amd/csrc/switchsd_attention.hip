@@ -118,112 +118,193 @@ __device__ __forceinline__ float cached(const void *base, int64_t at) {
 // work-group takes is found by the sums over all sequences of what comes before it.
 // With many items each work-group takes one whole; with few, kAttnGroups
 // work-groups take equal shares of all units, in order, and k_merge joins what
-// was cut.
+// was cut.  The host has seen to it that items, and with few of them units, fit 32
+// bits.
 struct Work {
-    int64_t items, units;  // of all sequences
-    int whole;             // one item for each work-group
-    int groups;            // work-groups that have work
+    uint32_t items, units;  // of all sequences
+    int whole;              // one item for each work-group
+    uint32_t groups;        // work-groups that have work
 };
 
-// What sequence b has: tiles of query rows and units of keys (1 at least, so that
-// every row is written).
-struct Share {
-    int tiles, units;
+// What sequence b has: its new rows, keys that there may be (positions of pages that are
+// held), tiles of query rows and units of keys (1 at least, so that every row is
+// written).
+struct Seq {
+    Chunk c;
+    int keys, tiles, units;
 };
-__device__ __forceinline__ int keys_of(const AttnParams &p, const Chunk &c, int b) {
-    const int held = clampi(p.a.held[b], 0, p.a.max_pages);
-    const int64_t end = (int64_t)c.pos + c.n, most = (int64_t)held * p.a.page_size;
-    return p.n_slots == 0 ? 0 : (int)(end < most ? end : most);
-}
 template <int TILE, int UNIT>
-__device__ __forceinline__ Share share_of(const AttnParams &p, int b) {
-    const Chunk c = chunk_of(p.a, b);
-    Share s;
-    s.tiles = (int)(((int64_t)c.n * p.G + TILE - 1) / TILE);
-    const int keys = keys_of(p, c, b);
-    s.units = keys > UNIT ? (keys + UNIT - 1) / UNIT : 1;
+__device__ __forceinline__ Seq seq_of(const AttnParams &p, int b) {
+    Seq s;
+    s.c = chunk_of(p.a, b);
+    const int held = clampi(p.a.held[b], 0, p.a.max_pages);
+    const int64_t end = (int64_t)s.c.pos + s.c.n, most = (int64_t)held * p.a.page_size;
+    s.keys = p.n_slots == 0 ? 0 : (int)(end < most ? end : most);
+    s.tiles = (int)(((int64_t)s.c.n * p.G + TILE - 1) / TILE);
+    s.units = s.keys > UNIT ? (s.keys + UNIT - 1) / UNIT : 1;
     return s;
 }
 
-__device__ __forceinline__ int64_t uniform64(int64_t v) {
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
-    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)v >> 32));
-    return (int64_t)((uint64_t)hi << 32 | lo);
-}
-
-__device__ __forceinline__ int64_t shfl_up64(int64_t v, int d) { return __shfl_up(v, d); }
-
 struct PlanShared {
-    int64_t sums[2][kThreads / 64];
-    int64_t off;
+    uint32_t sums[2][kThreads / 64];
+    uint32_t off, base;
     int b;
+    Seq seq;
 };
 
-// Total work; then, for work-group `group` (of items in the merge), the sequence
-// that its first unit (item) lies in and how many come before it there.
+// A lane's share of the sequences, with what comes before them.
+struct Plan {
+    Work w;
+    int b0, b1;
+    Seq seq;                // of b0, where it is the only one
+    uint32_t items, units;  // of its sequences
+    uint32_t items_before, units_before;
+};
+
 template <int TILE, int UNIT>
-__device__ __forceinline__ Work plan(const AttnParams &p, int64_t group, bool by_item,
-                                     PlanShared &sh, int &b_out, int64_t &off_out) {
+__device__ __forceinline__ Plan plan(const AttnParams &p, PlanShared &sh) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int per = (p.a.B + kThreads - 1) / kThreads;
-    const int b0 = tid * per, b1 = b0 + per < p.a.B ? b0 + per : p.a.B;
-    int64_t items = 0, units = 0;
-    for (int b = b0; b < b1; ++b) {
-        const Share s = share_of<TILE, UNIT>(p, b);
-        items += (int64_t)s.tiles * p.a.Hkv;
-        units += (int64_t)s.tiles * p.a.Hkv * s.units;
+    Plan q;
+    q.b0 = tid * per < p.a.B ? tid * per : p.a.B;
+    q.b1 = q.b0 + per < p.a.B ? q.b0 + per : p.a.B;
+    q.items = q.units = 0;
+    for (int b = q.b0; b < q.b1; ++b) {
+        q.seq = seq_of<TILE, UNIT>(p, b);
+        const uint32_t items = (uint32_t)(q.seq.tiles * p.a.Hkv);
+        q.items += items;
+        q.units += items * (uint32_t)q.seq.units;
     }
-    int64_t pi = items, pu = units;  // inclusive sums over the lanes
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t x = shfl_up64(pi, d), y = shfl_up64(pu, d);
-        pi += lane >= d ? x : 0;
-        pu += lane >= d ? y : 0;
-    }
+    uint32_t pi = (uint32_t)wave_scan((int)q.items), pu = (uint32_t)wave_scan((int)q.units);
     if (lane == 63) {
         sh.sums[0][wave] = pi;
         sh.sums[1][wave] = pu;
     }
-    if (tid == 0)
-        sh.b = -1;
     __syncthreads();
-    Work w;
-    w.items = w.units = 0;
+    uint32_t items = 0, units = 0;
 #pragma unroll
     for (int v = 0; v < kThreads / 64; ++v) {
         pi += v < wave ? sh.sums[0][v] : 0;
         pu += v < wave ? sh.sums[1][v] : 0;
-        w.items += sh.sums[0][v];
-        w.units += sh.sums[1][v];
+        items += sh.sums[0][v];
+        units += sh.sums[1][v];
     }
-    w.whole = p.whole || w.items >= kAttnWhole;
-    const int64_t most = w.units / kAttnLeast;
-    w.groups = (int)(w.whole ? w.items : most < 1 ? 1 : most < kAttnGroups ? most : kAttnGroups);
-    const int64_t at = w.whole || by_item ? group : group * w.units / w.groups;
-    int64_t before = w.whole || by_item ? pi - items : pu - units;
-    const int64_t mine = w.whole || by_item ? items : units;
-    if (w.items > 0 && at >= before && at < before + mine) {
-        for (int b = b0; b < b1; ++b) {
-            const Share s = share_of<TILE, UNIT>(p, b);
-            const int64_t n =
-                (int64_t)s.tiles * p.a.Hkv * (w.whole || by_item ? 1 : s.units);
-            if (at < before + n) {
+    q.items_before = pi - q.items;
+    q.units_before = pu - q.units;
+    // the same in every lane, which the compiler is told so that what follows from it
+    // stays in scalar registers
+    q.w.items = __builtin_amdgcn_readfirstlane(items);
+    q.w.units = __builtin_amdgcn_readfirstlane(units);
+    q.w.whole = p.whole || q.w.items >= kAttnWhole;
+    const uint32_t most = q.w.units / kAttnLeast;
+    q.w.groups = q.w.whole ? q.w.items : most < 1 ? 1 : most < kAttnGroups ? most : kAttnGroups;
+    return q;
+}
+
+// The first unit of work-group g: floor(g U / W); the work-group that unit u is in: the
+// last g with g U / W < u + 1.
+__device__ __forceinline__ uint32_t start_of(const Work &w, uint32_t g) {
+    if (w.units < (1u << 22))  // g and W are at most kAttnGroups
+        return g * w.units / w.groups;
+    return (uint32_t)((uint64_t)g * w.units / w.groups);
+}
+__device__ __forceinline__ uint32_t group_of(const Work &w, uint32_t u) {
+    if (w.units < (1u << 22))
+        return ((u + 1) * w.groups - 1) / w.units;
+    return (uint32_t)((((uint64_t)u + 1) * w.groups - 1) / w.units);
+}
+
+__device__ __forceinline__ Seq uniform(const Seq &x) {
+    Seq s;
+    s.c.n = __builtin_amdgcn_readfirstlane(x.c.n);
+    s.c.row = __builtin_amdgcn_readfirstlane(x.c.row);
+    s.c.pos = __builtin_amdgcn_readfirstlane(x.c.pos);
+    s.keys = __builtin_amdgcn_readfirstlane(x.keys);
+    s.tiles = __builtin_amdgcn_readfirstlane(x.tiles);
+    s.units = __builtin_amdgcn_readfirstlane(x.units);
+    return s;
+}
+
+// The sequence that item (or unit) `at` lies in, how many come before it there, and
+// the units before the sequence.  Every lane of the work-group calls it.
+template <int TILE, int UNIT>
+__device__ __forceinline__ int find(const AttnParams &p, const Plan &q, bool by_item, uint32_t at,
+                                    PlanShared &sh, Seq &seq, uint32_t &off, uint32_t &base) {
+    __syncthreads();
+    uint32_t before = by_item ? q.items_before : q.units_before;
+    if (at >= before && at - before < (by_item ? q.items : q.units)) {
+        uint32_t units = q.units_before;
+        for (int b = q.b0; b < q.b1; ++b) {
+            const Seq s = q.b1 - q.b0 == 1 ? q.seq : seq_of<TILE, UNIT>(p, b);
+            const uint32_t items = (uint32_t)(s.tiles * p.a.Hkv);
+            const uint32_t n = by_item ? items : items * (uint32_t)s.units;
+            if (at - before < n) {
                 sh.b = b;
                 sh.off = at - before;
+                sh.base = units;
+                sh.seq = s;
                 break;
             }
             before += n;
+            units += items * (uint32_t)s.units;
         }
     }
     __syncthreads();
-    // the same in every lane, which the compiler is told so that what follows from it
-    // stays in scalar registers
-    b_out = __builtin_amdgcn_readfirstlane(sh.b);
-    off_out = uniform64(sh.off);
-    w.items = uniform64(w.items);
-    w.units = uniform64(w.units);
-    w.whole = __builtin_amdgcn_readfirstlane(w.whole);
-    w.groups = __builtin_amdgcn_readfirstlane(w.groups);
-    return w;
+    off = __builtin_amdgcn_readfirstlane(sh.off);
+    base = __builtin_amdgcn_readfirstlane(sh.base);
+    seq = uniform(sh.seq);
+    return __builtin_amdgcn_readfirstlane(sh.b);
+}
+
+// A work-group's way through its units: pieces of items, one after another.
+struct Walk {
+    int b;
+    Seq seq;
+    uint32_t off;       // of the sequence's items (units)
+    uint32_t u, end;
+    int item, ua, ub;   // the present piece: units [ua, ub) of the item
+    bool whole, done;   // one item for each work-group; the piece is a whole item
+};
+template <int TILE, int UNIT>
+__device__ __forceinline__ bool begin(const AttnParams &p, PlanShared &sh, Walk &k) {
+    const Plan q = plan<TILE, UNIT>(p, sh);
+    if (blockIdx.x >= q.w.groups || q.w.items == 0)
+        return false;
+    k.u = q.w.whole ? 0 : start_of(q.w, blockIdx.x);
+    k.end = q.w.whole ? 1 : start_of(q.w, blockIdx.x + 1);
+    uint32_t base;
+    k.b = find<TILE, UNIT>(p, q, q.w.whole, q.w.whole ? blockIdx.x : k.u, sh, k.seq, k.off, base);
+    k.whole = q.w.whole;
+    return true;
+}
+__device__ __forceinline__ void piece(Walk &k) {
+    const uint32_t nu = (uint32_t)k.seq.units, left = k.end - k.u;
+    if (k.whole) {
+        k.item = (int)k.off;
+        k.ua = 0;
+        k.ub = (int)nu;
+        k.done = true;
+        return;
+    }
+    k.item = (int)(k.off / nu);
+    k.ua = (int)(k.off - (uint32_t)k.item * nu);
+    k.ub = left < nu - (uint32_t)k.ua ? k.ua + (int)left : (int)nu;
+    k.done = k.ua == 0 && k.ub == (int)nu;
+}
+template <int TILE, int UNIT>
+__device__ __forceinline__ bool next(const AttnParams &p, Walk &k) {
+    const uint32_t n = (uint32_t)(k.ub - k.ua);
+    if (k.whole)
+        return false;
+    k.u += n;
+    k.off += n;
+    if (k.u >= k.end)
+        return false;
+    while (k.off == (uint32_t)(k.seq.tiles * p.a.Hkv) * (uint32_t)k.seq.units) {
+        k.off = 0;
+        k.seq = uniform(seq_of<TILE, UNIT>(p, ++k.b));  // there are units left
+    }
+    return true;
 }
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -561,37 +642,16 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
     __shared__ PlanShared sh;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    int b;
-    int64_t off;
-    const Work w = plan<TILE, UNIT>(p, blockIdx.x, false, sh, b, off);
-    if ((int64_t)blockIdx.x >= w.groups || b < 0)
+    Walk k;
+    if (!begin<TILE, UNIT>(p, sh, k))
         return;
-    int64_t u = w.whole ? 0 : (int64_t)blockIdx.x * w.units / w.groups;
-    const int64_t u_end = w.whole ? 1 : ((int64_t)blockIdx.x + 1) * w.units / w.groups;
     char *const values = lds + wave * 32 * PITCH;
     bool first = true;
 
-    while (u < u_end) {
-        const Chunk c = chunk_of(p.a, b);
-        const int keys = keys_of(p, c, b);
-        const Share share = share_of<TILE, UNIT>(p, b);
-        const int nu = share.units;
-        if (share.tiles == 0) {  // a sequence without rows
-            ++b;
-            off = 0;
-            continue;
-        }
-        int item, ua, ub;
-        if (w.whole) {
-            item = (int)off;
-            ua = 0;
-            ub = nu;
-        } else {
-            item = (int)(off / nu);
-            ua = (int)(off - (int64_t)item * nu);
-            const int64_t left = u_end - u;
-            ub = left < nu - ua ? ua + (int)left : nu;
-        }
+    do {
+        piece(k);
+        const int b = k.b, item = k.item, ua = k.ua, ub = k.ub, keys = k.seq.keys;
+        const Chunk &c = k.seq.c;
         const int h = item % p.a.Hkv, tile = item / p.a.Hkv;
         const int32_t *table = p.a.table + (int64_t)b * p.a.max_pages;
         const float signed_factor = p.a.scale * kLog2e * (p.k_scale ? p.k_scale[h] : 1.0f);
@@ -730,8 +790,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
         }
 
         // join the four waves
-        const bool done = ua == 0 && ub == nu;
-        const int64_t place = done ? -1 : (int64_t)blockIdx.x * 2 + (first ? 0 : 1);
+        const int64_t place = k.done ? -1 : (int64_t)blockIdx.x * 2 + (first ? 0 : 1);
 #pragma unroll
         for (int x = 0; x < NQ; ++x) {
             l[x] += other_half(l[x]);
@@ -786,13 +845,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
             }
         }
         first = false;
-        u += w.whole ? 1 : ub - ua;
-        off += w.whole ? 1 : ub - ua;
-        if (!w.whole && off == (int64_t)share.tiles * p.a.Hkv * nu) {
-            ++b;
-            off = 0;
-        }
-    }
+    } while (next<TILE, UNIT>(p, k));
 }
 
 // Tiles of 128 query rows, 32 for each wave; the four waves share 64 keys and
@@ -814,40 +867,18 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
     __shared__ PlanShared sh;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    int b;
-    int64_t off;
-    const Work w = plan<TILE, UNIT>(p, blockIdx.x, false, sh, b, off);
-    if ((int64_t)blockIdx.x >= w.groups || b < 0)
+    Walk k;
+    if (!begin<TILE, UNIT>(p, sh, k))
         return;
-    int64_t u = w.whole ? 0 : (int64_t)blockIdx.x * w.units / w.groups;
-    const int64_t u_end = w.whole ? 1 : ((int64_t)blockIdx.x + 1) * w.units / w.groups;
     bool first = true;
 
-    while (u < u_end) {
-        const Chunk c = chunk_of(p.a, b);
-        const int keys = keys_of(p, c, b);
-        const Share share = share_of<TILE, UNIT>(p, b);
-        const int nu = share.units;
-        if (share.tiles == 0) {
-            ++b;
-            off = 0;
-            continue;
-        }
-        int item, ua, ub;
-        if (w.whole) {
-            item = (int)off;
-            ua = 0;
-            ub = nu;
-        } else {
-            item = (int)(off / nu);
-            ua = (int)(off - (int64_t)item * nu);
-            const int64_t left = u_end - u;
-            ub = left < nu - ua ? ua + (int)left : nu;
-        }
-        const int taken = ub - ua;
-        const bool done = ua == 0 && ub == nu;
+    do {
+        piece(k);
+        const int b = k.b, item = k.item, ua = k.ua, keys = k.seq.keys;
+        const Chunk &c = k.seq.c;
+        int ub = k.ub;
         // the last tiles first: without a mask they see the most keys
-        const int h = item % p.a.Hkv, tile = share.tiles - 1 - item / p.a.Hkv;
+        const int h = item % p.a.Hkv, tile = k.seq.tiles - 1 - item / p.a.Hkv;
         const int32_t *table = p.a.table + (int64_t)b * p.a.max_pages;
         const float signed_factor = p.a.scale * kLog2e * (p.k_scale ? p.k_scale[h] : 1.0f);
         const float factor = signed_factor == 0.0f ? 1.0f : fabsf(signed_factor);
@@ -1028,105 +1059,91 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
         }
 
         l += other_half(l);
-        const int64_t place = done ? -1 : (int64_t)blockIdx.x * 2 + (first ? 0 : 1);
+        const int64_t place = k.done ? -1 : (int64_t)blockIdx.x * 2 + (first ? 0 : 1);
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt)
             put<TYPE, D, TILE>(p, r, h, wave * 32 + (lane & 31), place, dt, o[dt], m, l);
         first = false;
-        u += w.whole ? 1 : taken;
-        off += w.whole ? 1 : taken;
-        if (!w.whole && off == (int64_t)share.tiles * p.a.Hkv * nu) {
-            ++b;
-            off = 0;
-        }
-    }
+    } while (next<TILE, UNIT>(p, k));
 }
 
 // Joins the partial results of the items that were cut.  Of a work-group's lanes,
 // D / 4 take four elements each of a row; `parts` such groups of lanes take every
 // parts-th result of one row, the others another row.
 template <int TYPE, int D, int TILE, int UNIT, bool LAST_FIRST>
-__global__ void __launch_bounds__(kThreads) k_merge(const AttnParams p, int parts) {
+__global__ void __launch_bounds__(kThreads) k_merge(const AttnParams p, int parts, uint32_t groups) {
     constexpr int LANES = D / 4, kSets = kThreads / LANES;
     __shared__ PlanShared sh;
-    __shared__ int64_t base[kThreads / 64];
     __shared__ f32x4 so[kThreads];
     __shared__ float2 sml[kThreads];
-    const int64_t id = blockIdx.x;
     const int tid = threadIdx.x;
-    int b;
-    int64_t item;
-    const Work w = plan<TILE, UNIT>(p, id, true, sh, b, item);
-    if (w.whole || id >= w.items || b < 0)
+    const Plan pl = plan<TILE, UNIT>(p, sh);
+    const Work &w = pl.w;
+    if (w.whole)
         return;
-    // units before the item: those of earlier sequences are summed anew
-    int64_t sum = 0;
-    for (int x = tid; x < b; x += kThreads) {
-        const Share s = share_of<TILE, UNIT>(p, x);
-        sum += (int64_t)s.tiles * p.a.Hkv * s.units;
-    }
-    for (int d = 32; d; d >>= 1)
-        sum += __shfl_xor((long long)sum, d);
-    if ((tid & 63) == 0)
-        base[tid >> 6] = sum;
-    __syncthreads();
-    const Chunk c = chunk_of(p.a, b);
-    const Share s = share_of<TILE, UNIT>(p, b);
-    const int64_t u0 = base[0] + base[1] + base[2] + base[3] + item * s.units, u1 = u0 + s.units;
-    // work-group g takes the units from floor(g U / W) on: unit u is in the last g
-    // with g U / W < u + 1
-    const int64_t U = w.units, W = w.groups;
-    const int64_t g0 = ((u0 + 1) * W - 1) / U, g1 = (u1 * W - 1) / U;
-    if (g0 == g1)
-        return;  // one work-group had the whole item
-    const bool late = g0 * U / W < u0;  // the item is not the first one of g0
-    const int h = (int)(item % p.a.Hkv);
-    const int tile =
-        LAST_FIRST ? s.tiles - 1 - (int)(item / p.a.Hkv) : (int)(item / p.a.Hkv);
     const int set = tid / LANES, lane = tid % LANES, d = lane * 4;
-    const int row = blockIdx.y * (kSets / parts) + set / parts;
-    const Row r = row_of(p, c, h, tile * TILE + row);
-    const bool on = row < TILE && r.ok;
-    float m = -INFINITY, l = 0.0f;
-    f32x4 o = f32x4{0};
-    if (on) {
-        const int64_t stride = TILE * (D + 2);
+    // the row groups of all items in equal shares
+    const uint32_t all = w.items * groups;
+    const uint32_t from = (uint32_t)((uint64_t)blockIdx.x * all / gridDim.x);
+    const uint32_t to = (uint32_t)(((uint64_t)blockIdx.x + 1) * all / gridDim.x);
+    uint32_t found = ~0u, item = 0, base = 0;
+    Seq s;
+    for (uint32_t id = from; id < to; ++id) {
+        if (id / groups != found) {
+            found = id / groups;
+            find<TILE, UNIT>(p, pl, true, found, sh, s, item, base);
+        }
+        const Chunk &c = s.c;
+        const uint32_t u0 = base + item * (uint32_t)s.units, u1 = u0 + (uint32_t)s.units;
+        const uint32_t g0 = group_of(w, u0), g1 = group_of(w, u1 - 1);
+        if (g0 == g1)
+            continue;  // one work-group had the whole item
+        const bool late = start_of(w, g0) < u0;  // the item is not the first one of g0
+        const int h = (int)item % p.a.Hkv;
+        const int tile = LAST_FIRST ? s.tiles - 1 - (int)item / p.a.Hkv : (int)item / p.a.Hkv;
+        const int row = (int)(id % groups) * (kSets / parts) + set / parts;
+        const Row r = row_of(p, c, h, tile * TILE + row);
+        const bool on = row < TILE && r.ok;
+        float m = -INFINITY, l = 0.0f;
+        f32x4 o = f32x4{0};
+        if (on) {
+            const int64_t stride = TILE * (D + 2);
 #pragma unroll 4
-        for (int64_t g = g0 + set % parts; g <= g1; g += parts) {
-            const float *part = p.part + (g * 2 + (g == g0 && late ? 1 : 0)) * stride;
-            const float pm = part[TILE * D + row], pl = part[TILE * D + TILE + row];
-            const f32x4 po = *(const f32x4 *)(part + row * D + d);
-            const float mn = fmaxf(m, pm), at = mn == -INFINITY ? 0.0f : mn;
-            const float f = __builtin_amdgcn_exp2f(m - at), pf = __builtin_amdgcn_exp2f(pm - at);
-            m = mn;
-            l = l * f + pl * pf;
-            o = o * f + po * pf;
+            for (uint32_t g = g0 + set % parts; g <= g1; g += parts) {
+                const float *part = p.part + ((int64_t)g * 2 + (g == g0 && late ? 1 : 0)) * stride;
+                const float pm = part[TILE * D + row], pl = part[TILE * D + TILE + row];
+                const f32x4 po = *(const f32x4 *)(part + row * D + d);
+                const float mn = fmaxf(m, pm), at = mn == -INFINITY ? 0.0f : mn;
+                const float f = __builtin_amdgcn_exp2f(m - at), pf = __builtin_amdgcn_exp2f(pm - at);
+                m = mn;
+                l = l * f + pl * pf;
+                o = o * f + po * pf;
+            }
         }
-    }
-    if (parts > 1) {
-        so[tid] = o;
-        sml[tid] = make_float2(m, l);
-        __syncthreads();
-        if (set % parts)
-            return;
-        for (int x = 1; x < parts; ++x) {
-            const float2 y = sml[tid + x * LANES];
-            const f32x4 po = so[tid + x * LANES];
-            const float mn = fmaxf(m, y.x), at = mn == -INFINITY ? 0.0f : mn;
-            const float f = __builtin_amdgcn_exp2f(m - at), pf = __builtin_amdgcn_exp2f(y.x - at);
-            m = mn;
-            l = l * f + y.y * pf;
-            o = o * f + po * pf;
+        if (parts > 1) {
+            __syncthreads();  // the last row group's use of LDS
+            so[tid] = o;
+            sml[tid] = make_float2(m, l);
+            __syncthreads();
+            for (int x = 1; x < parts && set % parts == 0; ++x) {
+                const float2 y = sml[tid + x * LANES];
+                const f32x4 po = so[tid + x * LANES];
+                const float mn = fmaxf(m, y.x), at = mn == -INFINITY ? 0.0f : mn;
+                const float f = __builtin_amdgcn_exp2f(m - at), pf = __builtin_amdgcn_exp2f(y.x - at);
+                m = mn;
+                l = l * f + y.y * pf;
+                o = o * f + po * pf;
+            }
         }
+        if (!on || set % parts)
+            continue;
+        o = l == 0.0f ? f32x4{0} : o * ((p.v_scale ? p.v_scale[h] : 1.0f) / l);
+        *(uint2 *)((char *)p.out + ((r.row * p.a.Hq + r.head) * D + d) * 2) =
+            make_uint2(pack2<TYPE>(o[0], o[1]), pack2<TYPE>(o[2], o[3]));
+        if (p.lse && d == 0)
+            p.lse[r.row * p.a.Hq + r.head] =
+                l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
     }
-    if (!on)
-        return;
-    o = l == 0.0f ? f32x4{0} : o * ((p.v_scale ? p.v_scale[h] : 1.0f) / l);
-    *(uint2 *)((char *)p.out + ((r.row * p.a.Hq + r.head) * D + d) * 2) =
-        make_uint2(pack2<TYPE>(o[0], o[1]), pack2<TYPE>(o[2], o[3]));
-    if (p.lse && d == 0)
-        p.lse[r.row * p.a.Hq + r.head] =
-            l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 int launched() { return hipGetLastError() == hipSuccess ? SWITCHSD_OK : SWITCHSD_EHIP; }
@@ -1155,16 +1172,17 @@ namespace {
 template <int TYPE, int D, int TILE, int UNIT, bool LAST_FIRST>
 void launch_merge(const AttnParams &p, int64_t items, hipStream_t stream) {
     constexpr int kSets = kThreads / (D / 4);
-    // about the results of an item, at most one set of lanes for each
-    int parts = 1;
-    while (parts < kSets && parts * items < kAttnGroups)
-        parts *= 2;
-    const int sets = kSets / parts;
+    // lanes for a row's results beside each other while there are too few rows
     const int64_t rows = (int64_t)p.a.R * p.G < TILE ? (int64_t)p.a.R * p.G : TILE;
+    items = items < kAttnWhole ? items : kAttnWhole;
+    int parts = 1;
+    const auto groups = [&]() { return (rows * parts + kSets - 1) / kSets; };
+    while (parts < kSets && parts * items < kAttnGroups && items * groups() < kAttnMerge)
+        parts *= 2;
+    const int64_t all = items * groups();
     hipLaunchKernelGGL((k_merge<TYPE, D, TILE, UNIT, LAST_FIRST>),
-                       dim3((unsigned)(items < kAttnWhole ? items : kAttnWhole),
-                            (unsigned)((rows + sets - 1) / sets)),
-                       dim3(kThreads), 0, stream, p, parts);
+                       dim3((unsigned)(all < kAttnMerge ? all : kAttnMerge)), dim3(kThreads), 0,
+                       stream, p, parts, (uint32_t)groups());
 }
 
 template <int TYPE, bool E4M3, int D>
@@ -1178,7 +1196,10 @@ int launch_attend(AttnParams p, hipStream_t stream) {
     items *= p.a.Hkv;
     const int64_t cap = (int64_t)p.a.max_pages * p.a.page_size;
     const int64_t len = (int64_t)p.a.Lmax + p.a.R;
-    p.whole = (len < cap ? len : cap) <= kAttnShort;
+    const int64_t keys = len < cap ? len : cap;
+    // never cut: short contexts, and lengths whose units would not fit 32 bits
+    p.whole = keys <= kAttnShort ||
+              (items < kAttnWhole ? items : kAttnWhole) * (keys / 64 + 1) >= (1ll << 31);
     const int64_t groups = p.whole || items > kAttnGroups ? items : kAttnGroups;
     if (groups >= 1 << 24)
         return SWITCHSD_ESHAPE;

@@ -305,6 +305,7 @@ constexpr int kAttnGroups = 512;
 constexpr int kAttnWhole = 2048;
 constexpr int kAttnLeast = 2;
 constexpr int kAttnShort = 1024;
+constexpr int kAttnMerge = 1024;  // work-groups that join what was cut
 
 // Query rows (new tokens times query heads of one head of the cache) of a
 // work-group, by the most that a sequence has.

@@ -325,10 +325,11 @@ int launch_attention_kernel(const AttnParams &p, int32_t type, int32_t cache_typ
 
 // ---- log probabilities (switchsd_logprobs.hip)
 
-// Along accepted paths a sequence has few entries: work-groups for 8 of them, each of
-// which takes every eighth.
+// Along accepted paths a large batch's sequences have few entries of their R:
+// work-groups for kLogprobSlots of them, each of which takes every so many-th.
+constexpr int kLogprobSlots = 8;
 inline int32_t logprob_slots(const switchsd_logprob_args &a) {
-    return a.accept_node && a.R > 8 ? 8 : a.R;
+    return a.accept_node && a.R > kLogprobSlots && (int64_t)a.B * a.R > 512 ? kLogprobSlots : a.R;
 }
 // Pieces of a row, for about kLogprobGroups work-groups together; a piece is at
 // least two vectors of each lane.

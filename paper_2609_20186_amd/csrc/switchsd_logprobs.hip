@@ -298,25 +298,47 @@ __device__ __forceinline__ void select(Selection &sel, const char *row, int V, i
     const int winners = sel.winners;
     const unsigned long long bar =
         winners < k ? (unsigned long long)(kMinusInf + 1) << 32 : sel.bar;
-    const int rounds = (j1 - j0 + kThreads - 1) / kThreads, per = rounds * 2;
-    for (int x = tid; x < winners * per; x += kThreads) {
-        const int w = x / per, y = x - w * per;
-        const int j = j0 + y / 2 * kThreads + sel.winner[w] * 2 + y % 2;
-        if (j >= j1)
-            continue;
-        const u32x4 q = j < full ? load_vec<TYPE>(row, j) : load_last<TYPE>(row, j, V);
-        unsigned take = 0;
+    // four vectors of a lane are asked for at once
+    const uint32_t per = (uint32_t)((j1 - j0 + kThreads - 1) / kThreads) * 2;
+    const uint32_t tasks = (uint32_t)winners * per;
+    for (uint32_t x0 = 0; x0 < tasks; x0 += 4 * kThreads) {
+        u32x4 q[4];
+        int at[4];
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float l = element<TYPE>(q, e);
-            take |= l == l && order_key(l, j) >= bar ? 1u << e : 0u;
+        for (int u = 0; u < 4; ++u) {
+            const uint32_t x = x0 + u * kThreads + tid;
+            at[u] = -1;
+            q[u] = u32x4{~0u, ~0u, ~0u, ~0u};
+            if (x < tasks) {
+                const uint32_t w = x / per, y = x - w * per;
+                const int j = j0 + (int)(y / 2) * kThreads + sel.winner[w] * 2 + (int)(y % 2);
+                if (j < j1) {
+                    at[u] = j;
+                    q[u] = j < full ? load_vec<TYPE>(row, j) : load_last<TYPE>(row, j, V);
+                }
+            }
         }
-        while (take) {
-            const int e = __builtin_ctz(take);
-            take &= take - 1;
-            const int at = atomicAdd(&sel.count, 1);
-            if (at < kList)
-                sel.list[at] = order_key(load_logit<TYPE>(row, j * N + e), j * N + e);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (x0 + u * kThreads >= tasks)
+                break;
+            // of the bar's own logit the vectors up to its own
+            const uint32_t least =
+                (uint32_t)(bar >> 32) + (0xFFFFFFFFu - (uint32_t)at[u] >= (uint32_t)bar ? 0 : 1);
+            unsigned hits = 0;
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                hits |= order_of(element<TYPE>(q[u], e)) >= least ? 1u << e : 0u;
+            if (hits == 0)
+                continue;
+            int to = atomicAdd(&sel.count, __popc(hits));
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (hits & 1u << e) {
+                    if (to < kList)
+                        sel.list[to] = order_key(element<TYPE>(q[u], e), at[u] * N + e);
+                    ++to;
+                }
         }
     }
     __syncthreads();
@@ -383,7 +405,7 @@ __device__ __forceinline__ float high(unsigned long long v) {
 // exponential among them, which at full rate is what 5 to 6 TB/s of 16-bit logits
 // bring: a row is cut rather than left to one compute unit.
 template <int TYPE>
-__global__ void __launch_bounds__(kThreads) k_logprob(const LogprobParams p) {
+__global__ void __launch_bounds__(kThreads, 4) k_logprob(const LogprobParams p) {
     constexpr int N = kPerVec<TYPE>;
     constexpr int U = 4;  // vectors in flight per lane
     const switchsd_logprob_args &a = p.a;
@@ -407,6 +429,18 @@ __global__ void __launch_bounds__(kThreads) k_logprob(const LogprobParams p) {
         const int64_t e = (int64_t)b * a.R + i;
         const char *row = (const char *)a.logits +
                           ((int64_t)b * a.R + row_of(all, i, path)) * V * kSize<TYPE>;
+        // the first vectors are asked for before the token, and its logit behind it
+        u32x4 x[U];
+        const auto ask = [&](int at) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int j = at + u * kThreads + tid;
+                x[u] = nothing;
+                if (j < whole)
+                    x[u] = load_vec<TYPE>(row, j);
+            }
+        };
+        ask(j0);
         const int tok = a.tokens ? a.tokens[e] : -1;
         const bool in = tok >= 0 && tok < V;
         const float lt = in ? load_logit<TYPE>(row, tok) : 0.0f;
@@ -432,14 +466,8 @@ __global__ void __launch_bounds__(kThreads) k_logprob(const LogprobParams p) {
                 ahead += above_low<TYPE>(j == own ? nothing : x, lt, j < own);
         };
         for (int at = j0; at < whole; at += kThreads * U) {
-            u32x4 x[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int j = at + u * kThreads + tid;
-                x[u] = nothing;
-                if (j < whole)
-                    x[u] = load_vec<TYPE>(row, j);
-            }
+            if (at > j0)
+                ask(at);
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (at + u * kThreads + wave * 64 < whole)
@@ -518,9 +546,16 @@ __global__ void __launch_bounds__(kThreads) k_logprob(const LogprobParams p) {
                 sel.count = 0;
                 sel.bar = ~0ull;
             }
-            // pieces are few (at most kThreads): a lane for each
+            // what the pieces left is asked for together: sums (pieces are few, a lane
+            // for each) and the first of the keys
             float pm = -INFINITY, ps = 0.0f, pt = 0.0f;
             ahead = 0;
+            unsigned long long keys[2] = {0, 0};
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+                if (tid + y * kThreads < p.pieces * k)
+                    keys[y] = ld_u64(&of_row[(tid + y * kThreads) / k]
+                                          .best[(tid + y * kThreads) % k]);
             if (tid < p.pieces) {
                 const unsigned long long x = ld_u64(&of_row[tid].sums[0]);
                 const unsigned long long y = ld_u64(&of_row[tid].sums[1]);
@@ -560,13 +595,19 @@ __global__ void __launch_bounds__(kThreads) k_logprob(const LogprobParams p) {
             if (k > 0) {
                 // pieces' first ceil(k / pieces) tokens make k together: the last
                 // of them bounds the row's
-                const int q = (k + p.pieces - 1) / p.pieces - 1;
-                if (tid < p.pieces)
-                    atomicMin(&sel.bar, ld_u64(&of_row[tid].best[q]));
+                const int q = (k + p.pieces - 1) / p.pieces - 1, all = p.pieces * k;
+                const auto key_of = [&](int x) {
+                    return x < kThreads       ? keys[0]
+                           : x < 2 * kThreads ? keys[1]
+                                              : ld_u64(&of_row[x / k].best[x % k]);
+                };
+                for (int x = tid; x < all; x += kThreads)
+                    if (x % k == q)
+                        atomicMin(&sel.bar, key_of(x));
                 __syncthreads();
                 const unsigned long long bar = sel.bar;
-                for (int x = tid; x < p.pieces * k; x += kThreads) {
-                    const unsigned long long key = ld_u64(&of_row[x / k].best[x % k]);
+                for (int x = tid; x < all; x += kThreads) {
+                    const unsigned long long key = key_of(x);
                     if (key && key >= bar) {
                         const int at = atomicAdd(&sel.count, 1);
                         if (at < kList)

@@ -197,7 +197,8 @@ __device__ __forceinline__ Plan plan(const AttnParams &p, PlanShared &sh) {
     q.w.units = __builtin_amdgcn_readfirstlane(units);
     q.w.whole = p.whole || q.w.items >= kAttnWhole;
     const uint32_t most = q.w.units / kAttnLeast;
-    q.w.groups = q.w.whole ? q.w.items : most < 1 ? 1 : most < kAttnGroups ? most : kAttnGroups;
+    const uint32_t limit = (uint32_t)p.groups;
+    q.w.groups = q.w.whole ? q.w.items : most < 1 ? 1 : most < limit ? most : limit;
     return q;
 }
 
@@ -401,21 +402,36 @@ __device__ __forceinline__ Row row_of(const AttnParams &p, const Chunk &c, int h
 }
 
 // The query rows as the products' right operand: lane l holds row l % 32, and of
-// step kk the 8 elements that the keys' operand has there.  The sign of the
-// softmax's factor is taken into them, and a factor of 0 (the scores are then
-// taken as they are, all 0), so that what is not seen can be -inf before it.
+// step kk the 8 elements that the keys' operand has there.
 template <bool E4M3, int D>
-__device__ __forceinline__ void load_query(const AttnParams &p, const Row &r, float signed_factor,
+__device__ __forceinline__ void load_query(const AttnParams &p, const Row &r,
                                            u32x4 (&q)[D / 16]) {
     const int half = (threadIdx.x >> 5) & 1;
     const char *src = (const char *)p.q + (r.row * p.q_stride + (int64_t)r.head * D) * 2;
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) {
         const int d = E4M3 ? kk / 2 * 32 + half * 16 + kk % 2 * 8 : kk * 16 + half * 8;
-        q[kk] = r.ok && signed_factor != 0.0f ? *(const u32x4 *)(src + d * 2) : u32x4{0, 0, 0, 0};
-        if (signed_factor < 0.0f)
-            q[kk] ^= 0x80008000u;
+        q[kk] = r.ok ? *(const u32x4 *)(src + d * 2) : u32x4{0, 0, 0, 0};
     }
+}
+
+// The softmax's factor, as what brings products to powers of two: a magnitude that they
+// are multiplied with once the maximum is known, and a sign (or 0, with the magnitude
+// 1) that the query rows take, so that what is not seen can be -inf before it.
+struct Factor {
+    float size, sign;
+};
+__device__ __forceinline__ Factor factor_of(const AttnParams &p, int h) {
+    const float f = p.a.scale * kLog2e * (p.k_scale ? p.k_scale[h] : 1.0f);
+    return {f == 0.0f ? 1.0f : fabsf(f), f == 0.0f ? 0.0f : f < 0.0f ? -1.0f : 1.0f};
+}
+template <int N>
+__device__ __forceinline__ void apply_sign(u32x4 (&q)[N], float sign) {
+    if (sign == 1.0f)  // the same for all lanes; the rows are not waited for
+        return;
+#pragma unroll
+    for (int x = 0; x < N; ++x)
+        q[x] = sign == 0.0f ? u32x4{0, 0, 0, 0} : q[x] ^ 0x80008000u;
 }
 
 // Which of the 32 cache positions from kb on row r sees, of those in `valid`.
@@ -636,7 +652,8 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
     constexpr int TILE = 32 * NQ, UNIT = 128;
     constexpr int CH = E4M3 ? D / 32 : D / 16;  // 16-byte pieces of a row per half wave
     constexpr int PITCH = D * 2 + 32;
-    constexpr int kVBytes = 4 * 32 * PITCH, kOBytes = 4 * 2 * 4 * 64 * 16;
+    constexpr int COLS = D / 32 < 4 ? D / 32 : 4;  // blocks of 32 columns joined at once
+    constexpr int kVBytes = 4 * 32 * PITCH, kOBytes = 4 * COLS * 4 * 64 * 16;
     __shared__ __attribute__((aligned(16))) char lds[kVBytes > kOBytes ? kVBytes : kOBytes];
     __shared__ float sm[4][TILE], sl[4][TILE];
     __shared__ PlanShared sh;
@@ -654,8 +671,8 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
         const Chunk &c = k.seq.c;
         const int h = item % p.a.Hkv, tile = item / p.a.Hkv;
         const int32_t *table = p.a.table + (int64_t)b * p.a.max_pages;
-        const float signed_factor = p.a.scale * kLog2e * (p.k_scale ? p.k_scale[h] : 1.0f);
-        const float factor = signed_factor == 0.0f ? 1.0f : fabsf(signed_factor);
+        const Factor fac = factor_of(p, h);
+        const float factor = fac.size;
 
         Row r[NQ];
         u32x4 q[NQ][D / 16];
@@ -664,7 +681,8 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
 #pragma unroll
         for (int x = 0; x < NQ; ++x) {
             r[x] = row_of(p, c, h, tile * TILE + x * 32 + (lane & 31));
-            load_query<E4M3, D>(p, r[x], signed_factor, q[x]);
+            load_query<E4M3, D>(p, r[x], q[x]);
+            apply_sign(q[x], fac.sign);
             m[x] = -INFINITY;
             l[x] = 0.0f;
 #pragma unroll
@@ -813,33 +831,34 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
                 sum += sm[v][row] == -INFINITY ? 0.0f
                                                : sl[v][row] * __builtin_amdgcn_exp2f(sm[v][row] - top);
             const float f = m[x] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[x] - top);
-            // two columns of 32 at a time: LDS holds them for four waves
+            // each wave adds up one block of columns
 #pragma unroll
-            for (int d0 = 0; d0 < D / 32; d0 += 2) {
+            for (int d0 = 0; d0 < D / 32; d0 += COLS) {
 #pragma unroll
-                for (int y = 0; y < 2; ++y)
+                for (int y = 0; y < COLS; ++y)
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
                         f32x4 v;
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             v[e] = o[x][d0 + y][g * 4 + e] * f;
-                        *(f32x4 *)(lds + (((wave * 2 + y) * 4 + g) * 64 + lane) * 16) = v;
+                        *(f32x4 *)(lds + (((wave * COLS + y) * 4 + g) * 64 + lane) * 16) = v;
                     }
                 __syncthreads();
-                if (wave < 2) {
+                if (wave < COLS) {
                     f32x16 t = f32x16{0};
 #pragma unroll
                     for (int v = 0; v < 4; ++v)
 #pragma unroll
                         for (int g = 0; g < 4; ++g) {
-                            const f32x4 y =
-                                *(const f32x4 *)(lds + (((v * 2 + wave) * 4 + g) * 64 + lane) * 16);
+                            const f32x4 y = *(const f32x4 *)(
+                                lds + (((v * COLS + wave) * 4 + g) * 64 + lane) * 16);
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
                                 t[g * 4 + e] += y[e];
                         }
-                    put<TYPE, D, TILE>(p, r[x], h, row, place, d0 + wave, t, top, sum);
+                    put<TYPE, D, TILE>(p, r[x], h, x * 32 + (lane & 31), place, d0 + wave, t, top,
+                                       sum);
                 }
                 __syncthreads();
             }
@@ -880,8 +899,8 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
         // the last tiles first: without a mask they see the most keys
         const int h = item % p.a.Hkv, tile = k.seq.tiles - 1 - item / p.a.Hkv;
         const int32_t *table = p.a.table + (int64_t)b * p.a.max_pages;
-        const float signed_factor = p.a.scale * kLog2e * (p.k_scale ? p.k_scale[h] : 1.0f);
-        const float factor = signed_factor == 0.0f ? 1.0f : fabsf(signed_factor);
+        const Factor fac = factor_of(p, h);
+        const float factor = fac.size;
         // keys that the tile's (the wave's) last row sees
         int lim = keys, wlim = keys;
         if (!p.a.mask) {
@@ -896,7 +915,8 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
         const Row r = row_of(p, c, h, tile * TILE + wave * 32 + (lane & 31));
         const bool rows = __any(r.ok);
         u32x4 q[D / 16];
-        load_query<false, D>(p, r, signed_factor, q);
+        load_query<false, D>(p, r, q);
+        apply_sign(q, fac.sign);
         f32x16 o[D / 32];
         float m = -INFINITY, l = 0.0f;
 #pragma unroll
@@ -1177,7 +1197,7 @@ void launch_merge(const AttnParams &p, int64_t items, hipStream_t stream) {
     items = items < kAttnWhole ? items : kAttnWhole;
     int parts = 1;
     const auto groups = [&]() { return (rows * parts + kSets - 1) / kSets; };
-    while (parts < kSets && parts * items < kAttnGroups && items * groups() < kAttnMerge)
+    while (parts < kSets && parts * items < p.groups && items * groups() < kAttnMerge)
         parts *= 2;
     const int64_t all = items * groups();
     hipLaunchKernelGGL((k_merge<TYPE, D, TILE, UNIT, LAST_FIRST>),
@@ -1200,7 +1220,10 @@ int launch_attend(AttnParams p, hipStream_t stream) {
     // never cut: short contexts, and lengths whose units would not fit 32 bits
     p.whole = keys <= kAttnShort ||
               (items < kAttnWhole ? items : kAttnWhole) * (keys / 64 + 1) >= (1ll << 31);
-    const int64_t groups = p.whole || items > kAttnGroups ? items : kAttnGroups;
+    // as many as the device holds at once: two on a compute unit where their registers
+    // allow it
+    p.groups = D == 256 || tile == 64 ? kAttnGroups / 2 : kAttnGroups;
+    const int64_t groups = p.whole || items > p.groups ? items : p.groups;
     if (groups >= 1 << 24)
         return SWITCHSD_ESHAPE;
     const dim3 g((unsigned)groups), t(kThreads);

@@ -296,6 +296,7 @@ struct AttnParams {
     int32_t G;         // query heads per head of the cache
     int32_t page_log;  // page_size = 2^page_log, or -1
     int32_t whole;     // no item is cut
+    int32_t groups;    // work-groups that share the keys of few items
 };
 
 // Work-groups that share an attention's keys where there are few rows, and the

@@ -173,14 +173,18 @@ __device__ __forceinline__ void take(Sums &a, u32x4 x, int vec, float c, float d
         a.ref = ref;
         a.lim = ref + delay;
     }
+    // a vector's own sums first: fewer roundings of the long ones
+    float s = 0.0f, t = 0.0f;
 #pragma unroll
     for (int e = 0; e < N; ++e) {
         // NaN (and -inf beside itself) weighs nothing: the maximum drops it
         const float y = fmaxf((f[e] - a.ref) * c, -150.0f);
         const float w = __builtin_amdgcn_exp2f(y);
-        a.s += w;
-        a.t = fmaf(w, y, a.t);
+        s += w;
+        t = fmaf(w, y, t);
     }
+    a.s += s;
+    a.t += t;
 }
 
 // How many elements of a wave's vectors are ahead of a number above -inf: those

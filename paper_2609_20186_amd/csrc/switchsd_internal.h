@@ -327,14 +327,18 @@ int launch_attention_kernel(const AttnParams &p, int32_t type, int32_t cache_typ
 // ---- log probabilities (switchsd_logprobs.hip)
 
 // Along accepted paths a large batch's sequences have few entries of their R:
-// work-groups for kLogprobSlots of them, each of which takes every so many-th.
-constexpr int kLogprobSlots = 8;
+// work-groups for kLogprobSlots of them, each of which takes every so many-th.  32
+// paths of 1 to 9 entries, rows of 128256 16-bit logits: 29.6 us with 16, with 4 and 8
+// 41 and 35 (a path's second round waits for its first), with 32 29.6.
+constexpr int kLogprobSlots = 16;
 inline int32_t logprob_slots(const switchsd_logprob_args &a) {
     return a.accept_node && a.R > kLogprobSlots && (int64_t)a.B * a.R > 512 ? kLogprobSlots : a.R;
 }
-// Pieces of a row, for about kLogprobGroups work-groups together; a piece is at
-// least two vectors of each lane.
-constexpr int kLogprobGroups = 1024;
+// Pieces of a row, for about kLogprobGroups work-groups together, which is as many as
+// are held at once (145 rows of 27830 16-bit logits: 15.5 us; for 2048 22.5), or for
+// twice as many where the most of a path's have no work (those 32 paths: 29.6; for 1024
+// 35.0, for 4096 35.3).  A piece is at least two vectors of each lane.
+constexpr int kLogprobGroups = 1024, kLogprobPathGroups = 2048;
 constexpr int kLogprobPieces = 64;
 constexpr size_t kLogprobRecord = 16 + 8 * SWITCHSD_MAX_TOP;
 struct LogprobCut {
@@ -344,7 +348,8 @@ inline LogprobCut logprob_cut(const switchsd_logprob_args &a, bool may) {
     const int64_t rows = (int64_t)a.B * logprob_slots(a);
     const int64_t per = a.logits_type == SWITCHSD_F32 ? 4 : 8;
     const int64_t vecs = (a.V + per - 1) / per, least = 2 * kThreads;
-    int64_t n = may && rows > 0 ? kLogprobGroups / rows : 1;
+    const int64_t most = logprob_slots(a) < a.R ? kLogprobPathGroups : kLogprobGroups;
+    int64_t n = may && rows > 0 ? most / rows : 1;
     n = n < vecs / least ? n : vecs / least;
     n = n < kLogprobPieces ? n : kLogprobPieces;
     n = n > 1 ? n : 1;

@@ -541,7 +541,7 @@ int switchsd_compact_cache(void *cache, int32_t planes, int64_t plane_stride, in
  *   keys, values: n rows of Hkv heads of D elements of `type` (SWITCHSD_BF16 or
  *   SWITCHSD_F16), key_stride and value_stride elements apart (at least Hkv * D:
  *   they may be parts of one projection's output); slots [n] int64, distinct where
- *   they name a slot (of rows that share one, any or a mixture stays); count [1] int32 on
+ *   they name a slot (of rows that share one any, or a mixture, stays); count [1] int32 on
  *   the device or NULL; k_cache, v_cache [n_slots, Hkv, D] of cache_type (`type` or
  *   SWITCHSD_E4M3), n_slots < 2^31; k_scale, v_scale [Hkv] float.  D is 64, 128 or 256,
  *   1 <= Hkv <= SWITCHSD_MAX_HEADS; keys, values, caches and strides aligned to 16 bytes.
@@ -575,8 +575,9 @@ int switchsd_store_cache(const void *keys, int64_t key_stride, const void *value
  *   (drafted: B * R).  scale multiplies the products of queries and keys.
  *   D is 64, 128 or 256; Hkv divides Hq <= SWITCHSD_MAX_HEADS; query head h reads
  *   head h / (Hq / Hkv) of the cache.  B <= SWITCHSD_MAX_PLAN_B, R <= 2^20, Lmax <=
- *   2^30, B * max_pages < 2^31, n_slots < 2^31, 1 <= page_size <= 65536; shapes that would take
- *   2^24 work-groups or more (of 32 rows and query heads and more) are refused. */
+ *   2^30, B * max_pages < 2^31, n_slots < 2^31, 1 <= page_size <= 65536; shapes that
+ *   would take 2^24 work-groups or more (of 32 to 128 rows and query heads), and B
+ *   sequences of R rows each that would take 2^31, are refused. */
 typedef struct {
     int32_t B, R, rows, Hq, Hkv, D;
     int32_t Lmax, page_size, max_pages;
@@ -610,8 +611,8 @@ int switchsd_paged_attention(const switchsd_attention_args *args, const void *q,
                              hipStream_t stream);
 
 /* Bytes of the workspace that attention of these sizes needs (only B, R, rows,
- * Hq, Hkv and D are read; the pointers may be NULL); 0 for sizes that
- * switchsd_paged_attention refuses. */
+ * Hq, Hkv and D are read; the pointers may be NULL); 0 for sizes out of their
+ * ranges. */
 size_t switchsd_attention_workspace_bytes(const switchsd_attention_args *args);
 
 /* ---- Probabilities of what was emitted ------------------------------------ */

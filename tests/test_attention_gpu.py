@@ -220,6 +220,22 @@ def test_packed_chunks(hq):
     check(a, *run(a)[:2], "packed, broken")
 
 
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (5, 1), (6, 2)])
+@pytest.mark.parametrize("held", [True, False])
+def test_chunks_that_are_most_of_their_context(Hq, Hkv, held):
+    """Few items whose tiles see more and more keys, cut by what they see, beside a
+    single token and a short chunk of a long context; pages that end early; values that
+    are not finite."""
+    a = make([0, 1700, 390, 5, 1203], [700, 1, 517, 385, 90], Hq=Hq, Hkv=Hkv, D=64, page=16,
+             packed=True, Lmax=2000, seed=Hq)
+    if not held:
+        a["held"] = np.minimum(a["held"], np.array([21, 107, 33, 2, 0], np.int32))
+    v = a["v_cache"]
+    v[int(a["table"][0, 20]) * 16 + 3, 0, 7] = math.inf
+    v[int(a["table"][2, 30]) * 16 + 5, 0, 40] = math.nan
+    check(a, *run(a)[:2], f"{Hq}/{Hkv} held {held}")
+
+
 @pytest.mark.parametrize("R,Hq", [(5, 4), (40, 4), (70, 8), (33, 2)])
 def test_masks(R, Hq):
     """Random masks, masks that leave rows empty, masks of several words."""

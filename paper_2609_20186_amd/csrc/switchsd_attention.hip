@@ -428,6 +428,16 @@ __device__ __forceinline__ uint2 read_transposed(uint32_t at) {
                               __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(uintptr_t)at));
 }
 
+// The kernel's parameters, read from memory again: what was read of them before is not kept
+// for what follows.  Left alone the compiler reads all of them at the start and, with
+// too few scalar registers for them, carries them in lanes of vector registers through
+// everything.
+__device__ __forceinline__ const AttnParams &reread() {
+    uint64_t at = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    return *(const AttnParams *)(const __attribute__((address_space(4))) AttnParams *)at;
+}
+
 // What a lane holds of one query row (its column of the products).
 struct Row {
     int64_t row;  // in q and out
@@ -690,7 +700,7 @@ __device__ __forceinline__ int slot_of(const AttnParams &p, const int32_t *table
 // their own, so that no wave waits for another before the end.
 template <int TYPE, bool E4M3, int D, int NQ>
 __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
-    k_attend_few(const AttnParams p) {
+    k_attend_few(const AttnParams) {
     constexpr int TILE = 32 * NQ, UNIT = 128;
     constexpr int CH = E4M3 ? D / 32 : D / 16;  // 16-byte pieces of a row per half wave
     constexpr int PITCH = D * 2 + 32;
@@ -702,12 +712,13 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     Walk k;
-    if (!begin<TILE, UNIT>(p, sh, k))
+    if (!begin<TILE, UNIT>(reread(), sh, k))
         return;
     char *const values = lds + wave * 32 * PITCH;
     bool first = true;
 
     do {
+        const AttnParams &p = reread();
         piece<TILE, UNIT>(p, k);
         const int b = k.b, item = k.item, ua = k.ua, ub = k.ub, keys = k.seq.keys;
         const Chunk &c = k.seq.c;
@@ -836,6 +847,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
             next = ahead;
         }
         if (poisoned) {
+            const AttnParams &p = reread();
             for (int t = ua; t < stop; ++t) {
                 const int kb = t * UNIT + wave * 32;
                 const int at = slot_of(p, table, t * UNIT + kl, keys);
@@ -850,6 +862,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
         }
 
         // join the four waves
+        const AttnParams &pe = reread();
         const int64_t place = k.done ? -1 : (int64_t)blockIdx.x * 2 + (first ? 0 : 1);
 #pragma unroll
         for (int x = 0; x < NQ; ++x) {
@@ -899,21 +912,21 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
                             for (int e = 0; e < 4; ++e)
                                 t[g * 4 + e] += y[e];
                         }
-                    put<TYPE, D, TILE>(p, r[x], h, x * 32 + (lane & 31), place, d0 + wave, t, top,
-                                       sum);
+                    put<TYPE, D, TILE>(pe, r[x], h, x * 32 + (lane & 31), place, d0 + wave, t,
+                                       top, sum);
                 }
                 __syncthreads();
             }
         }
         first = false;
-    } while (next<TILE, UNIT>(p, k));
+    } while (next<TILE, UNIT>(reread(), k));
 }
 
 // Tiles of 128 query rows, 32 for each wave; the four waves share 64 keys and
 // values at a time in LDS, two buffers of them, the next ones on their way through
 // registers while the present ones are used.
 template <int TYPE, bool E4M3, int D>
-__global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(const AttnParams p) {
+__global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(const AttnParams) {
     constexpr int TILE = 128, UNIT = 64;
     constexpr int CH = E4M3 ? D / 16 : D / 8;  // 16-byte pieces of a row in the cache
     constexpr int RPI = 64 / CH;               // rows that a wave reads at once
@@ -929,11 +942,12 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     Walk k;
-    if (!begin<TILE, UNIT>(p, sh, k))
+    if (!begin<TILE, UNIT>(reread(), sh, k))
         return;
     bool first = true;
 
     do {
+        const AttnParams &p = reread();
         piece<TILE, UNIT>(p, k);
         const int b = k.b, item = k.item, ua = k.ua, keys = k.seq.keys;
         const Chunk &c = k.seq.c;
@@ -1114,6 +1128,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
         const bool poisoned = s_poison != 0;
         __syncthreads();  // before the next item's first tile is stored
         if (poisoned) {
+            const AttnParams &p = reread();
             for (int kb = ua * UNIT; kb < ub * UNIT && kb < wlim; kb += 32) {
                 const int at = slot_of(p, table, kb + (lane & 31), lim);
                 const uint32_t valid = (uint32_t)__ballot(at >= 0);
@@ -1122,26 +1137,29 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
             }
         }
 
+        const AttnParams &pe = reread();
         l += other_half(l);
         const int64_t place = k.done ? -1 : (int64_t)blockIdx.x * 2 + (first ? 0 : 1);
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt)
-            put<TYPE, D, TILE>(p, r, h, wave * 32 + (lane & 31), place, dt, o[dt], m, l);
+            put<TYPE, D, TILE>(pe, r, h, wave * 32 + (lane & 31), place, dt, o[dt], m, l);
         first = false;
-    } while (next<TILE, UNIT>(p, k));
+    } while (next<TILE, UNIT>(reread(), k));
 }
 
 // Joins the partial results of the items that were cut.  Of a work-group's lanes,
 // D / 4 take four elements each of a row; `parts` such groups of lanes take every
 // parts-th result of one row, the others another row.
 template <int TYPE, int D, int TILE, int UNIT>
-__global__ void __launch_bounds__(kThreads) k_merge(const AttnParams p, int parts, uint32_t groups) {
+__global__ void __launch_bounds__(kThreads) k_merge(const AttnParams, int parts,
+                                                    uint32_t groups) {
     constexpr int LANES = D / 4, kSets = kThreads / LANES;
     __shared__ PlanShared sh;
     __shared__ f32x4 so[kThreads];
     __shared__ float2 sml[kThreads];
     const int tid = threadIdx.x;
-    const Plan pl = plan<TILE, UNIT>(p, sh);
+    const Plan pl = plan<TILE, UNIT>(reread(), sh);
+    const AttnParams &p = reread();
     const Work &w = pl.w;
     if (w.whole)
         return;

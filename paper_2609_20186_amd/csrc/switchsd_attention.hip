@@ -708,6 +708,12 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
     constexpr int kVBytes = 4 * 32 * PITCH, kOBytes = 4 * COLS * 4 * 64 * 16;
     __shared__ __attribute__((aligned(16))) char lds[kVBytes > kOBytes ? kVBytes : kOBytes];
     __shared__ float sm[4][TILE], sl[4][TILE];
+    // wide rows of the query stand in LDS, which all waves read them from: in registers
+    // they leave too few for keys and values on their way (67 x 32 heads over 2651 keys
+    // of 256: 311 us, so 229)
+    constexpr bool kSharedQ = D > 128;
+    constexpr int QP = D * 2 + 16, NK = kSharedQ ? 1 : D / 16;
+    __shared__ __attribute__((aligned(16))) char sq[kSharedQ ? TILE * QP : 16];
     __shared__ PlanShared sh;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -728,14 +734,37 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
         const float factor = fac.size;
 
         Row r[NQ];
-        u32x4 q[NQ][D / 16];
+        u32x4 q[NQ][NK], part[4];
         f32x16 o[NQ][D / 32];
         float m[NQ], l[NQ];
+        constexpr int kStep = kThreads * 16 / (D * 2);  // rows that all lanes read at once
+        if constexpr (kSharedQ) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const Row y = row_of(p, c, h, tile * TILE + x * kStep + tid / (D / 8));
+                part[x] = u32x4{0, 0, 0, 0};
+                if (y.ok)
+                    part[x] = *(const u32x4 *)((const char *)p.q +
+                                               (y.row * p.q_stride + (int64_t)y.head * D) * 2 +
+                                               tid % (D / 8) * 16);
+            }
+            apply_sign(part, fac.sign);
+        }
+        int at_q = (lane & 31) * QP + half * (E4M3 ? 32 : 16);
+        // the query's operand of step kk
+        const auto query = [&](int x, int kk) {
+            if constexpr (!kSharedQ)
+                return q[x][kk];
+            else
+                return *(const u32x4 *)(sq + at_q + (E4M3 ? kk / 2 * 64 + kk % 2 * 16 : kk * 32));
+        };
 #pragma unroll
         for (int x = 0; x < NQ; ++x) {
             r[x] = row_of(p, c, h, tile * TILE + x * 32 + (lane & 31));
-            load_query<E4M3, D>(p, r[x], q[x]);
-            apply_sign(q[x], fac.sign);
+            if constexpr (!kSharedQ) {
+                load_query<E4M3, D>(p, r[x], q[x]);
+                apply_sign(q[x], fac.sign);
+            }
             m[x] = -INFINITY;
             l[x] = 0.0f;
 #pragma unroll
@@ -769,12 +798,21 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
             load(kr, kbase, slot);
             load(vr, vbase, slot);
         }
+        if constexpr (kSharedQ) {
+            static_assert(!kSharedQ || (NQ == 1 && 4 * kStep == TILE), "four pieces for a lane");
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                *(u32x4 *)(sq + (x * kStep + tid / (D / 8)) * QP + tid % (D / 8) * 16) = part[x];
+            __syncthreads();
+        }
         for (int t = ua; t < stop; ++t) {
             const int kb = t * UNIT + wave * 32;
             const uint32_t valid = (uint32_t)__ballot(slot >= 0);
             const bool plain = valid == ~0u && kb + 31 < c.pos;
             f32x16 s[NQ][1];
             const int ahead = slot_in(p, entry, (t + 2) * UNIT + kl, keys);
+            if (kSharedQ)  // read in every unit, not kept in registers
+                asm volatile("" : "+v"(at_q));
             // before the next keys and values, which it is not to wait for
             entry = entry_of(p, table, (t + 3) * UNIT + kl, keys);
 #pragma unroll
@@ -787,16 +825,21 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
                     widen<TYPE>(kr[k], lo, hi);
 #pragma unroll
                     for (int x = 0; x < NQ; ++x) {
-                        s[x][0] = mfma<TYPE>(lo, q[x][k * 2], s[x][0]);
-                        s[x][0] = mfma<TYPE>(hi, q[x][k * 2 + 1], s[x][0]);
+                        s[x][0] = mfma<TYPE>(lo, query(x, k * 2), s[x][0]);
+                        s[x][0] = mfma<TYPE>(hi, query(x, k * 2 + 1), s[x][0]);
                     }
                 } else {
 #pragma unroll
                     for (int x = 0; x < NQ; ++x)
-                        s[x][0] = mfma<TYPE>(kr[k], q[x][k], s[x][0]);
+                        s[x][0] = mfma<TYPE>(kr[k], query(x, k), s[x][0]);
                 }
             }
-            load(kr, kbase, next);
+            // behind the last unit nothing more is read (17 x 32 heads over 1481 keys of 128:
+            // 33 -> 30 us), but where the branches cost more than the reads: 8-bit keys and
+            // 256-wide heads (67 x 32 over 2651: 229 us, with the branches 243)
+            const bool more = E4M3 || D > 128 || t + 1 < stop;
+            if (more)
+                load(kr, kbase, next);
             // values into LDS
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             char *dst = values + (lane & 31) * PITCH;
@@ -830,12 +873,12 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
                 }
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            load(vr, vbase, next);
+            if (more)
+                load(vr, vbase, next);
 #pragma unroll
             for (int x = 0; x < NQ; ++x) {
-                if (!plain) {
+                if (!plain)
                     hide(s[x][0], seen_bits(p, c, r[x], kb, valid));
-                }
                 const float alpha = follow<1>(s[x], factor, m[x], l[x]);
                 if (__any(alpha != 1.0f))
                     scale_rows<D>(o[x], alpha);

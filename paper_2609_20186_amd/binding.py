@@ -702,16 +702,19 @@ _DT["half"] = tuple(_HALF)
 def _rows(t, name, dev, heads=None):
     """Shape, row stride and device pointer of [rows, heads, D] elements whose rows
     may lie apart (parts of one projection's output)."""
-    if not isinstance(t, _Tensor) or not t.is_cuda or t.dim() != 3:
-        raise ValueError(f"{name} must be a device tensor [rows, heads, D]")
-    if t.dtype not in _HALF:
-        raise ValueError(f"{name} has dtype {t.dtype}, expected one of {_DT['half']}")
-    if t.get_device() != dev:
+    # the accepted case first, as in _arr
+    if not isinstance(t, _Tensor) or t.get_device() != dev or t.dtype not in _HALF or \
+            t.dim() != 3:
+        if not isinstance(t, _Tensor) or not t.is_cuda or t.dim() != 3:
+            raise ValueError(f"{name} must be a device tensor [rows, heads, D]")
+        if t.dtype not in _HALF:
+            raise ValueError(f"{name} has dtype {t.dtype}, expected one of {_DT['half']}")
         _here(t, name, dev)
-    n, H, D = shape = t.shape
+    shape = t.shape
     if heads is not None and shape != heads:
         raise ValueError(f"{name} has shape {tuple(shape)}, expected {tuple(heads)}")
     row, head, one = t.stride()
+    n, H, D = shape
     if (one != 1 and D > 1) or (head != D and H > 1):
         raise ValueError(f"the heads of {name} must be contiguous")
     return shape, row if n > 1 else max(row, H * D), t.data_ptr()
@@ -727,6 +730,8 @@ def _caches(k_cache, v_cache, dtype, Hkv, D, k_scale, v_scale, dev):
             _arr(v_cache, "cache", "v_cache", (n, Hkv, D), dev))
     if v_cache.dtype != kind or (kind != dtype and _CACHES[kind] != E4M3):
         raise ValueError(f"caches of {kind} and {v_cache.dtype} for rows of {dtype}")
+    if k_scale is None and v_scale is None:
+        return _CACHES[kind], n, ptrs, (None, None)
     return _CACHES[kind], n, ptrs, (
         None if k_scale is None else _arr(k_scale, "f32", "k_scale", (Hkv,), dev),
         None if v_scale is None else _arr(v_scale, "f32", "v_scale", (Hkv,), dev))
@@ -746,12 +751,13 @@ def switchsd_store_cache(keys, values, slots, k_cache, v_cache, count=None, k_sc
         raise ValueError(f"keys have dtype {keys.dtype}, values {values.dtype}")
     if not isinstance(slots, _Tensor) or slots.numel() != n:
         raise ValueError(f"slots must be a device tensor of {n} elements")
-    _sizes(n=n, Hkv=Hkv, D=D)
+    if n > _INT_MAX or Hkv > _INT_MAX or D > _INT_MAX:
+        _sizes(n=n, Hkv=Hkv, D=D)
     kind, n_slots, (p_kc, p_vc), (p_ks, p_vs) = _caches(k_cache, v_cache, keys.dtype, Hkv, D,
                                                         k_scale, v_scale, dev)
     _check("switchsd_store_cache", lib.switchsd_store_cache(
-        p_k, k_stride, p_v, v_stride, _HALF[keys.dtype], _arr(slots, "i64", "slots", slots.shape,
-                                                              dev), n,
+        p_k, k_stride, p_v, v_stride, _HALF[keys.dtype],
+        _arr(slots, "i64", "slots", slots.shape, dev), n,
         None if count is None else _arr(count, "i32", "count", (1,), dev), Hkv, D, p_kc, p_vc,
         kind, n_slots, p_ks, p_vs, _stream(stream)))
 
@@ -832,8 +838,9 @@ def build_logprob_args(logits, tokens=None, dn=None, dpar=None, accept_node=None
     (bf16 or its bits, fp16 or fp32), tokens [B, R] int32 (None where neither logprob
     nor rank is wanted), dn [B] (None: all rows); with accept_node [B], and dpar [B, R]
     (None: chains), the rows along each accepted path, tokens being the step's
-    out_tokens.  workspace: zeroed, of logprob_workspace_bytes, None: one of its own; switchsd_token_logprobs calls that share it (the result too) must be
-    ordered.  The tensors are kept alive by the result."""
+    out_tokens.  workspace: zeroed, of logprob_workspace_bytes, None: one of its own;
+    switchsd_token_logprobs calls that share it (the result too) must be ordered.  The
+    tensors are kept alive by the result."""
     if not isinstance(logits, _Tensor) or logits.dim() != 3:
         raise ValueError("logits must be a device tensor [B, R, V]")
     B, R, V = logits.shape
@@ -885,7 +892,8 @@ def switchsd_token_logprobs(args, logprob=None, lse=None, entropy=None, rank=Non
     top = (*shape, n_top)
     _check("switchsd_token_logprobs", lib.switchsd_token_logprobs(
         ctypes.byref(args), _arr(logprob, "f32", "logprob", shape, dev, True),
-        _arr(lse, "f32", "lse", shape, dev, True), _arr(entropy, "f32", "entropy", shape, dev, True),
+        _arr(lse, "f32", "lse", shape, dev, True),
+        _arr(entropy, "f32", "entropy", shape, dev, True),
         _arr(rank, "i32", "rank", shape, dev, True), n_top,
         _arr(top_ids, "i32", "top_ids", top, dev, True),
         _arr(top_logprobs, "f32", "top_logprobs", top, dev, True), _stream(stream)))

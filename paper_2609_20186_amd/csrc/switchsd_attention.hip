@@ -41,9 +41,10 @@ __device__ __forceinline__ int pack_e4m3(float a, float b, int old) {
     return __builtin_amdgcn_cvt_pk_fp8_f32(a, b, old, HIGH);
 }
 
-// A lane per 16 bytes of a row's keys or values.  Moves 4 Hkv D bytes in and as
-// many (or half) out: bound by its launch for the rows of a step, by the memory
-// for prompts.
+// A lane per 16 bytes of a row's keys or values, so that loads and stores are whole
+// vectors whatever the slots' order.  Moves 4 Hkv D bytes in and as many (or half)
+// out: bound by its launch for the rows of a step (256 rows of 8 heads of 128: 2.8 us),
+// by the memory for prompts (16 of up to 2048 tokens, 8 heads of 64: 18.8 us, 5.4 TB/s).
 template <int TYPE, bool E4M3>
 __global__ void __launch_bounds__(kThreads) k_store(const StoreParams p) {
     const uint32_t vecs = (uint32_t)(p.Hkv * p.D) / 8;
@@ -81,6 +82,15 @@ __global__ void __launch_bounds__(kThreads) k_store(const StoreParams p) {
 }
 
 // ---- attention
+//
+// For a query row q and the keys k_j that it sees, s_j = scale q . k_j, the output is
+// sum_j e^(s_j - m) v_j / sum_j e^(s_j - m) for any m: one pass over the keys with a
+// running m, the sums multiplied by e^(m - m') when it moves.  All query heads of a head of
+// the cache and all new tokens are rows of one matrix, so that a key is read once for
+// all of them.  S^T = K Q^T and O^T = V^T P^T: a column of the products is a query
+// row, so a lane holds (half of) one row's weights, which are the second product's
+// operand as they stand.  Few rows (k_attend_few) are bound by the bytes of the
+// cache, many (k_attend_many) by the exponentials and the matrix instructions.
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
@@ -519,7 +529,9 @@ __device__ __forceinline__ void hide(f32x16 &s, uint32_t seen) {
 // Running softmax of one query row per lane (both halves of a wave hold the same
 // rows, each the keys that its half of the products has): m is the maximum that
 // the weights are taken against, in powers of two; it follows the true one with
-// a delay of up to kDelay, which weights of up to 2^kDelay carry.
+// a delay of up to kDelay, which weights of up to 2^kDelay carry.  (Sums in 32 bits have
+// room for them, and fp16's largest number, 65504, is far from 256; a row's sums are
+// multiplied a few times in all, not in every other tile.)
 constexpr float kDelay = 8.0f;
 
 __device__ __forceinline__ float other_half(float v) {
@@ -550,7 +562,10 @@ __device__ __forceinline__ float follow(const f32x16 (&s)[N], float factor, floa
     return alpha;
 }
 // Products -> weights, in 32 bits in s, summed to l; the weights in 16 bits as the
-// right operand of 2 N products with 16 keys each.
+// right operand of 2 N products with 16 keys each.  That rounding is the price of the
+// matrix instructions, whose operands are both of the values' type: at most half a step of
+// a weight, 2^-8 of it (bf16) or 2^-11 (fp16), less for a sum of many.  The sum of the
+// weights is that of the unrounded ones.
 template <int TYPE, int N>
 __device__ __forceinline__ void weigh(f32x16 (&s)[N], float factor, float m, float &l,
                                       u32x4 (&w)[2 * N]) {
@@ -697,7 +712,13 @@ __device__ __forceinline__ int slot_of(const AttnParams &p, const int32_t *table
 // Up to 32 NQ query rows (all new tokens and query heads of one head of the
 // cache): the four waves take 32 keys each of every unit of 128, keys straight
 // into the registers that the products read, values through a part of LDS of
-// their own, so that no wave waits for another before the end.
+// their own, so that no wave waits for another before the end.  The next unit's keys
+// and values are on their way while the present one's are multiplied; the page table's
+// entries are read two units ahead, since loads come back in order.
+//   32 x 8 rows (32 + 8 heads of 128, bf16) over up to 4096 keys: 91 us, 4.3 TB/s, and
+// 8 of k_merge; 96 x 32 heads, one token, over 3682: 219 us, 4.9 TB/s; the first keys
+// arrive some 10 us after the launch.  One token over 512 keys: 12.4 us, a chain of
+// plan, page table, first keys and the join of four waves.
 template <int TYPE, bool E4M3, int D, int NQ>
 __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
     k_attend_few(const AttnParams) {
@@ -927,7 +948,8 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
 #pragma unroll
             for (int v = 0; v < 4; ++v)
                 sum += sm[v][row] == -INFINITY ? 0.0f
-                                               : sl[v][row] * __builtin_amdgcn_exp2f(sm[v][row] - top);
+                                               : sl[v][row] *
+                                                     __builtin_amdgcn_exp2f(sm[v][row] - top);
             const float f = m[x] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[x] - top);
             // each wave adds up one block of columns
 #pragma unroll
@@ -967,7 +989,13 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
 
 // Tiles of 128 query rows, 32 for each wave; the four waves share 64 keys and
 // values at a time in LDS, two buffers of them, the next ones on their way through
-// registers while the present ones are used.
+// registers while the present ones are used.  (Loads straight into LDS save those registers,
+// but the compiler waits for all of them before any read of LDS.)
+//   Chunks of prompts, 32 + 8 heads of 128, bf16: 880 us, 920 TFLOP/s; 256 x 60 drafted
+// nodes over up to 2048 keys: 620 us, 530 TFLOP/s.  A wave needs 1024 cycles of matrix
+// instructions for a tile of 32 rows and 64 keys, and some 1450 of vector ones (512 of
+// them the exponentials): two waves on a SIMD are bound by those, and in part by waits,
+// with the matrix unit in use for a third of the time.
 template <int TYPE, bool E4M3, int D>
 __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(const AttnParams) {
     constexpr int TILE = 128, UNIT = 64;
@@ -1005,7 +1033,8 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
         // keys that the tile's (the wave's) last row sees
         int lim = keys, wlim = keys;
         if (!p.a.mask) {
-            const int i1 = (tile * TILE + TILE - 1) / p.G, i2 = (tile * TILE + wave * 32 + 31) / p.G;
+            const int i1 = (tile * TILE + TILE - 1) / p.G;
+            const int i2 = (tile * TILE + wave * 32 + 31) / p.G;
             const int64_t e1 = (int64_t)c.pos + (i1 < c.n ? i1 + 1 : c.n);
             const int64_t e2 = (int64_t)c.pos + (i2 < c.n ? i2 + 1 : c.n);
             lim = e1 < keys ? (int)e1 : keys;
@@ -1165,7 +1194,8 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
                 add_values<TYPE, D, 2>(weights, V, VP, o);
             }
             if (t + 1 < ub)
-                stash((uint32_t)((j < 3 ? valid : valid_next) >> ((j + 1) & 3) * 16) & 0xFFFFu, t + 1);
+                stash((uint32_t)((j < 3 ? valid : valid_next) >> ((j + 1) & 3) * 16) & 0xFFFFu,
+                      t + 1);
         }
         __syncthreads();
         const bool poisoned = s_poison != 0;
@@ -1190,13 +1220,23 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
     } while (next<TILE, UNIT>(reread(), k));
 }
 
+// A partial result added to a row's.
+__device__ __forceinline__ void add_part(float &m, float &l, f32x4 &o, float pm, float ps,
+                                         f32x4 po) {
+    const float mn = fmaxf(m, pm), at = mn == -INFINITY ? 0.0f : mn;
+    const float f = __builtin_amdgcn_exp2f(m - at), pf = __builtin_amdgcn_exp2f(pm - at);
+    m = mn;
+    l = l * f + ps * pf;
+    o = o * f + po * pf;
+}
+
 // Joins the partial results of the items that were cut.  Of a work-group's lanes,
 // D / 4 take four elements each of a row; `parts` such groups of lanes take every
 // parts-th result of one row, the others another row.
-template <int TYPE, int D, int TILE, int UNIT>
+template <int TYPE, int D, int TILE, int UNIT, int kRows>
 __global__ void __launch_bounds__(kThreads) k_merge(const AttnParams, int parts,
                                                     uint32_t groups) {
-    constexpr int LANES = D / 4, kSets = kThreads / LANES;
+    constexpr int LANES = D / 4, kSets = kThreads / LANES, kLoops = 4 / kRows;
     __shared__ PlanShared sh;
     __shared__ f32x4 so[kThreads];
     __shared__ float2 sml[kThreads];
@@ -1213,11 +1253,14 @@ __global__ void __launch_bounds__(kThreads) k_merge(const AttnParams, int parts,
     const uint32_t to = (uint32_t)(((uint64_t)blockIdx.x + 1) * all / gridDim.x);
     uint32_t found = ~0u, item = 0, base = 0;
     Seq s;
-    for (uint32_t id = from; id < to; ++id) {
+    for (uint32_t id = from, n; id < to; id += n) {
         if (id / groups != found) {
             found = id / groups;
             find<TILE, UNIT>(p, pl, true, found, sh, s, item, base);
         }
+        n = groups - id % groups;
+        n = n < to - id ? n : to - id;
+        n = n < kRows ? n : kRows;
         const Chunk &c = s.c;
         uint32_t nu = (uint32_t)s.units, u0 = base + item * nu;
         if (TILE > UNIT && s.grow) {
@@ -1233,48 +1276,59 @@ __global__ void __launch_bounds__(kThreads) k_merge(const AttnParams, int parts,
         const int h = (int)item % p.a.Hkv;
         const int tile = TILE > UNIT && !s.grow ? s.tiles - 1 - (int)item / p.a.Hkv
                                                 : (int)item / p.a.Hkv;
-        const int row = (int)(id % groups) * (kSets / parts) + set / parts;
-        const Row r = row_of(p, c, h, tile * TILE + row);
-        const bool on = row < TILE && r.ok;
-        float m = -INFINITY, l = 0.0f;
-        f32x4 o = f32x4{0};
-        if (on) {
-            const int64_t stride = TILE * (D + 2);
-#pragma unroll 4
-            for (uint32_t g = g0 + set % parts; g <= g1; g += parts) {
-                const float *part = p.part + ((int64_t)g * 2 + (g == g0 && late ? 1 : 0)) * stride;
-                const float pm = part[TILE * D + row], pl = part[TILE * D + TILE + row];
-                const f32x4 po = *(const f32x4 *)(part + row * D + d);
-                const float mn = fmaxf(m, pm), at = mn == -INFINITY ? 0.0f : mn;
-                const float f = __builtin_amdgcn_exp2f(m - at), pf = __builtin_amdgcn_exp2f(pm - at);
-                m = mn;
-                l = l * f + pl * pf;
-                o = o * f + po * pf;
-            }
+        Row r[kRows];
+        int row[kRows];
+        bool on[kRows];
+        float m[kRows], l[kRows];
+        f32x4 o[kRows];
+#pragma unroll
+        for (int y = 0; y < kRows; ++y) {
+            const int at = (int)(id % groups + y) * (kSets / parts) + set / parts;
+            r[y] = row_of(p, c, h, tile * TILE + at);
+            on[y] = (uint32_t)y < n && at < TILE && r[y].ok;
+            row[y] = on[y] ? at : 0;  // read all the same
+            m[y] = -INFINITY;
+            l[y] = 0.0f;
+            o[y] = f32x4{0};
         }
-        if (parts > 1) {
-            __syncthreads();  // the last row group's use of LDS
-            so[tid] = o;
-            sml[tid] = make_float2(m, l);
-            __syncthreads();
-            for (int x = 1; x < parts && set % parts == 0; ++x) {
-                const float2 y = sml[tid + x * LANES];
-                const f32x4 po = so[tid + x * LANES];
-                const float mn = fmaxf(m, y.x), at = mn == -INFINITY ? 0.0f : mn;
-                const float f = __builtin_amdgcn_exp2f(m - at), pf = __builtin_amdgcn_exp2f(y.x - at);
-                m = mn;
-                l = l * f + y.y * pf;
-                o = o * f + po * pf;
+#pragma unroll kLoops
+        for (uint32_t g = g0 + set % parts; g <= g1; g += parts) {
+            const float *part =
+                p.part + ((int64_t)g * 2 + (g == g0 && late ? 1 : 0)) * (TILE * (D + 2));
+            float pm[kRows], ps[kRows];
+            f32x4 po[kRows];
+#pragma unroll
+            for (int y = 0; y < kRows; ++y) {
+                pm[y] = part[TILE * D + row[y]];
+                ps[y] = part[TILE * D + TILE + row[y]];
+                po[y] = *(const f32x4 *)(part + row[y] * D + d);
             }
+#pragma unroll
+            for (int y = 0; y < kRows; ++y)
+                add_part(m[y], l[y], o[y], pm[y], ps[y], po[y]);
         }
-        if (!on || set % parts)
-            continue;
-        o = l == 0.0f ? f32x4{0} : o * ((p.v_scale ? p.v_scale[h] : 1.0f) / l);
-        *(uint2 *)((char *)p.out + ((r.row * p.a.Hq + r.head) * D + d) * 2) =
-            make_uint2(pack2<TYPE>(o[0], o[1]), pack2<TYPE>(o[2], o[3]));
-        if (p.lse && d == 0)
-            p.lse[r.row * p.a.Hq + r.head] =
-                l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+#pragma unroll
+        for (int y = 0; y < kRows; ++y) {
+            if (parts > 1) {
+                __syncthreads();  // the last row's use of LDS
+                so[tid] = o[y];
+                sml[tid] = make_float2(m[y], l[y]);
+                __syncthreads();
+                for (int x = 1; x < parts && set % parts == 0; ++x) {
+                    const float2 z = sml[tid + x * LANES];
+                    add_part(m[y], l[y], o[y], z.x, z.y, so[tid + x * LANES]);
+                }
+            }
+            if (!on[y] || set % parts)
+                continue;
+            const float f = l[y] == 0.0f ? 0.0f : (p.v_scale ? p.v_scale[h] : 1.0f) / l[y];
+            const f32x4 v = l[y] == 0.0f ? f32x4{0} : o[y] * f;
+            *(uint2 *)((char *)p.out + ((r[y].row * p.a.Hq + r[y].head) * D + d) * 2) =
+                make_uint2(pack2<TYPE>(v[0], v[1]), pack2<TYPE>(v[2], v[3]));
+            if (p.lse && d == 0)
+                p.lse[r[y].row * p.a.Hq + r[y].head] =
+                    l[y] == 0.0f ? -INFINITY : (m[y] + __builtin_amdgcn_logf(l[y])) * kLn2;
+        }
     }
 }
 
@@ -1312,9 +1366,16 @@ void launch_merge(const AttnParams &p, int64_t items, hipStream_t stream) {
     while (parts < kSets && parts * items < p.groups && items * groups() < kAttnMerge)
         parts *= 2;
     const int64_t all = items * groups();
-    hipLaunchKernelGGL((k_merge<TYPE, D, TILE, UNIT>),
-                       dim3((unsigned)(all < kAttnMerge ? all : kAttnMerge)), dim3(kThreads), 0,
-                       stream, p, parts, (uint32_t)groups());
+    const dim3 g((unsigned)(all < kAttnMerge ? all : kAttnMerge)), t(kThreads);
+    // four rows of an item at once where a work-group has eight and more groups of them (242 x
+    // 95 rows over 1718 keys: 267 -> 261 us); with fewer, four results of one (3 x 324 over
+    // 1749: 36 us, four rows at once 41)
+    if (all >= 8 * kAttnMerge)
+        hipLaunchKernelGGL((k_merge<TYPE, D, TILE, UNIT, 4>), g, t, 0, stream, p, parts,
+                           (uint32_t)groups());
+    else
+        hipLaunchKernelGGL((k_merge<TYPE, D, TILE, UNIT, 1>), g, t, 0, stream, p, parts,
+                           (uint32_t)groups());
 }
 
 template <int TYPE, bool E4M3, int D>

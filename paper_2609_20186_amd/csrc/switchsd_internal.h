@@ -299,17 +299,28 @@ struct AttnParams {
     int32_t groups;    // work-groups that share the keys of few items
 };
 
-// Work-groups that share an attention's keys where there are few rows, and the
-// items (tiles of rows and heads) from which each takes a whole one; the fewest
-// units of keys per work-group; the longest contexts that are never cut.
+// Work-groups that share an attention's keys where there are few items (tiles of rows
+// and heads of the cache): as many as the device holds at once, two on a compute unit
+// (half as many where registers allow one).
 constexpr int kAttnGroups = 512;
+// With so many items each work-group takes a whole one: four rounds of work-groups end
+// evenly enough, and nothing has to be joined.
 constexpr int kAttnWhole = 2048;
+// The fewest units of keys for a work-group.  With 4 one token over 17195 keys takes 23.4
+// us (20.7), 17 drafted ones over 8972 28.8 (27.1).
 constexpr int kAttnLeast = 2;
+// Contexts of up to so many tokens are never cut: the join costs more than it saves.  13
+// prompts of 285 tokens (40 + 8 heads of 256) take 85 us so, 147 where 512 is the most; 7 x
+// 128 heads over 924 keys 13.6 and 21.7.
 constexpr int kAttnShort = 1024;
-constexpr int kAttnMerge = 1024;  // work-groups that join what was cut
+// Work-groups that join what was cut.  With 2048 13 x 35 rows over 1859 keys take 38.9
+// us (36.2), with 4096 48.7.
+constexpr int kAttnMerge = 1024;
 
 // Query rows (new tokens times query heads of one head of the cache) of a
-// work-group, by the most that a sequence has.
+// work-group, by the most that a sequence has: up to 64 (32 of 256-wide heads) the keys
+// and values go straight into each wave's registers, beyond that four waves share
+// them in LDS.
 constexpr int attention_tile(int64_t most, int32_t D) {
     return most <= 32 ? 32 : most <= 64 && D <= 128 ? 64 : 128;
 }

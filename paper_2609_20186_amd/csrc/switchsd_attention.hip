@@ -126,7 +126,7 @@ __device__ __forceinline__ float cached(const void *base, int64_t at) {
 // The work of a launch, cut on the device: items are (sequence, tile of query
 // rows, head of the cache), an item's keys are cut into units, and what a
 // work-group takes is found by the sums over all sequences of what comes before it.
-// With many items each work-group takes one whole; with few, kAttnGroups
+// With many items each work-group takes one whole; with few, up to kAttnGroups
 // work-groups take equal shares of all units, in order, and k_merge joins what
 // was cut.  The host has seen to it that items, and with few of them units, fit 32
 // bits.
@@ -228,7 +228,7 @@ __device__ __forceinline__ Plan plan(const AttnParams &p, PlanShared &sh) {
     // stays in scalar registers
     q.w.items = __builtin_amdgcn_readfirstlane(items);
     q.w.units = __builtin_amdgcn_readfirstlane(units);
-    q.w.whole = p.whole || q.w.items >= kAttnWhole;
+    q.w.whole = p.whole || q.w.items >= attention_whole(TILE);
     const uint32_t most = q.w.units / kAttnLeast;
     const uint32_t limit = (uint32_t)p.groups;
     q.w.groups = q.w.whole ? q.w.items : most < 1 ? 1 : most < limit ? most : limit;
@@ -709,7 +709,7 @@ __device__ __forceinline__ int slot_of(const AttnParams &p, const int32_t *table
     return slot_in(p, entry_of(p, table, pos, keys), pos, keys);
 }
 
-// Up to 32 NQ query rows (all new tokens and query heads of one head of the
+// Up to 32 query rows (all new tokens and query heads of one head of the
 // cache): the four waves take 32 keys each of every unit of 128, keys straight
 // into the registers that the products read, values through a part of LDS of
 // their own, so that no wave waits for another before the end.  The next unit's keys
@@ -719,10 +719,9 @@ __device__ __forceinline__ int slot_of(const AttnParams &p, const int32_t *table
 // 8 of k_merge; 96 x 32 heads, one token, over 3682: 219 us, 4.9 TB/s; the first keys
 // arrive some 10 us after the launch.  One token over 512 keys: 12.4 us, a chain of
 // plan, page table, first keys and the join of four waves.
-template <int TYPE, bool E4M3, int D, int NQ>
-__global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
-    k_attend_few(const AttnParams) {
-    constexpr int TILE = 32 * NQ, UNIT = 128;
+template <int TYPE, bool E4M3, int D>
+__global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_few(const AttnParams) {
+    constexpr int TILE = 32, UNIT = 128;
     constexpr int CH = E4M3 ? D / 32 : D / 16;  // 16-byte pieces of a row per half wave
     constexpr int PITCH = D * 2 + 32;
     constexpr int COLS = D / 32 < 4 ? D / 32 : 4;  // blocks of 32 columns joined at once
@@ -754,10 +753,10 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
         const Factor fac = factor_of(p, h);
         const float factor = fac.size;
 
-        Row r[NQ];
-        u32x4 q[NQ][NK], part[4];
-        f32x16 o[NQ][D / 32];
-        float m[NQ], l[NQ];
+        const Row r = row_of(p, c, h, tile * TILE + (lane & 31));
+        u32x4 q[NK], part[4];
+        f32x16 o[D / 32];
+        float m = -INFINITY, l = 0.0f;
         constexpr int kStep = kThreads * 16 / (D * 2);  // rows that all lanes read at once
         if constexpr (kSharedQ) {
 #pragma unroll
@@ -773,25 +772,19 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
         }
         int at_q = (lane & 31) * QP + half * (E4M3 ? 32 : 16);
         // the query's operand of step kk
-        const auto query = [&](int x, int kk) {
+        const auto query = [&](int kk) {
             if constexpr (!kSharedQ)
-                return q[x][kk];
+                return q[kk];
             else
                 return *(const u32x4 *)(sq + at_q + (E4M3 ? kk / 2 * 64 + kk % 2 * 16 : kk * 32));
         };
-#pragma unroll
-        for (int x = 0; x < NQ; ++x) {
-            r[x] = row_of(p, c, h, tile * TILE + x * 32 + (lane & 31));
-            if constexpr (!kSharedQ) {
-                load_query<E4M3, D>(p, r[x], q[x]);
-                apply_sign(q[x], fac.sign);
-            }
-            m[x] = -INFINITY;
-            l[x] = 0.0f;
-#pragma unroll
-            for (int dt = 0; dt < D / 32; ++dt)
-                o[x][dt] = f32x16{0};
+        if constexpr (!kSharedQ) {
+            load_query<E4M3, D>(p, r, q);
+            apply_sign(q, fac.sign);
         }
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+            o[dt] = f32x16{0};
 
         // a lane's key is its number within 32; both halves of a row are read by
         // the two lanes of its number
@@ -820,7 +813,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
             load(vr, vbase, slot);
         }
         if constexpr (kSharedQ) {
-            static_assert(!kSharedQ || (NQ == 1 && 4 * kStep == TILE), "four pieces for a lane");
+            static_assert(!kSharedQ || 4 * kStep == TILE, "four pieces for a lane");
 #pragma unroll
             for (int x = 0; x < 4; ++x)
                 *(u32x4 *)(sq + (x * kStep + tid / (D / 8)) * QP + tid % (D / 8) * 16) = part[x];
@@ -830,29 +823,21 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
             const int kb = t * UNIT + wave * 32;
             const uint32_t valid = (uint32_t)__ballot(slot >= 0);
             const bool plain = valid == ~0u && kb + 31 < c.pos;
-            f32x16 s[NQ][1];
+            f32x16 s[1] = {f32x16{0}};
             const int ahead = slot_in(p, entry, (t + 2) * UNIT + kl, keys);
             if (kSharedQ)  // read in every unit, not kept in registers
                 asm volatile("" : "+v"(at_q));
             // before the next keys and values, which it is not to wait for
             entry = entry_of(p, table, (t + 3) * UNIT + kl, keys);
 #pragma unroll
-            for (int x = 0; x < NQ; ++x)
-                s[x][0] = f32x16{0};
-#pragma unroll
             for (int k = 0; k < CH; ++k) {
                 if (E4M3) {
                     u32x4 lo, hi;
                     widen<TYPE>(kr[k], lo, hi);
-#pragma unroll
-                    for (int x = 0; x < NQ; ++x) {
-                        s[x][0] = mfma<TYPE>(lo, query(x, k * 2), s[x][0]);
-                        s[x][0] = mfma<TYPE>(hi, query(x, k * 2 + 1), s[x][0]);
-                    }
+                    s[0] = mfma<TYPE>(lo, query(k * 2), s[0]);
+                    s[0] = mfma<TYPE>(hi, query(k * 2 + 1), s[0]);
                 } else {
-#pragma unroll
-                    for (int x = 0; x < NQ; ++x)
-                        s[x][0] = mfma<TYPE>(kr[k], query(x, k), s[x][0]);
+                    s[0] = mfma<TYPE>(kr[k], query(k), s[0]);
                 }
             }
             // behind the last unit nothing more is read (17 x 32 heads over 1481 keys of 128:
@@ -896,17 +881,14 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             if (more)
                 load(vr, vbase, next);
-#pragma unroll
-            for (int x = 0; x < NQ; ++x) {
-                if (!plain)
-                    hide(s[x][0], seen_bits(p, c, r[x], kb, valid));
-                const float alpha = follow<1>(s[x], factor, m[x], l[x]);
-                if (__any(alpha != 1.0f))
-                    scale_rows<D>(o[x], alpha);
-                u32x4 weights[2];
-                weigh<TYPE, 1>(s[x], factor, m[x], l[x], weights);
-                add_values<TYPE, D, 1>(weights, values, PITCH, o[x]);
-            }
+            if (!plain)
+                hide(s[0], seen_bits(p, c, r, kb, valid));
+            const float alpha = follow<1>(s, factor, m, l);
+            if (__any(alpha != 1.0f))
+                scale_rows<D>(o, alpha);
+            u32x4 weights[2];
+            weigh<TYPE, 1>(s, factor, m, l, weights);
+            add_values<TYPE, D, 1>(weights, values, PITCH, o);
             slot = next;
             next = ahead;
         }
@@ -918,70 +900,59 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && D <= 128 ? 2 : 1)
                 const uint32_t valid = (uint32_t)__ballot(at >= 0);
                 if (valid == ~0u && kb + 31 < c.pos)
                     continue;
-#pragma unroll
-                for (int x = 0; x < NQ; ++x)
-                    add_not_finite<TYPE, E4M3, D>(p, h, at, seen_bits(p, c, r[x], kb, valid),
-                                                  o[x]);
+                add_not_finite<TYPE, E4M3, D>(p, h, at, seen_bits(p, c, r, kb, valid), o);
             }
         }
 
         // join the four waves
         const AttnParams &pe = reread();
         const int64_t place = k.done ? -1 : (int64_t)blockIdx.x * 2 + (first ? 0 : 1);
-#pragma unroll
-        for (int x = 0; x < NQ; ++x) {
-            l[x] += other_half(l[x]);
-            if (half == 0) {
-                sm[wave][x * 32 + lane] = m[x];
-                sl[wave][x * 32 + lane] = l[x];
-            }
+        l += other_half(l);
+        const int row = lane & 31;
+        if (half == 0) {
+            sm[wave][row] = m;
+            sl[wave][row] = l;
         }
         __syncthreads();
+        float top = sm[0][row];
 #pragma unroll
-        for (int x = 0; x < NQ; ++x) {
-            const int row = x * 32 + (lane & 31);
-            float top = sm[0][row];
+        for (int v = 1; v < 4; ++v)
+            top = fmaxf(top, sm[v][row]);
+        float sum = 0.0f;
 #pragma unroll
-            for (int v = 1; v < 4; ++v)
-                top = fmaxf(top, sm[v][row]);
-            float sum = 0.0f;
+        for (int v = 0; v < 4; ++v)
+            sum += sm[v][row] == -INFINITY ? 0.0f
+                                           : sl[v][row] * __builtin_amdgcn_exp2f(sm[v][row] - top);
+        const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+        // each wave adds up one block of columns
 #pragma unroll
-            for (int v = 0; v < 4; ++v)
-                sum += sm[v][row] == -INFINITY ? 0.0f
-                                               : sl[v][row] *
-                                                     __builtin_amdgcn_exp2f(sm[v][row] - top);
-            const float f = m[x] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[x] - top);
-            // each wave adds up one block of columns
+        for (int d0 = 0; d0 < D / 32; d0 += COLS) {
 #pragma unroll
-            for (int d0 = 0; d0 < D / 32; d0 += COLS) {
+            for (int y = 0; y < COLS; ++y)
 #pragma unroll
-                for (int y = 0; y < COLS; ++y)
+                for (int g = 0; g < 4; ++g) {
+                    f32x4 v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        v[e] = o[d0 + y][g * 4 + e] * f;
+                    *(f32x4 *)(lds + (((wave * COLS + y) * 4 + g) * 64 + lane) * 16) = v;
+                }
+            __syncthreads();
+            if (wave < COLS) {
+                f32x16 t = f32x16{0};
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        f32x4 v;
+                        const f32x4 y =
+                            *(const f32x4 *)(lds + (((v * COLS + wave) * 4 + g) * 64 + lane) * 16);
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            v[e] = o[x][d0 + y][g * 4 + e] * f;
-                        *(f32x4 *)(lds + (((wave * COLS + y) * 4 + g) * 64 + lane) * 16) = v;
+                            t[g * 4 + e] += y[e];
                     }
-                __syncthreads();
-                if (wave < COLS) {
-                    f32x16 t = f32x16{0};
-#pragma unroll
-                    for (int v = 0; v < 4; ++v)
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            const f32x4 y = *(const f32x4 *)(
-                                lds + (((v * COLS + wave) * 4 + g) * 64 + lane) * 16);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                t[g * 4 + e] += y[e];
-                        }
-                    put<TYPE, D, TILE>(pe, r[x], h, x * 32 + (lane & 31), place, d0 + wave, t,
-                                       top, sum);
-                }
-                __syncthreads();
+                put<TYPE, D, TILE>(pe, r, h, row, place, d0 + wave, t, top, sum);
             }
+            __syncthreads();
         }
         first = false;
     } while (next<TILE, UNIT>(reread(), k));
@@ -1360,7 +1331,7 @@ void launch_merge(const AttnParams &p, int64_t items, hipStream_t stream) {
     constexpr int kSets = kThreads / (D / 4);
     // lanes for a row's results beside each other while there are too few rows
     const int64_t rows = (int64_t)p.a.R * p.G < TILE ? (int64_t)p.a.R * p.G : TILE;
-    items = items < kAttnWhole ? items : kAttnWhole;
+    items = items < attention_whole(TILE) ? items : attention_whole(TILE);
     int parts = 1;
     const auto groups = [&]() { return (rows * parts + kSets - 1) / kSets; };
     while (parts < kSets && parts * items < p.groups && items * groups() < kAttnMerge)
@@ -1380,7 +1351,8 @@ void launch_merge(const AttnParams &p, int64_t items, hipStream_t stream) {
 
 template <int TYPE, bool E4M3, int D>
 int launch_attend(AttnParams p, hipStream_t stream) {
-    const int64_t rows = (int64_t)p.a.R * p.G, tile = attention_tile(rows, D);
+    const int64_t rows = (int64_t)p.a.R * p.G, tile = attention_tile(rows);
+    const int64_t whole = attention_whole(tile);
     int64_t items = (int64_t)p.a.B * ((rows + tile - 1) / tile);
     // what a device's cu that does not ascend could ask for is to fit 32 bits too
     if (items * p.a.Hkv >= 1ll << 31)
@@ -1396,24 +1368,18 @@ int launch_attend(AttnParams p, hipStream_t stream) {
     const int64_t keys = len < cap ? len : cap;
     // never cut: short contexts, and lengths whose units would not fit 32 bits
     p.whole = keys <= kAttnShort ||
-              (cut < kAttnWhole ? cut : kAttnWhole) * (keys / 64 + 4) >= (1ll << 31);
+              (cut < whole ? cut : whole) * (keys / 64 + 4) >= (1ll << 31);
     // as many as the device holds at once: two on a compute unit where their registers
     // allow it
-    p.groups = D == 256 || tile == 64 ? kAttnGroups / 2 : kAttnGroups;
+    p.groups = D == 256 ? kAttnGroups / 2 : kAttnGroups;
     const int64_t groups = p.whole || items > p.groups ? items : p.groups;
     if (groups >= 1 << 24)
         return SWITCHSD_ESHAPE;
     const dim3 g((unsigned)groups), t(kThreads);
     if (tile == 32) {
-        hipLaunchKernelGGL((k_attend_few<TYPE, E4M3, D, 1>), g, t, 0, stream, p);
+        hipLaunchKernelGGL((k_attend_few<TYPE, E4M3, D>), g, t, 0, stream, p);
         if (!p.whole)
             launch_merge<TYPE, D, 32, 128>(p, items, stream);
-    } else if (tile == 64) {
-        if constexpr (D <= 128) {
-            hipLaunchKernelGGL((k_attend_few<TYPE, E4M3, D, 2>), g, t, 0, stream, p);
-            if (!p.whole)
-                launch_merge<TYPE, D, 64, 128>(p, items, stream);
-        }
     } else {
         hipLaunchKernelGGL((k_attend_many<TYPE, E4M3, D>), g, t, 0, stream, p);
         if (!p.whole)

@@ -303,9 +303,6 @@ struct AttnParams {
 // and heads of the cache): as many as the device holds at once, two on a compute unit
 // (half as many where registers allow one).
 constexpr int kAttnGroups = 512;
-// With so many items each work-group takes a whole one: four rounds of work-groups end
-// evenly enough, and nothing has to be joined.
-constexpr int kAttnWhole = 2048;
 // The fewest units of keys for a work-group.  With 4 one token over 17195 keys takes 23.4
 // us (20.7), 17 drafted ones over 8972 28.8 (27.1).
 constexpr int kAttnLeast = 2;
@@ -317,17 +314,23 @@ constexpr int kAttnShort = 1024;
 // us (36.2), with 4096 48.7.
 constexpr int kAttnMerge = 1024;
 
-// Query rows (new tokens times query heads of one head of the cache) of a
-// work-group, by the most that a sequence has: up to 64 (32 of 256-wide heads) the keys
-// and values go straight into each wave's registers, beyond that four waves share
-// them in LDS.
-constexpr int attention_tile(int64_t most, int32_t D) {
-    return most <= 32 ? 32 : most <= 64 && D <= 128 ? 64 : 128;
-}
+// Query rows (new tokens times query heads of one head of the cache) of a work-group,
+// by the most that a sequence has.  64 rows in the form for few took longer in the most
+// cases (20 x 64 over 6221 keys: 116 us, in the form for many 106; 183 x 60 over 99: 29
+// and 17).  17 to 32 rows in the form for many take less of long contexts (14 x 30 over
+// 8373: 34 us, not 38), more of short ones (7 x 31 over 317: 16.2, not 12.8) and of
+// 256-wide heads (54 x 29 over 9117: 408, not 307).
+constexpr int attention_tile(int64_t most) { return most <= 32 ? 32 : 128; }
+// With so many items each work-group takes a whole one, and nothing has to be joined: more
+// with few rows, whose work-groups are bound by the memory and end apart (1048 items of
+// 28 rows, 131 sequences of up to 8598 keys: 430 us, whole 574; 3696 of 30 rows over 1219:
+// 249, whole 264) than with many (1672 tiles of prompts: 156 us, cut 185; 4096 of trees:
+// 608, cut 735).
+constexpr uint32_t attention_whole(int64_t tile) { return tile == 32 ? 4096 : 1024; }
 // Floats of the partial results: each of kAttnGroups work-groups leaves at most
 // two, of as many rows as a work-group takes, D sums, a maximum and a sum each.
 constexpr size_t attention_part_floats(int64_t most, int32_t D) {
-    return (size_t)2 * kAttnGroups * attention_tile(most, D) * (D + 2);
+    return (size_t)2 * kAttnGroups * attention_tile(most) * (D + 2);
 }
 
 int launch_store_kernel(const StoreParams &p, int32_t type, int32_t cache_type,

@@ -154,7 +154,7 @@ HEADS = [(1, 1), (4, 1), (5, 5), (8, 2), (14, 2), (16, 1)]
                                         ("f16", "e4m3")])
 @pytest.mark.parametrize("form", ["single", "chain", "tree", "packed"])
 def test_types_and_forms(D, type, cache, form):
-    """Every kernel: one tile of 32 rows, of 64, several of 128, by the heads."""
+    """Every kernel: one tile of 32 rows, several of 128, by the heads."""
     for n, (Hq, Hkv) in enumerate([(4, 2), (16, 2), (8, 1)]):
         new = {"single": [1, 1, 1], "chain": [6, 1, 5], "tree": [13, 12, 7],
                "packed": [19, 1, 33]}[form]

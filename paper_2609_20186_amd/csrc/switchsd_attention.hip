@@ -172,7 +172,8 @@ __device__ __forceinline__ Seq seq_of(const AttnParams &p, int b) {
     s.tiles = (int)(((int64_t)s.c.n * p.G + TILE - 1) / TILE);
     s.units = s.keys > UNIT ? (s.keys + UNIT - 1) / UNIT : 1;
     s.grow = 0;
-    if (TILE > UNIT && !p.a.mask && s.tiles > p.G && s.c.n > s.keys / 4) {
+    // (units are bounded by the pages that there can be, so not where positions have none)
+    if (TILE > UNIT && !p.a.mask && s.tiles > p.G && s.c.n > s.keys / 4 && end <= most) {
         s.grow = TILE / UNIT;
         s.units = (s.c.pos + UNIT - 1) / UNIT + s.grow;
     }
@@ -979,7 +980,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
     __shared__ __attribute__((aligned(16))) char sk[2][UNIT * KP];
     __shared__ __attribute__((aligned(16))) char sv[2][UNIT * VP];
     __shared__ __attribute__((aligned(16))) uint64_t sflag[2][4];  // keys there are
-    __shared__ int s_poison;
+    __shared__ int s_poison[4];  // each wave's own: it clears it before it stores values
     __shared__ PlanShared sh;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1032,8 +1033,8 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
         const uint32_t row_bytes = (uint32_t)(p.a.Hkv * D * (E4M3 ? 1 : 2));
         u32x4 kr[NI], vr[NI];
         const uint64_t apart = (uint64_t)(vbase - kbase);
-        if (tid == 0)
-            s_poison = 0;
+        if (lane == 0)
+            s_poison[wave] = 0;
         // Slots by batches of four tiles: a lane has the slot of one key, of tile lane / 16
         // of the batch and of the 16 keys there that its wave fetches.  The table's
         // entries are asked for two batches ahead.  Positions without a key are fetched
@@ -1081,7 +1082,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
                 }
             }
             if (!plain && __any(bad) && lane == 0)
-                s_poison = 1;
+                s_poison[wave] = 1;
         };
 
         if (keys == 0)
@@ -1110,7 +1111,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
                 const u32x4 *f = (const u32x4 *)sflag[batch & 1];
                 const u32x4 both = f[0] & f[1];
                 all = (uint64_t)__builtin_amdgcn_readfirstlane(both[1] & both[3]) << 32 |
-                      __builtin_amdgcn_readfirstlane(both[0] & both[2]);
+                      (uint32_t)__builtin_amdgcn_readfirstlane(both[0] & both[2]);
                 slots = next;
                 valid = valid_next;
                 next = slots_of(entry, batch + 1, valid_next);
@@ -1169,7 +1170,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
                       t + 1);
         }
         __syncthreads();
-        const bool poisoned = s_poison != 0;
+        const bool poisoned = (s_poison[0] | s_poison[1] | s_poison[2] | s_poison[3]) != 0;
         __syncthreads();  // before the next item's first tile is stored
         if (poisoned) {
             const AttnParams &p = reread();

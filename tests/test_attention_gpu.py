@@ -236,6 +236,35 @@ def test_chunks_that_are_most_of_their_context(Hq, Hkv, held):
     check(a, *run(a)[:2], f"{Hq}/{Hkv} held {held}")
 
 
+@pytest.mark.parametrize("R,Hq", [(1, 4), (12, 4), (40, 8)])
+@pytest.mark.parametrize("mask", [None, "tree"])
+def test_holes_in_the_table(R, Hq, mask):
+    """Entries that name no page in the middle of long and short contexts, whole tiles and
+    parts of them, where no row's own positions are near."""
+    a = make([1500, 900, 1300, 40], [R, R, max(1, R - 1), 1], Hq=Hq, Hkv=2, D=64, page=16, mask=mask,
+             seed=7)
+    rng = np.random.default_rng(8)
+    a["table"] = np.where(rng.random(a["table"].shape) < 0.25, -1, a["table"]).astype(np.int32)
+    a["table"][0, 8:24] = a["n_slots"] // 16 + 5
+    check(a, *run(a)[:2], f"{R} rows, {Hq} heads, mask {mask}")
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (6, 2)])
+def test_positions_far_behind_the_pages(Hq, Hkv):
+    """Chunks at positions of up to 2^30 of which the table holds the first 2000 or so:
+    only those have keys, and the work is theirs."""
+    a = make([1500, 0, 700, 3], [500, 400, 300, 1], Hq=Hq, Hkv=Hkv, D=64, page=16, packed=True,
+             seed=2)
+    far, cap = 2 ** 30, a["table"].shape[1] * a["page"]
+    a["held"] = np.full(4, a["table"].shape[1], np.int32)
+    for begin in ([far, far - 1, 700, far], [far - 7] * 4):
+        a["begin"], a["Lmax"] = np.array(begin, np.int32), far
+        out, lse, _, _ = run(a)
+        # the same as right behind the last page
+        near = dict(a, begin=np.minimum(a["begin"], cap))
+        check(near, out, lse, f"{Hq}/{Hkv} from {begin[0]}")
+
+
 @pytest.mark.parametrize("R,Hq", [(5, 4), (40, 4), (70, 8), (33, 2)])
 def test_masks(R, Hq):
     """Random masks, masks that leave rows empty, masks of several words."""

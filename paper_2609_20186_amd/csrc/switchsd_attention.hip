@@ -481,20 +481,25 @@ __device__ __forceinline__ void load_query(const AttnParams &p, const Row &r,
 // The softmax's factor, as what brings products to powers of two: a magnitude that they
 // are multiplied with once the maximum is known, and a sign (or 0, with the magnitude
 // 1) that the query rows take, so that what is not seen can be -inf before it.
+// NaN is a sign too: the rows become NaN (0x7FFF in both types), and what is not seen stays
+// -inf.
 struct Factor {
     float size, sign;
 };
 __device__ __forceinline__ Factor factor_of(const AttnParams &p, int h) {
     const float f = p.a.scale * kLog2e * (p.k_scale ? p.k_scale[h] : 1.0f);
-    return {f == 0.0f ? 1.0f : fabsf(f), f == 0.0f ? 0.0f : f < 0.0f ? -1.0f : 1.0f};
+    return {f == 0.0f || f != f ? 1.0f : fabsf(f),
+            f == 0.0f || f != f ? f : f < 0.0f ? -1.0f : 1.0f};
 }
 template <int N>
 __device__ __forceinline__ void apply_sign(u32x4 (&q)[N], float sign) {
     if (sign == 1.0f)  // the same for all lanes; the rows are not waited for
         return;
+    const uint32_t keep = sign == -1.0f ? ~0u : 0u;
+    const uint32_t flip = sign == -1.0f ? 0x80008000u : sign == 0.0f ? 0u : 0x7FFF7FFFu;
 #pragma unroll
     for (int x = 0; x < N; ++x)
-        q[x] = sign == 0.0f ? u32x4{0, 0, 0, 0} : q[x] ^ 0x80008000u;
+        q[x] = (q[x] & keep) ^ flip;
 }
 
 // Which of the 32 cache positions from kb on row r sees, of those in `valid`.

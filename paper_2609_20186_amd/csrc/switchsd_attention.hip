@@ -924,12 +924,13 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_few(const
 #pragma unroll
         for (int v = 1; v < 4; ++v)
             top = fmaxf(top, sm[v][row]);
+        // a wave whose products were all NaN has the maximum -inf too, and a sum that is NaN
+        const float at = top == -INFINITY ? 0.0f : top;
         float sum = 0.0f;
 #pragma unroll
         for (int v = 0; v < 4; ++v)
-            sum += sm[v][row] == -INFINITY ? 0.0f
-                                           : sl[v][row] * __builtin_amdgcn_exp2f(sm[v][row] - top);
-        const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+            sum += sl[v][row] * __builtin_amdgcn_exp2f(sm[v][row] - at);
+        const float f = __builtin_amdgcn_exp2f(m - at);
         // each wave adds up one block of columns
 #pragma unroll
         for (int d0 = 0; d0 < D / 32; d0 += COLS) {

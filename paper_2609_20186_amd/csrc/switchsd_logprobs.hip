@@ -150,6 +150,10 @@ struct Sums {
 // A reference is moved when a weight would pass 2^kDelay (a sum of 2^26 of them is far
 // from the largest float).
 constexpr float kDelay = 20.0f;
+// The exponent that weights and factors stop at: it leaves nothing of a sum (2^46 at most) in
+// 32 bits, and an infinite distance, that of a mask of the lowest number, would make NaN of
+// what is multiplied with it and then with the weight 0.
+constexpr float kNothing = -150.0f;
 
 // The largest of the vector's logits is returned (NaN where all are).
 template <int TYPE>
@@ -168,7 +172,7 @@ __device__ __forceinline__ float take(Sums &a, u32x4 x, int vec, float c, float 
     a.vec = up ? vec : a.vec;
     if (__any(top > a.lim)) {
         const float ref = fmaxf(a.ref, top);
-        const float d = a.ref == -INFINITY ? 0.0f : (a.ref - ref) * c;
+        const float d = a.ref == -INFINITY ? 0.0f : fmaxf((a.ref - ref) * c, kNothing);
         const float f2 = __builtin_amdgcn_exp2f(d);
         a.t = f2 * (a.t + a.s * d);
         a.s *= f2;
@@ -180,7 +184,7 @@ __device__ __forceinline__ float take(Sums &a, u32x4 x, int vec, float c, float 
 #pragma unroll
     for (int e = 0; e < N; ++e) {
         // NaN (and -inf beside itself) weighs nothing: the maximum drops it
-        const float y = fmaxf((f[e] - a.ref) * c, -150.0f);
+        const float y = fmaxf((f[e] - a.ref) * c, kNothing);
         const float w = __builtin_amdgcn_exp2f(y);
         s += w;
         t = fmaf(w, y, t);
@@ -229,7 +233,7 @@ __device__ __forceinline__ int ahead_of_nan(u32x4 x, int j, int own) {
 
 // Sums against reference `from`, against `to` (not below it).
 __device__ __forceinline__ void move(float &s, float &t, float from, float to, float c) {
-    const float d = s > 0.0f ? (from - to) * c : 0.0f;
+    const float d = s > 0.0f ? fmaxf((from - to) * c, kNothing) : 0.0f;
     const float f = __builtin_amdgcn_exp2f(d);
     t = f * (t + s * d);
     s *= f;

@@ -533,11 +533,14 @@ __device__ __forceinline__ void hide(f32x16 &s, uint32_t seen) {
 }
 
 // Running softmax of one query row per lane (both halves of a wave hold the same
-// rows, each the keys that its half of the products has): m is the maximum that
-// the weights are taken against, in powers of two; it follows the true one with
-// a delay of up to kDelay, which weights of up to 2^kDelay carry.  (Sums in 32 bits have
-// room for them, and fp16's largest number, 65504, is far from 256; a row's sums are
-// multiplied a few times in all, not in every other tile.)
+// rows, each the keys that its half of the products has): m is what the weights are taken
+// against, in powers of two: the maximum less kLift, followed with a delay of up to kDelay, so
+// that weights go up to 2^(kLift + kDelay).  fp16 ends at 2^16 and has its smallest step at
+// 2^-24: the lift keeps small weights, of which there can be many, out of the range where
+// their rounding is a good part of them (bf16 has no such range).  (Sums in 32 bits have
+// room for them; a row's sums are multiplied a few times in all, not in every other tile.)
+template <int TYPE>
+constexpr float kLift = TYPE == SWITCHSD_F16 ? 7.0f : 0.0f;
 constexpr float kDelay = 8.0f;
 
 __device__ __forceinline__ float other_half(float v) {
@@ -549,7 +552,7 @@ __device__ __forceinline__ float other_half(float v) {
 // The largest of the lane's row's products of 32 N keys, in powers of two; moves m
 // where it has to, and returns what the sums so far have to be multiplied with (1:
 // nothing).
-template <int N>
+template <int TYPE, int N>
 __device__ __forceinline__ float follow(const f32x16 (&s)[N], float factor, float &m, float &l) {
     float top = s[0][0];
 #pragma unroll
@@ -559,8 +562,8 @@ __device__ __forceinline__ float follow(const f32x16 (&s)[N], float factor, floa
             top = fmaxf(top, s[x][e]);
     top = fmaxf(top, other_half(top)) * factor;
     float alpha = 1.0f;
-    if (__any(top > m + kDelay || (m == -INFINITY && top > m))) {
-        const float mn = fmaxf(m, top);
+    if (__any(top > m + (kLift<TYPE> + kDelay) || (m == -INFINITY && top > m))) {
+        const float mn = fmaxf(m, top - kLift<TYPE>);
         alpha = m == mn ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
         m = mn;
         l *= alpha;
@@ -570,8 +573,9 @@ __device__ __forceinline__ float follow(const f32x16 (&s)[N], float factor, floa
 // Products -> weights, in 32 bits in s, summed to l; the weights in 16 bits as the
 // right operand of 2 N products with 16 keys each.  That rounding is the price of the
 // matrix instructions, whose operands are both of the values' type: at most half a step of
-// a weight, 2^-8 of it (bf16) or 2^-11 (fp16), less for a sum of many.  The sum of the
-// weights is that of the unrounded ones.
+// a weight, 2^-8 of it (bf16), or of fp16 2^-11 of it or 2^-32 of the largest weight,
+// whichever is more; less for a sum of many.  The sum of the weights is that of the
+// unrounded ones.
 template <int TYPE, int N>
 __device__ __forceinline__ void weigh(f32x16 (&s)[N], float factor, float m, float &l,
                                       u32x4 (&w)[2 * N]) {
@@ -889,7 +893,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_few(const
                 load(vr, vbase, next);
             if (!plain)
                 hide(s[0], seen_bits(p, c, r, kb, valid));
-            const float alpha = follow<1>(s, factor, m, l);
+            const float alpha = follow<TYPE, 1>(s, factor, m, l);
             if (__any(alpha != 1.0f))
                 scale_rows<D>(o, alpha);
             u32x4 weights[2];
@@ -1164,7 +1168,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(cons
                                        ((uint32_t)(f[y * 2] >> x) & 0xFFFFu) |
                                            (uint32_t)(f[y * 2 + 1] >> x) << 16));
                 }
-                const float alpha = follow<2>(s, factor, m, l);
+                const float alpha = follow<TYPE, 2>(s, factor, m, l);
                 if (__any(alpha != 1.0f))
                     scale_rows<D>(o, alpha);
                 u32x4 weights[4];

@@ -838,9 +838,12 @@ def build_logprob_args(logits, tokens=None, dn=None, dpar=None, accept_node=None
     (bf16 or its bits, fp16 or fp32), tokens [B, R] int32 (None where neither logprob
     nor rank is wanted), dn [B] (None: all rows); with accept_node [B], and dpar [B, R]
     (None: chains), the rows along each accepted path, tokens being the step's
-    out_tokens.  workspace: zeroed, of logprob_workspace_bytes, None: one of its own;
-    switchsd_token_logprobs calls that share it (the result too) must be ordered.  The
-    tensors are kept alive by the result."""
+    out_tokens.  workspace: zeroed, of logprob_workspace_bytes, None: one of its own, zeroed
+    on the current stream: the first call waits for that whatever its stream, but for a
+    captured one, which needs it done before the capture begins (torch.cuda.graph
+    waits for the device); what is built in a capture is for that capture.
+    switchsd_token_logprobs calls that share a workspace (the result too) must be ordered.
+    The tensors are kept alive by the result."""
     if not isinstance(logits, _Tensor) or logits.dim() != 3:
         raise ValueError("logits must be a device tensor [B, R, V]")
     B, R, V = logits.shape
@@ -858,8 +861,11 @@ def build_logprob_args(logits, tokens=None, dn=None, dpar=None, accept_node=None
     a.accept_node = _arr(accept_node, "i32", "accept_node", (B,), dev, True)
     a.temperature = float(temperature)
     need = logprob_workspace_bytes(a)
+    a.zeroed = None
     if workspace is None and need:
         workspace = torch.zeros(need, dtype=torch.uint8, device=logits.device)
+        if not torch.cuda.is_current_stream_capturing():
+            a.zeroed = torch.cuda.current_stream().record_event()
     if workspace is not None:
         a.workspace, a.workspace_bytes = _workspace(workspace, dev), workspace.numel()
     a.shape, a.device = (B, R, V), dev
@@ -872,8 +878,20 @@ def logprob_workspace_bytes(args):
 
 
 def alloc_logprob_workspace(args, device="cuda"):
-    """Zeroed once here; the kernels keep it usable for every later call."""
+    """Zeroed once here, on the current stream; the kernels keep it usable for every later
+    call."""
     return torch.zeros(max(logprob_workspace_bytes(args), 256), dtype=torch.uint8, device=device)
+
+
+def _after_zeroing(args, stream):
+    """The first call's stream waits for the workspace that build_logprob_args zeroed;
+    later calls are ordered behind that call."""
+    stream = torch.cuda.current_stream() if stream is None else stream
+    with torch.cuda.stream(stream):
+        if torch.cuda.is_current_stream_capturing():
+            return  # a capture cannot wait for what lies outside of it
+    stream.wait_event(args.zeroed)
+    args.zeroed = None
 
 
 def switchsd_token_logprobs(args, logprob=None, lse=None, entropy=None, rank=None, top_ids=None,
@@ -890,6 +908,8 @@ def switchsd_token_logprobs(args, logprob=None, lse=None, entropy=None, rank=Non
         n_top = one.shape[2]
         _sizes(n_top=n_top)
     top = (*shape, n_top)
+    if args.zeroed is not None:
+        _after_zeroing(args, stream)
     _check("switchsd_token_logprobs", lib.switchsd_token_logprobs(
         ctypes.byref(args), _arr(logprob, "f32", "logprob", shape, dev, True),
         _arr(lse, "f32", "lse", shape, dev, True),

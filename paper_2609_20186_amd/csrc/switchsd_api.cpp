@@ -1357,13 +1357,20 @@ int switchsd_paged_attention(const switchsd_attention_args *a, const void *q, in
 
 namespace {
 
+bool logprob_type_ok(const switchsd_logprob_args *a) {
+    return a->logits_type >= SWITCHSD_BF16 && a->logits_type <= SWITCHSD_F32;
+}
+
+bool logprob_shape_ok(const switchsd_logprob_args *a) {
+    return shape_ok_B(a->B) && a->R >= 1 && a->R <= SWITCHSD_MAX_R && a->V >= 1 &&
+           a->V <= (1 << 26) && (a->B == 0 || launch_ok((int64_t)a->B * a->R));
+}
+
 int check_logprobs(const switchsd_logprob_args *a) {
-    if (!a || a->logits_type < SWITCHSD_BF16 || a->logits_type > SWITCHSD_F32 ||
-        !(a->temperature > 0.0f && a->temperature < INFINITY) ||
+    if (!a || !logprob_type_ok(a) || !(a->temperature > 0.0f && a->temperature < INFINITY) ||
         !(1.0f / a->temperature < INFINITY))
         return SWITCHSD_EINVAL;
-    if (!shape_ok_B(a->B) || a->R < 1 || a->R > SWITCHSD_MAX_R || a->V < 1 || a->V > (1 << 26) ||
-        (a->B > 0 && !launch_ok((int64_t)a->B * a->R)))
+    if (!logprob_shape_ok(a))
         return SWITCHSD_ESHAPE;
     if (a->B > 0 && (!a->logits || !aligned(a->logits, type_size(a->logits_type))))
         return SWITCHSD_EINVAL;
@@ -1375,7 +1382,7 @@ int check_logprobs(const switchsd_logprob_args *a) {
 extern "C" {
 
 size_t switchsd_logprob_workspace_bytes(const switchsd_logprob_args *a) {
-    if (!a || a->B < 1 || a->R < 1 || a->V < 1 || !launch_ok((int64_t)a->B * a->R))
+    if (!a || !logprob_type_ok(a) || !logprob_shape_ok(a) || a->B == 0)
         return 0;
     const LogprobCut cut = logprob_cut(*a, true);
     if (cut.pieces == 1)

@@ -628,7 +628,8 @@ size_t switchsd_attention_workspace_bytes(const switchsd_attention_args *args);
  * Entries that there are not are neither read nor written.
  *   logits [B, R, V] of logits_type, aligned to its elements, V <= 2^26, R <=
  *   SWITCHSD_MAX_R; tokens [B, R] int32 (NULL where neither logprob nor rank is
- *   wanted); temperature > 0 and finite.  Fewer than 2^24 entries. */
+ *   wanted); temperature > 0 and finite, and log2(e) / temperature a finite float (from
+ *   4.3e-39 on).  Fewer than 2^24 entries. */
 typedef struct {
     const void *logits;
     int32_t logits_type; /* switchsd_type */

@@ -1368,7 +1368,7 @@ bool logprob_shape_ok(const switchsd_logprob_args *a) {
 
 int check_logprobs(const switchsd_logprob_args *a) {
     if (!a || !logprob_type_ok(a) || !(a->temperature > 0.0f && a->temperature < INFINITY) ||
-        !(1.0f / a->temperature < INFINITY))
+        !(1.0f / a->temperature * 1.44269504088896340736f < INFINITY))
         return SWITCHSD_EINVAL;
     if (!logprob_shape_ok(a))
         return SWITCHSD_ESHAPE;

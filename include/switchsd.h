@@ -659,7 +659,8 @@ size_t switchsd_logprob_workspace_bytes(const switchsd_logprob_args *args);
  * row without a finite maximum (every value NaN or -inf, or +inf present) puts
  * all weight on its greedy choice (the lowest index of the maximum, 0 for all
  * NaN): its logprob is 0, that of others -inf, the entropy 0, and lse is the
- * maximum (-inf for all NaN).  A token outside [0, V) has logprob -inf and rank -1.
+ * maximum (-inf for all NaN); a finite one's lse is finite too, the largest float where
+ * it would be more.  A token outside [0, V) has logprob -inf and rank -1.
  * Sums are held in 32 bits or more.  The order of logits depends on the logits
  * alone, not on the temperature.
  *   logprob, lse, entropy [B, R] float, rank [B, R] int32, top_ids [B, R, n_top]
@@ -674,8 +675,9 @@ int switchsd_token_logprobs(const switchsd_logprob_args *args, float *logprob, f
  *   grad[v] = (g_logprob * ((v == token) - p[v])
  *              - g_entropy * p[v] * (log p[v] + entropy)) / temperature,
  * a weight p of 0 adding nothing to either product.  lse and entropy [B, R] are what
- * switchsd_token_logprobs gave for the same logits.  A NaN logit has p = 0.  A row
- * whose lse is not finite (no finite maximum) has the gradient 0.
+ * switchsd_token_logprobs gave for the same logits; where |lse| is 1024 or more, and its
+ * 32 bits have too little room for log p, p comes from the row's own sum instead.  A NaN
+ * logit has p = 0.  A row whose lse is not finite (no finite maximum) has the gradient 0.
  *   lse [B, R] float; g_logprob [B, R] float or NULL; g_entropy [B, R] float or
  *   NULL, with entropy [B, R]; tokens may be NULL without g_logprob; grad [B, R, V]
  *   of logits_type, rounded once: apart from the logits or the logits themselves.

@@ -154,6 +154,7 @@ constexpr float kDelay = 20.0f;
 // 32 bits, and an infinite distance, that of a mask of the lowest number, would make NaN of
 // what is multiplied with it and then with the weight 0.
 constexpr float kNothing = -150.0f;
+constexpr float kLargest = 3.402823466e38f;
 
 // The largest of the vector's logits is returned (NaN where all are).
 template <int TYPE>
@@ -691,7 +692,8 @@ __global__ void __launch_bounds__(kThreads, 4) k_logprob(const LogprobParams p) 
             if (p.logprob)
                 p.logprob[e] = in ? logprob(lt, tok) : -INFINITY;
             if (p.lse)
-                p.lse[e] = flat ? M : M * p.inv_t + lnS;
+                // finite where the maximum is
+                p.lse[e] = flat ? M : fminf(fmaxf(M * p.inv_t + lnS, -kLargest), kLargest);
             if (p.entropy)
                 p.entropy[e] = flat ? 0.0f : lnS - t / S * kLn2;
         }
@@ -707,6 +709,47 @@ __global__ void __launch_bounds__(kThreads, 4) k_logprob(const LogprobParams p) 
 }
 
 // ---- gradient
+
+// From this |lse| on 32 bits leave too little of the logarithm beside the maximum (2^-15 of p
+// below it, up to all of p): the row's sum is taken again.  The first of the row's
+// work-groups does that and all of its pieces, since the gradient may take the row's place.
+constexpr float kFar = 1024.0f;
+
+// The maximum of a row and the logarithm of its sum against it.  Every lane of the
+// work-group calls it.
+template <int TYPE>
+__device__ __forceinline__ float2 row_sum(const char *row, int V, float c) {
+    constexpr int N = kPerVec<TYPE>;
+    __shared__ float red[2][kThreads / 64];
+    const int full = V / N, wave = threadIdx.x >> 6;
+    float m = -INFINITY, s = 0.0f;
+    for (int j = threadIdx.x; j <= full; j += kThreads) {
+        const u32x4 x = j < full ? load_vec<TYPE>(row, j) : load_last<TYPE>(row, j, V);
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            m = fmaxf(m, element<TYPE>(x, e));
+    }
+    for (int d = 32; d; d >>= 1)
+        m = fmaxf(m, __shfl_xor(m, d));
+    red[0][wave] = m;
+    __syncthreads();
+    for (int w = 0; w < kThreads / 64; ++w)
+        m = fmaxf(m, red[0][w]);
+    for (int j = threadIdx.x; j <= full; j += kThreads) {
+        const u32x4 x = j < full ? load_vec<TYPE>(row, j) : load_last<TYPE>(row, j, V);
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            s += __builtin_amdgcn_exp2f(fmaxf((element<TYPE>(x, e) - m) * c, kNothing));
+    }
+    for (int d = 32; d; d >>= 1)
+        s += __shfl_xor(s, d);
+    red[1][wave] = s;
+    __syncthreads();
+    s = 0.0f;
+    for (int w = 0; w < kThreads / 64; ++w)
+        s += red[1][w];
+    return make_float2(m, __builtin_amdgcn_logf(s) * kLn2);
+}
 
 // A work-group per entry and piece of its row: one read, one write, bound by the memory.
 // 4 x up to 1024 rows of 128256 bf16 logits: 330 us, 5.6 TB/s; 23 rows of 50257 floats 4.5.
@@ -732,13 +775,23 @@ __global__ void __launch_bounds__(kThreads) k_logprob_grad(const LogprobParams p
     const float H = p.g_entropy ? p.in_entropy[e] : 0.0f;
     const int tok = p.g_logprob ? a.tokens[e] : -1;
     const bool flat = !(fabsf(lse) < INFINITY);
-    const auto slope = [&](float l, int v) {
+    // log p = (l - base) / T - low
+    const auto slope_of = [&](float l, int v, float base, float low) {
         // NaN and -inf weigh nothing: the maximum drops them
-        const float x = fmaxf(fmaf(l, p.inv_t, -lse), -150.0f);
+        const float x = fmaxf(fmaf(l - base, p.inv_t, -low), -150.0f);
         const float w = l == l ? __builtin_amdgcn_exp2f(x * kLog2e) : 0.0f;
         const float d = (v == tok ? g : 0.0f) - w * fmaf(ge, x + H, g);
         return flat ? 0.0f : d * p.inv_t;
     };
+    if (!flat && fabsf(lse) >= kFar) {
+        if (piece != 0)
+            return;
+        const float2 s = row_sum<TYPE>(row, V, p.inv_t * kLog2e);
+        for (int v = threadIdx.x; v < V; v += kThreads)
+            store_logit<TYPE>(out, v, slope_of(load_logit<TYPE>(row, v), v, s.x, s.y));
+        return;
+    }
+    const auto slope = [&](float l, int v) { return slope_of(l, v, 0.0f, lse); };
     const int j0 = piece * (kThreads * kGradVecs) + threadIdx.x;
     u32x4 x[kGradVecs];
 #pragma unroll

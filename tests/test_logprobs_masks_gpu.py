@@ -79,8 +79,7 @@ def check(a, T, x, first, want, out, what):
             tok = int(a["tokens"][b, i])
             at = f"{what} {b} {i}"
             assert abs(o["entropy"][b, i] - h) <= tolerance(V, T, big, h), (at, o["entropy"][b, i], h)
-            with np.errstate(over="ignore"):
-                near = np.float32(lse)
+            near = np.float32(np.clip(lse, LOWEST["f32"], -LOWEST["f32"]))
             assert o["lse"][b, i] == near or \
                 abs(o["lse"][b, i] - lse) <= tolerance(V, T, big, lse), (at, o["lse"][b, i], lse)
             if 0 <= tok < V:
@@ -127,7 +126,7 @@ def test_masks(type, low, where):
             for b in range(2):
                 for i in range(2):
                     if (x[b, i] < -1e4).all():
-                        continue              # p is not exp(z - lse) in 32 bits
+                        continue              # p is not exp(z - lse) in 32 bits (below)
                     lse, h = float(out["lse"][b, i]), float(out["entropy"][b, i])
                     want = ref.grad_row(x[b, i], T, int(a["tokens"][b, i]), lse, h,
                                         float(g[b, i]), float(ge[b, i]))
@@ -168,3 +167,75 @@ def test_logits_far_apart(type, low):
                 assert abs(got["entropy"] - h) <= tolerance(V, 1.0, big, h), (V, i, got, h)
                 assert abs(got["lse"] - lse) <= tolerance(V, 1.0, big, lse), (V, i, got, lse)
                 np.testing.assert_array_equal(out["top_ids"][0, i].cpu(), order(rows[0, i])[:5])
+
+
+def gradient(a, T, logits, g, ge):
+    """The forward pass's entropy and the gradient."""
+    from paper_2609_20186_amd import binding as sd
+    out, args = run(a, T, 0, args=args_of(a, T, logits))
+    grad = torch.full_like(logits, 5.0)
+    call = (out["lse"], out["entropy"], g.to(DEV), ge.to(DEV))
+    sd.switchsd_token_logprobs_grad(args, *call, grad)
+    sd.switchsd_token_logprobs_grad(args, *call, logits)   # in the logits' place
+    bits = torch.int32 if logits.dtype == torch.float32 else torch.int16
+    assert torch.equal(grad.view(bits), logits.view(bits))
+    return out, ref.f64(grad)
+
+
+def check_gradient(a, T, x, got, g, ge, what):
+    """Against the formula with the row's own probabilities, whatever lse has of them in 32
+    bits.  log p is off by 8 roundings of |z - max| and the sum's, sqrt V and 32 of them; the
+    products by a few of their own."""
+    B, R, V = x.shape
+    u = ref.U[a["type"]]
+    for b in range(B):
+        for i in range(R):
+            _, lp, h = reference(x[b, i], T)
+            lp = np.clip(lp, -1e3, None)
+            p = np.exp(lp)
+            gl, gh = float(g[b, i]), float(ge[b, i])
+            hit = np.arange(V) == int(a["tokens"][b, i])
+            want = (gl * (hit - p) - gh * p * (lp + h)) / T
+            err = 2.0 ** -24 * (8 * np.abs(lp) + math.sqrt(V) + 32)
+            part = p * (abs(gl) + abs(gh) * (np.abs(lp) + abs(h)))
+            tol = 1.01 * u * np.abs(want) + (part * err + p * abs(gh) * (err + 2.0 ** -23 * math.sqrt(V))
+                                             + 2.0 ** -22 * (part + abs(gl) * hit)) / T
+            tol += {"bf16": 1e-38, "f16": 2.0 ** -25, "f32": 1e-38}[a["type"]]
+            d = np.abs(got[b, i] - want)
+            assert (d <= tol).all(), (what, b, i, float(d.max()), float(want[d.argmax()]))
+
+
+@pytest.mark.parametrize("type,low", [("bf16", LOWEST["bf16"]), ("bf16", -1e30), ("bf16", 1e37),
+                                      ("f16", LOWEST["f16"]), ("f32", LOWEST["f32"]),
+                                      ("f32", -1e9), ("f32", 3e38)])
+def test_gradient_of_rows_of_one_value(type, low):
+    """All masked, with a value beside which the logarithm of the sum has no place in 32
+    bits: every token is as likely, and with T below 1 z itself is beyond the largest number."""
+    g, ge = torch.tensor([[0.7, -1.0, 0.0]]), torch.tensor([[0.2, 0.5, 1.0]])
+    for V in (1, 9, 300, 5003, 50257):
+        a = make(1, 3, V, type, seed=V, dn=False)
+        a["logits"][:] = torch.tensor(low).to(TYPES[type])
+        if V > 4:                             # a likelier one beside the others
+            a["logits"][0, 1, V // 2] = torch.tensor(low * 0.5 if low < 0 else low * 1.1).to(
+                TYPES[type])
+        x = ref.f64(a["logits"])
+        for T in (0.7, 1.0, 1.6):
+            out, got = gradient(a, T, a["logits"].to(DEV), g, ge)
+            assert torch.isfinite(out["lse"]).all()
+            check_gradient(a, T, x, got, g, ge, f"{type} {low:.2g} V={V} T={T}")
+
+
+@pytest.mark.parametrize("type", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("T", [2.0 ** -6, 1e-3, 1e-5])
+def test_gradient_at_low_temperatures(type, T):
+    """Rows of which a few tokens are nearly as likely, with |z| of 10^3 to 10^6."""
+    g, ge = torch.tensor([[0.7, -1.0, 0.4]]) * T, torch.tensor([[0.2, 0.5, 0.0]]) * T
+    for V in (9, 5003, 50257):
+        a = make(1, 3, V, type, seed=V, dn=False)
+        at = V // 3
+        step = 2.0 ** -3 if type != "f32" else T    # apart by what the type has at 20
+        for i in range(3):
+            a["logits"][0, i, at:at + 3] = (20.0 + i + step * torch.arange(3)).to(TYPES[type])
+        x = ref.f64(a["logits"])
+        _, got = gradient(a, T, a["logits"].to(DEV), g, ge)
+        check_gradient(a, T, x, got, g, ge, f"{type} V={V} T={T}")

@@ -564,7 +564,7 @@ int switchsd_store_cache(const void *keys, int64_t key_stride, const void *value
  *   packed rows (cu != NULL): sequence b's rows are cu[b] + i, i < n_b =
  *     cu[b+1] - cu[b] (no more than R, none where cu descends or leaves [0,
  *     rows]), at the positions p_b + i, p_b = clamp(begin[b], 0, Lmax), as
- *     switchsd_span_slots lists them.
+ *     switchsd_span_slots lists them; a row belongs to one sequence at most.
  * Position p lies in slot table[b, p / page_size] * page_size + p % page_size;
  * where p / page_size >= clamp(held[b], 0, max_pages), or the slot is not in [0,
  * n_slots), there is no key.  Row i sees the positions p < p_b and of the new ones
@@ -589,12 +589,13 @@ typedef struct {
 } switchsd_attention_args;
 
 /* out[row, h, :] = sum over seen positions of exp(s - lse) v, s = scale * q . k,
- * lse[row, h] = log of the sum of exp(s).  A row that sees nothing has out = 0 and
- * lse = -inf; rows that belong to no sequence are left as they are.  Keys and
- * values that a row does not see do not reach it, whatever they hold (NaN and
- * infinities too).  Products, sums and the softmax are held in 32 bits; the
- * weights exp(s - m) are rounded to q's type for the product with the values, as
- * out is.  A cache in SWITCHSD_E4M3 stands for its values times k_scale[h],
+ * lse[row, h] = log of the sum of exp(s).  A row that sees nothing, or products of -inf
+ * only, has out = 0 and lse = -inf; one that sees a product of NaN or +inf has NaN in
+ * both; rows that belong to no sequence are left as they are.  Keys and values that a
+ * row does not see do not reach it, whatever they hold (NaN and infinities too).
+ * Products, sums and the softmax are held in 32 bits; the weights exp(s - m) are rounded
+ * to q's type for the product with the values (in fp16 to no less than 2^-32 of the
+ * largest), as out is.  A cache in SWITCHSD_E4M3 stands for its values times k_scale[h],
  * v_scale[h] ([Hkv] float, NULL: 1).
  *   q: `rows` rows of Hq heads of D elements of `type` (SWITCHSD_BF16 or
  *   SWITCHSD_F16), q_stride elements apart (at least Hq * D); k_cache, v_cache

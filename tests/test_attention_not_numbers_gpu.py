@@ -137,3 +137,34 @@ def test_scales_of_values(R, Hq, L):
     assert np.isnan(out[:R, :Hq // 2]).all() and np.isfinite(out[:R, Hq // 2:]).all()
     assert np.isfinite(lse[:R]).all()
     assert (out[R:] == 0).all() and (lse[R:] == -math.inf).all()
+
+
+@pytest.mark.parametrize("R,Hq,L", FORMS)
+@pytest.mark.parametrize("scale", [0.2, -0.2])
+def test_infinite_products(R, Hq, L, scale):
+    """+inf is NaN for the rows that see it; -inf weighs nothing, and a row that sees nothing
+    else is as one that sees nothing."""
+    inf = math.inf if scale > 0 else -math.inf
+    for L0 in (L, 1):
+        a = make([L0, L], [R, 1], R=R, Hq=Hq, Hkv=2, D=64, page=16, scale=scale, seed=5)
+        a["q"][:, :, 5] = 1.0
+        slots = ref.slots_of(a, 0, L0 - 1 + R)
+        at = slots[L0 // 2]
+        a["k_cache"][at, 0, 5] = inf
+        out, lse, _, _ = run(a)
+        out, lse = ref.f64(out[:R]), ref.f64(lse[:R])
+        assert np.isnan(out[:, :Hq // 2]).all() and np.isnan(lse[:, :Hq // 2]).all()
+        assert np.isfinite(out[:, Hq // 2:]).all() and np.isfinite(lse[:, Hq // 2:]).all()
+        a["k_cache"][at, 0, 5] = -inf
+        out, lse, _, _ = run(a)
+        if L0 == 1:
+            assert (out[0, :Hq // 2] == 0).all() and (lse[0, :Hq // 2] == -math.inf).all()
+        a["table"][0, L0 // 2 // 16] = -1      # the page of the key with it
+        a["k_cache"][slots[L0 // 2 // 16 * 16:][:16], 0, 5] = -inf
+        few = run(a)
+        a["table"][0, L0 // 2 // 16] = at // 16
+        full = run(a)
+        assert torch.equal(full[0][:R, :Hq // 2].isfinite(), few[0][:R, :Hq // 2].isfinite())
+        d = (full[1][:R, :Hq // 2] - few[1][:R, :Hq // 2]).abs()
+        same = full[1][:R, :Hq // 2] == few[1][:R, :Hq // 2]      # -inf both
+        assert (same | (d <= (L + 64) * 2.0 ** -23)).all()   # the order of the sums

@@ -44,7 +44,8 @@ __device__ __forceinline__ int pack_e4m3(float a, float b, int old) {
 // A lane per 16 bytes of a row's keys or values, so that loads and stores are whole
 // vectors whatever the slots' order.  Moves 4 Hkv D bytes in and as many (or half)
 // out: bound by its launch for the rows of a step (256 rows of 8 heads of 128: 2.8 us),
-// by the memory for prompts (16 of up to 2048 tokens, 8 heads of 64: 18.8 us, 5.4 TB/s).
+// by the memory for prompts (16 of up to 2048 tokens, 8 heads of 64: 19.1 us, 5.3 TB/s;
+// of 128: 31.5 us, into 8 bits 38.3, for the division).
 template <int TYPE, bool E4M3>
 __global__ void __launch_bounds__(kThreads) k_store(const StoreParams p) {
     const uint32_t vecs = (uint32_t)(p.Hkv * p.D) / 8;
@@ -442,7 +443,8 @@ __device__ __forceinline__ uint2 read_transposed(uint32_t at) {
 // The kernel's parameters, read from memory again: what was read of them before is not kept
 // for what follows.  Left alone the compiler reads all of them at the start and, with
 // too few scalar registers for them, carries them in lanes of vector registers through
-// everything.
+// everything (as it still does with others of the scalars: 167 for 128-wide heads in the
+// form for many, some ten of them moved back in front of every tile's products).
 __device__ __forceinline__ const AttnParams &reread() {
     uint64_t at = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
     asm volatile("" : "+s"(at));
@@ -733,7 +735,7 @@ __device__ __forceinline__ int slot_of(const AttnParams &p, const int32_t *table
 // and values are on their way while the present one's are multiplied; the page table's
 // entries are read two units ahead, since loads come back in order.
 //   32 x 8 rows (32 + 8 heads of 128, bf16) over up to 4096 keys: 91 us, 4.3 TB/s, and
-// 8 of k_merge; 96 x 32 heads, one token, over 3682: 219 us, 4.9 TB/s; the first keys
+// 8 of k_merge (8-bit keys: 58 together); 96 x 32 heads, one token, over 3682: 219 us, 4.9 TB/s; the first keys
 // arrive some 10 us after the launch.  One token over 512 keys: 12.4 us, a chain of
 // plan, page table, first keys and the join of four waves.
 template <int TYPE, bool E4M3, int D>
@@ -980,11 +982,11 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_few(const
 // values at a time in LDS, two buffers of them, the next ones on their way through
 // registers while the present ones are used.  (Loads straight into LDS save those registers,
 // but the compiler waits for all of them before any read of LDS.)
-//   Chunks of prompts, 32 + 8 heads of 128, bf16: 880 us, 920 TFLOP/s; 256 x 60 drafted
-// nodes over up to 2048 keys: 620 us, 530 TFLOP/s.  A wave needs 1024 cycles of matrix
-// instructions for a tile of 32 rows and 64 keys, and some 1450 of vector ones (512 of
-// them the exponentials): two waves on a SIMD are bound by those, and in part by waits,
-// with the matrix unit in use for a third of the time.
+//   Chunks of prompts, 32 + 8 heads of 128, bf16: 969 us and more, up to 840 TFLOP/s; 256 x 60
+// drafted nodes over up to 2048 keys: 630 us, 530 TFLOP/s.  A wave needs 1024 cycles of
+// matrix instructions for a tile of 32 rows and 64 keys, and some 1450 of vector ones (512 of
+// them the exponentials), and a SIMD takes 2770 (prompts) to 3400 (trees) for it: the
+// rest are waits, and the matrix unit is in use for a third of the time.
 template <int TYPE, bool E4M3, int D>
 __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) k_attend_many(const AttnParams) {
     constexpr int TILE = 128, UNIT = 64;

@@ -423,8 +423,8 @@ __device__ __forceinline__ float high(unsigned long long v) {
 // work-group to arrive joins the pieces.  About 13 lane operations an element, the
 // exponential among them, which at full rate is what 5 to 6 TB/s of 16-bit logits
 // bring: a row is cut rather than left to one compute unit.
-//   8 x up to 512 rows of 151936 bf16 logits, one alternative: 243 us, 4.5 TB/s (without
-// ranks 204, 5.3).  32 paths of 1 to 9 entries of 128256, 20 alternatives: 29.6 us, of
+//   8 x up to 512 rows of 151936 bf16 logits, one alternative: 233 to 246 us, 4.4 to 4.7 TB/s
+// (without ranks 204, 5.3; 8 x up to 256 rows of floats 204).  32 paths of 1 to 9 entries of 128256, 20 alternatives: 29.6 us, of
 // which 6.6 for the alternatives and 3.1 for the ranks; the rest is the path, the
 // first bytes and the join of the pieces.
 template <int TYPE>
@@ -756,7 +756,8 @@ __device__ __forceinline__ float2 row_sum(const char *row, int V, float c) {
 }
 
 // A work-group per entry and piece of its row: one read, one write, bound by the memory.
-// 4 x up to 1024 rows of 128256 bf16 logits: 330 us, 5.6 TB/s; 23 rows of 50257 floats 4.5.
+// 4 x up to 1024 rows of 128256 bf16 logits: 332 to 348 us, 5.3 to 5.5 TB/s; 23 rows of 50257
+// floats 4.8; along 32 paths, most of whose work-groups have no entry, 28.
 constexpr int kGradVecs = 4;  // vectors of a lane
 template <int TYPE>
 __global__ void __launch_bounds__(kThreads) k_logprob_grad(const LogprobParams p, int pieces) {

@@ -886,7 +886,10 @@ def alloc_logprob_workspace(args, device="cuda"):
 def _after_zeroing(args, stream):
     """The first call's stream waits for the workspace that build_logprob_args zeroed;
     later calls are ordered behind that call."""
-    stream = torch.cuda.current_stream() if stream is None else stream
+    if stream is None:
+        stream = torch.cuda.current_stream()
+    elif not isinstance(stream, torch.cuda.Stream):  # what has a handle, as for all calls
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
     with torch.cuda.stream(stream):
         if torch.cuda.is_current_stream_capturing():
             return  # a capture cannot wait for what lies outside of it

@@ -23,7 +23,14 @@ def busy(x):
         torch.mm(x, x)
 
 
-@pytest.mark.parametrize("first", ["other", "same"])
+class Handle:
+    """A stream of another library: its handle alone."""
+
+    def __init__(self, stream):
+        self.cuda_stream = stream.cuda_stream
+
+
+@pytest.mark.parametrize("first", ["other", "handle", "same"])
 def test_first_call_waits_for_the_zeroing(first):
     """The memory held something else before and the building stream is busy; a call on
     another stream, or one there behind a call on the building stream."""
@@ -47,7 +54,7 @@ def test_first_call_waits_for_the_zeroing(first):
         if first == "same":
             run(a, 1.0, 5, args=args, out=out)
             other.wait_stream(torch.cuda.current_stream())
-        run(a, 1.0, 5, args=args, out=out, stream=other)
+        run(a, 1.0, 5, args=args, out=out, stream=Handle(other) if first == "handle" else other)
         other.synchronize()
         got = {n: t.clone() for n, t in out.items()}
         check(a, 1.0, 5, got, f"{first} stream first")
